@@ -6,7 +6,8 @@
  *
  *   - the KV cache is stored as FP8 (E4M3) with max-calibrated dequantisation
  *     scales (paper, Section "KV Quantization"); a bf16 cache is the comparison
- *     variant the paper measures against;
+ *     variant the paper measures against, and a 4-bit cache (E2M1 codes, one
+ *     E4M3 scale per 16 channels) takes the same idea one step further;
  *   - every layer is either full-context attention or window attention that
  *     sees only the most recent W tokens (paper, Section "Window attention for
  *     long-context inference"); which layers are which is the per-layer choice
@@ -47,6 +48,15 @@
  * Cache layout (both K and V):  [num_blocks][num_kv_heads][block_size][head_dim]
  *   elements u8 (E4M3 codes) or bf16; one (block, KV head) is 1 KiB (FP8) or
  *   2 KiB (bf16) contiguous.  Base pointers must be 16-byte aligned.
+ * 4-bit cache:  [num_blocks][num_kv_heads][PUZZLE_FP4_BLOCK_BYTES], per (block, KV head) 512 bytes of E2M1 codes and
+ *   then 64 E4M3 scales, one per token and group of 16 channels.  Channel d of token t (t < 16) of the block, b = d / 16:
+ *     K code: byte 32 t + d / 2, even d in the low nibble;   K scale: byte 512 + 16 b + 2 (t % 8) + t / 8
+ *     V code: byte 256 (d / 32) + 32 (t / 2) + d % 32, even t in the low nibble;
+ *                                       V scale: byte 512 + 16 b + 4 ((t % 8) / 2) + 2 (t / 8) + t % 2
+ *   x ~ code * scale * k_scale[h] (v_scale[h]), so the calibrated scales of the FP8 cache serve it too.  An append
+ *   computes, with y the float32 quotient x / k_scale[h], scale = E4M3(max |y| / 6) over the group (float32 quotient,
+ *   to nearest even, saturating at 448) and code = E2M1(y / scale) (to nearest even, saturating at 6); a group whose
+ *   scale is zero holds zeros, one with a NaN has the scale 0x7F (and so reads as NaN).
  */
 #ifndef PUZZLE_ATTN_H_
 #define PUZZLE_ATTN_H_
@@ -73,12 +83,14 @@ typedef enum {
   PUZZLE_ERR_CUDA = 5         /* a CUDA call or launch failed */
 } puzzle_status;
 
-typedef enum { PUZZLE_KV_FP8_E4M3 = 0, PUZZLE_KV_BF16 = 1 } puzzle_kv_dtype;
+typedef enum { PUZZLE_KV_FP8_E4M3 = 0, PUZZLE_KV_BF16 = 1, PUZZLE_KV_FP4_E2M1 = 2 } puzzle_kv_dtype;
+#define PUZZLE_FP4_BLOCK_BYTES 576 /* one (block, KV head) of the 4-bit cache, K or V */
 
 /* bits of *dev_status */
 #define PUZZLE_DEV_BAD_BLOCK 1u  /* block-table entry outside [0, num_blocks) */
 #define PUZZLE_DEV_SEQ_TOO_LONG 2u /* seq_len > max_blocks_per_seq * block_size (clamped) */
 #define PUZZLE_DEV_WAIT_EXPIRED 4u /* a bounded wait on a copy ran out; results invalid */
+#define PUZZLE_DEV_BAD_POSITION 8u /* a token's position outside the rotation table (the token is skipped) */
 
 /* One per layer: the layer's attention choice (host struct). */
 typedef struct {
@@ -101,7 +113,7 @@ typedef struct {
                                  Entries for blocks that lie wholly outside the visible range are never read. */
   int32_t max_blocks_per_seq;
   const int32_t* seq_lens;    /* [batch], length AFTER this step's append; 0 is legal */
-  const float* k_scale;       /* [num_kv_heads] dequantisation scales (x ~= code * scale); NULL = 1; FP8 only */
+  const float* k_scale;       /* [num_kv_heads] dequantisation scales (x ~= code * scale); NULL = 1; ignored for bf16 */
   const float* v_scale;
 } puzzle_kv_view;
 
@@ -126,7 +138,8 @@ PUZZLE_API puzzle_status puzzle_kv_scales_from_amax(const float* amax, int32_t n
 
 /* Quantise-and-append of the new token's K and V (one token per sequence).
  * FP8: code = E4M3(round-to-nearest-even, saturating at +-448, of the float32
- * quotient x / scale[h]); NaN -> 0x7F.  bf16: the value is copied.  The token
+ * quotient x / scale[h]); NaN -> 0x7F.  bf16: the value is copied.  4-bit: see
+ * "4-bit cache" above.  The token
  * lands at logical position seq_lens[b]-1 through the block table.  This is
  * the FP8 KV quantisation of Section "KV Quantization" applied at decode time.
  *   k_new, v_new: bf16 [batch][num_kv_heads][head_dim].
@@ -146,6 +159,61 @@ PUZZLE_API puzzle_status puzzle_kv_append(const puzzle_layer_desc* desc, const p
 PUZZLE_API puzzle_status puzzle_kv_append_tokens(const puzzle_layer_desc* desc, const puzzle_kv_view* kv,
                                  const void* k_new, const void* v_new, const int32_t* new_lens, int32_t batch,
                                  int32_t n_new, int32_t* dev_status, void* stream);
+
+/* Position rotation of a layer's queries and keys (host struct).  Row p of the table holds the rotary_dim / 2 cosines of
+ * position p and then its rotary_dim / 2 sines, so any choice of frequencies (and a constant factor on both) is the
+ * caller's.  Channels at and beyond rotary_dim stay as they are. */
+typedef struct {
+  const float* cos_sin;      /* device [num_positions][rotary_dim], 16-byte aligned */
+  int64_t num_positions;
+  int32_t rotary_dim;        /* a multiple of 16 up to head_dim */
+  int32_t interleaved;       /* 0: channels (i, i + rotary_dim / 2) turn together; else channels (2 i, 2 i + 1) */
+  const int32_t* pos_offset; /* device [batch], added to a token's place in its cache to give its position (a cache that
+                                holds a slice of a sequence, or one whose oldest tokens were dropped); NULL = 0 */
+} puzzle_rope;
+
+/* The new tokens' queries, keys and values as a projection leaves them: bf16, row (b, i, h) of q at
+ * q + b * q_seq_stride + i * q_token_stride + h * head_dim (host struct; strides in elements, multiples of 8, not
+ * negative; pointers 16-byte aligned).  The three may be slices of one [batch][n_new][Hq + 2 Hkv][head_dim] array. */
+typedef struct {
+  const void* q; /* NULL: no queries */
+  const void* k;
+  const void* v;
+  int64_t q_seq_stride, q_token_stride;
+  int64_t k_seq_stride, k_token_stride;
+  int64_t v_seq_stride, v_token_stride;
+} puzzle_qkv;
+
+/* puzzle_kv_append_tokens with the position rotation of q and k applied on the way, in one launch: keys are rotated in
+ * float32 and quantised from there (no rounding to bf16 in between), values are quantised as they are, rotated queries
+ * are written to q_out as bf16.  (Paper: KV cache quantised as it is written, Section "KV Quantization"; the model's
+ * rotation itself is upstream of everything the paper changes.)  Token i of sequence b lands at place
+ * seq_lens[b] - new_lens[b] + i of its cache, and its position is that place plus pos_offset[b].  With the table's c
+ * and s at that position:  out[i] = x[i] c - x[j] s,  out[j] = x[j] c + x[i] s,  every product and sum rounded to
+ * float32 on its own, so that the bytes are defined to the last bit for every cache type.
+ *   q_out: device bf16 [batch][n_new][num_q_heads][head_dim], 16-byte aligned, required when qkv->q is given; it may be
+ *     qkv->q itself if that is contiguous.  Rows of tokens that are skipped are left as they were;
+ *   new_lens: as for puzzle_kv_append_tokens.  Skipped: tokens i >= new_lens[b], tokens that would land before place 0,
+ *     all of a sequence longer than its table row (PUZZLE_DEV_SEQ_TOO_LONG), tokens whose position the table does
+ *     not have (PUZZLE_DEV_BAD_POSITION).  A bad block-table entry skips the token's key and value only;
+ *   tokens of one sequence must land in different cache slots: over a ring of R blocks, at most 16 (R - 1) at a time.
+ * n_new == 1 runs a kernel laid out for latency, chunks one laid out for bandwidth; the results are the same. */
+PUZZLE_API puzzle_status puzzle_kv_append_rope(const puzzle_layer_desc* desc, const puzzle_kv_view* kv,
+                                 const puzzle_rope* rope, const puzzle_qkv* qkv, void* q_out, const int32_t* new_lens,
+                                 int32_t batch, int32_t n_new, int32_t* dev_status, void* stream);
+
+/* Cached tokens back as bf16, dequantised: the last read_lens[b] tokens of every sequence, token i from place
+ * seq_lens[b] - read_lens[b] + i.  For the attention of a prompt chunk over its own rounded keys and values, for a cache
+ * that moves to another worker, and to look into a 4-bit cache (its quantisation is that of Section "KV
+ * Quantization" taken to four bits).  value = bf16(float32(code * group scale * k_scale[h])).
+ *   k_out, v_out: device bf16 [batch][n_read][num_kv_heads][head_dim], 16-byte aligned; rows i >= read_lens[b], rows of
+ *     tokens before place 0 and rows of a sequence longer than its table row are left as they were; a bad block-table
+ *     entry gives zeros;
+ *   read_lens: device int32 [batch], clamped to [0, n_read]; NULL = n_read for every sequence.
+ * Errors and dev_status as puzzle_kv_append_tokens. */
+PUZZLE_API puzzle_status puzzle_kv_read_tokens(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, void* k_out,
+                                 void* v_out, const int32_t* read_lens, int32_t batch, int32_t n_read,
+                                 int32_t* dev_status, void* stream);
 
 /* Values of num_splits below 1: the balanced schedule, with the kernel chosen by the library or pinned. */
 #define PUZZLE_SCHED_AUTO 0

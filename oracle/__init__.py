@@ -24,6 +24,7 @@ _lib = None
 
 KV_FP8_E4M3 = 0
 KV_BF16 = 1
+KV_FP4_E2M1 = 2     # caches uint8 [num_blocks][Hkv][576]; attention only
 
 
 def build(force: bool = False) -> str:
@@ -45,6 +46,8 @@ def _load():
             lib = ctypes.CDLL(build())
             lib.oracle_e4m3_decode.restype = ctypes.c_double
             lib.oracle_e4m3_decode.argtypes = [ctypes.c_uint8]
+            lib.oracle_e2m1_decode.restype = ctypes.c_double
+            lib.oracle_e2m1_decode.argtypes = [ctypes.c_uint8]
             lib.oracle_e4m3_encode.restype = ctypes.c_uint8
             lib.oracle_e4m3_encode.argtypes = [ctypes.c_float]
             _lib = lib
@@ -72,6 +75,10 @@ def host_cores() -> int:
 
 def e4m3_decode(code: int) -> float:
     return float(_load().oracle_e4m3_decode(int(code) & 0xFF))
+
+
+def e2m1_decode(code: int) -> float:
+    return float(_load().oracle_e2m1_decode(int(code) & 0xF))
 
 
 def e4m3_encode(y: float) -> int:
@@ -119,6 +126,14 @@ def kv_append(k_cache, v_cache, kv_dtype, block_size, block_table, max_blocks_pe
     )
 
 
+def _cache_shape(cache, kv_dtype):
+    """(Hkv, block size, D) of a cache array."""
+    if kv_dtype == KV_FP4_E2M1:
+        assert cache.dtype == np.uint8 and cache.shape[2:] == (576,)
+        return cache.shape[1], 16, 64
+    return cache.shape[1:]
+
+
 def _items(items, batch, hq):
     if items is None:
         items = [(b, g) for b in range(batch) for g in range(hq)]
@@ -133,7 +148,7 @@ def decode_attn(k_cache, v_cache, kv_dtype, block_table, max_blocks_per_seq, seq
     ``items`` lists (sequence, query head) pairs; None means all, ordered
     [batch][Hq], so the result reshapes to [batch][Hq][D].
     """
-    _, hkv, bs, d = k_cache.shape
+    hkv, bs, d = _cache_shape(k_cache, kv_dtype)
     q = _arr(q, np.uint16)
     batch, hq, dq = q.shape
     assert dq == d
@@ -159,7 +174,7 @@ def decode_attn(k_cache, v_cache, kv_dtype, block_table, max_blocks_per_seq, seq
 def partial_attn(k_cache, v_cache, kv_dtype, block_table, max_blocks_per_seq, seq_lens, k_scale,
                  v_scale, q, sm_scale, t0, t1, items=None, threads=None):
     """Attention over keys [t0, t1) only, without sink: (out, lse) of one split."""
-    _, hkv, bs, d = k_cache.shape
+    hkv, bs, d = _cache_shape(k_cache, kv_dtype)
     q = _arr(q, np.uint16)
     batch, hq, _ = q.shape
     block_table = _arr(block_table, np.int32)

@@ -43,6 +43,7 @@
 
 #define ORACLE_KV_FP8_E4M3 0
 #define ORACLE_KV_BF16 1
+#define ORACLE_KV_FP4_E2M1 2 /* attention only */
 
 /* ---------------------------------------------------------------- bf16 --- */
 
@@ -210,8 +211,33 @@ typedef struct {
   pthread_mutex_t lock;
 } attn_job;
 
-static double cache_value(const void* cache, int kv_dtype, int64_t idx, double scale) {
-  if (kv_dtype == ORACLE_KV_BF16) return (double)bf16_bits_to_float(((const uint16_t*)cache)[idx]);
+/* 4-bit cache: value of channel d of token `slot` of one (block, head) of 576 bytes, 512 bytes of E2M1 codes and then
+ * one E4M3 scale per 16 channels of a token.  E2M1: sign, two exponent bits (bias 1), one fraction bit. */
+double oracle_e2m1_decode(uint8_t code) {
+  int e = (code >> 1) & 3, m = code & 1;
+  double v = e == 0 ? 0.5 * m : ldexp(1.0 + 0.5 * m, e - 1);
+  return (code & 8) ? -v : v;
+}
+static double fp4_value(const uint8_t* p, int is_v, int slot, int d) {
+  int byte, odd, at;
+  if (is_v) {
+    byte = 256 * (d / 32) + 32 * (slot / 2) + d % 32;
+    odd = slot % 2;
+    at = 16 * (d / 16) + 4 * ((slot % 8) / 2) + 2 * (slot / 8) + slot % 2;
+  } else {
+    byte = 32 * slot + d / 2;
+    odd = d % 2;
+    at = 16 * (d / 16) + 2 * (slot % 8) + slot / 8;
+  }
+  return oracle_e2m1_decode((uint8_t)((p[byte] >> (4 * odd)) & 15)) * oracle_e4m3_decode(p[512 + at]);
+}
+
+static double cache_value(const attn_job* J, int is_v, int64_t block, int h, int slot, int d, double scale) {
+  const void* cache = is_v ? J->v_cache : J->k_cache;
+  int64_t idx = cache_index(block, J->Hkv, J->block_size, J->D, h, slot, d);
+  if (J->kv_dtype == ORACLE_KV_BF16) return (double)bf16_bits_to_float(((const uint16_t*)cache)[idx]);
+  if (J->kv_dtype == ORACLE_KV_FP4_E2M1)
+    return fp4_value((const uint8_t*)cache + (block * J->Hkv + h) * 576, is_v, slot, d) * scale;
   return oracle_e4m3_decode(((const uint8_t*)cache)[idx]) * scale;
 }
 
@@ -222,8 +248,8 @@ static void attend_one(const attn_job* J, int b, int g, double* out, double* lse
   int h = g / (J->Hq / J->Hkv); /* grouped-query: consecutive query heads share a KV head */
   int64_t L = J->seq_lens[b];
   int64_t lo, hi;
-  double ks = (J->k_scale && J->kv_dtype == ORACLE_KV_FP8_E4M3) ? (double)J->k_scale[h] : 1.0;
-  double vs = (J->v_scale && J->kv_dtype == ORACLE_KV_FP8_E4M3) ? (double)J->v_scale[h] : 1.0;
+  double ks = (J->k_scale && J->kv_dtype != ORACLE_KV_BF16) ? (double)J->k_scale[h] : 1.0;
+  double vs = (J->v_scale && J->kv_dtype != ORACLE_KV_BF16) ? (double)J->v_scale[h] : 1.0;
   double sink = -INFINITY;
   double M, Z;
   double* s;
@@ -246,8 +272,7 @@ static void attend_one(const attn_job* J, int b, int g, double* out, double* lse
     double dot = 0.0;
     for (int d = 0; d < D; d++) {
       double qd = (double)bf16_bits_to_float(J->q[((int64_t)b * J->Hq + g) * D + d]);
-      double kd = cache_value(J->k_cache, J->kv_dtype,
-                              cache_index(block, J->Hkv, J->block_size, D, h, slot, d), ks);
+      double kd = cache_value(J, 0, block, h, slot, d, ks);
       dot += qd * kd;
     }
     s[j - lo] = dot * J->sm_scale;
@@ -266,8 +291,7 @@ static void attend_one(const attn_job* J, int b, int g, double* out, double* lse
     double p = exp(s[j - lo] - M);
     Z += p;
     for (int d = 0; d < D; d++)
-      out[d] += p * cache_value(J->v_cache, J->kv_dtype,
-                                cache_index(block, J->Hkv, J->block_size, D, h, slot, d), vs);
+      out[d] += p * cache_value(J, 1, block, h, slot, d, vs);
   }
   for (int d = 0; d < D; d++) out[d] /= Z;
   *lse_out = M + log(Z);

@@ -13,9 +13,12 @@ _lib = None
 
 KV_FP8_E4M3 = 0
 KV_BF16 = 1
+KV_FP4_E2M1 = 2
+FP4_BLOCK_BYTES = 576          # one (block, KV head) of the 4-bit cache: a cache is uint8 [num_blocks][Hkv][576]
 DEV_BAD_BLOCK = 1
 DEV_SEQ_TOO_LONG = 2
 DEV_WAIT_EXPIRED = 4
+DEV_BAD_POSITION = 8
 STATIC_SCRATCH_BYTES = 8 << 20
 SCHED_AUTO, SCHED_CTA, SCHED_WARP = 0, -1, -2      # num_splits values that select the balanced schedule
 
@@ -24,6 +27,8 @@ EXPORTS = (
     "puzzle_kv_scales_from_amax",
     "puzzle_kv_append",
     "puzzle_kv_append_tokens",
+    "puzzle_kv_append_rope",
+    "puzzle_kv_read_tokens",
     "puzzle_decode_attn_workspace_bytes",
     "puzzle_decode_attn_workspace_init",
     "puzzle_decode_attn",
@@ -62,6 +67,16 @@ class KVView(ctypes.Structure):
                 ("seq_lens", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
+class Rope(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("num_positions", ctypes.c_int64), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("pos_offset", ctypes.c_void_p)]
+
+
+class QKV(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
+        [(t + which, ctypes.c_int64) for t in "qkv" for which in ("_seq_stride", "_token_stride")]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -84,6 +99,12 @@ def _load():
         lib.puzzle_kv_append_tokens.restype = ctypes.c_int
         lib.puzzle_kv_append_tokens.argtypes = [ctypes.POINTER(LayerDesc), ctypes.POINTER(KVView), vp, vp, vp, i32, i32,
                                                 vp, vp]
+        lib.puzzle_kv_append_rope.restype = ctypes.c_int
+        lib.puzzle_kv_append_rope.argtypes = [ctypes.POINTER(LayerDesc), ctypes.POINTER(KVView), ctypes.POINTER(Rope),
+                                              ctypes.POINTER(QKV), vp, vp, i32, i32, vp, vp]
+        lib.puzzle_kv_read_tokens.restype = ctypes.c_int
+        lib.puzzle_kv_read_tokens.argtypes = [ctypes.POINTER(LayerDesc), ctypes.POINTER(KVView), vp, vp, vp, i32, i32,
+                                              vp, vp]
         lib.puzzle_decode_attn_workspace_bytes.restype = sz
         lib.puzzle_decode_attn_workspace_bytes.argtypes = [ctypes.POINTER(LayerDesc), i32, i32]
         lib.puzzle_decode_attn_workspace_init.restype = ctypes.c_int
@@ -156,7 +177,8 @@ def layer_desc(window: int = 0, kv_dtype: int = KV_FP8_E4M3, num_q_heads: int = 
 def kv_view(k_cache: torch.Tensor, v_cache: torch.Tensor, seq_lens: torch.Tensor,
             block_table: Optional[torch.Tensor] = None, max_blocks_per_seq: Optional[int] = None,
             k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None) -> KVView:
-    """Describe one layer's cache ([num_blocks][Hkv][16][D], uint8 codes or bf16) for this batch.
+    """Describe one layer's cache ([num_blocks][Hkv][16][D], uint8 codes or bf16; 4-bit: uint8
+    [num_blocks][Hkv][FP4_BLOCK_BYTES]) for this batch.
 
     The view holds raw pointers: keep the tensors alive while it is in use."""
     if block_table is not None:
@@ -235,6 +257,68 @@ def puzzle_kv_append_tokens(desc: LayerDesc, view: KVView, k_new: torch.Tensor, 
                                            _p(v_new, torch.bfloat16, "v_new"), _p(new_lens, torch.int32, "new_lens"),
                                            batch, n_new, _p(dev_status, torch.int32), _stream(stream)),
            "puzzle_kv_append_tokens")
+
+
+def rope_view(cos_sin: torch.Tensor, interleaved: bool = False, pos_offset: Optional[torch.Tensor] = None) -> Rope:
+    """Describe a rotation table: float32 [num_positions][rotary_dim], the cosines of a position and then its sines
+    (``rope_table`` makes one); pos_offset: int32 [batch] or None.  Keep the tensors alive while the view is in use."""
+    r = Rope()
+    r.cos_sin = _p(cos_sin, torch.float32, "cos_sin")
+    r.num_positions, r.rotary_dim = cos_sin.shape
+    r.interleaved = int(bool(interleaved))
+    r.pos_offset = _p(pos_offset, torch.int32, "pos_offset")
+    return r
+
+
+def _qkv(q, k, v) -> QKV:
+    x = QKV()
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if t is None:
+            continue
+        if not t.is_cuda or t.dtype != torch.bfloat16:
+            raise ValueError("%s must be a bf16 CUDA tensor" % name)
+        if t.dim() not in (3, 4):
+            raise ValueError("%s must be [batch][n_new][heads][D] or [batch][heads][D]" % name)
+        if t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != t.shape[-1]):
+            raise ValueError("the heads of a token of %s must be contiguous" % name)
+        setattr(x, name, t.data_ptr())
+        setattr(x, name + "_seq_stride", t.stride(0))
+        setattr(x, name + "_token_stride", t.stride(1) if t.dim() == 4 else 0)
+    return x
+
+
+def puzzle_kv_append_rope(desc: LayerDesc, view: KVView, rope: Rope, q: Optional[torch.Tensor], k_new: torch.Tensor,
+                          v_new: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+                          new_lens: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                          stream=None) -> None:
+    """q, k_new, v_new: bf16 [batch][n_new][heads][D] (or [batch][heads][D] for one token each), contiguous or slices
+    of a wider array along the heads; q_out: bf16 [batch][n_new][Hq][D] contiguous, may be q; q None: k and v only."""
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    shape = k_new.shape[:-2]
+    for name, t, heads in (("q", q, desc.num_q_heads), ("k_new", k_new, desc.num_kv_heads),
+                           ("v_new", v_new, desc.num_kv_heads), ("q_out", q_out, desc.num_q_heads)):
+        if t is not None and tuple(t.shape) != (*shape, heads, desc.head_dim):
+            raise ValueError("%s must be %s, got %s" % (name, (*shape, heads, desc.head_dim), tuple(t.shape)))
+    qkv = _qkv(q, k_new, v_new)
+    _check(_load().puzzle_kv_append_rope(ctypes.byref(desc), ctypes.byref(view), ctypes.byref(rope), ctypes.byref(qkv),
+                                         _p(q_out, torch.bfloat16, "q_out"), _p(new_lens, torch.int32, "new_lens"),
+                                         shape[0], shape[1] if len(shape) == 2 else 1, _p(dev_status, torch.int32),
+                                         _stream(stream)), "puzzle_kv_append_rope")
+
+
+def puzzle_kv_read_tokens(desc: LayerDesc, view: KVView, k_out: torch.Tensor, v_out: torch.Tensor,
+                          read_lens: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                          stream=None) -> None:
+    """k_out, v_out: bf16 [batch][n_read][Hkv][D]; read_lens: int32 [batch] or None (n_read tokens of every sequence)."""
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        if t.dim() != 4 or t.shape[:2] != k_out.shape[:2] or tuple(t.shape[2:]) != (desc.num_kv_heads, desc.head_dim):
+            raise ValueError("%s must be [batch][n_read][%d][%d]" % (name, desc.num_kv_heads, desc.head_dim))
+    batch, n_read = k_out.shape[0], k_out.shape[1]
+    _check(_load().puzzle_kv_read_tokens(ctypes.byref(desc), ctypes.byref(view), _p(k_out, torch.bfloat16, "k_out"),
+                                         _p(v_out, torch.bfloat16, "v_out"), _p(read_lens, torch.int32, "read_lens"),
+                                         batch, n_read, _p(dev_status, torch.int32), _stream(stream)),
+           "puzzle_kv_read_tokens")
 
 
 def puzzle_decode_attn_tokens_workspace_bytes(desc: LayerDesc, batch: int, n_q: int) -> int:

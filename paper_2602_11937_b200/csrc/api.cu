@@ -49,7 +49,8 @@ puzzle_status check_desc(const puzzle_layer_desc* d) {
   if (d->num_q_heads <= 0 || d->num_kv_heads <= 0 || d->head_dim <= 0 || d->block_size <= 0 || d->window < 0)
     return PUZZLE_ERR_SHAPE;
   if (d->num_q_heads % d->num_kv_heads != 0) return PUZZLE_ERR_SHAPE;
-  if (d->kv_dtype != PUZZLE_KV_FP8_E4M3 && d->kv_dtype != PUZZLE_KV_BF16) return PUZZLE_ERR_SHAPE;
+  if (d->kv_dtype != PUZZLE_KV_FP8_E4M3 && d->kv_dtype != PUZZLE_KV_BF16 && d->kv_dtype != PUZZLE_KV_FP4_E2M1)
+    return PUZZLE_ERR_SHAPE;
   if (d->head_dim != kHeadDim || d->block_size != kBlock || d->num_q_heads != kGroup * d->num_kv_heads)
     return PUZZLE_ERR_UNSUPPORTED;
   return PUZZLE_OK;
@@ -91,6 +92,41 @@ bool make_cache_map(CUtensorMap* m, void* base, long long rows, int elem_bytes, 
                    dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// The parameters of an append that the descriptors hold; the rest is set by the entry points.
+AppendParams append_params(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int batch, int n_new,
+                           const int32_t* new_lens, int32_t* dev_status) {
+  AppendParams A;
+  std::memset(&A, 0, sizeof A);
+  A.k_cache = kv->k_cache;
+  A.v_cache = kv->v_cache;
+  A.block_table = kv->block_table;
+  A.seq_lens = kv->seq_lens;
+  A.new_lens = new_lens;
+  A.k_scale = kv->k_scale;
+  A.v_scale = kv->v_scale;
+  A.dev_status = dev_status;
+  A.num_blocks = kv->num_blocks;
+  A.batch = batch;
+  A.n_new = n_new;
+  A.Hq = d->num_q_heads;
+  A.Hkv = d->num_kv_heads;
+  A.max_blocks_per_seq = kv->max_blocks_per_seq;
+  return A;
+}
+
+// The plain append of contiguous k_new, v_new [batch][n_new][Hkv][D] to a 4-bit cache.
+cudaError_t append_fp4(const puzzle_layer_desc* d, const puzzle_kv_view* kv, const void* k_new, const void* v_new,
+                       const int32_t* new_lens, int batch, int n_new, int32_t* dev_status, cudaStream_t s) {
+  AppendParams A = append_params(d, kv, batch, n_new, new_lens, dev_status);
+  A.k = static_cast<const __nv_bfloat16*>(k_new);
+  A.v = static_cast<const __nv_bfloat16*>(v_new);
+  A.k_token_stride = A.v_token_stride = (long long)d->num_kv_heads * d->head_dim;
+  A.k_seq_stride = A.v_seq_stride = A.k_token_stride * n_new;
+  return launch_append(A, d->kv_dtype, false, false, s);
 }
 
 int grid_ctas() { return device_info().sm_count > 0 ? device_info().sm_count : 1; }
@@ -174,6 +210,7 @@ puzzle_status check_decode_attn_args(const puzzle_layer_desc* desc, const puzzle
   if ((reinterpret_cast<uintptr_t>(q) & 7) || (reinterpret_cast<uintptr_t>(out) & 15)) return PUZZLE_ERR_SHAPE;
   if (num_splits == PUZZLE_SCHED_CTA && (tcgen05 || batch > kCtaMaxBatch)) return PUZZLE_ERR_UNSUPPORTED;
   if (tcgen05 && desc->kv_dtype != PUZZLE_KV_FP8_E4M3) return PUZZLE_ERR_UNSUPPORTED;   // that kernel reads E4M3 codes only
+  if (desc->kv_dtype == PUZZLE_KV_FP4_E2M1) return PUZZLE_ERR_UNSUPPORTED;
   return PUZZLE_OK;
 }
 
@@ -215,6 +252,12 @@ puzzle_status puzzle_kv_append(const puzzle_layer_desc* desc, const puzzle_kv_vi
   st = check_view(desc, kv, batch);
   if (st != PUZZLE_OK) return st;
   if (!k_new || !v_new) return PUZZLE_ERR_NULL;
+  if (desc->kv_dtype == PUZZLE_KV_FP4_E2M1) {
+    if (!aligned16(k_new) || !aligned16(v_new)) return PUZZLE_ERR_SHAPE;
+    const cudaError_t e = append_fp4(desc, kv, k_new, v_new, nullptr, batch, 1, dev_status, static_cast<cudaStream_t>(stream));
+    count_launch();
+    return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
+  }
   const long long threads = 2ll * batch * desc->num_kv_heads * (kHeadDim / 2);
   const int grid = (int)((threads + 255) / 256);
   const cudaError_t e = launch_dependent(
@@ -238,12 +281,93 @@ puzzle_status puzzle_kv_append_tokens(const puzzle_layer_desc* desc, const puzzl
   if ((reinterpret_cast<uintptr_t>(k_new) & 15) || (reinterpret_cast<uintptr_t>(v_new) & 15)) return PUZZLE_ERR_SHAPE;
   const long long per_seq = (long long)n_new * desc->num_kv_heads * (kHeadDim / 8);
   if (per_seq > 0x7fffffffll || batch > 65535) return PUZZLE_ERR_SHAPE;
+  if (desc->kv_dtype == PUZZLE_KV_FP4_E2M1) {
+    const cudaError_t e = append_fp4(desc, kv, k_new, v_new, new_lens, batch, n_new, dev_status,
+                                     static_cast<cudaStream_t>(stream));
+    count_launch();
+    return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
+  }
   const dim3 grid((unsigned)((per_seq + 255) / 256), (unsigned)batch, 2);
   const cudaError_t e = launch_dependent(
       kv_append_tokens_kernel, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), kv->k_cache, kv->v_cache,
       static_cast<const uint4*>(k_new), static_cast<const uint4*>(v_new), new_lens, kv->block_table, kv->seq_lens,
       kv->k_scale, kv->v_scale, kv->num_blocks, batch, n_new, desc->num_kv_heads, kv->max_blocks_per_seq,
       desc->kv_dtype, dev_status);
+  count_launch();
+  return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
+}
+
+puzzle_status puzzle_kv_append_rope(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const puzzle_rope* rope,
+                                    const puzzle_qkv* qkv, void* q_out, const int32_t* new_lens, int32_t batch,
+                                    int32_t n_new, int32_t* dev_status, void* stream) {
+  puzzle_status st = check_desc(desc);
+  if (st != PUZZLE_OK) return st;
+  st = check_view(desc, kv, batch);
+  if (st != PUZZLE_OK) return st;
+  if (!rope || !rope->cos_sin || !qkv || !qkv->k || !qkv->v || (qkv->q && !q_out)) return PUZZLE_ERR_NULL;
+  if (n_new <= 0 || n_new > (1 << 20) || rope->num_positions <= 0) return PUZZLE_ERR_SHAPE;
+  if (rope->rotary_dim <= 0 || rope->rotary_dim > desc->head_dim) return PUZZLE_ERR_SHAPE;
+  if (rope->rotary_dim % 16) return PUZZLE_ERR_UNSUPPORTED;
+  if (!aligned16(rope->cos_sin) || !aligned16(qkv->q) || !aligned16(qkv->k) || !aligned16(qkv->v) ||
+      (qkv->q && !aligned16(q_out)))
+    return PUZZLE_ERR_SHAPE;
+  const int64_t strides[6] = {qkv->q_seq_stride, qkv->q_token_stride, qkv->k_seq_stride,
+                              qkv->k_token_stride, qkv->v_seq_stride, qkv->v_token_stride};
+  for (int i = qkv->q ? 0 : 2; i < 6; ++i)
+    if (strides[i] < 0 || strides[i] % 8) return PUZZLE_ERR_SHAPE;   // rows are read 16 bytes at a time
+  // in place: every row has to lie where its rotated form goes, or one row would overwrite another before it is read
+  const int64_t row = (int64_t)desc->num_q_heads * desc->head_dim;
+  if (qkv->q && q_out == qkv->q &&
+      ((n_new > 1 && qkv->q_token_stride != row) || (batch > 1 && qkv->q_seq_stride != row * n_new)))
+    return PUZZLE_ERR_SHAPE;
+  AppendParams A = append_params(desc, kv, batch, n_new, new_lens, dev_status);
+  A.q = static_cast<const __nv_bfloat16*>(qkv->q);
+  A.k = static_cast<const __nv_bfloat16*>(qkv->k);
+  A.v = static_cast<const __nv_bfloat16*>(qkv->v);
+  A.q_seq_stride = qkv->q_seq_stride;
+  A.q_token_stride = qkv->q_token_stride;
+  A.k_seq_stride = qkv->k_seq_stride;
+  A.k_token_stride = qkv->k_token_stride;
+  A.v_seq_stride = qkv->v_seq_stride;
+  A.v_token_stride = qkv->v_token_stride;
+  A.q_out = static_cast<__nv_bfloat16*>(q_out);
+  A.pos_offset = rope->pos_offset;
+  A.cos_sin = rope->cos_sin;
+  A.num_positions = rope->num_positions;
+  A.rotary = rope->rotary_dim;
+  const cudaError_t e =
+      launch_append(A, desc->kv_dtype, true, rope->interleaved != 0, static_cast<cudaStream_t>(stream));
+  count_launch();
+  return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
+}
+
+puzzle_status puzzle_kv_read_tokens(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, void* k_out, void* v_out,
+                                    const int32_t* read_lens, int32_t batch, int32_t n_read, int32_t* dev_status,
+                                    void* stream) {
+  puzzle_status st = check_desc(desc);
+  if (st != PUZZLE_OK) return st;
+  st = check_view(desc, kv, batch);
+  if (st != PUZZLE_OK) return st;
+  if (!k_out || !v_out) return PUZZLE_ERR_NULL;
+  if (n_read <= 0 || n_read > (1 << 24) || !aligned16(k_out) || !aligned16(v_out)) return PUZZLE_ERR_SHAPE;
+  ReadParams R;
+  std::memset(&R, 0, sizeof R);
+  R.k_cache = kv->k_cache;
+  R.v_cache = kv->v_cache;
+  R.block_table = kv->block_table;
+  R.seq_lens = kv->seq_lens;
+  R.read_lens = read_lens;
+  R.k_scale = kv->k_scale;
+  R.v_scale = kv->v_scale;
+  R.k_out = static_cast<__nv_bfloat16*>(k_out);
+  R.v_out = static_cast<__nv_bfloat16*>(v_out);
+  R.dev_status = dev_status;
+  R.num_blocks = kv->num_blocks;
+  R.batch = batch;
+  R.n_read = n_read;
+  R.Hkv = desc->num_kv_heads;
+  R.max_blocks_per_seq = kv->max_blocks_per_seq;
+  const cudaError_t e = launch_read_tokens(R, desc->kv_dtype, static_cast<cudaStream_t>(stream));
   count_launch();
   return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
 }

@@ -103,6 +103,32 @@ __global__ void kv_append_tokens_kernel(void* k_cache, void* v_cache, const uint
                                         int n_new, int Hkv, int max_blocks_per_seq, int kv_dtype, int32_t* dev_status);
 __global__ void hbm_read_probe_kernel(const uint4* buf, size_t n16, unsigned long long* sink);
 
+// Appends with the position rotation of q and k, and all appends to the 4-bit cache (kv_rope.cu); q null: no queries.
+struct AppendParams {
+  const __nv_bfloat16 *q, *k, *v;
+  long long q_seq_stride, q_token_stride, k_seq_stride, k_token_stride, v_seq_stride, v_token_stride;   // in elements
+  __nv_bfloat16* q_out;
+  void *k_cache, *v_cache;
+  const int32_t *block_table, *seq_lens, *new_lens, *pos_offset;
+  const float *k_scale, *v_scale, *cos_sin;
+  int32_t* dev_status;
+  long long num_blocks, num_positions;
+  int batch, n_new, Hq, Hkv, max_blocks_per_seq, rotary;
+};
+cudaError_t launch_append(const AppendParams& P, int kv_dtype, bool rotate, bool adjacent, cudaStream_t s);
+
+// Cached tokens back as bf16 (kv_read.cu).
+struct ReadParams {
+  const void *k_cache, *v_cache;
+  const int32_t *block_table, *seq_lens, *read_lens;
+  const float *k_scale, *v_scale;
+  __nv_bfloat16 *k_out, *v_out;
+  int32_t* dev_status;
+  long long num_blocks;
+  int batch, n_read, Hkv, max_blocks_per_seq;
+};
+cudaError_t launch_read_tokens(const ReadParams& P, int kv_dtype, cudaStream_t s);
+
 // Max calibration (calibrate.cu).
 cudaError_t launch_amax_update(const void* x, long long n_tokens, int Hkv, int D, float* amax, int sm_count,
                                cudaStream_t s);
