@@ -32,8 +32,9 @@ EncodeTiledFn encode_tiled() {
 
 struct DeviceInfo {
   int sm_count = 0;
-  // per split-KV kernel (warp-scheduled FP8, bf16; tensor-memory FP8; CTA-balanced FP8, bf16); 0 = not raised yet
-  int smem_limit[8] = {0, 0, 0, 0, 0, 0, 0, 0};   // [5]: the multi-token kernel, [6..7]: the small-launch kernel
+  // dynamic shared-memory limits already set per kernel and cache type; 0 = not raised yet
+  int smem_warp[3] = {0, 0, 0}, smem_cta[3] = {0, 0, 0}, smem_small[3] = {0, 0, 0};
+  int smem_tc = 0, smem_tokens = 0;
 };
 DeviceInfo& device_info() {
   static DeviceInfo info[64];
@@ -131,7 +132,12 @@ cudaError_t append_fp4(const puzzle_layer_desc* d, const puzzle_kv_view* kv, con
 
 int grid_ctas() { return device_info().sm_count > 0 ? device_info().sm_count : 1; }
 
-int decode_warps(int kv_dtype) { return kv_dtype == PUZZLE_KV_FP8_E4M3 ? kDecodeWarpsFp8 : kDecodeWarpsBf16; }
+int decode_warps(int kv_dtype) {
+  return kv_dtype == PUZZLE_KV_FP8_E4M3 ? kDecodeWarpsFp8 : (kv_dtype == PUZZLE_KV_BF16 ? kDecodeWarpsBf16 : kDecodeWarpsFp4);
+}
+int tile_tokens(int kv_dtype) {
+  return kv_dtype == PUZZLE_KV_FP8_E4M3 ? kTileFp8 : (kv_dtype == PUZZLE_KV_BF16 ? kTileBf16 : kTileFp4);
+}
 
 // The workspace starts with the CTA-speed words of the CTA-balanced kernel, then one arrival counter per (sequence,
 // KV head), then the partials.  Every completed call leaves the arrival counters at zero.  The counter block has room
@@ -151,7 +157,7 @@ size_t counter_bytes(int batch, int Hkv) {
 // what the host knows: the window, or the length of a block-table row.
 // Upper bound on the tiles of one (sequence, KV head) from what the host knows.
 long long tiles_per_pair_bound(const puzzle_layer_desc* d, const puzzle_kv_view* kv) {
-  const int tt = d->kv_dtype == PUZZLE_KV_FP8_E4M3 ? kTileFp8 : kTileBf16;
+  const int tt = tile_tokens(d->kv_dtype);
   long long per_pair = ((long long)kv->max_blocks_per_seq * kBlock + tt - 1) / tt;
   if (d->window > 0) per_pair = std::min<long long>(per_pair, (d->window + tt - 1) / tt + 1);
   return per_pair;
@@ -210,7 +216,6 @@ puzzle_status check_decode_attn_args(const puzzle_layer_desc* desc, const puzzle
   if ((reinterpret_cast<uintptr_t>(q) & 7) || (reinterpret_cast<uintptr_t>(out) & 15)) return PUZZLE_ERR_SHAPE;
   if (num_splits == PUZZLE_SCHED_CTA && (tcgen05 || batch > kCtaMaxBatch)) return PUZZLE_ERR_UNSUPPORTED;
   if (tcgen05 && desc->kv_dtype != PUZZLE_KV_FP8_E4M3) return PUZZLE_ERR_UNSUPPORTED;   // that kernel reads E4M3 codes only
-  if (desc->kv_dtype == PUZZLE_KV_FP4_E2M1) return PUZZLE_ERR_UNSUPPORTED;
   return PUZZLE_OK;
 }
 
@@ -385,7 +390,6 @@ static puzzle_status decode_attn_impl(const puzzle_layer_desc* desc, const puzzl
   puzzle_status st = check_decode_attn_args(desc, kv, q, out, batch, num_splits, tcgen05);
   if (st != PUZZLE_OK) return st;
   const int Hkv = desc->num_kv_heads;
-  const bool fp8 = desc->kv_dtype == PUZZLE_KV_FP8_E4M3;
   const size_t cbytes = counter_bytes(batch, Hkv);
   const int splits = num_splits > 0 ? num_splits : 0;   // the kernels know explicit splits (S) and balanced (0)
   const size_t pfloats = workspace_floats(batch, Hkv, splits, desc->kv_dtype);
@@ -400,14 +404,22 @@ static puzzle_status decode_attn_impl(const puzzle_layer_desc* desc, const puzzl
 
   DecodeParams P;
   std::memset(&P, 0, sizeof P);
-  const int eb = fp8 ? 1 : 2;
   const bool tc = tcgen05;
-  const int row_bytes = tc ? 64 : 128;
-  const int rows_per_block = kBlock * kHeadDim * eb / row_bytes;
-  const long long cache_rows = kv->num_blocks * Hkv * (long long)rows_per_block;
-  if (!make_cache_map(&P.tmK, kv->k_cache, cache_rows, eb, row_bytes) ||
-      !make_cache_map(&P.tmV, kv->v_cache, cache_rows, eb, row_bytes))
-    return PUZZLE_ERR_CUDA;
+  if (desc->kv_dtype == PUZZLE_KV_FP4_E2M1) {
+    P.k_cache = static_cast<const uint8_t*>(kv->k_cache);
+    P.v_cache = static_cast<const uint8_t*>(kv->v_cache);
+    P.rows_per_block = 1;
+    P.oob_row = -1;
+  } else {
+    const int eb = desc->kv_dtype == PUZZLE_KV_FP8_E4M3 ? 1 : 2;
+    const int row_bytes = tc ? 64 : 128;
+    P.rows_per_block = kBlock * kHeadDim * eb / row_bytes;
+    const long long cache_rows = kv->num_blocks * Hkv * (long long)P.rows_per_block;
+    P.oob_row = (int)cache_rows;
+    if (!make_cache_map(&P.tmK, kv->k_cache, cache_rows, eb, row_bytes) ||
+        !make_cache_map(&P.tmV, kv->v_cache, cache_rows, eb, row_bytes))
+      return PUZZLE_ERR_CUDA;
+  }
   P.q = static_cast<const __nv_bfloat16*>(q);
   P.block_table = kv->block_table;
   P.seq_lens = kv->seq_lens;
@@ -428,27 +440,25 @@ static puzzle_status decode_attn_impl(const puzzle_layer_desc* desc, const puzzl
   P.max_blocks_per_seq = kv->max_blocks_per_seq;
   P.window = desc->window;
   P.num_splits = splits;
-  P.oob_row = (int)cache_rows;
-  P.rows_per_block = rows_per_block;
   P.sm_scale_log2e = desc->sm_scale * 1.4426950408889634f;
 
   cudaError_t le;
   if (tc) {
-    le = launch_decode_attn_tc(P, ctas, s, device_info().smem_limit + 2);
+    le = launch_decode_attn_tc(P, ctas, s, &device_info().smem_tc);
   } else {
     switch (pick_kernel(desc, kv, batch, num_splits)) {
       case Kernel::kCta:
-        le = launch_decode_attn_cta(P, fp8, ctas, s, device_info().smem_limit + 3);
+        le = launch_decode_attn_cta(P, desc->kv_dtype, ctas, s, device_info().smem_cta);
         break;
       case Kernel::kSmall:
-        le = launch_decode_attn_small(P, fp8, ctas, s, device_info().smem_limit + 6);
+        le = launch_decode_attn_small(P, desc->kv_dtype, ctas, s, device_info().smem_small);
         break;
       case Kernel::kWarpWholePairs:
         P.num_splits = 1;
-        le = launch_decode_attn(P, fp8, ctas, s, device_info().smem_limit);
+        le = launch_decode_attn(P, desc->kv_dtype, ctas, s, device_info().smem_warp);
         break;
       default:
-        le = launch_decode_attn(P, fp8, ctas, s, device_info().smem_limit);
+        le = launch_decode_attn(P, desc->kv_dtype, ctas, s, device_info().smem_warp);
     }
   }
   if (le != cudaSuccess) return PUZZLE_ERR_CUDA;
@@ -597,7 +607,7 @@ puzzle_status puzzle_decode_attn_tokens(const puzzle_layer_desc* desc, const puz
   P.oob_row = (int)cache_rows;
   P.rows_per_block = kBlock * kHeadDim / 128;
   P.sm_scale_log2e = desc->sm_scale * 1.4426950408889634f;
-  if (launch_decode_attn_tokens(P, grid_ctas(), static_cast<cudaStream_t>(stream), device_info().smem_limit + 5) !=
+  if (launch_decode_attn_tokens(P, grid_ctas(), static_cast<cudaStream_t>(stream), &device_info().smem_tokens) !=
       cudaSuccess)
     return PUZZLE_ERR_CUDA;
   count_launch();

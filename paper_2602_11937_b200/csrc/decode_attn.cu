@@ -1,4 +1,5 @@
-// Split-KV decode attention over a paged KV cache (FP8 E4M3 codes, or bf16), sm_100a: the warp-scheduled kernel.
+// Split-KV decode attention over a paged KV cache (FP8 E4M3 codes, bf16, or 4-bit codes), sm_100a: the warp-scheduled
+// kernel.
 //
 // The paper's long-context decode is bound by KV-cache I/O (Section "Optimized
 // Scenarios"); FP8 KV halves those bytes (Section "KV Quantization") and window
@@ -30,6 +31,7 @@
 #include "decode_attn.cuh"
 #include "decode_sched.cuh"
 #include "decode_tile.cuh"
+#include "decode_tile_fp4.cuh"
 
 namespace puzzle {
 
@@ -69,7 +71,7 @@ struct Producer {
     lookup(P, lane);
   }
   // Issues the pending tile into `stage_addr` and looks the next one up.  Returns false if nothing was pending.
-  template <int BLOCK_BYTES>
+  template <typename F>
   __device__ __forceinline__ bool issue(const DecodeParams& P, const int* cum, const int* lens, int w, int lane,
                                         uint32_t stage_addr, uint32_t bar) {
     if (!ok) return false;
@@ -87,11 +89,8 @@ struct Producer {
 #pragma unroll
     for (int i = 0; i < NB; ++i) rows[i] = __shfl_sync(0xffffffffu, row, i);
     if (elect_one()) {
-      mbar_arrive_expect_tx(bar, 2 * NB * BLOCK_BYTES);
-#pragma unroll
-      for (int i = 0; i < NB; ++i) tma_load_2d(stage_addr + i * BLOCK_BYTES, &P.tmK, 0, rows[i], bar);
-#pragma unroll
-      for (int i = 0; i < NB; ++i) tma_load_2d(stage_addr + (NB + i) * BLOCK_BYTES, &P.tmV, 0, rows[i], bar);
+      mbar_arrive_expect_tx(bar, 2 * NB * F::kBlockBytes);
+      F::template load_tile<NB>(P, stage_addr, rows, bar);
     }
     if (++seg.t == seg.t_end) {
       ok = next_segment<TT>(cur, seg, P, cum, lens, w);
@@ -104,12 +103,11 @@ struct Producer {
 
 }  // namespace
 
-// NW warps per CTA, NS stages per warp, TT tokens per tile; FP8 selects the E4M3 cache (else bf16).
-template <int NW, int NS, int TT, bool FP8>
+// NW warps per CTA, NS stages per warp, TT tokens per tile; F: the cache type (SwizzledTile or Fp4Tile).
+template <int NW, int NS, int TT, typename F>
 __global__ void __launch_bounds__(NW * 32, 1) decode_attn_kernel(const __grid_constant__ DecodeParams P) {
   constexpr int NB = TT / kBlock;                       // blocks per tile
-  constexpr int EB = FP8 ? 1 : 2;                       // bytes per cache element
-  constexpr int BLOCK_BYTES = kBlock * kHeadDim * EB;   // one (block, KV head): 1 KiB or 2 KiB
+  constexpr int BLOCK_BYTES = F::kBlockBytes;
   constexpr int STAGE_BYTES = 2 * NB * BLOCK_BYTES;
   constexpr int PIPE_BYTES = NW * NS * STAGE_BYTES;
 
@@ -129,10 +127,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_kernel(const __grid_co
     for (int i = 0; i < NS; ++i) mbar_init(bars + 8 * i, 1);
     fence_mbar_init();
   }
-  if (threadIdx.x == 0) {
-    tma_prefetch_desc(&P.tmK);
-    tma_prefetch_desc(&P.tmV);
-  }
+  if (threadIdx.x == 0) F::prefetch(P);
   release_dependents();
   grid_dependency_wait();   // nothing above reads or writes global memory
   build_schedule(cum, lens, P.seq_lens, P.batch, P.Hkv, P.window, P.max_blocks_per_seq * kBlock, TT, P.dev_status);
@@ -159,7 +154,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_kernel(const __grid_co
     cc.step = 1;
   }
 
-  LaneOffsets<FP8> lo;
+  typename F::Lanes lo;
   lo.init(lane);
 
   Producer<TT> prod;
@@ -167,7 +162,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_kernel(const __grid_co
   int inflight = 0;
 #pragma unroll 1
   for (int i = 0; i < NS; ++i)
-    if (prod.template issue<BLOCK_BYTES>(P, cum, lens, w, lane, pipe + i * STAGE_BYTES, bars + 8 * i)) ++inflight;
+    if (prod.template issue<F>(P, cum, lens, w, lane, pipe + i * STAGE_BYTES, bars + 8 * i)) ++inflight;
 
   int stage = 0;
   uint32_t phase = 0;
@@ -180,9 +175,9 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_kernel(const __grid_co
       arrive_and_merge(P, cs.b, cs.kvh, cum, nW, lane);
       continue;
     }
-    TileState st;
-    st.template load_query<FP8>(P.q + ((size_t)cs.b * (P.Hkv * kGroup) + cs.kvh * kGroup + g) * kHeadDim,
-                                P.k_scale && FP8 ? P.k_scale[cs.kvh] : 1.f, P.sm_scale_log2e, c);
+    typename F::State st;
+    F::load_query(st, P.q + ((size_t)cs.b * (P.Hkv * kGroup) + cs.kvh * kGroup + g) * kHeadDim,
+                  P.k_scale && F::kScaled ? P.k_scale[cs.kvh] : 1.f, P.sm_scale_log2e, lane);
     st.reset();
     // one split per pair: this warp's result is final, so the sink is fetched while the tiles are in flight
     const float sink_g = (P.num_splits == 1 && P.sinks) ? P.sinks[cs.kvh * kGroup + g] : -INFINITY;
@@ -199,56 +194,41 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_kernel(const __grid_co
       const uint32_t vbase = kbase + NB * BLOCK_BYTES;
       const int tok0 = t * TT;
       if ((tok0 < cs.lo) || (tok0 + TT > cs.L))
-        st.template tile<TT, FP8, true>(lo, kbase, vbase, tok0, cs.lo, cs.L, c);
+        F::template tile<TT, true>(st, lo, kbase, vbase, tok0, cs.lo, cs.L, lane);
       else
-        st.template tile<TT, FP8, false>(lo, kbase, vbase, tok0, cs.lo, cs.L, c);
+        F::template tile<TT, false>(st, lo, kbase, vbase, tok0, cs.lo, cs.L, lane);
 
       // ---- refill this stage with the tile NS ahead
       __syncwarp();
-      if (prod.template issue<BLOCK_BYTES>(P, cum, lens, w, lane, kbase, bars + 8 * stage)) ++inflight;
+      if (prod.template issue<F>(P, cum, lens, w, lane, kbase, bars + 8 * stage)) ++inflight;
       if (++stage == NS) { stage = 0; phase ^= 1u; }
     }
     if (failed) break;
 
     // ---- partial (o, lse) of this run of tiles
-    float l_tot = st.l_run;
-    l_tot += __shfl_xor_sync(0xffffffffu, l_tot, 1);
-    l_tot += __shfl_xor_sync(0xffffffffu, l_tot, 2);
-    const float vs = P.v_scale && FP8 ? P.v_scale[cs.kvh] : 1.f;
+    float m, l_tot, o[8][2];
+    F::finish(st, m, l_tot, o, lane);
+    const float vs = P.v_scale && F::kScaled ? P.v_scale[cs.kvh] : 1.f;
     if (P.num_splits == 1) {
       // the whole (sequence, KV head) was this warp's: fold the sink in and store the output, no partial, no arrival
       const long long row_out = (long long)cs.b * (P.Hkv * kGroup) + cs.kvh * kGroup + g;
       const float s2 = sink_g * 1.4426950408889634f;
-      const float M = fmaxf(l_tot > 0.f ? st.m_ref : -INFINITY, s2);
+      const float M = fmaxf(l_tot > 0.f ? m : -INFINITY, s2);
       float f = 0.f, Z = 0.f;
       if (M != -INFINITY) {
-        const float wa = l_tot > 0.f ? ex2(st.m_ref - M) : 0.f;
+        const float wa = l_tot > 0.f ? ex2(m - M) : 0.f;
         Z = l_tot * wa + (s2 == -INFINITY ? 0.f : ex2(s2 - M));
         f = wa * vs / Z;
       }
-      if (P.out_f32) {
-        float* dst = P.out_f32 + row_out * kHeadDim + 2 * c;
-#pragma unroll
-        for (int nd = 0; nd < 8; ++nd)
-          *reinterpret_cast<float2*>(dst + 8 * nd) =
-              make_float2((st.O[nd][0] + st.O[nd][2]) * f, (st.O[nd][1] + st.O[nd][3]) * f);
-      } else {
-        __nv_bfloat16* dst = P.out + row_out * kHeadDim + 2 * c;
-#pragma unroll
-        for (int nd = 0; nd < 8; ++nd)
-          *reinterpret_cast<uint32_t*>(dst + 8 * nd) =
-              f32x2_to_bf16x2((st.O[nd][0] + st.O[nd][2]) * f, (st.O[nd][1] + st.O[nd][3]) * f);
-      }
+      if (P.out_f32) F::store(P.out_f32 + row_out * kHeadDim, o, f, c);
+      else F::store(P.out + row_out * kHeadDim, o, f, c);
       if (P.lse_out && c == 0) P.lse_out[row_out] = Z > 0.f ? (M + log2f(Z)) * 0.6931471805599453f : -INFINITY;
       continue;
     }
     const float inv = l_tot > 0.f ? vs / l_tot : 0.f;
-    const float lse = l_tot > 0.f ? (st.m_ref + log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
+    const float lse = l_tot > 0.f ? (m + log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
     const size_t row = (size_t)cs.prow + (size_t)g * cs.pstride;
-    float* po = P.part_o + row * kHeadDim + 2 * c;
-#pragma unroll
-    for (int nd = 0; nd < 8; ++nd)
-      *reinterpret_cast<float2*>(po + 8 * nd) = make_float2((st.O[nd][0] + st.O[nd][2]) * inv, (st.O[nd][1] + st.O[nd][3]) * inv);
+    F::store(P.part_o + row * kHeadDim, o, inv, c);
     if (c == 0) P.part_lse[row] = lse;
     arrive_and_merge(P, cs.b, cs.kvh, cum, nW, lane);
   }
@@ -270,15 +250,15 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_kernel(const __grid_co
   }
 }
 
-template <int NW, int NS, int TT, bool FP8>
+template <int NW, int NS, int TT, typename F>
 static size_t smem_bytes_of(int batch) {
-  constexpr int STAGE_BYTES = 2 * (TT / kBlock) * kBlock * kHeadDim * (FP8 ? 1 : 2);
+  constexpr int STAGE_BYTES = 2 * (TT / kBlock) * F::kBlockBytes;
   return 1024 + (size_t)NW * NS * STAGE_BYTES + NW * NS * 8 + (size_t)(2 * batch + 2) * sizeof(int);
 }
 
-template <int NW, int NS, int TT, bool FP8>
+template <int NW, int NS, int TT, typename F>
 static cudaError_t launch_variant(const DecodeParams& P, int ctas, cudaStream_t s, int& smem_limit) {
-  auto kern = decode_attn_kernel<NW, NS, TT, FP8>;
+  auto kern = decode_attn_kernel<NW, NS, TT, F>;
   if (smem_limit == 0) {  // first launch of this variant on this device: raise its dynamic shared-memory limit
     int dev = 0, optin = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -287,15 +267,19 @@ static cudaError_t launch_variant(const DecodeParams& P, int ctas, cudaStream_t 
     if (e != cudaSuccess) return e;
     smem_limit = optin;
   }
-  const size_t need = smem_bytes_of<NW, NS, TT, FP8>(P.batch);
+  const size_t need = smem_bytes_of<NW, NS, TT, F>(P.batch);
   if (need > (size_t)smem_limit) return cudaErrorInvalidValue;  // batch too large for the schedule arrays
   return launch_dependent(kern, dim3(ctas), dim3(NW * 32), need, s, P);
 }
 
-cudaError_t launch_decode_attn(const DecodeParams& P, bool fp8, int ctas, cudaStream_t s, int* smem_limit) {
-  return fp8 ? launch_variant<kDecodeWarpsFp8, kDecodeStagesFp8, kTileFp8, true>(P, ctas, s, smem_limit[0])
-             : launch_variant<kDecodeWarpsBf16, kDecodeStagesBf16, kTileBf16, false>(P, ctas, s, smem_limit[1]);
+cudaError_t launch_decode_attn(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit) {
+  switch (kv_dtype) {
+    case PUZZLE_KV_FP8_E4M3:
+      return launch_variant<kDecodeWarpsFp8, kDecodeStagesFp8, kTileFp8, SwizzledTile<true>>(P, ctas, s, smem_limit[0]);
+    case PUZZLE_KV_BF16:
+      return launch_variant<kDecodeWarpsBf16, kDecodeStagesBf16, kTileBf16, SwizzledTile<false>>(P, ctas, s, smem_limit[1]);
+    default: return launch_variant<kDecodeWarpsFp4, kDecodeStagesFp4, kTileFp4, Fp4Tile>(P, ctas, s, smem_limit[2]);
+  }
 }
 
 }  // namespace puzzle
-

@@ -13,6 +13,8 @@ namespace puzzle {
 struct alignas(64) DecodeParams {
   CUtensorMap tmK;  // rows of 128 bytes (two FP8 tokens or one bf16 token), box = one 16-token block of one KV head
   CUtensorMap tmV;
+  const uint8_t* k_cache;  // the 4-bit cache goes without tensor maps: a block is one bulk copy from here
+  const uint8_t* v_cache;
   const __nv_bfloat16* q;
   const int32_t* block_table;
   const int32_t* seq_lens;
@@ -32,8 +34,8 @@ struct alignas(64) DecodeParams {
   int num_splits;  // 0 = balanced schedule
   int n_q;         // multi-token kernel: query tokens per sequence in q / out ([batch][n_q][Hq][D]); else unused
   const int32_t* q_lens;  // multi-token kernel: real query tokens per sequence [batch], or null (= n_q)
-  int oob_row;     // a row coordinate outside the tensor maps: loads from it return zeros
-  int rows_per_block;  // tensor-map rows (128 bytes each) per (block, KV head): 8 (FP8) or 16 (bf16)
+  int oob_row;     // a row coordinate outside the tensor maps: loads from it return zeros (4-bit cache: -1)
+  int rows_per_block;  // tensor-map rows (128 bytes each) per (block, KV head): 8 (FP8) or 16 (bf16); 4-bit cache: 1
   float sm_scale_log2e;
 };
 
@@ -52,6 +54,7 @@ struct MergeParams {
 // warp and tokens per tile (the unit of the schedule and of one pipeline stage).
 constexpr int kDecodeWarpsFp8 = 12, kDecodeStagesFp8 = 2, kTileFp8 = 64;
 constexpr int kDecodeWarpsBf16 = 12, kDecodeStagesBf16 = 2, kTileBf16 = 32;
+constexpr int kDecodeWarpsFp4 = 16, kDecodeStagesFp4 = 2, kTileFp4 = 64;
 // The CTA-balanced kernel keeps its schedule arrays beside the TMA rings and the deposit buffers in shared memory,
 // which bounds the batch it takes.  Launches with at least kCtaRateMinTiles tiles per CTA note the speed of every
 // CTA slot at the start of the workspace (before the arrival counters: a CTA counter, the buffer switch, two pad words, then two
@@ -62,17 +65,17 @@ constexpr int kCtaRateMinTiles = 256;
 constexpr int kWholePairTiles = 4;       // up to this many tiles per (sequence, KV head) a pair goes to one warp whole
 inline size_t cta_rate_words(int ctas) { return 4 + 2 * (size_t)ctas; }
 
-// Launches the split-KV kernel for an FP8 (fp8 = true) or bf16 cache on `ctas` CTAs.  smem_limit[2] caches,
-// per variant, the dynamic shared-memory limit set for the kernel on the current device (0 = not set yet).
-cudaError_t launch_decode_attn(const DecodeParams& P, bool fp8, int ctas, cudaStream_t s, int* smem_limit);
+// Launches the split-KV kernel for a cache of type kv_dtype on `ctas` CTAs.  smem_limit[3] caches, per type, the
+// dynamic shared-memory limit set for the kernel on the current device (0 = not set yet).
+cudaError_t launch_decode_attn(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit);
 // The CTA-balanced kernel (balanced schedule only, batch <= kCtaMaxBatch).  Its partial row blocks: one per
 // (CTA, pair) meeting, ctas + batch*Hkv at most.
-cudaError_t launch_decode_attn_cta(const DecodeParams& P, bool fp8, int ctas, cudaStream_t s, int* smem_limit);
+cudaError_t launch_decode_attn_cta(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit);
 // The kernel for launches in which no (sequence, KV head) has more than kWholePairTiles tiles (narrow windows, very
 // short contexts): a group of four warps per pair, one tile each, combined in shared memory; no workspace use.
-// smem_limit[2] as above.  It pays up to decode_attn_small_max_pairs(ctas) pairs; beyond, the warp-scheduled kernel
+// smem_limit[3] as above.  It pays up to decode_attn_small_max_pairs(ctas) pairs; beyond, the warp-scheduled kernel
 // with one split per pair keeps its TMA rings full.
-cudaError_t launch_decode_attn_small(const DecodeParams& P, bool fp8, int ctas, cudaStream_t s, int* smem_limit);
+cudaError_t launch_decode_attn_small(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit);
 int decode_attn_small_max_pairs(int ctas);
 // The multi-token kernel (FP8 cache, balanced schedule): P.n_q, P.q_lens set; P.counters has one word per
 // (sequence, token pair, KV head); partial rows: decode_attn_tokens_partial_rows(...).

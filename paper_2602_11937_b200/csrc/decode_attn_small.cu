@@ -11,7 +11,7 @@
 //    before it);
 //  * the four running states meet in shared memory behind one named barrier of the group; its first warp combines
 //    them, folds the sink in and stores the bf16 rows.  Nothing goes through the workspace.
-// The arithmetic per tile is decode_tile.cuh's, the one of the two larger kernels.
+// The arithmetic per tile is decode_tile.cuh's (decode_tile_fp4.cuh's), the one of the two larger kernels.
 #include <cuda.h>
 
 #include <climits>
@@ -19,6 +19,7 @@
 #include "common.cuh"
 #include "decode_attn.cuh"
 #include "decode_tile.cuh"
+#include "decode_tile_fp4.cuh"
 
 namespace puzzle {
 
@@ -35,14 +36,12 @@ __device__ __forceinline__ void group_barrier(int group) {
 
 }  // namespace
 
-template <int TT, bool FP8>
+template <int TT, typename F>
 __global__ void __launch_bounds__(kSmallWarps * 32, 1) decode_attn_small_kernel(const __grid_constant__ DecodeParams P) {
   constexpr int NW = kSmallWarps, GW = kSmallGroup;
   constexpr int NB = TT / kBlock;                       // blocks per tile
-  constexpr int EB = FP8 ? 1 : 2;                       // bytes per cache element
-  constexpr int BLOCK_BYTES = kBlock * kHeadDim * EB;   // one (block, KV head): 1 KiB or 2 KiB
+  constexpr int BLOCK_BYTES = F::kBlockBytes;
   constexpr int STAGE_BYTES = 2 * NB * BLOCK_BYTES;     // K and V of one tile
-  constexpr int kNotVisible = INT_MIN;
 
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -63,15 +62,12 @@ __global__ void __launch_bounds__(kSmallWarps * 32, 1) decode_attn_small_kernel(
     mbar_init(bar, 1);
     fence_mbar_init();
   }
-  if (threadIdx.x == 0) {
-    tma_prefetch_desc(&P.tmK);
-    tma_prefetch_desc(&P.tmV);
-  }
+  if (threadIdx.x == 0) F::prefetch(P);
   release_dependents();
   grid_dependency_wait();   // nothing above reads or writes global memory
   __syncwarp();
 
-  LaneOffsets<FP8> lo;
+  typename F::Lanes lo;
   lo.init(lane);
   uint32_t phase = 0;
   const int pairs = P.batch * P.Hkv;
@@ -85,7 +81,7 @@ __global__ void __launch_bounds__(kSmallWarps * 32, 1) decode_attn_small_kernel(
     const int nt = min(r.ntile, GW);       // the host chose this kernel because no pair can have more tiles
     const bool have = wi < nt;
 
-    TileState st;
+    typename F::State st;
     st.reset();
     float sink_g = -INFINITY, vs = 1.f;
     if (have) {
@@ -106,24 +102,21 @@ __global__ void __launch_bounds__(kSmallWarps * 32, 1) decode_attn_small_kernel(
       for (int i = 0; i < NB; ++i) rows[i] = __shfl_sync(0xffffffffu, row, i);
       if (elect_one()) {
         mbar_arrive_expect_tx(bar, STAGE_BYTES);
-#pragma unroll
-        for (int i = 0; i < NB; ++i) tma_load_2d(stage + i * BLOCK_BYTES, &P.tmK, 0, rows[i], bar);
-#pragma unroll
-        for (int i = 0; i < NB; ++i) tma_load_2d(stage + (NB + i) * BLOCK_BYTES, &P.tmV, 0, rows[i], bar);
+        F::template load_tile<NB>(P, stage, rows, bar);
       }
       // ---- query, scales and sink while the tile is in flight
-      st.template load_query<FP8>(P.q + ((size_t)b * (P.Hkv * kGroup) + kvh * kGroup + g) * kHeadDim,
-                                  P.k_scale && FP8 ? P.k_scale[kvh] : 1.f, P.sm_scale_log2e, c);
+      F::load_query(st, P.q + ((size_t)b * (P.Hkv * kGroup) + kvh * kGroup + g) * kHeadDim,
+                    P.k_scale && F::kScaled ? P.k_scale[kvh] : 1.f, P.sm_scale_log2e, lane);
       st.reset();
-      vs = P.v_scale && FP8 ? P.v_scale[kvh] : 1.f;
+      vs = P.v_scale && F::kScaled ? P.v_scale[kvh] : 1.f;
       if (wi == 0 && P.sinks) sink_g = P.sinks[kvh * kGroup + g];
       if (mbar_wait_bounded(bar, phase)) {
         const uint32_t kbase = stage, vbase = stage + NB * BLOCK_BYTES;
         const int tok0 = t * TT;
         if ((tok0 < r.lo) || (tok0 + TT > r.L))
-          st.template tile<TT, FP8, true>(lo, kbase, vbase, tok0, r.lo, r.L, c);
+          F::template tile<TT, true>(st, lo, kbase, vbase, tok0, r.lo, r.L, lane);
         else
-          st.template tile<TT, FP8, false>(lo, kbase, vbase, tok0, r.lo, r.L, c);
+          F::template tile<TT, false>(st, lo, kbase, vbase, tok0, r.lo, r.L, lane);
       } else {
         // the copy did not land in time: report it, contribute nothing, and keep in step with the group
         if (P.dev_status && lane == 0) atomicOr(P.dev_status, (int)PUZZLE_DEV_WAIT_EXPIRED);
@@ -134,16 +127,8 @@ __global__ void __launch_bounds__(kSmallWarps * 32, 1) decode_attn_small_kernel(
       if (P.sinks) sink_g = P.sinks[kvh * kGroup + g];   // a pair without visible keys: the output is the sink's
     }
 
-    float l_tot = st.l_run;
-    l_tot += __shfl_xor_sync(0xffffffffu, l_tot, 1);
-    l_tot += __shfl_xor_sync(0xffffffffu, l_tot, 2);
-    float m = st.m_ref;
-    float o[8][2];
-#pragma unroll
-    for (int nd = 0; nd < 8; ++nd) {
-      o[nd][0] = st.O[nd][0] + st.O[nd][2];
-      o[nd][1] = st.O[nd][1] + st.O[nd][3];
-    }
+    float m, l_tot, o[8][2];
+    F::finish(st, m, l_tot, o, lane);
 
     if (nt > 1) {   // uniform in the group
       if (wi != 0 && have) {
@@ -190,26 +175,17 @@ __global__ void __launch_bounds__(kSmallWarps * 32, 1) decode_attn_small_kernel(
         Z = l_tot * wa + (s2 == -INFINITY ? 0.f : ex2(s2 - M));
         f = wa * vs / Z;
       }
-      if (P.out_f32) {
-        float* dst = P.out_f32 + row_out * kHeadDim + 2 * c;
-#pragma unroll
-        for (int nd = 0; nd < 8; ++nd)
-          *reinterpret_cast<float2*>(dst + 8 * nd) = make_float2(o[nd][0] * f, o[nd][1] * f);
-      } else {
-        __nv_bfloat16* dst = P.out + row_out * kHeadDim + 2 * c;
-#pragma unroll
-        for (int nd = 0; nd < 8; ++nd)
-          *reinterpret_cast<uint32_t*>(dst + 8 * nd) = f32x2_to_bf16x2(o[nd][0] * f, o[nd][1] * f);
-      }
+      if (P.out_f32) F::store(P.out_f32 + row_out * kHeadDim, o, f, c);
+      else F::store(P.out + row_out * kHeadDim, o, f, c);
       if (P.lse_out && c == 0) P.lse_out[row_out] = Z > 0.f ? (M + log2f(Z)) * 0.6931471805599453f : -INFINITY;
     }
   }
 }
 
-template <int TT, bool FP8>
+template <int TT, typename F>
 static cudaError_t launch_small_variant(const DecodeParams& P, int ctas, cudaStream_t s, int& smem_limit) {
-  auto kern = decode_attn_small_kernel<TT, FP8>;
-  constexpr int STAGE_BYTES = 2 * (TT / kBlock) * kBlock * kHeadDim * (FP8 ? 1 : 2);
+  auto kern = decode_attn_small_kernel<TT, F>;
+  constexpr int STAGE_BYTES = 2 * (TT / kBlock) * F::kBlockBytes;
   const size_t need = 1024 + (size_t)kSmallWarps * STAGE_BYTES + kSmallWarps * 8 + 16 +
                       (size_t)kSmallWarps * 4 * 32 * sizeof(float4) + 2 * kSmallWarps * kGroup * sizeof(float);
   if (smem_limit == 0) {  // first launch of this variant on this device: raise its dynamic shared-memory limit
@@ -220,9 +196,12 @@ static cudaError_t launch_small_variant(const DecodeParams& P, int ctas, cudaStr
   return launch_dependent(kern, dim3(ctas), dim3(kSmallWarps * 32), need, s, P);
 }
 
-cudaError_t launch_decode_attn_small(const DecodeParams& P, bool fp8, int ctas, cudaStream_t s, int* smem_limit) {
-  return fp8 ? launch_small_variant<kTileFp8, true>(P, ctas, s, smem_limit[0])
-             : launch_small_variant<kTileBf16, false>(P, ctas, s, smem_limit[1]);
+cudaError_t launch_decode_attn_small(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit) {
+  switch (kv_dtype) {
+    case PUZZLE_KV_FP8_E4M3: return launch_small_variant<kTileFp8, SwizzledTile<true>>(P, ctas, s, smem_limit[0]);
+    case PUZZLE_KV_BF16: return launch_small_variant<kTileBf16, SwizzledTile<false>>(P, ctas, s, smem_limit[1]);
+    default: return launch_small_variant<kTileFp4, Fp4Tile>(P, ctas, s, smem_limit[2]);
+  }
 }
 
 int decode_attn_small_max_pairs(int ctas) { return 2 * kSmallGroups * ctas; }

@@ -320,5 +320,60 @@ struct TileState {
   }
 };
 
+// A cache type as the split-KV kernels see it: how a tile is fetched, computed, and brought into the form in which
+// running states are combined and stored (head g on the four lanes of g).  This one is the E4M3 and the bf16 cache;
+// Fp4Tile (decode_tile_fp4.cuh) is the 4-bit one.
+template <bool FP8>
+struct SwizzledTile {
+  static constexpr int kBlockBytes = kBlock * kHeadDim * (FP8 ? 1 : 2);   // one (block, KV head) of K or of V
+  static constexpr bool kScaled = FP8;
+  using Lanes = LaneOffsets<FP8>;
+  using State = TileState;
+
+  static __device__ __forceinline__ void prefetch(const DecodeParams& P) {
+    tma_prefetch_desc(&P.tmK);
+    tma_prefetch_desc(&P.tmV);
+  }
+  // Issued by one lane; rows[i]: first row of block i in the tensor maps (P.oob_row: the block is fetched as zeros).
+  template <int NB>
+  static __device__ __forceinline__ void load_tile(const DecodeParams& P, uint32_t stage, const int (&rows)[NB],
+                                                   uint32_t bar) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i) tma_load_2d(stage + i * kBlockBytes, &P.tmK, 0, rows[i], bar);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) tma_load_2d(stage + (NB + i) * kBlockBytes, &P.tmV, 0, rows[i], bar);
+  }
+  static __device__ __forceinline__ void load_query(State& st, const __nv_bfloat16* qrow, float ks, float sm, int lane) {
+    st.template load_query<FP8>(qrow, ks, sm, lane & 3);
+  }
+  template <int TT, bool EDGE>
+  static __device__ __forceinline__ void tile(State& st, const Lanes& at, uint32_t kbase, uint32_t vbase, int tok0, int lo,
+                                              int L, int lane) {
+    st.template tile<TT, FP8, EDGE>(at, kbase, vbase, tok0, lo, L, lane & 3);
+  }
+  // Lane c of the four gets channels 8 nd + 2c and the next in o[nd].
+  static __device__ __forceinline__ void finish(const State& st, float& m, float& l, float (&o)[8][2], int) {
+    l = st.l_run;
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    m = st.m_ref;
+#pragma unroll
+    for (int nd = 0; nd < 8; ++nd) {
+      o[nd][0] = st.O[nd][0] + st.O[nd][2];
+      o[nd][1] = st.O[nd][1] + st.O[nd][3];
+    }
+  }
+  static __device__ __forceinline__ void store(float* row, const float (&o)[8][2], float f, int c) {
+#pragma unroll
+    for (int nd = 0; nd < 8; ++nd)
+      *reinterpret_cast<float2*>(row + 2 * c + 8 * nd) = make_float2(o[nd][0] * f, o[nd][1] * f);
+  }
+  static __device__ __forceinline__ void store(__nv_bfloat16* row, const float (&o)[8][2], float f, int c) {
+#pragma unroll
+    for (int nd = 0; nd < 8; ++nd)
+      *reinterpret_cast<uint32_t*>(row + 2 * c + 8 * nd) = f32x2_to_bf16x2(o[nd][0] * f, o[nd][1] * f);
+  }
+};
+
 }  // namespace
 }  // namespace puzzle
