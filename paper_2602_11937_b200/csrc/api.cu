@@ -34,7 +34,7 @@ struct DeviceInfo {
   int sm_count = 0;
   // dynamic shared-memory limits already set per kernel and cache type; 0 = not raised yet
   int smem_warp[3] = {0, 0, 0}, smem_cta[3] = {0, 0, 0}, smem_small[3] = {0, 0, 0};
-  int smem_tc = 0, smem_tokens = 0;
+  int smem_tc = 0, smem_tokens[2] = {0, 0};
 };
 DeviceInfo& device_info() {
   static DeviceInfo info[64];
@@ -93,6 +93,22 @@ bool make_cache_map(CUtensorMap* m, void* base, long long rows, int elem_bytes, 
                    dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
+}
+
+// How a kernel reaches the cache: tensor maps of rows of row_bytes bytes, or the plain addresses of a 4-bit cache.
+bool set_cache(DecodeParams* P, const puzzle_layer_desc* d, const puzzle_kv_view* kv, int row_bytes) {
+  if (d->kv_dtype == PUZZLE_KV_FP4_E2M1) {
+    P->k_cache = static_cast<const uint8_t*>(kv->k_cache);
+    P->v_cache = static_cast<const uint8_t*>(kv->v_cache);
+    P->rows_per_block = 1;
+    P->oob_row = -1;
+    return true;
+  }
+  const int eb = d->kv_dtype == PUZZLE_KV_FP8_E4M3 ? 1 : 2;
+  P->rows_per_block = kBlock * kHeadDim * eb / row_bytes;
+  const long long rows = kv->num_blocks * d->num_kv_heads * (long long)P->rows_per_block;
+  P->oob_row = (int)rows;
+  return make_cache_map(&P->tmK, kv->k_cache, rows, eb, row_bytes) && make_cache_map(&P->tmV, kv->v_cache, rows, eb, row_bytes);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -405,21 +421,7 @@ static puzzle_status decode_attn_impl(const puzzle_layer_desc* desc, const puzzl
   DecodeParams P;
   std::memset(&P, 0, sizeof P);
   const bool tc = tcgen05;
-  if (desc->kv_dtype == PUZZLE_KV_FP4_E2M1) {
-    P.k_cache = static_cast<const uint8_t*>(kv->k_cache);
-    P.v_cache = static_cast<const uint8_t*>(kv->v_cache);
-    P.rows_per_block = 1;
-    P.oob_row = -1;
-  } else {
-    const int eb = desc->kv_dtype == PUZZLE_KV_FP8_E4M3 ? 1 : 2;
-    const int row_bytes = tc ? 64 : 128;
-    P.rows_per_block = kBlock * kHeadDim * eb / row_bytes;
-    const long long cache_rows = kv->num_blocks * Hkv * (long long)P.rows_per_block;
-    P.oob_row = (int)cache_rows;
-    if (!make_cache_map(&P.tmK, kv->k_cache, cache_rows, eb, row_bytes) ||
-        !make_cache_map(&P.tmV, kv->v_cache, cache_rows, eb, row_bytes))
-      return PUZZLE_ERR_CUDA;
-  }
+  if (!set_cache(&P, desc, kv, tc ? 64 : 128)) return PUZZLE_ERR_CUDA;
   P.q = static_cast<const __nv_bfloat16*>(q);
   P.block_table = kv->block_table;
   P.seq_lens = kv->seq_lens;
@@ -552,7 +554,7 @@ size_t puzzle_decode_attn_tokens_workspace_bytes(const puzzle_layer_desc* desc, 
   if (check_desc(desc) != PUZZLE_OK || batch <= 0 || n_q <= 0 || (long long)batch * ((n_q + 1) / 2) > kTokMaxRows)
     return 0;
   return tokens_counter_bytes(batch, n_q, desc->num_kv_heads) +
-         decode_attn_tokens_partial_rows(grid_ctas(), batch, n_q, desc->num_kv_heads) * (kHeadDim + 1) * sizeof(float);
+         decode_attn_tokens_partial_rows(grid_ctas(), batch, n_q, desc->num_kv_heads, desc->kv_dtype) * (kHeadDim + 1) * sizeof(float);
 }
 
 puzzle_status puzzle_decode_attn_tokens_workspace_init(const puzzle_layer_desc* desc, int32_t batch, int32_t n_q,
@@ -574,17 +576,15 @@ puzzle_status puzzle_decode_attn_tokens(const puzzle_layer_desc* desc, const puz
   puzzle_status st = check_decode_attn_args(desc, kv, q, out, batch, 0, false);
   if (st != PUZZLE_OK) return st;
   if (n_q <= 0 || (long long)batch * ((n_q + 1) / 2) > kTokMaxRows) return PUZZLE_ERR_SHAPE;
-  if (desc->kv_dtype != PUZZLE_KV_FP8_E4M3) return PUZZLE_ERR_UNSUPPORTED;   // the bf16 cache goes one row per token
+  if (desc->kv_dtype == PUZZLE_KV_BF16) return PUZZLE_ERR_UNSUPPORTED;   // the bf16 cache goes one row per token
   const int Hkv = desc->num_kv_heads;
   const size_t need = puzzle_decode_attn_tokens_workspace_bytes(desc, batch, n_q);
   if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15)) return PUZZLE_ERR_WORKSPACE;
   const size_t cbytes = tokens_counter_bytes(batch, n_q, Hkv);
-  const size_t rows = decode_attn_tokens_partial_rows(grid_ctas(), batch, n_q, Hkv);
+  const size_t rows = decode_attn_tokens_partial_rows(grid_ctas(), batch, n_q, Hkv, desc->kv_dtype);
   DecodeParams P;
   std::memset(&P, 0, sizeof P);
-  const long long cache_rows = kv->num_blocks * Hkv * (long long)(kBlock * kHeadDim / 128);
-  if (!make_cache_map(&P.tmK, kv->k_cache, cache_rows, 1) || !make_cache_map(&P.tmV, kv->v_cache, cache_rows, 1))
-    return PUZZLE_ERR_CUDA;
+  if (!set_cache(&P, desc, kv, 128)) return PUZZLE_ERR_CUDA;
   P.q = static_cast<const __nv_bfloat16*>(q);
   P.block_table = kv->block_table;
   P.seq_lens = kv->seq_lens;
@@ -604,11 +604,9 @@ puzzle_status puzzle_decode_attn_tokens(const puzzle_layer_desc* desc, const puz
   P.window = desc->window;
   P.n_q = n_q;
   P.q_lens = q_lens;
-  P.oob_row = (int)cache_rows;
-  P.rows_per_block = kBlock * kHeadDim / 128;
   P.sm_scale_log2e = desc->sm_scale * 1.4426950408889634f;
-  if (launch_decode_attn_tokens(P, grid_ctas(), static_cast<cudaStream_t>(stream), &device_info().smem_tokens) !=
-      cudaSuccess)
+  if (launch_decode_attn_tokens(P, desc->kv_dtype, grid_ctas(), static_cast<cudaStream_t>(stream),
+                                device_info().smem_tokens) != cudaSuccess)
     return PUZZLE_ERR_CUDA;
   count_launch();
   return PUZZLE_OK;

@@ -77,10 +77,11 @@ cudaError_t launch_decode_attn_cta(const DecodeParams& P, int kv_dtype, int ctas
 // with one split per pair keeps its TMA rings full.
 cudaError_t launch_decode_attn_small(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit);
 int decode_attn_small_max_pairs(int ctas);
-// The multi-token kernel (FP8 cache, balanced schedule): P.n_q, P.q_lens set; P.counters has one word per
-// (sequence, token pair, KV head); partial rows: decode_attn_tokens_partial_rows(...).
-cudaError_t launch_decode_attn_tokens(const DecodeParams& P, int ctas, cudaStream_t s, int* smem_limit);
-size_t decode_attn_tokens_partial_rows(int ctas, int batch, int n_q, int Hkv);
+// The multi-token kernel (FP8 or 4-bit cache, balanced schedule): P.n_q, P.q_lens set; P.counters has one word per
+// (sequence, token pair, KV head); partial rows: decode_attn_tokens_partial_rows(...); smem_limit[2] as above.
+cudaError_t launch_decode_attn_tokens(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit);
+size_t decode_attn_tokens_partial_rows(int ctas, int batch, int n_q, int Hkv, int kv_dtype);
+constexpr int kTokWarpsFp8 = 12, kTokWarpsFp4 = 12;
 size_t decode_attn_tokens_counters(int batch, int n_q, int Hkv);
 constexpr int kTokMaxRows = 8192;   // (sequence, token pair) rows its shared-memory schedule holds
 

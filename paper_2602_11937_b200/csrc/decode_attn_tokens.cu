@@ -1,6 +1,6 @@
 // Decode attention for several new tokens per sequence (a multi-token decode step, or a chunk of a prompt after
 // its bulk append: the input half of the paper's fixed-length scenarios, Section "Optimized Scenarios") over the
-// FP8 cache, sm_100a.
+// FP8 cache and the 4-bit cache, sm_100a.
 //
 // The bytes of a step do not grow with the number of query tokens, only the arithmetic does, so query tokens are
 // processed in pairs that share one pass over the K/V tiles: in the single-token kernels rows 8-15 of the
@@ -10,6 +10,9 @@
 // causal mask gives the earlier token one key fewer (and a window that starts one key earlier).  An odd last
 // token is paired with itself.  Sequences with more than two new tokens take several rows, whose repeated reads
 // of the same blocks are neighbours in the schedule and are served by L2.
+//
+// Over the 4-bit cache the heads are MMA columns (decode_tile_fp4.cuh), so nothing is empty there; what a pair shares is
+// the conversion of the tile (half of that cache's instructions), and each token issues its own 32 MMAs per tile.
 //
 // Everything else is the warp-scheduled kernel's design (decode_attn.cu): every warp an independent worker with
 // a private ring of TMA stages, the tile space of all rows cut evenly over the workers, one float32 partial
@@ -24,11 +27,12 @@
 #include "common.cuh"
 #include "decode_attn.cuh"
 #include "decode_tile.cuh"
+#include "decode_tile_fp4.cuh"
 
 namespace puzzle {
 namespace {
 
-constexpr int kTokWarps = 12, kTokStages = 2, kTokTile = 64;
+constexpr int kTokStages = 2, kTokTile = 64;
 constexpr int kPairRows = 2 * kGroup;  // partial rows per (worker, row, KV head): 8 heads of each of the two tokens
 
 // One row of the schedule: query tokens t0 and t1 (= t0 + 1, or t0 again for an odd last token) of sequence b.
@@ -255,6 +259,101 @@ struct TileState2 {
   }
 };
 
+// The two cache types as the kernel sees them: copies, state of a pair, one tile, and a token's state as it is stored.
+struct Fp8Pair {
+  static constexpr int kWarps = kTokWarpsFp8;
+  using Tile = SwizzledTile<true>;
+  using State = TileState2;
+  static __device__ __forceinline__ void load_query(State& st, int tok, const __nv_bfloat16* qrow, float ks, float sm,
+                                                    int lane) {
+    st.load_query(tok, qrow, ks, sm, lane & 3);
+  }
+  template <bool EDGE>
+  static __device__ __forceinline__ void tile(State& st, const Tile::Lanes& at, uint32_t kbase, uint32_t vbase, int tok0,
+                                              int loA, int LA, int lo, int L, int lane) {
+    st.tile<EDGE>(at, kbase, vbase, tok0, loA, LA, lo, L, lane & 3);
+  }
+  static __device__ __forceinline__ void finish(const State& st, int tok, float& m, float& l, float (&o)[8][2], int) {
+    l = st.l_run[tok];
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    m = st.m_ref[tok];
+#pragma unroll
+    for (int nd = 0; nd < 8; ++nd) { o[nd][0] = st.O[nd][2 * tok]; o[nd][1] = st.O[nd][2 * tok + 1]; }
+  }
+};
+
+struct Fp4Pair {
+  static constexpr int kWarps = kTokWarpsFp4;
+  using Tile = Fp4Tile;
+  struct State {
+    Fp4State t[2];
+    __device__ __forceinline__ void reset() { t[0].reset(); t[1].reset(); }
+  };
+  static __device__ __forceinline__ void load_query(State& st, int tok, const __nv_bfloat16* qrow, float ks, float sm,
+                                                    int lane) {
+    st.t[tok].load_query(qrow, ks, sm, lane);
+  }
+  // EDGE as in TileState2::tile; V scales outside [loA, L) are cleared (the keys in [LA, L) are real tokens, and so are
+  // those in [loA, lo): the other token's weights for them are zero).
+  template <bool EDGE>
+  static __device__ __forceinline__ void tile(State& st, const Tile::Lanes& at, uint32_t kbase, uint32_t vbase, int tok0,
+                                              int loA, int LA, int lo, int L, int lane) {
+    constexpr int NB = kTokTile / kBlock;
+    const int g = lane >> 2, c = lane & 3;
+    float s[2][NB][4];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+      uint32_t a[4][4];
+      fp4_k_fragments(kbase + blk * kFp4BlockBytes, at, a);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) mma_f16_z(s[t][blk], a[0][0], a[0][1], a[0][2], a[0][3], st.t[t].q[0][0], st.t[t].q[0][1]);
+#pragma unroll
+      for (int k = 1; k < 4; ++k)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          mma_f16(s[t][blk], a[k][0], a[k][1], a[k][2], a[k][3], st.t[t].q[k][0], st.t[t].q[k][1]);
+    }
+    if constexpr (EDGE) {
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int tk = tok0 + kBlock * blk + g + 8 * e;
+          if (tk < loA || tk >= LA) s[0][blk][2 * e] = s[0][blk][2 * e + 1] = -INFINITY;
+          if (tk < lo || tk >= L) s[1][blk][2 * e] = s[1][blk][2 * e + 1] = -INFINITY;
+        }
+    }
+    float neg[2][2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) {
+        mx[0] = fmaxf(mx[0], fmaxf(s[t][blk][0], s[t][blk][2]));
+        mx[1] = fmaxf(mx[1], fmaxf(s[t][blk][1], s[t][blk][3]));
+      }
+      st.t[t].raise(mx);
+      neg[t][0] = st.t[t].negated(0);
+      neg[t][1] = st.t[t].negated(1);
+    }
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+      uint32_t b[2][2], a[4][4];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) st.t[t].weights(s[t][blk], neg[t][0], neg[t][1], b[t][0], b[t][1]);
+      fp4_v_fragments<EDGE>(vbase + blk * kFp4BlockBytes, at, tok0 + kBlock * blk + 2 * c, loA, L, a);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) mma_f16(st.t[t].O[i], a[i][0], a[i][1], a[i][2], a[i][3], b[t][0], b[t][1]);
+    }
+  }
+  static __device__ __forceinline__ void finish(const State& st, int tok, float& m, float& l, float (&o)[8][2], int lane) {
+    Fp4Tile::finish(st.t[tok], m, l, o, lane);
+  }
+};
+
 // Log-sum-exp merge of the `count` partials of one (row, KV head) by one warp, one token after the other: the
 // quad of lanes g = lane / 4 owns query head g of the group, lane c of the quad channels 16c .. 16c + 15.  Part k
 // of head g of token half h is partial row first + 8 h + g + 16 k.  The formula is merge_rows' (decode_sched.cuh).
@@ -306,10 +405,11 @@ __device__ __noinline__ void merge_tok_rows(const DecodeParams& P, const RowInfo
 
 }  // namespace
 
-__global__ void __launch_bounds__(kTokWarps * 32, 1) decode_attn_tokens_kernel(const __grid_constant__ DecodeParams P) {
-  constexpr int NW = kTokWarps, NS = kTokStages, TT = kTokTile;
+template <typename F>
+__global__ void __launch_bounds__(F::kWarps * 32, 1) decode_attn_tokens_kernel(const __grid_constant__ DecodeParams P) {
+  constexpr int NW = F::kWarps, NS = kTokStages, TT = kTokTile;
   constexpr int NB = TT / kBlock;
-  constexpr int BLOCK_BYTES = kBlock * kHeadDim;
+  constexpr int BLOCK_BYTES = F::Tile::kBlockBytes;
   constexpr int STAGE_BYTES = 2 * NB * BLOCK_BYTES;
   constexpr int PIPE_BYTES = NW * NS * STAGE_BYTES;
   constexpr int kNotVisible = INT_MIN;
@@ -330,10 +430,7 @@ __global__ void __launch_bounds__(kTokWarps * 32, 1) decode_attn_tokens_kernel(c
     for (int i = 0; i < NS; ++i) mbar_init(bars + 8 * i, 1);
     fence_mbar_init();
   }
-  if (threadIdx.x == 0) {
-    tma_prefetch_desc(&P.tmK);
-    tma_prefetch_desc(&P.tmV);
-  }
+  if (threadIdx.x == 0) F::Tile::prefetch(P);
   release_dependents();
   grid_dependency_wait();   // nothing above reads or writes global memory
   // ---- schedule: tiles of every row, prefix sums
@@ -366,7 +463,7 @@ __global__ void __launch_bounds__(kTokWarps * 32, 1) decode_attn_tokens_kernel(c
   const int share = (T + nW - 1) / nW;
   const int w_lo = min(w * share, T), w_hi = min(w_lo + share, T);
 
-  LaneOffsets<true> lo;
+  typename F::Tile::Lanes lo;
   lo.init(lane);
 
   // ---- producer side: tiles of this worker's run, block-table entries fetched one tile ahead
@@ -398,10 +495,7 @@ __global__ void __launch_bounds__(kTokWarps * 32, 1) decode_attn_tokens_kernel(c
     for (int i = 0; i < NB; ++i) rws[i] = __shfl_sync(0xffffffffu, row, i);
     if (elect_one()) {
       mbar_arrive_expect_tx(bar, 2 * NB * BLOCK_BYTES);
-#pragma unroll
-      for (int i = 0; i < NB; ++i) tma_load_2d(stage_addr + i * BLOCK_BYTES, &P.tmK, 0, rws[i], bar);
-#pragma unroll
-      for (int i = 0; i < NB; ++i) tma_load_2d(stage_addr + (NB + i) * BLOCK_BYTES, &P.tmV, 0, rws[i], bar);
+      F::Tile::template load_tile<NB>(P, stage_addr, rws, bar);
     }
     if (++ps.t == ps.t_end) p_ok = next_tok_segment(p_pos, w_hi, ps, P, cum, rows, w);
     lookup();
@@ -420,13 +514,13 @@ __global__ void __launch_bounds__(kTokWarps * 32, 1) decode_attn_tokens_kernel(c
   TokSegment cs;
 #pragma unroll 1
   while (!failed && next_tok_segment(c_pos, w_hi, cs, P, cum, rows, w)) {
-    TileState2 st;
+    typename F::State st;
     const int Hq = P.Hkv * kGroup;
     const float ks = P.k_scale ? P.k_scale[cs.kvh] : 1.f;
-    st.load_query(0, P.q + (((size_t)cs.row.b * P.n_q + cs.row.t0) * Hq + cs.kvh * kGroup + g) * kHeadDim, ks,
-                  P.sm_scale_log2e, c);
-    st.load_query(1, P.q + (((size_t)cs.row.b * P.n_q + cs.row.t1) * Hq + cs.kvh * kGroup + g) * kHeadDim, ks,
-                  P.sm_scale_log2e, c);
+    F::load_query(st, 0, P.q + (((size_t)cs.row.b * P.n_q + cs.row.t0) * Hq + cs.kvh * kGroup + g) * kHeadDim, ks,
+                  P.sm_scale_log2e, lane);
+    F::load_query(st, 1, P.q + (((size_t)cs.row.b * P.n_q + cs.row.t1) * Hq + cs.kvh * kGroup + g) * kHeadDim, ks,
+                  P.sm_scale_log2e, lane);
     st.reset();
 #pragma unroll 1
     for (int t = cs.t; t < cs.t_end; ++t) {
@@ -440,9 +534,9 @@ __global__ void __launch_bounds__(kTokWarps * 32, 1) decode_attn_tokens_kernel(c
       const uint32_t vbase = kbase + NB * BLOCK_BYTES;
       const int tok0 = t * TT;
       if ((tok0 < cs.row.lo) || (tok0 + TT > cs.row.LA))
-        st.tile<true>(lo, kbase, vbase, tok0, cs.row.loA, cs.row.LA, cs.row.lo, cs.row.L, c);
+        F::template tile<true>(st, lo, kbase, vbase, tok0, cs.row.loA, cs.row.LA, cs.row.lo, cs.row.L, lane);
       else
-        st.tile<false>(lo, kbase, vbase, tok0, cs.row.loA, cs.row.LA, cs.row.lo, cs.row.L, c);
+        F::template tile<false>(st, lo, kbase, vbase, tok0, cs.row.loA, cs.row.LA, cs.row.lo, cs.row.L, lane);
       __syncwarp();
       if (issue(kbase, bars + 8 * stage)) ++inflight;
       if (++stage == NS) { stage = 0; phase ^= 1u; }
@@ -453,17 +547,12 @@ __global__ void __launch_bounds__(kTokWarps * 32, 1) decode_attn_tokens_kernel(c
     const float vs = P.v_scale ? P.v_scale[cs.kvh] : 1.f;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      float l_tot = st.l_run[t];
-      l_tot += __shfl_xor_sync(0xffffffffu, l_tot, 1);
-      l_tot += __shfl_xor_sync(0xffffffffu, l_tot, 2);
+      float m, l_tot, o[8][2];
+      F::finish(st, t, m, l_tot, o, lane);
       const float inv = l_tot > 0.f ? vs / l_tot : 0.f;
       const size_t row = (size_t)cs.prow + 8 * t + g;
-      float* po = P.part_o + row * kHeadDim + 2 * c;
-#pragma unroll
-      for (int nd = 0; nd < 8; ++nd)
-        *reinterpret_cast<float2*>(po + 8 * nd) =
-            make_float2(st.O[nd][2 * t] * inv, st.O[nd][2 * t + 1] * inv);
-      if (c == 0) P.part_lse[row] = l_tot > 0.f ? (st.m_ref[t] + log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
+      F::Tile::store(P.part_o + row * kHeadDim, o, inv, c);
+      if (c == 0) P.part_lse[row] = l_tot > 0.f ? (m + log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
     }
     // ---- arrival; the warp that completes the (row, KV head) merges it and leaves the counter at zero
     {
@@ -505,25 +594,32 @@ __global__ void __launch_bounds__(kTokWarps * 32, 1) decode_attn_tokens_kernel(c
 // Arrival counters (one per (sequence, token pair, KV head)) and partial rows of the kernel for a batch of `batch`
 // sequences with up to n_q query tokens each.
 size_t decode_attn_tokens_counters(int batch, int n_q, int Hkv) { return (size_t)batch * ((n_q + 1) / 2) * Hkv; }
-size_t decode_attn_tokens_partial_rows(int ctas, int batch, int n_q, int Hkv) {
-  return ((size_t)ctas * kTokWarps + (size_t)batch * ((n_q + 1) / 2) * Hkv) * kPairRows;
+size_t decode_attn_tokens_partial_rows(int ctas, int batch, int n_q, int Hkv, int kv_dtype) {
+  const int warps = kv_dtype == PUZZLE_KV_FP4_E2M1 ? kTokWarpsFp4 : kTokWarpsFp8;
+  return ((size_t)ctas * warps + (size_t)batch * ((n_q + 1) / 2) * Hkv) * kPairRows;
 }
 
-cudaError_t launch_decode_attn_tokens(const DecodeParams& P, int ctas, cudaStream_t s, int* smem_limit) {
-  if (*smem_limit == 0) {
+template <typename F>
+static cudaError_t launch_tokens_variant(const DecodeParams& P, int ctas, cudaStream_t s, int& smem_limit) {
+  auto kern = decode_attn_tokens_kernel<F>;
+  if (smem_limit == 0) {
     int dev = 0, optin = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
-    if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(decode_attn_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, optin);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, optin);
     if (e != cudaSuccess) return e;
-    *smem_limit = optin;
+    smem_limit = optin;
   }
   const int rows = P.batch * ((P.n_q + 1) / 2);
-  const size_t need = 1024 + (size_t)kTokWarps * kTokStages * 2 * (kTokTile / kBlock) * kBlock * kHeadDim +
-                      kTokWarps * kTokStages * 8 + (size_t)(rows + 1) * sizeof(int);
-  if (need > (size_t)*smem_limit) return cudaErrorInvalidValue;  // too many rows for the schedule array
-  return launch_dependent(decode_attn_tokens_kernel, dim3(ctas), dim3(kTokWarps * 32), need, s, P);
+  const size_t need = 1024 + (size_t)F::kWarps * kTokStages * 2 * (kTokTile / kBlock) * F::Tile::kBlockBytes +
+                      F::kWarps * kTokStages * 8 + (size_t)(rows + 1) * sizeof(int);
+  if (need > (size_t)smem_limit) return cudaErrorInvalidValue;  // too many rows for the schedule array
+  return launch_dependent(kern, dim3(ctas), dim3(F::kWarps * 32), need, s, P);
+}
+
+cudaError_t launch_decode_attn_tokens(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit) {
+  return kv_dtype == PUZZLE_KV_FP4_E2M1 ? launch_tokens_variant<Fp4Pair>(P, ctas, s, smem_limit[1])
+                                        : launch_tokens_variant<Fp8Pair>(P, ctas, s, smem_limit[0]);
 }
 
 }  // namespace puzzle

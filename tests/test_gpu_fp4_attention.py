@@ -291,3 +291,87 @@ def test_partials_over_context_shards_merge_to_the_whole():
                                 world, lse_out=lse_out)
     torch.cuda.synchronize()
     c.check(out.double().cpu().numpy(), lse_out.double().cpu().numpy())
+
+
+def _tokens(c, ws=None):
+    P = c.P
+    if ws is None:
+        ws = torch.empty(P.puzzle_decode_attn_tokens_workspace_bytes(c.desc, c.batch, c.n_q), dtype=torch.uint8,
+                         device="cuda").fill_(0xFF)
+        P.puzzle_decode_attn_tokens_workspace_init(c.desc, c.batch, c.n_q, ws)
+    out = torch.full((c.batch, c.n_q, c.hq, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((c.batch, c.n_q, c.hq), 7.0, device="cuda")
+    P.puzzle_decode_attn_tokens(c.desc, c.view, c.d["q"], c.d["sinks"], out, lse, q_lens=c.d["q_lens"], workspace=ws,
+                                dev_status=c.status)
+    torch.cuda.synchronize()
+    return out.double().cpu().numpy(), lse.double().cpu().numpy()
+
+
+def _check_tokens(c, ws=None):
+    got, lse = _tokens(c, ws)
+    ql = np.full(c.batch, c.n_q) if c.q_lens is None else np.clip(c.q_lens, 0, c.n_q)
+    for i in range(c.n_q):
+        real = np.flatnonzero(i < ql)
+        c.check(got[:, i], lse[:, i], token=i, rows=real)
+        rest = np.flatnonzero(i >= ql)
+        assert (got[rest, i] == 7.0).all() and (lse[rest, i] == 7.0).all()      # rows behind the last token
+    assert int(c.status.item()) == 0
+
+
+@pytest.mark.parametrize("n_q", [1, 2, 3, 4, 5, 8])
+@pytest.mark.parametrize("window", [0, 1, 16, 100])
+def test_several_tokens(n_q, window):
+    """Every query token against the oracle's single step at its position: ragged counts, sequences shorter than their
+    tokens, tokens behind the last one."""
+    for q_lens in (None, [n_q, 1, 2, 0, n_q, 3, n_q, -1, 1, n_q + 4]):
+        _check_tokens(Case([700, 1, 2, 16, 17, 333, 64, 65, 3, 2100], window=window, seed=n_q + window, n_q=n_q,
+                           q_lens=q_lens).upload())
+
+
+@pytest.mark.parametrize("hkv", [1, 3, 8])
+def test_several_tokens_head_counts_without_sinks(hkv):
+    _check_tokens(Case([130, 0, 257, 48], hkv=hkv, paged=hkv != 3, sinks=False, seed=hkv, n_q=3).upload())
+
+
+@pytest.mark.parametrize("length", [1, 2, 15, 16, 17, 63, 64, 65, 66, 127, 128, 129])
+def test_several_tokens_at_tile_edges(length):
+    _check_tokens(Case([length, length + 1], hkv=1, max_blocks=20, seed=length, n_q=2).upload())
+    _check_tokens(Case([length, length + 1], hkv=1, max_blocks=20, seed=length, n_q=2, window=33).upload())
+
+
+def test_several_tokens_on_one_workspace_and_in_a_graph():
+    import paper_2602_11937_b200 as P
+    d = P.layer_desc(kv_dtype=P.KV_FP4_E2M1, num_q_heads=16, num_kv_heads=2)
+    ws = torch.empty(P.puzzle_decode_attn_tokens_workspace_bytes(d, 4, 5), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    P.puzzle_decode_attn_tokens_workspace_init(d, 4, 1, ws)
+    for n_q in (5, 2, 4, 1, 5):
+        c = Case([900, 65, 3, 400], seed=n_q, n_q=n_q).upload()
+        _check_tokens(c, ws)
+    out, lse = torch.empty_like(c.d["q"]), torch.empty(4, 5, 16, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        P.puzzle_decode_attn_tokens(c.desc, c.view, c.d["q"], c.d["sinks"], out, lse, workspace=ws)
+    for _ in range(2):
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        for i in range(5):
+            c.check(out[:, i].double().cpu().numpy(), lse[:, i].double().cpu().numpy(), token=i)
+
+
+def test_single_steps_and_several_tokens_agree():
+    """One decode row per query token (paging.multi_token_args) and the paired form: the same values."""
+    import paper_2602_11937_b200 as P
+    c = Case([700, 129, 5], seed=30, n_q=3).upload()
+    lens, table = P.multi_token_args(c.d["lens"], c.d["table"], 3)
+    view = P.kv_view(c.d["k"], c.d["v"], lens, block_table=table, k_scale=c.d["k_scale"], v_scale=c.d["v_scale"])
+    ws = torch.empty(P.puzzle_decode_attn_workspace_bytes(c.desc, 9, 0), dtype=torch.uint8, device="cuda")
+    P.puzzle_decode_attn_workspace_init(c.desc, 9, ws)
+    out = torch.empty(9, 16, 64, dtype=torch.bfloat16, device="cuda")
+    lse = torch.empty(9, 16, device="cuda")
+    P.puzzle_decode_attn(c.desc, view, c.d["q"].view(9, 16, 64), c.d["sinks"], out, lse, workspace=ws)
+    torch.cuda.synchronize()
+    for i in range(3):
+        c.check(out.view(3, 3, 16, 64)[:, i].double().cpu().numpy(), lse.view(3, 3, 16)[:, i].double().cpu().numpy(), token=i)
+    _check_tokens(c)
