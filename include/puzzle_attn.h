@@ -267,9 +267,10 @@ PUZZLE_API puzzle_status puzzle_decode_attn_workspace_init(const puzzle_layer_de
  *     of many short contexts, are cut evenly over all warps, which has the shorter set-up; and
  *     when no (sequence, KV head) can have more than four tiles (narrow windows, very short
  *     contexts) nothing is cut: a group of four warps, or one warp when there are very many
- *     pairs, takes the pair whole and writes the output itself.  PUZZLE_SCHED_CTA and
+ *     pairs, takes the pair whole and writes the output itself.  (On the 4-bit cache a fourth kernel, whole
+ *     pairs by groups of 1 to 16 warps, serves launches that fill the device without being cut.)  PUZZLE_SCHED_CTA and
  *     PUZZLE_SCHED_WARP pin the first or the second kernel (PUZZLE_SCHED_CTA needs batch <= 1024,
- *     else PUZZLE_ERR_UNSUPPORTED);
+ *     4-bit cache 640, else PUZZLE_ERR_UNSUPPORTED);
  *   workspace: device scratch of at least puzzle_decode_attn_workspace_bytes(...) bytes, 16-byte
  *     aligned, prepared once by puzzle_decode_attn_workspace_init; calls that share a workspace must
  *     not overlap on the GPU.  Besides partials and counters it keeps the CTA speeds between calls:
@@ -341,7 +342,7 @@ PUZZLE_API puzzle_status puzzle_decode_step_host(const puzzle_layer_desc* desc, 
 /* Decode attention for up to n_q new tokens per sequence in one call: the tokens of a multi-token decode step, or
  * a chunk of a prompt after its bulk append (puzzle_kv_append_tokens), i.e. the input half of the paper's
  * fixed-length scenarios (Section "Optimized Scenarios"), on full and window layers (Section "Window attention for
- * long-context inference") over the FP8 cache (Section "KV Quantization").  Query token i of sequence b sits at
+ * long-context inference") over the FP8 cache (Section "KV Quantization") or the 4-bit one.  Query token i of sequence b sits at
  * position p = seq_lens[b] - q_lens[b] + i (seq_lens counted AFTER the append of all q_lens[b] tokens) and is one
  * decode step of puzzle_decode_attn over the keys [p + 1 - min(W, p + 1), p] (all of [0, p] when window == 0): the
  * mask is causal.  Pairs of query tokens share one pass over the cache tiles, so two tokens cost little more than
@@ -442,7 +443,7 @@ PUZZLE_API const char* puzzle_status_string(puzzle_status s);
 
 /* Which of the library's kernels puzzle_decode_attn would launch for these
  * arguments ("decode_attn_cta_kernel", "decode_attn_kernel",
- * "decode_attn_small_kernel"; host string, never NULL; "invalid arguments" when
+ * "decode_attn_small_kernel", "decode_attn_group_kernel"; host string, never NULL; "invalid arguments" when
  * the call would be refused).  The choice follows from desc, the batch, the
  * width of a block-table row and num_splits alone, so nothing is launched or
  * read on the device.  For logs and benchmarks that name what they time; the

@@ -34,7 +34,7 @@ struct DeviceInfo {
   int sm_count = 0;
   // dynamic shared-memory limits already set per kernel and cache type; 0 = not raised yet
   int smem_warp[3] = {0, 0, 0}, smem_cta[3] = {0, 0, 0}, smem_small[3] = {0, 0, 0};
-  int smem_tc = 0, smem_tokens[2] = {0, 0};
+  int smem_tc = 0, smem_tokens[2] = {0, 0}, smem_group[5] = {0, 0, 0, 0, 0};
 };
 DeviceInfo& device_info() {
   static DeviceInfo info[64];
@@ -95,14 +95,27 @@ bool make_cache_map(CUtensorMap* m, void* base, long long rows, int elem_bytes, 
   return r == CUDA_SUCCESS;
 }
 
-// How a kernel reaches the cache: tensor maps of rows of row_bytes bytes, or the plain addresses of a 4-bit cache.
+// 2-D view of a 4-bit cache: one row per (block, KV head), fetched four rows at a time (box of one row, as a gather
+// wants it), unswizzled.
+bool make_fp4_map(CUtensorMap* m, void* base, long long rows) {
+  EncodeTiledFn enc = encode_tiled();
+  if (!enc) return false;
+  const cuuint64_t dims[2] = {PUZZLE_FP4_BLOCK_BYTES / 4, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {PUZZLE_FP4_BLOCK_BYTES};
+  const cuuint32_t box[2] = {PUZZLE_FP4_BLOCK_BYTES / 4, 1};
+  const cuuint32_t estr[2] = {1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_INT32, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// How a kernel reaches the cache: tensor maps of rows of row_bytes bytes (4-bit cache: of whole blocks).
 bool set_cache(DecodeParams* P, const puzzle_layer_desc* d, const puzzle_kv_view* kv, int row_bytes) {
   if (d->kv_dtype == PUZZLE_KV_FP4_E2M1) {
-    P->k_cache = static_cast<const uint8_t*>(kv->k_cache);
-    P->v_cache = static_cast<const uint8_t*>(kv->v_cache);
+    const long long rows = kv->num_blocks * d->num_kv_heads;
     P->rows_per_block = 1;
-    P->oob_row = -1;
-    return true;
+    P->oob_row = (int)rows;
+    return make_fp4_map(&P->tmK, kv->k_cache, rows) && make_fp4_map(&P->tmV, kv->v_cache, rows);
   }
   const int eb = d->kv_dtype == PUZZLE_KV_FP8_E4M3 ? 1 : 2;
   P->rows_per_block = kBlock * kHeadDim * eb / row_bytes;
@@ -171,6 +184,7 @@ size_t counter_bytes(int batch, int Hkv) {
 // launch can be large: with at most a few tiles per warp (window layers, short contexts) a launch is a chain of
 // latencies, which the warp-scheduled kernel's shorter set-up serves better.  The bound on the tiles comes from
 // what the host knows: the window, or the length of a block-table row.
+int cta_max_batch(int kv_dtype) { return kv_dtype == PUZZLE_KV_FP4_E2M1 ? kCtaMaxBatchFp4 : kCtaMaxBatch; }
 // Upper bound on the tiles of one (sequence, KV head) from what the host knows.
 long long tiles_per_pair_bound(const puzzle_layer_desc* d, const puzzle_kv_view* kv) {
   const int tt = tile_tokens(d->kv_dtype);
@@ -181,7 +195,7 @@ long long tiles_per_pair_bound(const puzzle_layer_desc* d, const puzzle_kv_view*
 
 bool use_cta_kernel(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int batch, int num_splits) {
   if (num_splits == PUZZLE_SCHED_CTA) return true;
-  if (num_splits != 0 || batch > kCtaMaxBatch) return false;
+  if (num_splits != 0 || batch > cta_max_batch(d->kv_dtype)) return false;
   // What the CTA-balanced kernel wins (no tail, CTAs cut by speed) grows with the length of the launch and of the
   // pairs; what it costs (a longer set-up, a claim and a hand-over per piece) weighs most on many short pairs.
   // Measured crossovers, in tiles per CTA: 64 with pairs of 256 tiles or more, about 200 at 128 tiles per pair,
@@ -192,8 +206,34 @@ bool use_cta_kernel(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int ba
 }
 
 // The kernel a call of puzzle_decode_attn runs on.
-enum class Kernel { kCta, kWarp, kWarpWholePairs, kSmall };
+enum class Kernel { kCta, kWarp, kWarpWholePairs, kSmall, kGroup };
+
+// The 4-bit cache (times below: uniform lengths, 148 SMs).  A group kernel lasts as long as the SM with the most tiles
+// (0.109 us a tile), the balanced kernels by the mean (0.122 us, and 18 us besides).  Lengths may be ragged behind the
+// bound the host has, so the group kernel has to promise a fifth, unless an SM gets so many pairs that their sum evens
+// out.  (8 x 8192 tokens: 18.3 against 24.5 us; 16 x 16384 34.8 / 44; but 8 x 32768 62 / 44, 24 x 30000 111 / 92.)
+// Of the balanced kernels the CTA-balanced one has few partials per pair and a longer set-up and tile: it wins where the
+// other would merge 32 partials or more (1 x 4096: 17.5 against 26.3 us, 8 x 16384 30.9 / 33.8) and on very long pairs
+// (16 x 65536 117 / 123).
+Kernel pick_fp4_kernel(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int batch) {
+  const long long tiles = tiles_per_pair_bound(d, kv), pairs = (long long)batch * d->num_kv_heads, sms = grid_ctas();
+  if (tiles <= kWholePairTiles && pairs <= decode_attn_small_max_pairs((int)sms)) return Kernel::kSmall;
+  const long long pairs_per_sm = (pairs + sms - 1) / sms;
+  if (pairs_per_sm * tiles <= (pairs * tiles * 9) / (sms * 10) + 91 || (pairs_per_sm >= 5 && tiles <= 64)) return Kernel::kGroup;
+  if (batch > kCtaMaxBatchFp4) return Kernel::kWarp;
+  const long long partials = std::min(tiles, sms * kDecodeWarpsFp4 / pairs);
+  return partials >= 32 || tiles >= 1024 ? Kernel::kCta : Kernel::kWarp;
+}
+// Warps per pair: as many as leave every SM's sixteen warps a pair at once; fewer still when an SM has pairs to go
+// round, where a smaller group waits less at their ends (512 x 1024 tokens: 4 warps 72.8 us, 2 65.2, 1 59.6; but with long
+// pairs one warp's share is too coarse: 256 x 4096 114, 110, 116).
+int group_warps(long long tiles, long long pairs) {
+  const long long n = (pairs + grid_ctas() - 1) / grid_ctas();
+  return n <= 1 ? 16 : n <= 2 ? 8 : n <= 4 ? 4 : (n <= 8 || tiles > 16) ? 2 : 1;
+}
+
 Kernel pick_kernel(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int batch, int num_splits) {
+  if (d->kv_dtype == PUZZLE_KV_FP4_E2M1 && num_splits == 0) return pick_fp4_kernel(d, kv, batch);
   if (use_cta_kernel(d, kv, batch, num_splits)) return Kernel::kCta;
   // Narrow windows and short contexts: with at most kWholePairTiles tiles per (sequence, KV head) a pair is not cut
   // at all.  A group of four warps (few pairs) or one warp (many pairs, or the warp-scheduled kernel pinned) takes
@@ -230,7 +270,7 @@ puzzle_status check_decode_attn_args(const puzzle_layer_desc* desc, const puzzle
   if (!q || !out) return PUZZLE_ERR_NULL;
   if (num_splits < PUZZLE_SCHED_WARP || num_splits > 65536) return PUZZLE_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(q) & 7) || (reinterpret_cast<uintptr_t>(out) & 15)) return PUZZLE_ERR_SHAPE;
-  if (num_splits == PUZZLE_SCHED_CTA && (tcgen05 || batch > kCtaMaxBatch)) return PUZZLE_ERR_UNSUPPORTED;
+  if (num_splits == PUZZLE_SCHED_CTA && (tcgen05 || batch > cta_max_batch(desc->kv_dtype))) return PUZZLE_ERR_UNSUPPORTED;
   if (tcgen05 && desc->kv_dtype != PUZZLE_KV_FP8_E4M3) return PUZZLE_ERR_UNSUPPORTED;   // that kernel reads E4M3 codes only
   return PUZZLE_OK;
 }
@@ -262,6 +302,7 @@ const char* puzzle_decode_attn_kernel_name(const puzzle_layer_desc* desc, const 
   switch (pick_kernel(desc, kv, batch, num_splits)) {
     case Kernel::kCta: return "decode_attn_cta_kernel";
     case Kernel::kSmall: return "decode_attn_small_kernel";
+    case Kernel::kGroup: return "decode_attn_group_kernel";
     default: return "decode_attn_kernel";
   }
 }
@@ -449,6 +490,10 @@ static puzzle_status decode_attn_impl(const puzzle_layer_desc* desc, const puzzl
     le = launch_decode_attn_tc(P, ctas, s, &device_info().smem_tc);
   } else {
     switch (pick_kernel(desc, kv, batch, num_splits)) {
+      case Kernel::kGroup:
+        le = launch_decode_attn_group(P, group_warps(tiles_per_pair_bound(desc, kv), batch * Hkv), ctas, s,
+                                      device_info().smem_group);
+        break;
       case Kernel::kCta:
         le = launch_decode_attn_cta(P, desc->kv_dtype, ctas, s, device_info().smem_cta);
         break;

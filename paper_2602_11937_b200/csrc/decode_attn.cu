@@ -83,15 +83,7 @@ struct Producer {
         if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
       }
     }
-    // the copies are issued by one lane, which collects the row coordinates first: a TMA instruction takes
-    // warp-uniform operands, so issuing from several lanes would be serialised lane by lane anyway
-    int rows[NB];
-#pragma unroll
-    for (int i = 0; i < NB; ++i) rows[i] = __shfl_sync(0xffffffffu, row, i);
-    if (elect_one()) {
-      mbar_arrive_expect_tx(bar, 2 * NB * F::kBlockBytes);
-      F::template load_tile<NB>(P, stage_addr, rows, bar);
-    }
+    F::template load_tile<NB>(P, stage_addr, row, bar, lane, [] {});
     if (++seg.t == seg.t_end) {
       ok = next_segment<TT>(cur, seg, P, cum, lens, w);
       skip_empty(P, cum, lens, w);
@@ -201,7 +193,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_kernel(const __grid_co
       // ---- refill this stage with the tile NS ahead
       __syncwarp();
       if (prod.template issue<F>(P, cum, lens, w, lane, kbase, bars + 8 * stage)) ++inflight;
-      if (++stage == NS) { stage = 0; phase ^= 1u; }
+        if (++stage == NS) { stage = 0; phase ^= 1u; }
     }
     if (failed) break;
 

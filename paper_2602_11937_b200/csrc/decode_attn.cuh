@@ -11,10 +11,9 @@
 namespace puzzle {
 
 struct alignas(64) DecodeParams {
-  CUtensorMap tmK;  // rows of 128 bytes (two FP8 tokens or one bf16 token), box = one 16-token block of one KV head
+  CUtensorMap tmK;  // rows of 128 bytes (two FP8 tokens or one bf16 token), box = one 16-token block of one KV head;
+                    // 4-bit cache: rows of one block of one KV head
   CUtensorMap tmV;
-  const uint8_t* k_cache;  // the 4-bit cache goes without tensor maps: a block is one bulk copy from here
-  const uint8_t* v_cache;
   const __nv_bfloat16* q;
   const int32_t* block_table;
   const int32_t* seq_lens;
@@ -34,7 +33,7 @@ struct alignas(64) DecodeParams {
   int num_splits;  // 0 = balanced schedule
   int n_q;         // multi-token kernel: query tokens per sequence in q / out ([batch][n_q][Hq][D]); else unused
   const int32_t* q_lens;  // multi-token kernel: real query tokens per sequence [batch], or null (= n_q)
-  int oob_row;     // a row coordinate outside the tensor maps: loads from it return zeros (4-bit cache: -1)
+  int oob_row;     // a row coordinate outside the tensor maps: loads from it return zeros
   int rows_per_block;  // tensor-map rows (128 bytes each) per (block, KV head): 8 (FP8) or 16 (bf16); 4-bit cache: 1
   float sm_scale_log2e;
 };
@@ -54,12 +53,20 @@ struct MergeParams {
 // warp and tokens per tile (the unit of the schedule and of one pipeline stage).
 constexpr int kDecodeWarpsFp8 = 12, kDecodeStagesFp8 = 2, kTileFp8 = 64;
 constexpr int kDecodeWarpsBf16 = 12, kDecodeStagesBf16 = 2, kTileBf16 = 32;
+// 16 warps of 64-token tiles (128 registers, a few words spilled outside the tile loop): 122 us at 256 x 4096 against
+// 132 with 12 warps and no spill.
 constexpr int kDecodeWarpsFp4 = 16, kDecodeStagesFp4 = 2, kTileFp4 = 64;
+// The 4-bit cache on the CTA-balanced kernel: what a tile costs besides its arithmetic (claim, table look-up, record,
+// wait) weighs half again as much as on the E4M3 cache, so tiles are 128 tokens there, and eleven warps are what
+// shared memory holds of them (64 tokens: 16 x 64K at 131 us with 12 or 16 warps; 128: 127 with 8, 121 with 10, 117
+// with 11).
+constexpr int kCtaWarpsFp4 = 11, kCtaTileFp4 = 128;
 // The CTA-balanced kernel keeps its schedule arrays beside the TMA rings and the deposit buffers in shared memory,
 // which bounds the batch it takes.  Launches with at least kCtaRateMinTiles tiles per CTA note the speed of every
 // CTA slot at the start of the workspace (before the arrival counters: a CTA counter, the buffer switch, two pad words, then two
 // float buffers of one speed per CTA) and are cut by the speeds the launch before them noted.
 constexpr int kCtaMaxBatch = 1024;
+constexpr int kCtaMaxBatchFp4 = 640;     // its rings leave less room for the schedule
 constexpr int kCtaMinTilesPerCta = 64;   // below this bound on the tiles per CTA the warp-scheduled kernel is used (more with short pairs)
 constexpr int kCtaRateMinTiles = 256;
 constexpr int kWholePairTiles = 4;       // up to this many tiles per (sequence, KV head) a pair goes to one warp whole
@@ -77,6 +84,10 @@ cudaError_t launch_decode_attn_cta(const DecodeParams& P, int kv_dtype, int ctas
 // with one split per pair keeps its TMA rings full.
 cudaError_t launch_decode_attn_small(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit);
 int decode_attn_small_max_pairs(int ctas);
+// The group kernel of the 4-bit cache: workers of 1, 2, 4, 8 or 16 warps take whole pairs; no workspace use.
+// smem_limit[5] as above.
+cudaError_t launch_decode_attn_group(const DecodeParams& P, int warps, int ctas, cudaStream_t s, int* smem_limit);
+
 // The multi-token kernel (FP8 or 4-bit cache, balanced schedule): P.n_q, P.q_lens set; P.counters has one word per
 // (sequence, token pair, KV head); partial rows: decode_attn_tokens_partial_rows(...); smem_limit[2] as above.
 cudaError_t launch_decode_attn_tokens(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit);

@@ -210,6 +210,11 @@ struct ClaimProducer {
   __device__ __forceinline__ int issue(uint32_t ctl_a, const DecodeParams& P, const int* cum, uint32_t pc_a,
                                        uint32_t rec_a, int lane, uint32_t stage_addr, uint32_t bar, uint32_t desc_a) {
     if (d.n <= 0) return 0;
+    if constexpr (F::kLeanClaims) {   // everything but the next tile's index and the count lives in the claim's record
+      const int4 a = lds128_volatile(rec_a), z = lds128_volatile(rec_a + 16);
+      d.b = a.x; d.kvh = a.y; d.k = a.w;
+      d.total = z.x; d.L = z.y; d.lo = z.z;
+    }
     int row = P.oob_row;
     if (lane < NB) {
       if (phys >= 0 && phys < P.num_blocks) {
@@ -218,17 +223,10 @@ struct ClaimProducer {
         if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
       }
     }
-    // the copies are issued by one lane, which collects the row coordinates first: a TMA instruction takes
-    // warp-uniform operands, so issuing from several lanes would be serialised lane by lane anyway
-    int rows[NB];
-#pragma unroll
-    for (int i = 0; i < NB; ++i) rows[i] = __shfl_sync(0xffffffffu, row, i);
-    if (elect_one()) {
+    F::template load_tile<NB>(P, stage_addr, row, bar, lane, [&] {
       sts128(desc_a, make_int4(d.b, d.kvh, d.t, d.k));
       sts128(desc_a + 16, make_int4(d.total, d.L, d.lo, 0));
-      mbar_arrive_expect_tx(bar, 2 * NB * F::kBlockBytes);
-      F::template load_tile<NB>(P, stage_addr, rows, bar);
-    }
+    });
     ++d.t;
     bool ok = true;
     if (--d.n == 0) ok = claim(ctl_a, P, cum, pc_a, rec_a, lane);
@@ -266,7 +264,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
 
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
-  uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  uint8_t* smem = smem_raw + (((raw + F::kAlign - 1u) & ~(F::kAlign - 1u)) - raw);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, c = lane & 3;  // this lane's query head within the group / column quad
@@ -380,7 +378,8 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
   // Every CTA evaluates the same expressions on the same numbers, so all agree on the cuts.
   {
     const int T = cum[P.batch];
-    const bool large = T / nC >= kCtaRateMinTiles && nC <= 256;
+    constexpr int kLarge = TT > 64 ? kCtaRateMinTiles * 64 / TT : kCtaRateMinTiles;
+    const bool large = T / nC >= kLarge && nC <= 256;
     const int nR = large ? nC : max(1, min(nC, T));
     const int snap = max(1, (T / nR) >> 5);
     const float per_share = (float)T / (float)share[nC];
@@ -440,6 +439,13 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
       const int pos = ctl.lo + warp * first_n;
       prod.d.b = s0.z; prod.d.kvh = s0.w; prod.d.t = s1.x + (pos - s0.x); prod.d.k = 0;
       prod.d.total = min(s0.y, ctl.end) - max(s0.x, ctl.lo); prod.d.L = s1.y; prod.d.lo = s1.z; prod.d.n = first_n;
+      if constexpr (F::kLeanClaims) {
+        if (lane == 0) {
+          sts128(rec_a, make_int4(prod.d.b, prod.d.kvh, prod.d.t, prod.d.k));
+          sts128(rec_a + 16, make_int4(prod.d.total, prod.d.L, prod.d.lo, first_n));
+        }
+        __syncwarp();
+      }
     } else {
       __syncwarp();
       failed = !prod.claim(ctl_a, P, cum, pc_a, rec_a, lane);
@@ -659,7 +665,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
 template <int NW, int NS, int TT, typename F>
 static size_t cta_smem_bytes(int batch, int ctas) {
   constexpr int STAGE_BYTES = 2 * (TT / kBlock) * F::kBlockBytes;
-  return 1024 + (size_t)NW * NS * STAGE_BYTES + NW * NS * 8 + (size_t)NW * NS * sizeof(TileDesc) +
+  return F::kAlign + (size_t)NW * NS * STAGE_BYTES + NW * NS * 8 + (size_t)NW * NS * sizeof(TileDesc) +
          NW * sizeof(TileDesc) + NW * sizeof(PairCache) + (size_t)NW * 4 * 32 * sizeof(float4) +
          2 * NW * kGroup * sizeof(float) + 32 * sizeof(int) + 2 * kPieceSlots * sizeof(int) + sizeof(CtaCtl) +
          2 * (size_t)((ctas + 1 + 3) & ~3) * sizeof(int) + (size_t)(batch + 1) * sizeof(int);
@@ -688,7 +694,7 @@ cudaError_t launch_decode_attn_cta(const DecodeParams& P, int kv_dtype, int ctas
     case PUZZLE_KV_BF16:
       return launch_cta_variant<kDecodeWarpsBf16, kDecodeStagesBf16, kTileBf16, SwizzledTile<false>>(P, ctas, s,
                                                                                                       smem_limit[1]);
-    default: return launch_cta_variant<kDecodeWarpsFp4, kDecodeStagesFp4, kTileFp4, Fp4Tile>(P, ctas, s, smem_limit[2]);
+    default: return launch_cta_variant<kCtaWarpsFp4, kDecodeStagesFp4, kCtaTileFp4, Fp4Tile>(P, ctas, s, smem_limit[2]);
   }
 }
 

@@ -97,13 +97,7 @@ __global__ void __launch_bounds__(kSmallWarps * 32, 1) decode_attn_small_kernel(
           else if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
         }
       }
-      int rows[NB];
-#pragma unroll
-      for (int i = 0; i < NB; ++i) rows[i] = __shfl_sync(0xffffffffu, row, i);
-      if (elect_one()) {
-        mbar_arrive_expect_tx(bar, STAGE_BYTES);
-        F::template load_tile<NB>(P, stage, rows, bar);
-      }
+      F::template load_tile<NB>(P, stage, row, bar, lane, [] {});
       // ---- query, scales and sink while the tile is in flight
       F::load_query(st, P.q + ((size_t)b * (P.Hkv * kGroup) + kvh * kGroup + g) * kHeadDim,
                     P.k_scale && F::kScaled ? P.k_scale[kvh] : 1.f, P.sm_scale_log2e, lane);
@@ -200,7 +194,7 @@ cudaError_t launch_decode_attn_small(const DecodeParams& P, int kv_dtype, int ct
   switch (kv_dtype) {
     case PUZZLE_KV_FP8_E4M3: return launch_small_variant<kTileFp8, SwizzledTile<true>>(P, ctas, s, smem_limit[0]);
     case PUZZLE_KV_BF16: return launch_small_variant<kTileBf16, SwizzledTile<false>>(P, ctas, s, smem_limit[1]);
-    default: return launch_small_variant<kTileFp4, Fp4Tile>(P, ctas, s, smem_limit[2]);
+    default: return launch_small_variant<64, Fp4Tile>(P, ctas, s, smem_limit[2]);
   }
 }
 

@@ -324,24 +324,23 @@ struct Fp4Pair {
           if (tk < lo || tk >= L) s[1][blk][2 * e] = s[1][blk][2 * e + 1] = -INFINITY;
         }
     }
-    float neg[2][2];
+    float2 neg[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk) {
-        mx[0] = fmaxf(mx[0], fmaxf(s[t][blk][0], s[t][blk][2]));
-        mx[1] = fmaxf(mx[1], fmaxf(s[t][blk][1], s[t][blk][3]));
+        mx[0] = max3(mx[0], s[t][blk][0], s[t][blk][2]);
+        mx[1] = max3(mx[1], s[t][blk][1], s[t][blk][3]);
       }
       st.t[t].raise(mx);
-      neg[t][0] = st.t[t].negated(0);
-      neg[t][1] = st.t[t].negated(1);
+      neg[t] = st.t[t].negated();
     }
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) {
       uint32_t b[2][2], a[4][4];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) st.t[t].weights(s[t][blk], neg[t][0], neg[t][1], b[t][0], b[t][1]);
+      for (int t = 0; t < 2; ++t) st.t[t].weights(s[t][blk], neg[t], b[t][0], b[t][1]);
       fp4_v_fragments<EDGE>(vbase + blk * kFp4BlockBytes, at, tok0 + kBlock * blk + 2 * c, loA, L, a);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -490,13 +489,7 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) decode_attn_tokens_kernel(c
         if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
       }
     }
-    int rws[NB];
-#pragma unroll
-    for (int i = 0; i < NB; ++i) rws[i] = __shfl_sync(0xffffffffu, row, i);
-    if (elect_one()) {
-      mbar_arrive_expect_tx(bar, 2 * NB * BLOCK_BYTES);
-      F::Tile::template load_tile<NB>(P, stage_addr, rws, bar);
-    }
+    F::Tile::template load_tile<NB>(P, stage_addr, row, bar, lane, [] {});
     if (++ps.t == ps.t_end) p_ok = next_tok_segment(p_pos, w_hi, ps, P, cum, rows, w);
     lookup();
     return true;

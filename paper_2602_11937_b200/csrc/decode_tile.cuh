@@ -327,6 +327,8 @@ template <bool FP8>
 struct SwizzledTile {
   static constexpr int kBlockBytes = kBlock * kHeadDim * (FP8 ? 1 : 2);   // one (block, KV head) of K or of V
   static constexpr bool kScaled = FP8;
+  static constexpr bool kLeanClaims = false;
+  static constexpr int kAlign = 1024;   // of the stages in shared memory: the swizzle repeats every 1 KiB
   using Lanes = LaneOffsets<FP8>;
   using State = TileState;
 
@@ -334,14 +336,24 @@ struct SwizzledTile {
     tma_prefetch_desc(&P.tmK);
     tma_prefetch_desc(&P.tmV);
   }
-  // Issued by one lane; rows[i]: first row of block i in the tensor maps (P.oob_row: the block is fetched as zeros).
-  template <int NB>
-  static __device__ __forceinline__ void load_tile(const DecodeParams& P, uint32_t stage, const int (&rows)[NB],
-                                                   uint32_t bar) {
+  // Starts the copies of a tile of NB blocks into `stage`; all lanes call it.  row, in lane i < NB: first row of block i
+  // in the tensor maps (P.oob_row: the block is fetched as zeros).  note(): run by one lane on the way.
+  template <int NB, typename Note>
+  static __device__ __forceinline__ void load_tile(const DecodeParams& P, uint32_t stage, int row, uint32_t bar, int,
+                                                   Note note) {
+    // the copies are issued by one lane, which collects the row coordinates first: a TMA instruction takes
+    // warp-uniform operands, so issuing from several lanes would be serialised lane by lane anyway
+    int rows[NB];
 #pragma unroll
-    for (int i = 0; i < NB; ++i) tma_load_2d(stage + i * kBlockBytes, &P.tmK, 0, rows[i], bar);
+    for (int i = 0; i < NB; ++i) rows[i] = __shfl_sync(0xffffffffu, row, i);
+    if (elect_one()) {
+      note();
+      mbar_arrive_expect_tx(bar, 2 * NB * kBlockBytes);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) tma_load_2d(stage + (NB + i) * kBlockBytes, &P.tmV, 0, rows[i], bar);
+      for (int i = 0; i < NB; ++i) tma_load_2d(stage + i * kBlockBytes, &P.tmK, 0, rows[i], bar);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) tma_load_2d(stage + (NB + i) * kBlockBytes, &P.tmV, 0, rows[i], bar);
+    }
   }
   static __device__ __forceinline__ void load_query(State& st, const __nv_bfloat16* qrow, float ks, float sm, int lane) {
     st.template load_query<FP8>(qrow, ks, sm, lane & 3);

@@ -13,9 +13,11 @@
 //    eighth of the bf16 output's own rounding and independent from key to key.  The sum takes the float32 weights.
 //  * The running maximum is only raised (a reduction over the lanes, accumulators rescaled) when some lane sees a logit
 //    more than 2^8 above it: one vote per tile otherwise.
-//  * A block arrives by one bulk copy as it lies in HBM; every shared-memory read of a tile (8 bytes per lane of K and
+//  * A block arrives as it lies in HBM; every shared-memory read of a tile (8 bytes per lane of K and
 //    V, 2 and 4 of the scales) is conflict free because the format's order is the fragments' order.
 #pragma once
+
+#include <cuda_fp16.h>
 
 #include "common.cuh"
 #include "decode_attn.cuh"
@@ -24,9 +26,6 @@
 
 namespace puzzle {
 namespace {
-
-// What a tile reads for a block that is not there (a bad table entry, or wholly outside the visible keys): zeros.
-__device__ __align__(128) uint8_t fp4_zero_block[kFp4BlockBytes];
 
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
   uint2 v;
@@ -48,17 +47,52 @@ __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+// a * b with b's low (high) half on both sides: the half select is part of the multiply, not an instruction.
+__device__ __forceinline__ uint32_t hmul2_lo(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<__half2*>(&a), __low2half2(*reinterpret_cast<__half2*>(&b)));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t hmul2_hi(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<__half2*>(&a), __high2half2(*reinterpret_cast<__half2*>(&b)));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Two float32 operations in one instruction, and the largest of three in one.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 // 8x8 transpose of 16-bit cells: lane l holds row l / 4, columns 2 (l % 4) and the next, before and after.
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
   return r;
 }
-// Bulk copy global -> shared, completion counted in bytes on an mbarrier; addresses and size multiples of 16 bytes.
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(dst), "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(bar)
-               : "memory");
+// Four rows of a 2-D tensor (any four; rows outside it arrive as zeros), one below the other, in one tiled TMA load.
+// The map's box is one row; x * element size a multiple of 16 bytes.
+__device__ __forceinline__ void tma_gather4(uint32_t dst, const void* tmap, int x, int r0, int r1, int r2, int r3,
+                                            uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], "
+      "[%1, {%2, %3, %4, %5, %6}], [%7];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar)
+      : "memory");
 }
 
 struct Fp4Lanes {
@@ -88,15 +122,14 @@ __device__ __forceinline__ uint32_t fp4_visible_scales(uint32_t sc, int t, int l
 __device__ __forceinline__ void fp4_k_fragments(uint32_t block, const Fp4Lanes& at, uint32_t (&a)[4][4]) {
   const uint2 k0 = lds64(block + at.k), k1 = lds64(block + at.k + 256);
   const uint32_t sc = e4m3x2_to_f16x2(lds16(block + at.ks));
-  const uint32_t s0 = prmt(sc, 0u, 0x1010u), s1 = prmt(sc, 0u, 0x3232u);
   e2m1x8_to_f16x2x4(k0.x, a[0][0], a[0][2], a[1][0], a[1][2]);
   e2m1x8_to_f16x2x4(k0.y, a[2][0], a[2][2], a[3][0], a[3][2]);
   e2m1x8_to_f16x2x4(k1.x, a[0][1], a[0][3], a[1][1], a[1][3]);
   e2m1x8_to_f16x2x4(k1.y, a[2][1], a[2][3], a[3][1], a[3][3]);
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
-    a[s][0] = hmul2(a[s][0], s0); a[s][2] = hmul2(a[s][2], s0);
-    a[s][1] = hmul2(a[s][1], s1); a[s][3] = hmul2(a[s][3], s1);
+    a[s][0] = hmul2_lo(a[s][0], sc); a[s][2] = hmul2_lo(a[s][2], sc);
+    a[s][1] = hmul2_hi(a[s][1], sc); a[s][3] = hmul2_hi(a[s][3], sc);
   }
 }
 // V^T rows of m-tile i: channels 8g + 2i (row g) and 8g + 2i + 1 (row g + 8); columns: the 16 tokens in order.
@@ -122,12 +155,14 @@ __device__ __forceinline__ void fp4_v_fragments(uint32_t block, const Fp4Lanes& 
 // lane's columns.  O[i]: channels 8g + 2i (first two) and 8g + 2i + 1 (last two) of those heads.
 struct Fp4State {
   uint32_t q[4][2];
-  float alpha[2], m_ref[2], l_run[2];
+  float alpha[2], m_ref[2];
+  float2 l_run;
   float O[4][4];
 
   __device__ __forceinline__ void reset() {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) { m_ref[e] = -INFINITY; l_run[e] = 0.f; }
+    for (int e = 0; e < 2; ++e) m_ref[e] = -INFINITY;
+    l_run = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) O[i][0] = O[i][1] = O[i][2] = O[i][3] = 0.f;
   }
@@ -176,7 +211,7 @@ struct Fp4State {
       for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
       if (m > m_ref[e] + kLazyLog2) {
         const float corr = ex2(m_ref[e] - m);   // 0 on the first visible tile
-        l_run[e] *= corr;
+        if (e) l_run.y *= corr; else l_run.x *= corr;
 #pragma unroll
         for (int i = 0; i < 4; ++i) { O[i][e] *= corr; O[i][2 + e] *= corr; }
         m_ref[e] = m;
@@ -184,34 +219,48 @@ struct Fp4State {
     }
   }
   // Weights of one block's logits s[4] (token g: heads 2c, 2c+1; token g + 8) as the B operand of O^T += V^T P^T.
-  __device__ __forceinline__ void weights(const float (&s)[4], float neg0, float neg1, uint32_t& b0, uint32_t& b1) {
-    const float p0 = ex2(fmaf(s[0], alpha[0], neg0)), p1 = ex2(fmaf(s[1], alpha[1], neg1));
-    const float p2 = ex2(fmaf(s[2], alpha[0], neg0)), p3 = ex2(fmaf(s[3], alpha[1], neg1));
-    l_run[0] += p0 + p2;
-    l_run[1] += p1 + p3;
-    b0 = transpose8x8(f32x2_to_f16x2(p0, p1));
-    b1 = transpose8x8(f32x2_to_f16x2(p2, p3));
+  __device__ __forceinline__ void weights(const float (&s)[4], float2 neg, uint32_t& b0, uint32_t& b1) {
+    const float2 al = make_float2(alpha[0], alpha[1]);
+    const float2 t0 = fma2(make_float2(s[0], s[1]), al, neg), t1 = fma2(make_float2(s[2], s[3]), al, neg);
+    const float2 p0 = make_float2(ex2(t0.x), ex2(t0.y)), p1 = make_float2(ex2(t1.x), ex2(t1.y));
+    l_run = add2(l_run, add2(p0, p1));
+    b0 = transpose8x8(f32x2_to_f16x2(p0.x, p0.y));
+    b1 = transpose8x8(f32x2_to_f16x2(p1.x, p1.y));
   }
-  __device__ __forceinline__ float negated(int e) const { return m_ref[e] == -INFINITY ? 0.f : -m_ref[e]; }
+  __device__ __forceinline__ float2 negated() const {
+    return make_float2(m_ref[0] == -INFINITY ? 0.f : -m_ref[0], m_ref[1] == -INFINITY ? 0.f : -m_ref[1]);
+  }
 };
 
 // The 4-bit cache as the split-KV kernels see it (see SwizzledTile in decode_tile.cuh).
 struct Fp4Tile {
   static constexpr int kBlockBytes = kFp4BlockBytes;
   static constexpr bool kScaled = true;
+  static constexpr bool kLeanClaims = true;
+  static constexpr int kAlign = 128;
   using Lanes = Fp4Lanes;
   using State = Fp4State;
 
-  static __device__ __forceinline__ void prefetch(const DecodeParams&) {}
-  template <int NB>
-  static __device__ __forceinline__ void load_tile(const DecodeParams& P, uint32_t stage, const int (&rows)[NB],
-                                                   uint32_t bar) {
+  static __device__ __forceinline__ void prefetch(const DecodeParams& P) {
+    tma_prefetch_desc(&P.tmK);
+    tma_prefetch_desc(&P.tmV);
+  }
+  // One gather of four rows brings the K (V) blocks of 64 tokens, wherever they are: the tensor maps' rows are blocks.
+  template <int NB, typename Note>
+  static __device__ __forceinline__ void load_tile(const DecodeParams& P, uint32_t stage, int row, uint32_t bar, int,
+                                                   Note note) {
+    static_assert(NB % 4 == 0, "whole gathers");
+    int rows[NB];
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const long long at = (long long)rows[i] * kFp4BlockBytes;
-      const bool there = rows[i] != P.oob_row;
-      bulk_load(stage + i * kFp4BlockBytes, there ? P.k_cache + at : fp4_zero_block, kFp4BlockBytes, bar);
-      bulk_load(stage + (NB + i) * kFp4BlockBytes, there ? P.v_cache + at : fp4_zero_block, kFp4BlockBytes, bar);
+    for (int i = 0; i < NB; ++i) rows[i] = __shfl_sync(0xffffffffu, row, i);
+    if (elect_one()) {
+      note();
+      mbar_arrive_expect_tx(bar, 2 * NB * kBlockBytes);
+#pragma unroll
+      for (int i = 0; i < NB; i += 4) {
+        tma_gather4(stage + i * kBlockBytes, &P.tmK, 0, rows[i], rows[i + 1], rows[i + 2], rows[i + 3], bar);
+        tma_gather4(stage + (NB + i) * kBlockBytes, &P.tmV, 0, rows[i], rows[i + 1], rows[i + 2], rows[i + 3], bar);
+      }
     }
   }
   static __device__ __forceinline__ void load_query(State& st, const __nv_bfloat16* qrow, float ks, float sm, int lane) {
@@ -243,15 +292,15 @@ struct Fp4Tile {
     float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) {
-      mx[0] = fmaxf(mx[0], fmaxf(s[blk][0], s[blk][2]));
-      mx[1] = fmaxf(mx[1], fmaxf(s[blk][1], s[blk][3]));
+      mx[0] = max3(mx[0], s[blk][0], s[blk][2]);
+      mx[1] = max3(mx[1], s[blk][1], s[blk][3]);
     }
     st.raise(mx);
-    const float neg0 = st.negated(0), neg1 = st.negated(1);
+    const float2 neg = st.negated();
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) {
       uint32_t b0, b1, a[4][4];
-      st.weights(s[blk], neg0, neg1, b0, b1);
+      st.weights(s[blk], neg, b0, b1);
       fp4_v_fragments<EDGE>(vbase + blk * kFp4BlockBytes, at, tok0 + kBlock * blk + 2 * c, lo, L, a);
 #pragma unroll
       for (int i = 0; i < 4; ++i) mma_f16(st.O[i], a[i][0], a[i][1], a[i][2], a[i][3], b0, b1);
@@ -261,7 +310,7 @@ struct Fp4Tile {
   // 16c + j in o[j][0] and 16c + 8 + j in o[j][1].
   static __device__ __forceinline__ void finish(const State& st, float& m, float& l, float (&o)[8][2], int lane) {
     const int g = lane >> 2;
-    float l0 = st.l_run[0], l1 = st.l_run[1];
+    float l0 = st.l_run.x, l1 = st.l_run.y;
 #pragma unroll
     for (int d = 4; d < 32; d <<= 1) {
       l0 += __shfl_xor_sync(0xffffffffu, l0, d);

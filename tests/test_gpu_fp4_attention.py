@@ -146,6 +146,18 @@ def test_many_short_pairs():
     c.check(*c.run(0))
 
 
+@pytest.mark.parametrize("batch, hkv, longest", [(3, 2, 900), (18, 8, 300), (30, 8, 400), (64, 8, 300), (130, 8, 300),
+                                                 (170, 8, 300), (170, 8, 1100)])
+def test_whole_pairs_by_groups_of_every_size(batch, hkv, longest):
+    """One pair to an SM and up to ten: groups of 16, 8, 4, 2 and 1 warps, ragged lengths, empty and one-token ones."""
+    lens = np.random.default_rng(batch).integers(0, longest + 1, size=batch)
+    lens[:4] = [longest, 0, 1, 65][:len(lens[:4])]
+    c = Case(list(lens), hkv=hkv, seed=batch, max_blocks=-(-longest // 16)).upload()
+    assert c.P.puzzle_decode_attn_kernel_name(c.desc, c.view, batch) == "decode_attn_group_kernel"
+    c.check(*c.run(0))
+    assert int(c.status.item()) == 0
+
+
 @pytest.mark.parametrize("splits", [0, -1, -2, 4])
 def test_growing_logits_raise_the_reference(splits):
     """Keys that grow along the sequence: the running maximum is raised again and again, by less and by more than 2^8."""
