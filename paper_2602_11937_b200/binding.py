@@ -159,13 +159,19 @@ def _p(t: Optional[torch.Tensor], dtype=None, name="tensor"):
         raise ValueError("%s must be contiguous" % name)
     if dtype is not None and t.dtype != dtype:
         raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
+
+
+# The current stream's handle without a Stream object around it: a decode step's call is a few microseconds of host time.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None and torch.cuda.is_initialized():
+        return _raw_stream(torch._C._cuda_getDevice())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def layer_desc(window: int = 0, kv_dtype: int = KV_FP8_E4M3, num_q_heads: int = 64, num_kv_heads: int = 8,
@@ -270,21 +276,16 @@ def rope_view(cos_sin: torch.Tensor, interleaved: bool = False, pos_offset: Opti
     return r
 
 
-def _qkv(q, k, v) -> QKV:
-    x = QKV()
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        if t is None:
-            continue
-        if not t.is_cuda or t.dtype != torch.bfloat16:
-            raise ValueError("%s must be a bf16 CUDA tensor" % name)
-        if t.dim() not in (3, 4):
-            raise ValueError("%s must be [batch][n_new][heads][D] or [batch][heads][D]" % name)
-        if t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != t.shape[-1]):
-            raise ValueError("the heads of a token of %s must be contiguous" % name)
-        setattr(x, name, t.data_ptr())
-        setattr(x, name + "_seq_stride", t.stride(0))
-        setattr(x, name + "_token_stride", t.stride(1) if t.dim() == 4 else 0)
-    return x
+def _rows(t: Optional[torch.Tensor], name: str):
+    """Pointer, sequence stride and token stride of new tokens' rows [batch][n_new][heads][D] or [batch][heads][D]."""
+    if t is None:
+        return None, 0, 0
+    if not t.is_cuda or t.dtype != torch.bfloat16:
+        raise ValueError("%s must be a bf16 CUDA tensor" % name)
+    stride = t.stride()
+    if stride[-1] != 1 or (t.shape[-2] > 1 and stride[-2] != t.shape[-1]):
+        raise ValueError("the heads of a token of %s must be contiguous" % name)
+    return t.data_ptr(), stride[0], stride[1] if len(stride) == 4 else 0
 
 
 def puzzle_kv_append_rope(desc: LayerDesc, view: KVView, rope: Rope, q: Optional[torch.Tensor], k_new: torch.Tensor,
@@ -295,15 +296,18 @@ def puzzle_kv_append_rope(desc: LayerDesc, view: KVView, rope: Rope, q: Optional
     of a wider array along the heads; q_out: bf16 [batch][n_new][Hq][D] contiguous, may be q; q None: k and v only."""
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
-    shape = k_new.shape[:-2]
-    for name, t, heads in (("q", q, desc.num_q_heads), ("k_new", k_new, desc.num_kv_heads),
-                           ("v_new", v_new, desc.num_kv_heads), ("q_out", q_out, desc.num_q_heads)):
-        if t is not None and tuple(t.shape) != (*shape, heads, desc.head_dim):
-            raise ValueError("%s must be %s, got %s" % (name, (*shape, heads, desc.head_dim), tuple(t.shape)))
-    qkv = _qkv(q, k_new, v_new)
+    lead = tuple(k_new.shape[:-2])
+    if len(lead) not in (1, 2):
+        raise ValueError("k_new must be [batch][n_new][heads][D] or [batch][heads][D]")
+    kv_shape, q_shape = (*lead, desc.num_kv_heads, desc.head_dim), (*lead, desc.num_q_heads, desc.head_dim)
+    for name, t, shape in (("k_new", k_new, kv_shape), ("v_new", v_new, kv_shape), ("q", q, q_shape), ("q_out", q_out, q_shape)):
+        if t is not None and t.shape != shape:
+            raise ValueError("%s must be %s, got %s" % (name, shape, tuple(t.shape)))
+    k, v, qr = _rows(k_new, "k_new"), _rows(v_new, "v_new"), _rows(q, "q")
+    qkv = QKV(qr[0], k[0], v[0], qr[1], qr[2], k[1], k[2], v[1], v[2])
     _check(_load().puzzle_kv_append_rope(ctypes.byref(desc), ctypes.byref(view), ctypes.byref(rope), ctypes.byref(qkv),
                                          _p(q_out, torch.bfloat16, "q_out"), _p(new_lens, torch.int32, "new_lens"),
-                                         shape[0], shape[1] if len(shape) == 2 else 1, _p(dev_status, torch.int32),
+                                         lead[0], lead[1] if len(lead) == 2 else 1, _p(dev_status, torch.int32),
                                          _stream(stream)), "puzzle_kv_append_rope")
 
 
@@ -405,7 +409,7 @@ def puzzle_decode_step_host_staging_bytes(desc: LayerDesc, batch: int) -> int:
 def _host_ptr(t: torch.Tensor, name: str):
     if t.is_cuda or not t.is_contiguous() or t.dtype != torch.bfloat16:
         raise ValueError("%s must be a contiguous bf16 host tensor" % name)
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def puzzle_decode_step_host(desc: LayerDesc, view: KVView, q_host: torch.Tensor, k_new_host: torch.Tensor,

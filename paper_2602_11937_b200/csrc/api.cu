@@ -34,7 +34,7 @@ struct DeviceInfo {
   int sm_count = 0;
   // dynamic shared-memory limits already set per kernel and cache type; 0 = not raised yet
   int smem_warp[3] = {0, 0, 0}, smem_cta[3] = {0, 0, 0}, smem_small[3] = {0, 0, 0};
-  int smem_tc = 0, smem_tokens[2] = {0, 0}, smem_group[5] = {0, 0, 0, 0, 0};
+  int smem_tc = 0, smem_tokens[2] = {0, 0}, smem_group[5] = {0, 0, 0, 0, 0}, smem_tokens_group[5] = {0, 0, 0, 0, 0};
 };
 DeviceInfo& device_info() {
   static DeviceInfo info[64];
@@ -159,7 +159,7 @@ cudaError_t append_fp4(const puzzle_layer_desc* d, const puzzle_kv_view* kv, con
   return launch_append(A, d->kv_dtype, false, false, s);
 }
 
-int grid_ctas() { return device_info().sm_count > 0 ? device_info().sm_count : 1; }
+int grid_ctas() { return std::max(device_info().sm_count, 1); }
 
 int decode_warps(int kv_dtype) {
   return kv_dtype == PUZZLE_KV_FP8_E4M3 ? kDecodeWarpsFp8 : (kv_dtype == PUZZLE_KV_BF16 ? kDecodeWarpsBf16 : kDecodeWarpsFp4);
@@ -230,6 +230,20 @@ Kernel pick_fp4_kernel(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int
 int group_warps(long long tiles, long long pairs) {
   const long long n = (pairs + grid_ctas() - 1) / grid_ctas();
   return n <= 1 ? 16 : n <= 2 ? 8 : n <= 4 ? 4 : (n <= 8 || tiles > 16) ? 2 : 1;
+}
+
+// Rows of two query tokens over the 4-bit cache: the same choice for the multi-token kernels.  The group kernel takes
+// 0.155 us per tile of the SM with the most tiles, the evenly cut one 0.16 per mean tile and 20 us besides, more the more
+// partials a pair has.  (4 x 1024 tokens 8.4 against 30 us, 16 x 16384 47 / 68, but 8 x 65536 160 / 119.)
+bool use_tokens_group(long long tiles, long long pairs) {
+  const long long sms = grid_ctas(), per_sm = (pairs + sms - 1) / sms;
+  const long long partials = std::min(tiles, sms * kTokWarpsFp4 / pairs);
+  if (per_sm >= 5) return tiles <= 32;   // (128 x 4096: 105 us against 90; 128 x 1024 30 / 37)
+  return per_sm * tiles <= (pairs * tiles * 9) / (sms * 10) + 60 + 2 * partials;
+}
+int tokens_group_warps(long long tiles, long long pairs) {   // twelve warps per CTA
+  const long long n = (pairs + grid_ctas() - 1) / grid_ctas();
+  return n <= 1 ? 12 : n <= 2 ? 6 : n <= 3 ? 4 : (n <= 6 || tiles > 16) ? 2 : 1;
 }
 
 Kernel pick_kernel(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int batch, int num_splits) {
@@ -650,6 +664,16 @@ puzzle_status puzzle_decode_attn_tokens(const puzzle_layer_desc* desc, const puz
   P.n_q = n_q;
   P.q_lens = q_lens;
   P.sm_scale_log2e = desc->sm_scale * 1.4426950408889634f;
+  if (desc->kv_dtype == PUZZLE_KV_FP4_E2M1) {
+    const long long tiles = tiles_per_pair_bound(desc, kv), pairs = (long long)batch * ((n_q + 1) / 2) * Hkv;
+    if (use_tokens_group(tiles, pairs)) {
+      if (launch_decode_attn_tokens_group(P, tokens_group_warps(tiles, pairs), grid_ctas(), static_cast<cudaStream_t>(stream),
+                                          device_info().smem_tokens_group) != cudaSuccess)
+        return PUZZLE_ERR_CUDA;
+      count_launch();
+      return PUZZLE_OK;
+    }
+  }
   if (launch_decode_attn_tokens(P, desc->kv_dtype, grid_ctas(), static_cast<cudaStream_t>(stream),
                                 device_info().smem_tokens) != cudaSuccess)
     return PUZZLE_ERR_CUDA;

@@ -87,6 +87,8 @@ int decode_attn_small_max_pairs(int ctas);
 // The group kernel of the 4-bit cache: workers of 1, 2, 4, 8 or 16 warps take whole pairs; no workspace use.
 // smem_limit[5] as above.
 cudaError_t launch_decode_attn_group(const DecodeParams& P, int warps, int ctas, cudaStream_t s, int* smem_limit);
+// The same for rows of two query tokens (P.n_q, P.q_lens set): 1, 2, 4, 6 or 12 warps.
+cudaError_t launch_decode_attn_tokens_group(const DecodeParams& P, int warps, int ctas, cudaStream_t s, int* smem_limit);
 
 // The multi-token kernel (FP8 or 4-bit cache, balanced schedule): P.n_q, P.q_lens set; P.counters has one word per
 // (sequence, token pair, KV head); partial rows: decode_attn_tokens_partial_rows(...); smem_limit[2] as above.

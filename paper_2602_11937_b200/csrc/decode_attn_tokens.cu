@@ -28,42 +28,13 @@
 #include "decode_attn.cuh"
 #include "decode_tile.cuh"
 #include "decode_tile_fp4.cuh"
+#include "decode_tokens.cuh"
 
 namespace puzzle {
 namespace {
 
-constexpr int kTokStages = 2, kTokTile = 64;
+constexpr int kTokStages = 2;
 constexpr int kPairRows = 2 * kGroup;  // partial rows per (worker, row, KV head): 8 heads of each of the two tokens
-
-// One row of the schedule: query tokens t0 and t1 (= t0 + 1, or t0 again for an odd last token) of sequence b.
-struct RowInfo {
-  int b, t0, t1;
-  int L, LA;     // keys [lo, L) are visible to t1, [loA, LA) to t0 (LA = L - (t1 - t0))
-  int lo, loA;
-  int tlo, ntile;  // tiles that cover [loA, L)
-  bool present, too_long;
-};
-__device__ __forceinline__ RowInfo row_info(const DecodeParams& P, int r) {
-  RowInfo i;
-  const int npairs = (P.n_q + 1) >> 1;
-  i.b = r / npairs;
-  const int j = r - i.b * npairs;
-  const int qlen = P.q_lens ? max(0, min(P.q_lens[i.b], P.n_q)) : P.n_q;
-  i.t0 = 2 * j;
-  i.present = i.t0 < qlen;
-  i.t1 = min(i.t0 + 1, qlen - 1);
-  const int max_tokens = P.max_blocks_per_seq * kBlock;
-  const int len = P.seq_lens[i.b];
-  i.too_long = len > max_tokens;
-  const int Lb = len < 0 ? 0 : min(len, max_tokens);
-  i.L = i.present ? max(0, Lb - qlen + i.t1 + 1) : 0;
-  i.LA = max(0, i.L - (i.t1 - i.t0));
-  i.lo = (P.window > 0 && i.L > P.window) ? i.L - P.window : 0;
-  i.loA = (P.window > 0 && i.LA > P.window) ? i.LA - P.window : 0;
-  i.tlo = i.loA / kTokTile;
-  i.ntile = i.L > 0 ? (i.L + kTokTile - 1) / kTokTile - i.tlo : 0;
-  return i;
-}
 
 struct TokSegment {
   int r, kvh;
@@ -259,7 +230,8 @@ struct TileState2 {
   }
 };
 
-// The two cache types as the kernel sees them: copies, state of a pair, one tile, and a token's state as it is stored.
+// The E4M3 cache as the kernel sees it: copies, state of a pair, one tile, and a token's state as it is stored.  The 4-bit
+// cache: Fp4Pair (decode_tokens.cuh).
 struct Fp8Pair {
   static constexpr int kWarps = kTokWarpsFp8;
   using Tile = SwizzledTile<true>;
@@ -280,76 +252,6 @@ struct Fp8Pair {
     m = st.m_ref[tok];
 #pragma unroll
     for (int nd = 0; nd < 8; ++nd) { o[nd][0] = st.O[nd][2 * tok]; o[nd][1] = st.O[nd][2 * tok + 1]; }
-  }
-};
-
-struct Fp4Pair {
-  static constexpr int kWarps = kTokWarpsFp4;
-  using Tile = Fp4Tile;
-  struct State {
-    Fp4State t[2];
-    __device__ __forceinline__ void reset() { t[0].reset(); t[1].reset(); }
-  };
-  static __device__ __forceinline__ void load_query(State& st, int tok, const __nv_bfloat16* qrow, float ks, float sm,
-                                                    int lane) {
-    st.t[tok].load_query(qrow, ks, sm, lane);
-  }
-  // EDGE as in TileState2::tile; V scales outside [loA, L) are cleared (the keys in [LA, L) are real tokens, and so are
-  // those in [loA, lo): the other token's weights for them are zero).
-  template <bool EDGE>
-  static __device__ __forceinline__ void tile(State& st, const Tile::Lanes& at, uint32_t kbase, uint32_t vbase, int tok0,
-                                              int loA, int LA, int lo, int L, int lane) {
-    constexpr int NB = kTokTile / kBlock;
-    const int g = lane >> 2, c = lane & 3;
-    float s[2][NB][4];
-#pragma unroll
-    for (int blk = 0; blk < NB; ++blk) {
-      uint32_t a[4][4];
-      fp4_k_fragments(kbase + blk * kFp4BlockBytes, at, a);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) mma_f16_z(s[t][blk], a[0][0], a[0][1], a[0][2], a[0][3], st.t[t].q[0][0], st.t[t].q[0][1]);
-#pragma unroll
-      for (int k = 1; k < 4; ++k)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-          mma_f16(s[t][blk], a[k][0], a[k][1], a[k][2], a[k][3], st.t[t].q[k][0], st.t[t].q[k][1]);
-    }
-    if constexpr (EDGE) {
-#pragma unroll
-      for (int blk = 0; blk < NB; ++blk)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int tk = tok0 + kBlock * blk + g + 8 * e;
-          if (tk < loA || tk >= LA) s[0][blk][2 * e] = s[0][blk][2 * e + 1] = -INFINITY;
-          if (tk < lo || tk >= L) s[1][blk][2 * e] = s[1][blk][2 * e + 1] = -INFINITY;
-        }
-    }
-    float2 neg[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-      for (int blk = 0; blk < NB; ++blk) {
-        mx[0] = max3(mx[0], s[t][blk][0], s[t][blk][2]);
-        mx[1] = max3(mx[1], s[t][blk][1], s[t][blk][3]);
-      }
-      st.t[t].raise(mx);
-      neg[t] = st.t[t].negated();
-    }
-#pragma unroll
-    for (int blk = 0; blk < NB; ++blk) {
-      uint32_t b[2][2], a[4][4];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) st.t[t].weights(s[t][blk], neg[t], b[t][0], b[t][1]);
-      fp4_v_fragments<EDGE>(vbase + blk * kFp4BlockBytes, at, tok0 + kBlock * blk + 2 * c, loA, L, a);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) mma_f16(st.t[t].O[i], a[i][0], a[i][1], a[i][2], a[i][3], b[t][0], b[t][1]);
-    }
-  }
-  static __device__ __forceinline__ void finish(const State& st, int tok, float& m, float& l, float (&o)[8][2], int lane) {
-    Fp4Tile::finish(st.t[tok], m, l, o, lane);
   }
 };
 
@@ -375,18 +277,29 @@ __device__ __noinline__ void merge_tok_rows(const DecodeParams& P, const RowInfo
     for (int i = 0; i < 16; ++i) acc[i] = 0.f;
     float Z = 0.f;
     if (M != -INFINITY) {
-      for (int k = 0; k < count; ++k) {
-        const long long idx = base + (long long)k * kPairRows;
-        const float l = __ldcg(P.part_lse + idx);
-        if (l == -INFINITY) continue;  // an empty part: its payload is undefined
-        const float4* o = reinterpret_cast<const float4*>(P.part_o + idx * kHeadDim + 16 * c);
-        const float wgt = __expf(l - M);
-        Z += wgt;
+      // four parts per round, all loads before the first use, as in merge_rows: the merge is a chain of L2 round trips
+      for (int k0 = 0; k0 < count; k0 += 4) {
+        float l[4];
+        float4 v[4][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 v = __ldcg(o + i);
-          acc[4 * i + 0] += wgt * v.x; acc[4 * i + 1] += wgt * v.y;
-          acc[4 * i + 2] += wgt * v.z; acc[4 * i + 3] += wgt * v.w;
+        for (int j = 0; j < 4; ++j) {
+          const bool on = k0 + j < count;
+          const long long idx = base + (long long)(on ? k0 + j : k0) * kPairRows;
+          l[j] = on ? __ldcg(P.part_lse + idx) : -INFINITY;
+          const float4* o = reinterpret_cast<const float4*>(P.part_o + idx * kHeadDim + 16 * c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[j][i] = __ldcg(o + i);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (l[j] == -INFINITY) continue;  // an empty part: its payload is undefined
+          const float wgt = __expf(l[j] - M);
+          Z += wgt;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            acc[4 * i + 0] += wgt * v[j][i].x; acc[4 * i + 1] += wgt * v[j][i].y;
+            acc[4 * i + 2] += wgt * v[j][i].z; acc[4 * i + 3] += wgt * v[j][i].w;
+          }
         }
       }
       if (sink != -INFINITY) Z += __expf(sink - M);  // the sink is one more softmax column, counted once

@@ -340,6 +340,17 @@ def test_several_tokens(n_q, window):
                            q_lens=q_lens).upload())
 
 
+@pytest.mark.parametrize("batch, hkv, longest, n_q", [(3, 2, 900, 2), (18, 8, 300, 2), (16, 8, 400, 3), (16, 8, 300, 5),
+                                                      (40, 8, 300, 3), (64, 8, 300, 4), (40, 8, 1100, 6), (2, 2, 9000, 3)])
+def test_several_tokens_by_groups_of_every_size(batch, hkv, longest, n_q):
+    """One row of two tokens to an SM and up to seven (groups of 12, 6, 4, 2, 1 warps), and the evenly cut kernel."""
+    r = np.random.default_rng(batch)
+    lens = r.integers(0, longest + 1, size=batch)
+    lens[:4] = [longest, 1, 0, 65][:len(lens[:4])]
+    _check_tokens(Case(list(lens), hkv=hkv, seed=batch, max_blocks=-(-longest // 16), n_q=n_q, poison=False,
+                       q_lens=list(r.integers(0, n_q + 2, size=batch))).upload())
+
+
 @pytest.mark.parametrize("hkv", [1, 3, 8])
 def test_several_tokens_head_counts_without_sinks(hkv):
     _check_tokens(Case([130, 0, 257, 48], hkv=hkv, paged=hkv != 3, sinks=False, seed=hkv, n_q=3).upload())
