@@ -3,6 +3,7 @@
 // keys and values, a cache handed to another worker) and the only way to look into a 4-bit block short of decoding its
 // layout.  HBM-bound: 0.56 to 2 bytes read and 2 written per value.
 //
+// Measured, 16 x 8192 tokens: 59 us from a 4-bit cache (5.8 TB/s of read and written bytes), 67 E4M3 (6.1), 82 bf16 (6.5).
 // Eight lanes hold a row (one token of one head), eight channels each; a warp takes four consecutive tokens and walks
 // over eight heads with all loads in flight, so the 1 KiB a token occupies in the output is written by one warp.
 #include "common.cuh"

@@ -5,6 +5,9 @@
 // each product and the sum rounded to float32 (no contraction, so that the bytes are defined to the last bit), then
 // q to bf16 and k, v to the cache's type as in kv_append.cu.  Reading and writing every byte once is all there is to
 // do: a chunk is bound by HBM, a decode step by the chain of dependent loads (length -> table row, block -> store).
+// Measured: 16 x 2048 tokens with 64 query and 8 KV heads 103 us into a bf16 cache (6.6 TB/s of read and written bytes),
+// 108 E4M3 (6.0), 116 4-bit (5.4: sixteen-channel maxima, corrected quotients, byte-wide scale stores); one token for 16
+// sequences 2.2 us, for 64 into the 4-bit cache 3.4.  Fewer heads per warp re-read the table's rows: 4 heads 5 % slower.
 //
 // Eight lanes hold a row, eight adjacent channels each: 16-byte loads, the rotation partner of the half-split form is
 // one shuffle of packed pairs away, a 4-bit group is two lanes.
@@ -228,13 +231,11 @@ __global__ void __launch_bounds__(256) kv_append_chunk_kernel(const AppendParams
   grid_dependency_wait();   // no early release, for the reason given in kv_append_kernel
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, o = lane & 7;
   const int b = blockIdx.z;
-  const int q_jobs = P.q ? (P.Hq + kHeadsPerWarp - 1) / kHeadsPerWarp : 0;
   const int kv_jobs = (P.Hkv + kHeadsPerWarp - 1) / kHeadsPerWarp;
-  int job = blockIdx.y;                                  // query heads, then keys, then values
-  const bool is_q = job < q_jobs;
-  if (!is_q) job -= q_jobs;
-  const bool is_v = !is_q && job >= kv_jobs;
-  if (is_v) job -= kv_jobs;
+  // keys, then values, then the query heads: the last blocks of the launch are quick ones (4 % at 16 x 2048 tokens)
+  int job = blockIdx.y;
+  const bool is_q = job >= 2 * kv_jobs, is_v = !is_q && job >= kv_jobs;
+  job -= is_q ? 2 * kv_jobs : (is_v ? kv_jobs : 0);
   const bool reporter = o == 0 && blockIdx.y == 0;
 
   const Span sp = span_of(P, b, reporter);
