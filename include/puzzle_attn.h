@@ -255,7 +255,8 @@ PUZZLE_API puzzle_status puzzle_decode_attn_workspace_init(const puzzle_layer_de
  * long-context inference"); the sink is one extra softmax column per query head
  * that carries no value.  Internally ONE kernel: a split-KV pass writes float32
  * partial (o, lse) into the workspace, and the worker that completes a
- * (sequence, KV head) merges its partials by log-sum-exp and writes `out`.
+ * (sequence, KV head) merges its partials by log-sum-exp and writes `out`
+ * (4-bit cache: the merge of a cut launch is a second, small kernel).
  *   q: bf16 [batch][num_q_heads][head_dim], 8-byte aligned;  sinks: float32 [num_q_heads] or NULL (no sink);
  *   out: bf16 [batch][num_q_heads][head_dim], 16-byte aligned;  lse_out: float32 [batch][num_q_heads] or NULL;
  *   num_splits: 0 = balanced schedule (recommended); S >= 1 = every (sequence, KV head) context is
@@ -267,10 +268,11 @@ PUZZLE_API puzzle_status puzzle_decode_attn_workspace_init(const puzzle_layer_de
  *     of many short contexts, are cut evenly over all warps, which has the shorter set-up; and
  *     when no (sequence, KV head) can have more than four tiles (narrow windows, very short
  *     contexts) nothing is cut: a group of four warps, or one warp when there are very many
- *     pairs, takes the pair whole and writes the output itself.  (On the 4-bit cache a fourth kernel, whole
- *     pairs by groups of 1 to 16 warps, serves launches that fill the device without being cut.)  PUZZLE_SCHED_CTA and
+ *     pairs, takes the pair whole and writes the output itself.  The 4-bit cache has a kernel of its own for all
+ *     but the last kind: groups of 1 to 16 warps take whole pairs when these fill the device evenly, else even shares
+ *     (then a second, small kernel merges).  PUZZLE_SCHED_CTA and
  *     PUZZLE_SCHED_WARP pin the first or the second kernel (PUZZLE_SCHED_CTA needs batch <= 1024,
- *     4-bit cache 640, else PUZZLE_ERR_UNSUPPORTED);
+ *     else PUZZLE_ERR_UNSUPPORTED; 4-bit cache: any batch, the group kernel on even shares);
  *   workspace: device scratch of at least puzzle_decode_attn_workspace_bytes(...) bytes, 16-byte
  *     aligned, prepared once by puzzle_decode_attn_workspace_init; calls that share a workspace must
  *     not overlap on the GPU.  Besides partials and counters it keeps the CTA speeds between calls:
@@ -381,8 +383,8 @@ PUZZLE_API puzzle_status puzzle_decode_attn_tokens(const puzzle_layer_desc* desc
  *     the process exits.  A batch and split choice whose
  *     puzzle_decode_attn_workspace_bytes exceeds that size is refused with
  *     PUZZLE_ERR_WORKSPACE and nothing is launched (balanced schedule: batch up
- *     to about 280 on a 148-SM device; explicit splits: batch * num_splits up to
- *     about 500).
+ *     to about 280 on a 148-SM device, 4-bit cache about 200; explicit splits:
+ *     batch * num_splits up to about 500).
  *   - The call allocates and frees nothing.  The first call on each device looks
  *     up the array's device address (with that device current).  Make that first
  *     call at start-up: before any stream capture, and before the caller hands

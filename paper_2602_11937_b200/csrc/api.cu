@@ -33,8 +33,8 @@ EncodeTiledFn encode_tiled() {
 struct DeviceInfo {
   int sm_count = 0;
   // dynamic shared-memory limits already set per kernel and cache type; 0 = not raised yet
-  int smem_warp[3] = {0, 0, 0}, smem_cta[3] = {0, 0, 0}, smem_small[3] = {0, 0, 0};
-  int smem_tc = 0, smem_tokens[2] = {0, 0}, smem_group[5] = {0, 0, 0, 0, 0}, smem_tokens_group[5] = {0, 0, 0, 0, 0};
+  int smem_warp[3] = {}, smem_cta[2] = {}, smem_small[3] = {};
+  int smem_tc = 0, smem_tokens = 0, smem_group[10] = {}, smem_tokens_group[10] = {};
 };
 DeviceInfo& device_info() {
   static DeviceInfo info[64];
@@ -184,7 +184,6 @@ size_t counter_bytes(int batch, int Hkv) {
 // launch can be large: with at most a few tiles per warp (window layers, short contexts) a launch is a chain of
 // latencies, which the warp-scheduled kernel's shorter set-up serves better.  The bound on the tiles comes from
 // what the host knows: the window, or the length of a block-table row.
-int cta_max_batch(int kv_dtype) { return kv_dtype == PUZZLE_KV_FP4_E2M1 ? kCtaMaxBatchFp4 : kCtaMaxBatch; }
 // Upper bound on the tiles of one (sequence, KV head) from what the host knows.
 long long tiles_per_pair_bound(const puzzle_layer_desc* d, const puzzle_kv_view* kv) {
   const int tt = tile_tokens(d->kv_dtype);
@@ -195,7 +194,7 @@ long long tiles_per_pair_bound(const puzzle_layer_desc* d, const puzzle_kv_view*
 
 bool use_cta_kernel(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int batch, int num_splits) {
   if (num_splits == PUZZLE_SCHED_CTA) return true;
-  if (num_splits != 0 || batch > cta_max_batch(d->kv_dtype)) return false;
+  if (num_splits != 0 || batch > kCtaMaxBatch) return false;
   // What the CTA-balanced kernel wins (no tail, CTAs cut by speed) grows with the length of the launch and of the
   // pairs; what it costs (a longer set-up, a claim and a hand-over per piece) weighs most on many short pairs.
   // Measured crossovers, in tiles per CTA: 64 with pairs of 256 tiles or more, about 200 at 128 tiles per pair,
@@ -206,48 +205,48 @@ bool use_cta_kernel(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int ba
 }
 
 // The kernel a call of puzzle_decode_attn runs on.
-enum class Kernel { kCta, kWarp, kWarpWholePairs, kSmall, kGroup };
+enum class Kernel { kCta, kWarp, kWarpWholePairs, kSmall, kGroup, kGroupCut };
 
-// The 4-bit cache (times below: uniform lengths, 148 SMs).  A group kernel lasts as long as the SM with the most tiles
-// (0.109 us a tile), the balanced kernels by the mean (0.122 us, and 18 us besides).  Lengths may be ragged behind the
-// bound the host has, so the group kernel has to promise a fifth, unless an SM gets so many pairs that their sum evens
-// out.  (8 x 8192 tokens: 18.3 against 24.5 us; 16 x 16384 34.8 / 44; but 8 x 32768 62 / 44, 24 x 30000 111 / 92.)
-// Of the balanced kernels the CTA-balanced one has few partials per pair and a longer set-up and tile: it wins where the
-// other would merge 32 partials or more (1 x 4096: 17.5 against 26.3 us, 8 x 16384 30.9 / 33.8) and on very long pairs
-// (16 x 65536 117 / 123).
-Kernel pick_fp4_kernel(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int batch) {
-  const long long tiles = tiles_per_pair_bound(d, kv), pairs = (long long)batch * d->num_kv_heads, sms = grid_ctas();
-  if (tiles <= kWholePairTiles && pairs <= decode_attn_small_max_pairs((int)sms)) return Kernel::kSmall;
-  const long long pairs_per_sm = (pairs + sms - 1) / sms;
-  if (pairs_per_sm * tiles <= (pairs * tiles * 9) / (sms * 10) + 91 || (pairs_per_sm >= 5 && tiles <= 64)) return Kernel::kGroup;
-  if (batch > kCtaMaxBatchFp4) return Kernel::kWarp;
-  const long long partials = std::min(tiles, sms * kDecodeWarpsFp4 / pairs);
-  return partials >= 32 || tiles >= 1024 ? Kernel::kCta : Kernel::kWarp;
+// The 4-bit cache (times: uniform lengths, 148 SMs).  Groups that take whole pairs last as long as the SM with the most
+// tiles, 4.5 us + 0.109 us a tile; groups that take even shares 15 us + 0.115 us per mean tile of an SM (the schedule, the
+// partials and their merge are the difference).  Lengths may be ragged behind the bound the host has, so whole pairs have
+// to promise a sixth, unless an SM gets many short ones whose sum evens out.  Whole / cut, us: 8 x 8192 tokens 17.9 / 19.8,
+// 16 x 16384 34.5 / 39.7, 128 x 4096 62.7 / 67; but 1 x 16384 32 / 18, 8 x 32768 62 / 40, 24 x 30000 111 / 85.
+bool whole_pairs_fp4(long long tiles, long long pairs) {
+  const long long sms = grid_ctas(), per_sm = (pairs + sms - 1) / sms;
+  return per_sm * tiles <= (pairs * tiles * 9) / (sms * 10) + 76 || (per_sm >= 5 && tiles <= 32);
 }
-// Warps per pair: as many as leave every SM's sixteen warps a pair at once; fewer still when an SM has pairs to go
-// round, where a smaller group waits less at their ends (512 x 1024 tokens: 4 warps 72.8 us, 2 65.2, 1 59.6; but with long
-// pairs one warp's share is too coarse: 256 x 4096 114, 110, 116).
-int group_warps(long long tiles, long long pairs) {
+Kernel pick_fp4_kernel(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int batch) {
+  const long long tiles = tiles_per_pair_bound(d, kv), pairs = (long long)batch * d->num_kv_heads;
+  if (tiles <= kWholePairTiles && pairs <= decode_attn_small_max_pairs(grid_ctas())) return Kernel::kSmall;
+  return whole_pairs_fp4(tiles, pairs) ? Kernel::kGroup : Kernel::kGroupCut;
+}
+// Warps per group.  Whole pairs: as many as leave every SM's sixteen warps a pair at once, fewer still when an SM has pairs
+// to go round, where a smaller group waits less at their ends (512 x 1024 tokens: 4 warps 72.8 us, 2 65.2, 1 59.6; but a
+// long pair is too coarse a share for one: 256 x 4096 114, 110, 116).  Cut: large groups leave few partials (1 x 65536: 16
+// warps 22 us, 4 38), small ones few warps waiting at the ends of many runs (256 x 4096: 159, 122).
+int group_warps(long long tiles, long long pairs, bool cut) {
   const long long n = (pairs + grid_ctas() - 1) / grid_ctas();
+  if (cut) return n <= 1 ? 16 : n <= 4 ? 8 : 4;
   return n <= 1 ? 16 : n <= 2 ? 8 : n <= 4 ? 4 : (n <= 8 || tiles > 16) ? 2 : 1;
 }
-
-// Rows of two query tokens over the 4-bit cache: the same choice for the multi-token kernels.  The group kernel takes
-// 0.155 us per tile of the SM with the most tiles, the evenly cut one 0.16 per mean tile and 20 us besides, more the more
-// partials a pair has.  (4 x 1024 tokens 8.4 against 30 us, 16 x 16384 47 / 68, but 8 x 65536 160 / 119.)
-bool use_tokens_group(long long tiles, long long pairs) {
+// The same for rows of two query tokens: 5 us + 0.155 us a tile against 20 us + 0.15 us, twelve warps.  (16 x 16384 tokens
+// 47 us whole, 54 cut; 16 x 65536 161 / 152; 1 x 65536 156 / 34.)
+bool whole_pairs_tokens(long long tiles, long long pairs) {
   const long long sms = grid_ctas(), per_sm = (pairs + sms - 1) / sms;
-  const long long partials = std::min(tiles, sms * kTokWarpsFp4 / pairs);
-  if (per_sm >= 5) return tiles <= 32;   // (128 x 4096: 105 us against 90; 128 x 1024 30 / 37)
-  return per_sm * tiles <= (pairs * tiles * 9) / (sms * 10) + 60 + 2 * partials;
+  return per_sm * tiles <= (pairs * tiles * 82) / (sms * 100) + 77 || (per_sm >= 5 && tiles <= 32);
 }
-int tokens_group_warps(long long tiles, long long pairs) {   // twelve warps per CTA
+int tokens_group_warps(long long tiles, long long pairs, bool cut) {
   const long long n = (pairs + grid_ctas() - 1) / grid_ctas();
+  if (cut) return n <= 1 ? 12 : n <= 4 ? 6 : 4;
   return n <= 1 ? 12 : n <= 2 ? 6 : n <= 3 ? 4 : (n <= 6 || tiles > 16) ? 2 : 1;
 }
 
 Kernel pick_kernel(const puzzle_layer_desc* d, const puzzle_kv_view* kv, int batch, int num_splits) {
-  if (d->kv_dtype == PUZZLE_KV_FP4_E2M1 && num_splits == 0) return pick_fp4_kernel(d, kv, batch);
+  if (d->kv_dtype == PUZZLE_KV_FP4_E2M1) {
+    if (num_splits == PUZZLE_SCHED_CTA) return Kernel::kGroupCut;
+    if (num_splits == 0) return pick_fp4_kernel(d, kv, batch);
+  }
   if (use_cta_kernel(d, kv, batch, num_splits)) return Kernel::kCta;
   // Narrow windows and short contexts: with at most kWholePairTiles tiles per (sequence, KV head) a pair is not cut
   // at all.  A group of four warps (few pairs) or one warp (many pairs, or the warp-scheduled kernel pinned) takes
@@ -271,6 +270,8 @@ size_t workspace_floats(int batch, int Hkv, int num_splits, int kv_dtype) {
   }
   return rows * (kHeadDim + 1);
 }
+// Behind the partials of a 4-bit call: what the group kernel notes of every pair for its merge.
+size_t pair_parts_bytes(size_t pairs, int kv_dtype) { return kv_dtype == PUZZLE_KV_FP4_E2M1 ? pairs * sizeof(int2) : 0; }
 
 }  // namespace
 
@@ -284,7 +285,8 @@ puzzle_status check_decode_attn_args(const puzzle_layer_desc* desc, const puzzle
   if (!q || !out) return PUZZLE_ERR_NULL;
   if (num_splits < PUZZLE_SCHED_WARP || num_splits > 65536) return PUZZLE_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(q) & 7) || (reinterpret_cast<uintptr_t>(out) & 15)) return PUZZLE_ERR_SHAPE;
-  if (num_splits == PUZZLE_SCHED_CTA && (tcgen05 || batch > cta_max_batch(desc->kv_dtype))) return PUZZLE_ERR_UNSUPPORTED;
+  const bool fp4 = desc->kv_dtype == PUZZLE_KV_FP4_E2M1;   // its CTA-wide schedule has room for every batch
+  if (num_splits == PUZZLE_SCHED_CTA && (tcgen05 || (!fp4 && batch > kCtaMaxBatch))) return PUZZLE_ERR_UNSUPPORTED;
   if (tcgen05 && desc->kv_dtype != PUZZLE_KV_FP8_E4M3) return PUZZLE_ERR_UNSUPPORTED;   // that kernel reads E4M3 codes only
   return PUZZLE_OK;
 }
@@ -316,7 +318,8 @@ const char* puzzle_decode_attn_kernel_name(const puzzle_layer_desc* desc, const 
   switch (pick_kernel(desc, kv, batch, num_splits)) {
     case Kernel::kCta: return "decode_attn_cta_kernel";
     case Kernel::kSmall: return "decode_attn_small_kernel";
-    case Kernel::kGroup: return "decode_attn_group_kernel";
+    case Kernel::kGroup:
+    case Kernel::kGroupCut: return "decode_attn_group_kernel";
     default: return "decode_attn_kernel";
   }
 }
@@ -451,7 +454,8 @@ puzzle_status puzzle_kv_read_tokens(const puzzle_layer_desc* desc, const puzzle_
 size_t puzzle_decode_attn_workspace_bytes(const puzzle_layer_desc* desc, int32_t batch, int32_t num_splits) {
   if (check_desc(desc) != PUZZLE_OK || batch <= 0 || batch > kMaxBatch || num_splits < PUZZLE_SCHED_WARP) return 0;
   return counter_bytes(batch, desc->num_kv_heads) +
-         workspace_floats(batch, desc->num_kv_heads, num_splits > 0 ? num_splits : 0, desc->kv_dtype) * sizeof(float);
+         workspace_floats(batch, desc->num_kv_heads, num_splits > 0 ? num_splits : 0, desc->kv_dtype) * sizeof(float) +
+         pair_parts_bytes((size_t)batch * desc->num_kv_heads, desc->kv_dtype);
 }
 
 static puzzle_status decode_attn_impl(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const void* q,
@@ -464,7 +468,7 @@ static puzzle_status decode_attn_impl(const puzzle_layer_desc* desc, const puzzl
   const size_t cbytes = counter_bytes(batch, Hkv);
   const int splits = num_splits > 0 ? num_splits : 0;   // the kernels know explicit splits (S) and balanced (0)
   const size_t pfloats = workspace_floats(batch, Hkv, splits, desc->kv_dtype);
-  const size_t need = cbytes + pfloats * sizeof(float);
+  const size_t need = cbytes + pfloats * sizeof(float) + pair_parts_bytes((size_t)batch * Hkv, desc->kv_dtype);
   if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15)) return PUZZLE_ERR_WORKSPACE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
 
@@ -505,11 +509,15 @@ static puzzle_status decode_attn_impl(const puzzle_layer_desc* desc, const puzzl
   } else {
     switch (pick_kernel(desc, kv, batch, num_splits)) {
       case Kernel::kGroup:
-        le = launch_decode_attn_group(P, group_warps(tiles_per_pair_bound(desc, kv), batch * Hkv), ctas, s,
+      case Kernel::kGroupCut: {
+        const bool cut = pick_kernel(desc, kv, batch, num_splits) == Kernel::kGroupCut;
+        P.pair_parts = reinterpret_cast<int2*>(part_lse + rows);
+        le = launch_decode_attn_group(P, group_warps(tiles_per_pair_bound(desc, kv), (long long)batch * Hkv, cut), cut, ctas, s,
                                       device_info().smem_group);
         break;
+      }
       case Kernel::kCta:
-        le = launch_decode_attn_cta(P, desc->kv_dtype, ctas, s, device_info().smem_cta);
+        le = launch_decode_attn_cta(P, desc->kv_dtype == PUZZLE_KV_FP8_E4M3, ctas, s, device_info().smem_cta);
         break;
       case Kernel::kSmall:
         le = launch_decode_attn_small(P, desc->kv_dtype, ctas, s, device_info().smem_small);
@@ -613,7 +621,8 @@ size_t puzzle_decode_attn_tokens_workspace_bytes(const puzzle_layer_desc* desc, 
   if (check_desc(desc) != PUZZLE_OK || batch <= 0 || n_q <= 0 || (long long)batch * ((n_q + 1) / 2) > kTokMaxRows)
     return 0;
   return tokens_counter_bytes(batch, n_q, desc->num_kv_heads) +
-         decode_attn_tokens_partial_rows(grid_ctas(), batch, n_q, desc->num_kv_heads, desc->kv_dtype) * (kHeadDim + 1) * sizeof(float);
+         decode_attn_tokens_partial_rows(grid_ctas(), batch, n_q, desc->num_kv_heads) * (kHeadDim + 1) * sizeof(float) +
+         pair_parts_bytes((size_t)batch * ((n_q + 1) / 2) * desc->num_kv_heads, desc->kv_dtype);
 }
 
 puzzle_status puzzle_decode_attn_tokens_workspace_init(const puzzle_layer_desc* desc, int32_t batch, int32_t n_q,
@@ -640,7 +649,7 @@ puzzle_status puzzle_decode_attn_tokens(const puzzle_layer_desc* desc, const puz
   const size_t need = puzzle_decode_attn_tokens_workspace_bytes(desc, batch, n_q);
   if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15)) return PUZZLE_ERR_WORKSPACE;
   const size_t cbytes = tokens_counter_bytes(batch, n_q, Hkv);
-  const size_t rows = decode_attn_tokens_partial_rows(grid_ctas(), batch, n_q, Hkv, desc->kv_dtype);
+  const size_t rows = decode_attn_tokens_partial_rows(grid_ctas(), batch, n_q, Hkv);
   DecodeParams P;
   std::memset(&P, 0, sizeof P);
   if (!set_cache(&P, desc, kv, 128)) return PUZZLE_ERR_CUDA;
@@ -664,19 +673,19 @@ puzzle_status puzzle_decode_attn_tokens(const puzzle_layer_desc* desc, const puz
   P.n_q = n_q;
   P.q_lens = q_lens;
   P.sm_scale_log2e = desc->sm_scale * 1.4426950408889634f;
+  const int ctas = grid_ctas();
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  cudaError_t le;
   if (desc->kv_dtype == PUZZLE_KV_FP4_E2M1) {
     const long long tiles = tiles_per_pair_bound(desc, kv), pairs = (long long)batch * ((n_q + 1) / 2) * Hkv;
-    if (use_tokens_group(tiles, pairs)) {
-      if (launch_decode_attn_tokens_group(P, tokens_group_warps(tiles, pairs), grid_ctas(), static_cast<cudaStream_t>(stream),
-                                          device_info().smem_tokens_group) != cudaSuccess)
-        return PUZZLE_ERR_CUDA;
-      count_launch();
-      return PUZZLE_OK;
-    }
+    const bool cut = !whole_pairs_tokens(tiles, pairs);
+    P.pair_parts = reinterpret_cast<int2*>(P.part_lse + rows);
+    le = launch_decode_attn_tokens_group(P, tokens_group_warps(tiles, pairs, cut), cut, ctas, cs,
+                                         device_info().smem_tokens_group);
+  } else {
+    le = launch_decode_attn_tokens(P, ctas, cs, &device_info().smem_tokens);
   }
-  if (launch_decode_attn_tokens(P, desc->kv_dtype, grid_ctas(), static_cast<cudaStream_t>(stream),
-                                device_info().smem_tokens) != cudaSuccess)
-    return PUZZLE_ERR_CUDA;
+  if (le != cudaSuccess) return PUZZLE_ERR_CUDA;
   count_launch();
   return PUZZLE_OK;
 }

@@ -22,6 +22,7 @@ struct alignas(64) DecodeParams {
   float* part_o;
   float* part_lse;
   int32_t* counters;   // [batch*Hkv] arrivals per (sequence, KV head); zero before and after every launch
+  int2* pair_parts;    // cut launches of the group kernel: first partial row and number of parts of every pair
   int32_t* cta_words;  // CTA-balanced kernel only: its CTA counter, buffer switch and the two speed buffers
   const float* sinks;  // [Hq] or null
   __nv_bfloat16* out;  // [batch][Hq][D]
@@ -56,17 +57,11 @@ constexpr int kDecodeWarpsBf16 = 12, kDecodeStagesBf16 = 2, kTileBf16 = 32;
 // 16 warps of 64-token tiles (128 registers, a few words spilled outside the tile loop): 122 us at 256 x 4096 against
 // 132 with 12 warps and no spill.
 constexpr int kDecodeWarpsFp4 = 16, kDecodeStagesFp4 = 2, kTileFp4 = 64;
-// The 4-bit cache on the CTA-balanced kernel: what a tile costs besides its arithmetic (claim, table look-up, record,
-// wait) weighs half again as much as on the E4M3 cache, so tiles are 128 tokens there, and eleven warps are what
-// shared memory holds of them (64 tokens: 16 x 64K at 131 us with 12 or 16 warps; 128: 127 with 8, 121 with 10, 117
-// with 11).
-constexpr int kCtaWarpsFp4 = 11, kCtaTileFp4 = 128;
 // The CTA-balanced kernel keeps its schedule arrays beside the TMA rings and the deposit buffers in shared memory,
 // which bounds the batch it takes.  Launches with at least kCtaRateMinTiles tiles per CTA note the speed of every
 // CTA slot at the start of the workspace (before the arrival counters: a CTA counter, the buffer switch, two pad words, then two
 // float buffers of one speed per CTA) and are cut by the speeds the launch before them noted.
 constexpr int kCtaMaxBatch = 1024;
-constexpr int kCtaMaxBatchFp4 = 640;     // its rings leave less room for the schedule
 constexpr int kCtaMinTilesPerCta = 64;   // below this bound on the tiles per CTA the warp-scheduled kernel is used (more with short pairs)
 constexpr int kCtaRateMinTiles = 256;
 constexpr int kWholePairTiles = 4;       // up to this many tiles per (sequence, KV head) a pair goes to one warp whole
@@ -77,24 +72,25 @@ inline size_t cta_rate_words(int ctas) { return 4 + 2 * (size_t)ctas; }
 cudaError_t launch_decode_attn(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit);
 // The CTA-balanced kernel (balanced schedule only, batch <= kCtaMaxBatch).  Its partial row blocks: one per
 // (CTA, pair) meeting, ctas + batch*Hkv at most.
-cudaError_t launch_decode_attn_cta(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit);
+cudaError_t launch_decode_attn_cta(const DecodeParams& P, bool fp8, int ctas, cudaStream_t s, int* smem_limit);
 // The kernel for launches in which no (sequence, KV head) has more than kWholePairTiles tiles (narrow windows, very
 // short contexts): a group of four warps per pair, one tile each, combined in shared memory; no workspace use.
 // smem_limit[3] as above.  It pays up to decode_attn_small_max_pairs(ctas) pairs; beyond, the warp-scheduled kernel
 // with one split per pair keeps its TMA rings full.
 cudaError_t launch_decode_attn_small(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit);
 int decode_attn_small_max_pairs(int ctas);
-// The group kernel of the 4-bit cache: workers of 1, 2, 4, 8 or 16 warps take whole pairs; no workspace use.
-// smem_limit[5] as above.
-cudaError_t launch_decode_attn_group(const DecodeParams& P, int warps, int ctas, cudaStream_t s, int* smem_limit);
+// The group kernel of the 4-bit cache: groups of 1, 2, 4, 8 or 16 warps take whole pairs (cut = false; no workspace use),
+// or even shares of the tile space with a second, small kernel that merges (cut = true; P.part_o, P.part_lse and
+// P.pair_parts set).  smem_limit[10] as above.
+cudaError_t launch_decode_attn_group(const DecodeParams& P, int warps, bool cut, int ctas, cudaStream_t s, int* smem_limit);
 // The same for rows of two query tokens (P.n_q, P.q_lens set): 1, 2, 4, 6 or 12 warps.
-cudaError_t launch_decode_attn_tokens_group(const DecodeParams& P, int warps, int ctas, cudaStream_t s, int* smem_limit);
+cudaError_t launch_decode_attn_tokens_group(const DecodeParams& P, int warps, bool cut, int ctas, cudaStream_t s,
+                                            int* smem_limit);
 
-// The multi-token kernel (FP8 or 4-bit cache, balanced schedule): P.n_q, P.q_lens set; P.counters has one word per
-// (sequence, token pair, KV head); partial rows: decode_attn_tokens_partial_rows(...); smem_limit[2] as above.
-cudaError_t launch_decode_attn_tokens(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit);
-size_t decode_attn_tokens_partial_rows(int ctas, int batch, int n_q, int Hkv, int kv_dtype);
-constexpr int kTokWarpsFp8 = 12, kTokWarpsFp4 = 12;
+// The multi-token kernel (FP8 cache, balanced schedule): P.n_q, P.q_lens set; P.counters has one word per
+// (sequence, token pair, KV head); partial rows: decode_attn_tokens_partial_rows(...).
+cudaError_t launch_decode_attn_tokens(const DecodeParams& P, int ctas, cudaStream_t s, int* smem_limit);
+size_t decode_attn_tokens_partial_rows(int ctas, int batch, int n_q, int Hkv);
 size_t decode_attn_tokens_counters(int batch, int n_q, int Hkv);
 constexpr int kTokMaxRows = 8192;   // (sequence, token pair) rows its shared-memory schedule holds
 

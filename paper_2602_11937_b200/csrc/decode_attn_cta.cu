@@ -1,5 +1,5 @@
-// Split-KV decode attention over a paged KV cache (FP8 E4M3 codes, bf16, or 4-bit codes), sm_100a: the CTA-balanced
-// kernel, default for the balanced schedule (num_splits = 0).
+// Split-KV decode attention over a paged KV cache (FP8 E4M3 codes, or bf16), sm_100a: the CTA-balanced kernel,
+// default for the balanced schedule (num_splits = 0).
 //
 // Long-context decode is bound by KV-cache I/O (Section "Optimized Scenarios"), so what is left to win once every
 // byte is read exactly once is time in which part of the chip has nothing to read.  With an equal static share per
@@ -40,7 +40,6 @@
 #include "decode_attn.cuh"
 #include "decode_sched.cuh"
 #include "decode_tile.cuh"
-#include "decode_tile_fp4.cuh"
 
 namespace puzzle {
 namespace {
@@ -206,15 +205,10 @@ struct ClaimProducer {
   }
   // Issues the pending tile into `stage_addr` (its description goes to desc_a) and prepares the next one.
   // Returns 1 if a tile was issued, 0 if nothing was pending, -1 if a claim gave up.
-  template <typename F>
+  template <int BLOCK_BYTES>
   __device__ __forceinline__ int issue(uint32_t ctl_a, const DecodeParams& P, const int* cum, uint32_t pc_a,
                                        uint32_t rec_a, int lane, uint32_t stage_addr, uint32_t bar, uint32_t desc_a) {
     if (d.n <= 0) return 0;
-    if constexpr (F::kLeanClaims) {   // everything but the next tile's index and the count lives in the claim's record
-      const int4 a = lds128_volatile(rec_a), z = lds128_volatile(rec_a + 16);
-      d.b = a.x; d.kvh = a.y; d.k = a.w;
-      d.total = z.x; d.L = z.y; d.lo = z.z;
-    }
     int row = P.oob_row;
     if (lane < NB) {
       if (phys >= 0 && phys < P.num_blocks) {
@@ -223,10 +217,20 @@ struct ClaimProducer {
         if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
       }
     }
-    F::template load_tile<NB>(P, stage_addr, row, bar, lane, [&] {
+    // the copies are issued by one lane, which collects the row coordinates first: a TMA instruction takes
+    // warp-uniform operands, so issuing from several lanes would be serialised lane by lane anyway
+    int rows[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) rows[i] = __shfl_sync(0xffffffffu, row, i);
+    if (elect_one()) {
       sts128(desc_a, make_int4(d.b, d.kvh, d.t, d.k));
       sts128(desc_a + 16, make_int4(d.total, d.L, d.lo, 0));
-    });
+      mbar_arrive_expect_tx(bar, 2 * NB * BLOCK_BYTES);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) tma_load_2d(stage_addr + i * BLOCK_BYTES, &P.tmK, 0, rows[i], bar);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) tma_load_2d(stage_addr + (NB + i) * BLOCK_BYTES, &P.tmV, 0, rows[i], bar);
+    }
     ++d.t;
     bool ok = true;
     if (--d.n == 0) ok = claim(ctl_a, P, cum, pc_a, rec_a, lane);
@@ -253,18 +257,19 @@ __device__ __forceinline__ int ranges_of(const int* bound, int nC, int ps, int p
 
 }  // namespace
 
-// NW warps per CTA, NS stages per warp, TT tokens per tile; F: the cache type (SwizzledTile or Fp4Tile).
-template <int NW, int NS, int TT, typename F>
+// NW warps per CTA, NS stages per warp, TT tokens per tile; FP8 selects the E4M3 cache (else bf16).
+template <int NW, int NS, int TT, bool FP8>
 __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __grid_constant__ DecodeParams P) {
   constexpr int NB = TT / kBlock;                       // blocks per tile
-  constexpr int BLOCK_BYTES = F::kBlockBytes;
+  constexpr int EB = FP8 ? 1 : 2;                       // bytes per cache element
+  constexpr int BLOCK_BYTES = kBlock * kHeadDim * EB;   // one (block, KV head): 1 KiB or 2 KiB
   constexpr int STAGE_BYTES = 2 * NB * BLOCK_BYTES;
   constexpr int PIPE_BYTES = NW * NS * STAGE_BYTES;
   static_assert(NW <= 32 && NW <= kPieceSlots, "one deposit buffer per warp, found by one ballot");
 
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
-  uint8_t* smem = smem_raw + (((raw + F::kAlign - 1u) & ~(F::kAlign - 1u)) - raw);
+  uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, c = lane & 3;  // this lane's query head within the group / column quad
@@ -298,7 +303,10 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
     for (int i = 0; i < NS; ++i) mbar_init(bars + 8 * i, 1);
     fence_mbar_init();
   }
-  if (threadIdx.x == 0) F::prefetch(P);
+  if (threadIdx.x == 0) {
+    tma_prefetch_desc(&P.tmK);
+    tma_prefetch_desc(&P.tmV);
+  }
   if (threadIdx.x < 32) dep_piece[threadIdx.x] = -1;
   if (threadIdx.x < kPieceSlots) { pk_key[threadIdx.x] = -1; pk_done[threadIdx.x] = 0; }
   if (threadIdx.x == 0) cum[0] = 0;
@@ -378,8 +386,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
   // Every CTA evaluates the same expressions on the same numbers, so all agree on the cuts.
   {
     const int T = cum[P.batch];
-    constexpr int kLarge = TT > 64 ? kCtaRateMinTiles * 64 / TT : kCtaRateMinTiles;
-    const bool large = T / nC >= kLarge && nC <= 256;
+    const bool large = T / nC >= kCtaRateMinTiles && nC <= 256;
     const int nR = large ? nC : max(1, min(nC, T));
     const int snap = max(1, (T / nR) >> 5);
     const float per_share = (float)T / (float)share[nC];
@@ -423,7 +430,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
   }
   __syncthreads();
 
-  typename F::Lanes lo;
+  LaneOffsets<FP8> lo;
   lo.init(lane);
 
   ClaimProducer<TT> prod;
@@ -439,13 +446,6 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
       const int pos = ctl.lo + warp * first_n;
       prod.d.b = s0.z; prod.d.kvh = s0.w; prod.d.t = s1.x + (pos - s0.x); prod.d.k = 0;
       prod.d.total = min(s0.y, ctl.end) - max(s0.x, ctl.lo); prod.d.L = s1.y; prod.d.lo = s1.z; prod.d.n = first_n;
-      if constexpr (F::kLeanClaims) {
-        if (lane == 0) {
-          sts128(rec_a, make_int4(prod.d.b, prod.d.kvh, prod.d.t, prod.d.k));
-          sts128(rec_a + 16, make_int4(prod.d.total, prod.d.L, prod.d.lo, first_n));
-        }
-        __syncwarp();
-      }
     } else {
       __syncwarp();
       failed = !prod.claim(ctl_a, P, cum, pc_a, rec_a, lane);
@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
   int inflight = 0;
 #pragma unroll 1
   for (int i = 0; i < NS && !failed; ++i) {
-    const int r = prod.template issue<F>(ctl_a, P, cum, pc_a, rec_a, lane, pipe + i * STAGE_BYTES,
+    const int r = prod.template issue<BLOCK_BYTES>(ctl_a, P, cum, pc_a, rec_a, lane, pipe + i * STAGE_BYTES,
                                                    bars + 8 * i, desc_a + i * sizeof(TileDesc));
     if (r != 0) ++inflight;
     if (r < 0) failed = true;
@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
   int stage = 0;
   uint32_t phase = 0;
   int cur_k = -1, cur_b = 0, cur_kvh = 0, cur_total = 0, nacc = 0;
-  typename F::State st;
+  TileState st;
   st.reset();
 
 #pragma unroll 1
@@ -482,10 +482,18 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
       // ---- the piece changes (or nothing is left): hand this warp's share of the old piece over
       if (cur_k >= 0) {
         // fetched now, used at the very end (only the warp that completes the piece needs them)
-        const float vs = P.v_scale && F::kScaled ? __ldg(P.v_scale + cur_kvh) : 1.f;
+        const float vs = P.v_scale && FP8 ? __ldg(P.v_scale + cur_kvh) : 1.f;
         const float sink_g = P.sinks ? __ldg(P.sinks + cur_kvh * kGroup + g) : -INFINITY;
-        float m, l_tot, o[8][2];
-        F::finish(st, m, l_tot, o, lane);
+        float l_tot = st.l_run;
+        l_tot += __shfl_xor_sync(0xffffffffu, l_tot, 1);
+        l_tot += __shfl_xor_sync(0xffffffffu, l_tot, 2);
+        float m = st.m_ref;
+        float o[8][2];
+#pragma unroll
+        for (int nd = 0; nd < 8; ++nd) {
+          o[nd][0] = st.O[nd][0] + st.O[nd][2];
+          o[nd][1] = st.O[nd][1] + st.O[nd][3];
+        }
         bool complete = nacc == cur_total;
         if (!complete) {
           // deposit in this warp's buffer (free once the warp that completed its previous piece has read it)
@@ -575,14 +583,26 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
               Z = l_tot * wa + (s2 == -INFINITY ? 0.f : ex2(s2 - M));
               f = wa * vs / Z;
             }
-            if (P.out_f32) F::store(P.out_f32 + row_out * kHeadDim, o, f, c);
-            else F::store(P.out + row_out * kHeadDim, o, f, c);
+            if (P.out_f32) {
+              float* dst = P.out_f32 + row_out * kHeadDim + 2 * c;
+#pragma unroll
+              for (int nd = 0; nd < 8; ++nd)
+                *reinterpret_cast<float2*>(dst + 8 * nd) = make_float2(o[nd][0] * f, o[nd][1] * f);
+            } else {
+              __nv_bfloat16* dst = P.out + row_out * kHeadDim + 2 * c;
+#pragma unroll
+              for (int nd = 0; nd < 8; ++nd)
+                *reinterpret_cast<uint32_t*>(dst + 8 * nd) = f32x2_to_bf16x2(o[nd][0] * f, o[nd][1] * f);
+            }
             if (P.lse_out && c == 0)
               P.lse_out[row_out] = Z > 0.f ? (M + log2f(Z)) * 0.6931471805599453f : -INFINITY;
           } else {
             const float inv = l_tot > 0.f ? vs / l_tot : 0.f;
             const size_t row = (size_t)(blockIdx.x + p) * kGroup + g;
-            F::store(P.part_o + row * kHeadDim, o, inv, c);
+            float* po = P.part_o + row * kHeadDim + 2 * c;
+#pragma unroll
+            for (int nd = 0; nd < 8; ++nd)
+              *reinterpret_cast<float2*>(po + 8 * nd) = make_float2(o[nd][0] * inv, o[nd][1] * inv);
             if (c == 0) P.part_lse[row] = l_tot > 0.f ? (m + log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
             __threadfence();  // this lane's partial stores before the arrival
             __syncwarp();
@@ -600,8 +620,8 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
       if (!more) break;
       cur_k = d0.w; cur_b = d0.x; cur_kvh = d0.y; cur_total = d1.x;
       nacc = 0;
-      F::load_query(st, P.q + ((size_t)cur_b * (P.Hkv * kGroup) + cur_kvh * kGroup + g) * kHeadDim,
-                    P.k_scale && F::kScaled ? P.k_scale[cur_kvh] : 1.f, P.sm_scale_log2e, lane);
+      st.template load_query<FP8>(P.q + ((size_t)cur_b * (P.Hkv * kGroup) + cur_kvh * kGroup + g) * kHeadDim,
+                                  P.k_scale && FP8 ? P.k_scale[cur_kvh] : 1.f, P.sm_scale_log2e, c);
       st.reset();
     }
     if (!more) break;
@@ -614,14 +634,14 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
     const uint32_t vbase = kbase + NB * BLOCK_BYTES;
     const int tok0 = d0.z * TT;
     if ((tok0 < d1.z) || (tok0 + TT > d1.y))
-      F::template tile<TT, true>(st, lo, kbase, vbase, tok0, d1.z, d1.y, lane);
+      st.template tile<TT, FP8, true>(lo, kbase, vbase, tok0, d1.z, d1.y, c);
     else
-      F::template tile<TT, false>(st, lo, kbase, vbase, tok0, d1.z, d1.y, lane);
+      st.template tile<TT, FP8, false>(lo, kbase, vbase, tok0, d1.z, d1.y, c);
     ++nacc;
 
     // ---- refill this stage with the next tile this warp holds
     __syncwarp();
-    const int r = prod.template issue<F>(ctl_a, P, cum, pc_a, rec_a, lane, kbase, bars + 8 * stage,
+    const int r = prod.template issue<BLOCK_BYTES>(ctl_a, P, cum, pc_a, rec_a, lane, kbase, bars + 8 * stage,
                                                    desc_a + stage * sizeof(TileDesc));
     if (r != 0) ++inflight;
     if (++stage == NS) { stage = 0; phase ^= 1u; }
@@ -662,18 +682,18 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_cta_kernel(const __gri
   }
 }
 
-template <int NW, int NS, int TT, typename F>
+template <int NW, int NS, int TT, bool FP8>
 static size_t cta_smem_bytes(int batch, int ctas) {
-  constexpr int STAGE_BYTES = 2 * (TT / kBlock) * F::kBlockBytes;
-  return F::kAlign + (size_t)NW * NS * STAGE_BYTES + NW * NS * 8 + (size_t)NW * NS * sizeof(TileDesc) +
+  constexpr int STAGE_BYTES = 2 * (TT / kBlock) * kBlock * kHeadDim * (FP8 ? 1 : 2);
+  return 1024 + (size_t)NW * NS * STAGE_BYTES + NW * NS * 8 + (size_t)NW * NS * sizeof(TileDesc) +
          NW * sizeof(TileDesc) + NW * sizeof(PairCache) + (size_t)NW * 4 * 32 * sizeof(float4) +
          2 * NW * kGroup * sizeof(float) + 32 * sizeof(int) + 2 * kPieceSlots * sizeof(int) + sizeof(CtaCtl) +
          2 * (size_t)((ctas + 1 + 3) & ~3) * sizeof(int) + (size_t)(batch + 1) * sizeof(int);
 }
 
-template <int NW, int NS, int TT, typename F>
+template <int NW, int NS, int TT, bool FP8>
 static cudaError_t launch_cta_variant(const DecodeParams& P, int ctas, cudaStream_t s, int& smem_limit) {
-  auto kern = decode_attn_cta_kernel<NW, NS, TT, F>;
+  auto kern = decode_attn_cta_kernel<NW, NS, TT, FP8>;
   if (smem_limit == 0) {  // first launch of this variant on this device: raise its dynamic shared-memory limit
     int dev = 0, optin = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -682,20 +702,14 @@ static cudaError_t launch_cta_variant(const DecodeParams& P, int ctas, cudaStrea
     if (e != cudaSuccess) return e;
     smem_limit = optin;
   }
-  const size_t need = cta_smem_bytes<NW, NS, TT, F>(P.batch, ctas);
+  const size_t need = cta_smem_bytes<NW, NS, TT, FP8>(P.batch, ctas);
   if (need > (size_t)smem_limit) return cudaErrorInvalidValue;
   return launch_dependent(kern, dim3(ctas), dim3(NW * 32), need, s, P);
 }
 
-cudaError_t launch_decode_attn_cta(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit) {
-  switch (kv_dtype) {
-    case PUZZLE_KV_FP8_E4M3:
-      return launch_cta_variant<kDecodeWarpsFp8, kDecodeStagesFp8, kTileFp8, SwizzledTile<true>>(P, ctas, s, smem_limit[0]);
-    case PUZZLE_KV_BF16:
-      return launch_cta_variant<kDecodeWarpsBf16, kDecodeStagesBf16, kTileBf16, SwizzledTile<false>>(P, ctas, s,
-                                                                                                      smem_limit[1]);
-    default: return launch_cta_variant<kCtaWarpsFp4, kDecodeStagesFp4, kCtaTileFp4, Fp4Tile>(P, ctas, s, smem_limit[2]);
-  }
+cudaError_t launch_decode_attn_cta(const DecodeParams& P, bool fp8, int ctas, cudaStream_t s, int* smem_limit) {
+  return fp8 ? launch_cta_variant<kDecodeWarpsFp8, kDecodeStagesFp8, kTileFp8, true>(P, ctas, s, smem_limit[0])
+             : launch_cta_variant<kDecodeWarpsBf16, kDecodeStagesBf16, kTileBf16, false>(P, ctas, s, smem_limit[1]);
 }
 
 }  // namespace puzzle

@@ -1,6 +1,6 @@
 // Decode attention for several new tokens per sequence (a multi-token decode step, or a chunk of a prompt after
 // its bulk append: the input half of the paper's fixed-length scenarios, Section "Optimized Scenarios") over the
-// FP8 cache and the 4-bit cache, sm_100a.
+// FP8 cache, sm_100a.
 //
 // The bytes of a step do not grow with the number of query tokens, only the arithmetic does, so query tokens are
 // processed in pairs that share one pass over the K/V tiles: in the single-token kernels rows 8-15 of the
@@ -10,9 +10,6 @@
 // causal mask gives the earlier token one key fewer (and a window that starts one key earlier).  An odd last
 // token is paired with itself.  Sequences with more than two new tokens take several rows, whose repeated reads
 // of the same blocks are neighbours in the schedule and are served by L2.
-//
-// Over the 4-bit cache the heads are MMA columns (decode_tile_fp4.cuh), so nothing is empty there; what a pair shares is
-// the conversion of the tile (half of that cache's instructions), and each token issues its own 32 MMAs per tile.
 //
 // Everything else is the warp-scheduled kernel's design (decode_attn.cu): every warp an independent worker with
 // a private ring of TMA stages, the tile space of all rows cut evenly over the workers, one float32 partial
@@ -27,13 +24,12 @@
 #include "common.cuh"
 #include "decode_attn.cuh"
 #include "decode_tile.cuh"
-#include "decode_tile_fp4.cuh"
 #include "decode_tokens.cuh"
 
 namespace puzzle {
 namespace {
 
-constexpr int kTokStages = 2;
+constexpr int kTokWarps = 12, kTokStages = 2;
 constexpr int kPairRows = 2 * kGroup;  // partial rows per (worker, row, KV head): 8 heads of each of the two tokens
 
 struct TokSegment {
@@ -230,31 +226,6 @@ struct TileState2 {
   }
 };
 
-// The E4M3 cache as the kernel sees it: copies, state of a pair, one tile, and a token's state as it is stored.  The 4-bit
-// cache: Fp4Pair (decode_tokens.cuh).
-struct Fp8Pair {
-  static constexpr int kWarps = kTokWarpsFp8;
-  using Tile = SwizzledTile<true>;
-  using State = TileState2;
-  static __device__ __forceinline__ void load_query(State& st, int tok, const __nv_bfloat16* qrow, float ks, float sm,
-                                                    int lane) {
-    st.load_query(tok, qrow, ks, sm, lane & 3);
-  }
-  template <bool EDGE>
-  static __device__ __forceinline__ void tile(State& st, const Tile::Lanes& at, uint32_t kbase, uint32_t vbase, int tok0,
-                                              int loA, int LA, int lo, int L, int lane) {
-    st.tile<EDGE>(at, kbase, vbase, tok0, loA, LA, lo, L, lane & 3);
-  }
-  static __device__ __forceinline__ void finish(const State& st, int tok, float& m, float& l, float (&o)[8][2], int) {
-    l = st.l_run[tok];
-    l += __shfl_xor_sync(0xffffffffu, l, 1);
-    l += __shfl_xor_sync(0xffffffffu, l, 2);
-    m = st.m_ref[tok];
-#pragma unroll
-    for (int nd = 0; nd < 8; ++nd) { o[nd][0] = st.O[nd][2 * tok]; o[nd][1] = st.O[nd][2 * tok + 1]; }
-  }
-};
-
 // Log-sum-exp merge of the `count` partials of one (row, KV head) by one warp, one token after the other: the
 // quad of lanes g = lane / 4 owns query head g of the group, lane c of the quad channels 16c .. 16c + 15.  Part k
 // of head g of token half h is partial row first + 8 h + g + 16 k.  The formula is merge_rows' (decode_sched.cuh).
@@ -277,29 +248,18 @@ __device__ __noinline__ void merge_tok_rows(const DecodeParams& P, const RowInfo
     for (int i = 0; i < 16; ++i) acc[i] = 0.f;
     float Z = 0.f;
     if (M != -INFINITY) {
-      // four parts per round, all loads before the first use, as in merge_rows: the merge is a chain of L2 round trips
-      for (int k0 = 0; k0 < count; k0 += 4) {
-        float l[4];
-        float4 v[4][4];
+      for (int k = 0; k < count; ++k) {
+        const long long idx = base + (long long)k * kPairRows;
+        const float l = __ldcg(P.part_lse + idx);
+        if (l == -INFINITY) continue;  // an empty part: its payload is undefined
+        const float4* o = reinterpret_cast<const float4*>(P.part_o + idx * kHeadDim + 16 * c);
+        const float wgt = __expf(l - M);
+        Z += wgt;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bool on = k0 + j < count;
-          const long long idx = base + (long long)(on ? k0 + j : k0) * kPairRows;
-          l[j] = on ? __ldcg(P.part_lse + idx) : -INFINITY;
-          const float4* o = reinterpret_cast<const float4*>(P.part_o + idx * kHeadDim + 16 * c);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[j][i] = __ldcg(o + i);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (l[j] == -INFINITY) continue;  // an empty part: its payload is undefined
-          const float wgt = __expf(l[j] - M);
-          Z += wgt;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            acc[4 * i + 0] += wgt * v[j][i].x; acc[4 * i + 1] += wgt * v[j][i].y;
-            acc[4 * i + 2] += wgt * v[j][i].z; acc[4 * i + 3] += wgt * v[j][i].w;
-          }
+        for (int i = 0; i < 4; ++i) {
+          const float4 v = __ldcg(o + i);
+          acc[4 * i + 0] += wgt * v.x; acc[4 * i + 1] += wgt * v.y;
+          acc[4 * i + 2] += wgt * v.z; acc[4 * i + 3] += wgt * v.w;
         }
       }
       if (sink != -INFINITY) Z += __expf(sink - M);  // the sink is one more softmax column, counted once
@@ -317,11 +277,10 @@ __device__ __noinline__ void merge_tok_rows(const DecodeParams& P, const RowInfo
 
 }  // namespace
 
-template <typename F>
-__global__ void __launch_bounds__(F::kWarps * 32, 1) decode_attn_tokens_kernel(const __grid_constant__ DecodeParams P) {
-  constexpr int NW = F::kWarps, NS = kTokStages, TT = kTokTile;
+__global__ void __launch_bounds__(kTokWarps * 32, 1) decode_attn_tokens_kernel(const __grid_constant__ DecodeParams P) {
+  constexpr int NW = kTokWarps, NS = kTokStages, TT = kTokTile;
   constexpr int NB = TT / kBlock;
-  constexpr int BLOCK_BYTES = F::Tile::kBlockBytes;
+  constexpr int BLOCK_BYTES = kBlock * kHeadDim;
   constexpr int STAGE_BYTES = 2 * NB * BLOCK_BYTES;
   constexpr int PIPE_BYTES = NW * NS * STAGE_BYTES;
   constexpr int kNotVisible = INT_MIN;
@@ -342,7 +301,10 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) decode_attn_tokens_kernel(c
     for (int i = 0; i < NS; ++i) mbar_init(bars + 8 * i, 1);
     fence_mbar_init();
   }
-  if (threadIdx.x == 0) F::Tile::prefetch(P);
+  if (threadIdx.x == 0) {
+    tma_prefetch_desc(&P.tmK);
+    tma_prefetch_desc(&P.tmV);
+  }
   release_dependents();
   grid_dependency_wait();   // nothing above reads or writes global memory
   // ---- schedule: tiles of every row, prefix sums
@@ -375,7 +337,7 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) decode_attn_tokens_kernel(c
   const int share = (T + nW - 1) / nW;
   const int w_lo = min(w * share, T), w_hi = min(w_lo + share, T);
 
-  typename F::Tile::Lanes lo;
+  LaneOffsets<true> lo;
   lo.init(lane);
 
   // ---- producer side: tiles of this worker's run, block-table entries fetched one tile ahead
@@ -402,7 +364,16 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) decode_attn_tokens_kernel(c
         if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
       }
     }
-    F::Tile::template load_tile<NB>(P, stage_addr, row, bar, lane, [] {});
+    int rws[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) rws[i] = __shfl_sync(0xffffffffu, row, i);
+    if (elect_one()) {
+      mbar_arrive_expect_tx(bar, 2 * NB * BLOCK_BYTES);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) tma_load_2d(stage_addr + i * BLOCK_BYTES, &P.tmK, 0, rws[i], bar);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) tma_load_2d(stage_addr + (NB + i) * BLOCK_BYTES, &P.tmV, 0, rws[i], bar);
+    }
     if (++ps.t == ps.t_end) p_ok = next_tok_segment(p_pos, w_hi, ps, P, cum, rows, w);
     lookup();
     return true;
@@ -420,13 +391,13 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) decode_attn_tokens_kernel(c
   TokSegment cs;
 #pragma unroll 1
   while (!failed && next_tok_segment(c_pos, w_hi, cs, P, cum, rows, w)) {
-    typename F::State st;
+    TileState2 st;
     const int Hq = P.Hkv * kGroup;
     const float ks = P.k_scale ? P.k_scale[cs.kvh] : 1.f;
-    F::load_query(st, 0, P.q + (((size_t)cs.row.b * P.n_q + cs.row.t0) * Hq + cs.kvh * kGroup + g) * kHeadDim, ks,
-                  P.sm_scale_log2e, lane);
-    F::load_query(st, 1, P.q + (((size_t)cs.row.b * P.n_q + cs.row.t1) * Hq + cs.kvh * kGroup + g) * kHeadDim, ks,
-                  P.sm_scale_log2e, lane);
+    st.load_query(0, P.q + (((size_t)cs.row.b * P.n_q + cs.row.t0) * Hq + cs.kvh * kGroup + g) * kHeadDim, ks,
+                  P.sm_scale_log2e, c);
+    st.load_query(1, P.q + (((size_t)cs.row.b * P.n_q + cs.row.t1) * Hq + cs.kvh * kGroup + g) * kHeadDim, ks,
+                  P.sm_scale_log2e, c);
     st.reset();
 #pragma unroll 1
     for (int t = cs.t; t < cs.t_end; ++t) {
@@ -440,9 +411,9 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) decode_attn_tokens_kernel(c
       const uint32_t vbase = kbase + NB * BLOCK_BYTES;
       const int tok0 = t * TT;
       if ((tok0 < cs.row.lo) || (tok0 + TT > cs.row.LA))
-        F::template tile<true>(st, lo, kbase, vbase, tok0, cs.row.loA, cs.row.LA, cs.row.lo, cs.row.L, lane);
+        st.tile<true>(lo, kbase, vbase, tok0, cs.row.loA, cs.row.LA, cs.row.lo, cs.row.L, c);
       else
-        F::template tile<false>(st, lo, kbase, vbase, tok0, cs.row.loA, cs.row.LA, cs.row.lo, cs.row.L, lane);
+        st.tile<false>(lo, kbase, vbase, tok0, cs.row.loA, cs.row.LA, cs.row.lo, cs.row.L, c);
       __syncwarp();
       if (issue(kbase, bars + 8 * stage)) ++inflight;
       if (++stage == NS) { stage = 0; phase ^= 1u; }
@@ -453,12 +424,17 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) decode_attn_tokens_kernel(c
     const float vs = P.v_scale ? P.v_scale[cs.kvh] : 1.f;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      float m, l_tot, o[8][2];
-      F::finish(st, t, m, l_tot, o, lane);
+      float l_tot = st.l_run[t];
+      l_tot += __shfl_xor_sync(0xffffffffu, l_tot, 1);
+      l_tot += __shfl_xor_sync(0xffffffffu, l_tot, 2);
       const float inv = l_tot > 0.f ? vs / l_tot : 0.f;
       const size_t row = (size_t)cs.prow + 8 * t + g;
-      F::Tile::store(P.part_o + row * kHeadDim, o, inv, c);
-      if (c == 0) P.part_lse[row] = l_tot > 0.f ? (m + log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
+      float* po = P.part_o + row * kHeadDim + 2 * c;
+#pragma unroll
+      for (int nd = 0; nd < 8; ++nd)
+        *reinterpret_cast<float2*>(po + 8 * nd) =
+            make_float2(st.O[nd][2 * t] * inv, st.O[nd][2 * t + 1] * inv);
+      if (c == 0) P.part_lse[row] = l_tot > 0.f ? (st.m_ref[t] + log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
     }
     // ---- arrival; the warp that completes the (row, KV head) merges it and leaves the counter at zero
     {
@@ -500,32 +476,25 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) decode_attn_tokens_kernel(c
 // Arrival counters (one per (sequence, token pair, KV head)) and partial rows of the kernel for a batch of `batch`
 // sequences with up to n_q query tokens each.
 size_t decode_attn_tokens_counters(int batch, int n_q, int Hkv) { return (size_t)batch * ((n_q + 1) / 2) * Hkv; }
-size_t decode_attn_tokens_partial_rows(int ctas, int batch, int n_q, int Hkv, int kv_dtype) {
-  const int warps = kv_dtype == PUZZLE_KV_FP4_E2M1 ? kTokWarpsFp4 : kTokWarpsFp8;
-  return ((size_t)ctas * warps + (size_t)batch * ((n_q + 1) / 2) * Hkv) * kPairRows;
+size_t decode_attn_tokens_partial_rows(int ctas, int batch, int n_q, int Hkv) {
+  return ((size_t)ctas * kTokWarps + (size_t)batch * ((n_q + 1) / 2) * Hkv) * kPairRows;
 }
 
-template <typename F>
-static cudaError_t launch_tokens_variant(const DecodeParams& P, int ctas, cudaStream_t s, int& smem_limit) {
-  auto kern = decode_attn_tokens_kernel<F>;
-  if (smem_limit == 0) {
+cudaError_t launch_decode_attn_tokens(const DecodeParams& P, int ctas, cudaStream_t s, int* smem_limit) {
+  if (*smem_limit == 0) {
     int dev = 0, optin = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, optin);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(decode_attn_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, optin);
     if (e != cudaSuccess) return e;
-    smem_limit = optin;
+    *smem_limit = optin;
   }
   const int rows = P.batch * ((P.n_q + 1) / 2);
-  const size_t need = 1024 + (size_t)F::kWarps * kTokStages * 2 * (kTokTile / kBlock) * F::Tile::kBlockBytes +
-                      F::kWarps * kTokStages * 8 + (size_t)(rows + 1) * sizeof(int);
-  if (need > (size_t)smem_limit) return cudaErrorInvalidValue;  // too many rows for the schedule array
-  return launch_dependent(kern, dim3(ctas), dim3(F::kWarps * 32), need, s, P);
-}
-
-cudaError_t launch_decode_attn_tokens(const DecodeParams& P, int kv_dtype, int ctas, cudaStream_t s, int* smem_limit) {
-  return kv_dtype == PUZZLE_KV_FP4_E2M1 ? launch_tokens_variant<Fp4Pair>(P, ctas, s, smem_limit[1])
-                                        : launch_tokens_variant<Fp8Pair>(P, ctas, s, smem_limit[0]);
+  const size_t need = 1024 + (size_t)kTokWarps * kTokStages * 2 * (kTokTile / kBlock) * kBlock * kHeadDim +
+                      kTokWarps * kTokStages * 8 + (size_t)(rows + 1) * sizeof(int);
+  if (need > (size_t)*smem_limit) return cudaErrorInvalidValue;  // too many rows for the schedule array
+  return launch_dependent(decode_attn_tokens_kernel, dim3(ctas), dim3(kTokWarps * 32), need, s, P);
 }
 
 }  // namespace puzzle

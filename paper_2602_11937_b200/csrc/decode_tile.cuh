@@ -327,7 +327,6 @@ template <bool FP8>
 struct SwizzledTile {
   static constexpr int kBlockBytes = kBlock * kHeadDim * (FP8 ? 1 : 2);   // one (block, KV head) of K or of V
   static constexpr bool kScaled = FP8;
-  static constexpr bool kLeanClaims = false;
   static constexpr int kAlign = 1024;   // of the stages in shared memory: the swizzle repeats every 1 KiB
   using Lanes = LaneOffsets<FP8>;
   using State = TileState;

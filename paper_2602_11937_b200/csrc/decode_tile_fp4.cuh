@@ -236,7 +236,6 @@ struct Fp4State {
 struct Fp4Tile {
   static constexpr int kBlockBytes = kFp4BlockBytes;
   static constexpr bool kScaled = true;
-  static constexpr bool kLeanClaims = true;
   static constexpr int kAlign = 128;
   using Lanes = Fp4Lanes;
   using State = Fp4State;

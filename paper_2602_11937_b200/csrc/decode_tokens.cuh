@@ -42,7 +42,6 @@ __device__ __forceinline__ RowInfo row_info(const DecodeParams& P, int r) {
 }
 
 struct Fp4Pair {
-  static constexpr int kWarps = kTokWarpsFp4;
   using Tile = Fp4Tile;
   struct State {
     Fp4State t[2];
