@@ -43,7 +43,8 @@
  *     (a block-table entry outside [0, num_blocks), a sequence longer than its
  *     table row) set a bit in *dev_status, skip the access and never trap.
  *   - Shapes supported by this version: head_dim 64, block_size 16,
- *     num_q_heads == 8 * num_kv_heads, batch <= 4096.
+ *     num_q_heads == 8 * num_kv_heads, batch <= 4096 (num_kv_heads <= 4096 for
+ *     puzzle_kv_append_rope, puzzle_kv_read_tokens and appends to a 4-bit cache).
  *
  * Cache layout (both K and V):  [num_blocks][num_kv_heads][block_size][head_dim]
  *   elements u8 (E4M3 codes) or bf16; one (block, KV head) is 1 KiB (FP8) or
@@ -174,7 +175,8 @@ typedef struct {
 
 /* The new tokens' queries, keys and values as a projection leaves them: bf16, row (b, i, h) of q at
  * q + b * q_seq_stride + i * q_token_stride + h * head_dim (host struct; strides in elements, multiples of 8, not
- * negative; pointers 16-byte aligned).  The three may be slices of one [batch][n_new][Hq + 2 Hkv][head_dim] array. */
+ * negative, without meaning for a dimension of one; pointers 16-byte aligned).  The three may be slices of one
+ * [batch][n_new][Hq + 2 Hkv][head_dim] array. */
 typedef struct {
   const void* q; /* NULL: no queries */
   const void* k;
@@ -196,7 +198,9 @@ typedef struct {
  *   new_lens: as for puzzle_kv_append_tokens.  Skipped: tokens i >= new_lens[b], tokens that would land before place 0,
  *     all of a sequence longer than its table row (PUZZLE_DEV_SEQ_TOO_LONG), tokens whose position the table does
  *     not have (PUZZLE_DEV_BAD_POSITION).  A bad block-table entry skips the token's key and value only;
- *   tokens of one sequence must land in different cache slots: over a ring of R blocks, at most 16 (R - 1) at a time.
+ *   tokens of one call must land in different cache slots: over a ring of R blocks, at most 16 (R - 1) of a sequence at a
+ *     time, and no two sequences into one block (in a 4-bit block two tokens share V's bytes, which is why appends to it
+ *     read them: the other token's half is kept).
  * n_new == 1 runs a kernel laid out for latency, chunks one laid out for bandwidth; the results are the same. */
 PUZZLE_API puzzle_status puzzle_kv_append_rope(const puzzle_layer_desc* desc, const puzzle_kv_view* kv,
                                  const puzzle_rope* rope, const puzzle_qkv* qkv, void* q_out, const int32_t* new_lens,

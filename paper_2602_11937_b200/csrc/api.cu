@@ -124,6 +124,7 @@ bool set_cache(DecodeParams* P, const puzzle_layer_desc* d, const puzzle_kv_view
   return make_cache_map(&P->tmK, kv->k_cache, rows, eb, row_bytes) && make_cache_map(&P->tmV, kv->v_cache, rows, eb, row_bytes);
 }
 
+constexpr int kMaxAppendHeads = 4096;   // the head groups of a chunk are a grid dimension
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // The parameters of an append that the descriptors hold; the rest is set by the entry points.
@@ -333,6 +334,7 @@ puzzle_status puzzle_kv_append(const puzzle_layer_desc* desc, const puzzle_kv_vi
   if (!k_new || !v_new) return PUZZLE_ERR_NULL;
   if (desc->kv_dtype == PUZZLE_KV_FP4_E2M1) {
     if (!aligned16(k_new) || !aligned16(v_new)) return PUZZLE_ERR_SHAPE;
+    if (desc->num_kv_heads > kMaxAppendHeads) return PUZZLE_ERR_UNSUPPORTED;
     const cudaError_t e = append_fp4(desc, kv, k_new, v_new, nullptr, batch, 1, dev_status, static_cast<cudaStream_t>(stream));
     count_launch();
     return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
@@ -361,6 +363,7 @@ puzzle_status puzzle_kv_append_tokens(const puzzle_layer_desc* desc, const puzzl
   const long long per_seq = (long long)n_new * desc->num_kv_heads * (kHeadDim / 8);
   if (per_seq > 0x7fffffffll || batch > 65535) return PUZZLE_ERR_SHAPE;
   if (desc->kv_dtype == PUZZLE_KV_FP4_E2M1) {
+    if (desc->num_kv_heads > kMaxAppendHeads) return PUZZLE_ERR_UNSUPPORTED;
     const cudaError_t e = append_fp4(desc, kv, k_new, v_new, new_lens, batch, n_new, dev_status,
                                      static_cast<cudaStream_t>(stream));
     count_launch();
@@ -390,10 +393,12 @@ puzzle_status puzzle_kv_append_rope(const puzzle_layer_desc* desc, const puzzle_
   if (!aligned16(rope->cos_sin) || !aligned16(qkv->q) || !aligned16(qkv->k) || !aligned16(qkv->v) ||
       (qkv->q && !aligned16(q_out)))
     return PUZZLE_ERR_SHAPE;
-  const int64_t strides[6] = {qkv->q_seq_stride, qkv->q_token_stride, qkv->k_seq_stride,
-                              qkv->k_token_stride, qkv->v_seq_stride, qkv->v_token_stride};
-  for (int i = qkv->q ? 0 : 2; i < 6; ++i)
-    if (strides[i] < 0 || strides[i] % 8) return PUZZLE_ERR_SHAPE;   // rows are read 16 bytes at a time
+  if (desc->num_kv_heads > kMaxAppendHeads) return PUZZLE_ERR_UNSUPPORTED;
+  // rows are read 16 bytes at a time; the stride of a dimension of one means nothing
+  const int64_t seq[3] = {qkv->k_seq_stride, qkv->v_seq_stride, qkv->q ? qkv->q_seq_stride : 0};
+  const int64_t token[3] = {qkv->k_token_stride, qkv->v_token_stride, qkv->q ? qkv->q_token_stride : 0};
+  for (int i = 0; i < 3; ++i)
+    if ((batch > 1 && (seq[i] < 0 || seq[i] % 8)) || (n_new > 1 && (token[i] < 0 || token[i] % 8))) return PUZZLE_ERR_SHAPE;
   // in place: every row has to lie where its rotated form goes, or one row would overwrite another before it is read
   const int64_t row = (int64_t)desc->num_q_heads * desc->head_dim;
   if (qkv->q && q_out == qkv->q &&
@@ -428,6 +433,7 @@ puzzle_status puzzle_kv_read_tokens(const puzzle_layer_desc* desc, const puzzle_
   st = check_view(desc, kv, batch);
   if (st != PUZZLE_OK) return st;
   if (!k_out || !v_out) return PUZZLE_ERR_NULL;
+  if (desc->num_kv_heads > kMaxAppendHeads) return PUZZLE_ERR_UNSUPPORTED;
   if (n_read <= 0 || n_read > (1 << 24) || !aligned16(k_out) || !aligned16(v_out)) return PUZZLE_ERR_SHAPE;
   ReadParams R;
   std::memset(&R, 0, sizeof R);

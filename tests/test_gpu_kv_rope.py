@@ -294,3 +294,17 @@ def test_append_then_read(kind):
         bound = (t.expand(-1, -1, -1, -1, 16).flatten(-2)) * 1.0 + scale * 2.0 ** -9
     bound = bound + (x.abs() + bound) * 2.0 ** -8 * (kind != "bf16")
     assert bool((err <= bound).all())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("batch, n", [(3, 1), (1, 5), (1, 1)])
+def test_the_stride_of_a_dimension_of_one_means_nothing(kind, batch, n):
+    s = Setup(KINDS[kind], [70, 5, 33][:batch], n, seed=21)
+    s.upload()
+    parts = s.parts
+
+    def odd(t):
+        return [x.as_strided(x.shape, (x.stride(0) if batch > 1 else 3, x.stride(1) if n > 1 else 7, 64, 1),
+                             x.storage_offset()) for x in parts(t)]
+    s.parts = odd
+    s.run()

@@ -43,7 +43,8 @@ def _append(**over):
     (dict(rope__num_positions=0), SHAPE), (dict(rope__rotary_dim=0), SHAPE), (dict(rope__rotary_dim=80), SHAPE),
     (dict(rope__rotary_dim=24), UNSUPPORTED), (dict(rope__cos_sin=0x4008), SHAPE), (dict(qkv__q=0x5008), SHAPE),
     (dict(qkv__k=0x6008), SHAPE), (dict(qkv__v=0x7002), SHAPE), (dict(q_out=0x8008), SHAPE),
-    (dict(qkv__k_token_stride=-8), SHAPE), (dict(qkv__v_seq_stride=12), SHAPE), (dict(qkv__q_token_stride=4100), SHAPE),
+    (dict(qkv__k_token_stride=-8, n_new=2), SHAPE), (dict(qkv__v_seq_stride=12), SHAPE),
+    (dict(qkv__q_token_stride=4100, n_new=2), SHAPE), (dict(qkv__q_seq_stride=4100), SHAPE),
     # in place on a slice of a wider array: a row would land on another one that has not been read
     (dict(q_out=0x5000, qkv__q_seq_stride=5120), SHAPE), (dict(q_out=0x5000, n_new=2, qkv__q_token_stride=5120), SHAPE),
 ])
@@ -93,3 +94,15 @@ def test_binding_checks_shapes_before_it_calls():
         P.puzzle_kv_read_tokens(d, P.KVView(), x, x[:1])
     with pytest.raises(ValueError, match="CUDA tensor"):
         P.rope_view(torch.zeros(4, 64))
+
+
+@pytest.mark.parametrize("n_new", [1, 2])
+def test_more_heads_than_a_grid_dimension_holds_are_refused(n_new):
+    heads = dict(num_q_heads=8 * 4097, desc__num_kv_heads=4097)
+    wide = dict(heads, qkv__q_seq_stride=1 << 30, qkv__q_token_stride=1 << 24)
+    assert _append(**wide, n_new=n_new) == UNSUPPORTED
+    lib, d = _args(**heads, n_new=n_new)
+    desc, kv = ctypes.byref(d["desc"]), ctypes.byref(d["kv"])
+    assert lib.puzzle_kv_append(desc, kv, 0x6000, 0x7000, 4, None, None) == UNSUPPORTED
+    assert lib.puzzle_kv_append_tokens(desc, kv, 0x6000, 0x7000, None, 4, n_new, None, None) == UNSUPPORTED
+    assert lib.puzzle_kv_read_tokens(desc, kv, 0x9000, 0xA000, None, 4, n_new, None, None) == UNSUPPORTED
