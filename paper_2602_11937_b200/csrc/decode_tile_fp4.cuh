@@ -320,7 +320,10 @@ struct Fp4Tile {
     const float la = __shfl_sync(0xffffffffu, l0, g >> 1), lb = __shfl_sync(0xffffffffu, l1, g >> 1);
     m = (g & 1) ? mb : ma;
     l = (g & 1) ? lb : la;
-    if (!(l >= 0.f)) l = INFINITY;   // a NaN among the visible keys: nothing downstream may take this for an empty part
+    if (!(l >= 0.f)) {   // a NaN among the weights: nothing downstream may take this for an empty part
+      l = INFINITY;
+      if (m == -INFINITY) m = 0.f;
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {   // float32 8x8 transposes, as two 16-bit ones
       const uint32_t x = __float_as_uint(st.O[j >> 1][2 * (j & 1)]), y = __float_as_uint(st.O[j >> 1][2 * (j & 1) + 1]);

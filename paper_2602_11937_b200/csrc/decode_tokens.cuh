@@ -41,6 +41,10 @@ __device__ __forceinline__ RowInfo row_info(const DecodeParams& P, int r) {
   return i;
 }
 
+// Ones where a byte of four E4M3 values is a NaN.
+__device__ __forceinline__ uint32_t e4m3_nans(uint32_t x) { return __vcmpeq4(x & 0x7f7f7f7fu, 0x7f7f7f7fu); }
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
+
 struct Fp4Pair {
   using Tile = Fp4Tile;
   struct State {
@@ -51,13 +55,48 @@ struct Fp4Pair {
                                                     int lane) {
     st.t[tok].load_query(qrow, ks, sm, lane);
   }
-  // EDGE as in TileState2::tile; V scales outside [loA, L) are cleared (the keys in [LA, L) are real tokens, and so are
-  // those in [loA, lo): the other token's weights for them are zero).
+  // A key that only one of the two tokens sees (the newest, the oldest of a window) meets the other's weight of zero in the
+  // shared product, and a NaN among its V scales would make that a NaN.  Such a scale is cleared in shared memory, and the
+  // channels it covers become NaN for the token that sees the key.  Nothing of this is live beside the tile's registers:
+  // converting V once for each token instead costs 10 % of a long call (155 to 171 us, two tokens at 16 x 64K).
+  static __device__ __forceinline__ void lone_nans(State& st, const Tile::Lanes& at, uint32_t vbase, int first, int loA, int LA,
+                                                   int lo, int L) {
+    constexpr int NB = kTokTile / kBlock;
+    uint32_t any = 0;
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) any |= e4m3_nans(lds32(vbase + blk * kFp4BlockBytes + at.vs));
+    if (!__any_sync(0xffffffffu, any)) return;
+    uint32_t nan[2] = {0, 0};
+#pragma unroll 1
+    for (int blk = 0; blk < NB; ++blk) {
+      const uint32_t addr = vbase + blk * kFp4BlockBytes + at.vs, sc = lds32(addr), bad = e4m3_nans(sc);
+      const uint32_t a = fp4_visible_scales(bad, first + kBlock * blk, loA, LA);
+      const uint32_t b = fp4_visible_scales(bad, first + kBlock * blk, lo, L);
+      nan[0] |= a & ~b;
+      nan[1] |= b & ~a;
+      __syncwarp();   // lanes g and g ^ 1 hold the same scales: both have read them
+      if (a ^ b) sts32(addr, sc & ~(a ^ b));
+    }
+    fence_proxy_async();   // before the next copy into this stage
+    __syncwarp();
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {   // the four lanes of g hold four tokens each of the same channels
+      nan[t] |= __shfl_xor_sync(0xffffffffu, nan[t], 1);
+      nan[t] |= __shfl_xor_sync(0xffffffffu, nan[t], 2);
+      if (nan[t])
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) st.t[t].O[i][e] = __int_as_float(0x7fffffff);
+    }
+  }
+  // EDGE as in TileState2::tile; V scales outside [loA, L) are cleared.
   template <bool EDGE>
   static __device__ __forceinline__ void tile(State& st, const Tile::Lanes& at, uint32_t kbase, uint32_t vbase, int tok0,
                                               int loA, int LA, int lo, int L, int lane) {
     constexpr int NB = kTokTile / kBlock;
     const int g = lane >> 2, c = lane & 3;
+    if constexpr (EDGE) lone_nans(st, at, vbase, tok0 + 2 * c, loA, LA, lo, L);
     float s[2][NB][4];
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) {

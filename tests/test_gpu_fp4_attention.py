@@ -398,3 +398,50 @@ def test_single_steps_and_several_tokens_agree():
     for i in range(3):
         c.check(out.view(3, 3, 16, 64)[:, i].double().cpu().numpy(), lse.view(3, 3, 16)[:, i].double().cpu().numpy(), token=i)
     _check_tokens(c)
+
+
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("lens", [[64, 129, 5], [2000, 3001, 700]])
+def test_a_nan_of_one_token_stays_out_of_the_other(window, lens):
+    """The newest key is not visible to the earlier token of a pair, nor the oldest one of a window to the later: a NaN there
+    (K or V) is the business of the token that sees it."""
+    c = Case(lens, hkv=2, seed=40, n_q=2, window=window, poison=False)
+    for b, n in enumerate(lens):
+        newest = c.table[b, (n - 1) // 16]
+        (c.v if b != 1 else c.k)[newest, 1, (R.v_scale_at if b != 1 else R.k_scale_at)((n - 1) % 16, 2)] = 0x7F
+        if window and n > window:
+            t = n - 1 - window                                  # the oldest key of the earlier token
+            c.v[c.table[b, t // 16], 0, R.v_scale_at(t % 16, 0)] = 0x7F
+    c.upload()
+    got, lse = _tokens(c)
+    clean = Case(lens, hkv=2, seed=40, n_q=2, window=window, poison=False)
+    for token in (0, 1):
+        ref, ref_lse = clean.oracle(token)
+        bad = np.isnan(got[:, token])
+        for b, n in enumerate(lens):
+            want = np.zeros((16, 64), bool)
+            if token == 1:
+                want[8:, slice(None) if b == 1 else slice(32, 48)] = True
+            elif window and n > window:
+                want[:8, :16] = True
+            assert np.array_equal(bad[b], want), (token, b)
+        clean.check(np.where(bad, ref, got[:, token]), np.where(bad.all(-1), ref_lse, lse[:, token]), token=token)
+    assert int(c.status.item()) == 0
+
+
+@pytest.mark.parametrize("splits", [0, -1, -2, 3])
+def test_a_nan_in_a_query_head_shows_in_its_output_alone(splits):
+    """All logits of the head are NaN, so that its running maximum never leaves minus infinity."""
+    c = Case([1000, 1, 16], hkv=2, seed=12)
+    c.q[:, 0, 11, 5] = float("nan")
+    c.upload()
+    got, _ = c.run(splits)
+    assert np.isnan(got[:, 11]).all()
+    assert not np.isnan(np.delete(got, 11, axis=1)).any()
+    c = Case([1000, 5, 16], hkv=2, n_q=3, seed=12)
+    c.q[:, 1, 11, 5] = float("nan")
+    c.upload()
+    got, _ = _tokens(c)
+    assert np.isnan(got[:, 1, 11]).all()
+    got[:, 1, 11] = 0
+    assert not np.isnan(got).any()
