@@ -164,13 +164,19 @@ def _p(t: Optional[torch.Tensor], dtype=None, name="tensor"):
 
 # The current stream's handle without a Stream object around it: a decode step's call is a few microseconds of host time.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _stream(stream):
+def _stream(stream, tensor=None):
+    """Handle of `stream` (None: the current one).  tensor: one of the call's; kernels are launched on the current device,
+    so it has to lie there."""
+    if tensor is not None and tensor.get_device() != _current_device():
+        raise ValueError("the tensors are on cuda:%d, the current device is cuda:%d"
+                         % (tensor.get_device(), _current_device()))
     if stream is not None:
         return stream.cuda_stream
     if _raw_stream is not None and torch.cuda.is_initialized():
-        return _raw_stream(torch._C._cuda_getDevice())
+        return _raw_stream(_current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -226,7 +232,7 @@ def puzzle_kv_append(desc: LayerDesc, view: KVView, k_new: torch.Tensor, v_new: 
     batch = k_new.shape[0]
     _check(_load().puzzle_kv_append(ctypes.byref(desc), ctypes.byref(view), _p(k_new, torch.bfloat16, "k_new"),
                                     _p(v_new, torch.bfloat16, "v_new"), batch, _p(dev_status, torch.int32),
-                                    _stream(stream)), "puzzle_kv_append")
+                                    _stream(stream, k_new)), "puzzle_kv_append")
 
 
 def puzzle_kv_amax_update(x: torch.Tensor, amax: torch.Tensor, stream=None) -> None:
@@ -261,7 +267,7 @@ def puzzle_kv_append_tokens(desc: LayerDesc, view: KVView, k_new: torch.Tensor, 
     batch, n_new = k_new.shape[0], k_new.shape[1]
     _check(_load().puzzle_kv_append_tokens(ctypes.byref(desc), ctypes.byref(view), _p(k_new, torch.bfloat16, "k_new"),
                                            _p(v_new, torch.bfloat16, "v_new"), _p(new_lens, torch.int32, "new_lens"),
-                                           batch, n_new, _p(dev_status, torch.int32), _stream(stream)),
+                                           batch, n_new, _p(dev_status, torch.int32), _stream(stream, k_new)),
            "puzzle_kv_append_tokens")
 
 
@@ -276,14 +282,12 @@ def rope_view(cos_sin: torch.Tensor, interleaved: bool = False, pos_offset: Opti
     return r
 
 
-def _rows(t: Optional[torch.Tensor], name: str):
-    """Pointer, sequence stride and token stride of new tokens' rows [batch][n_new][heads][D] or [batch][heads][D]."""
-    if t is None:
-        return None, 0, 0
-    if not t.is_cuda or t.dtype != torch.bfloat16:
+def _rows(t: torch.Tensor, name: str, row: int):
+    """Pointer, sequence stride and token stride of new tokens' rows [batch][n_new][heads][row] or [batch][heads][row]."""
+    if not t.is_cuda or t.dtype is not torch.bfloat16:
         raise ValueError("%s must be a bf16 CUDA tensor" % name)
     stride = t.stride()
-    if stride[-1] != 1 or (t.shape[-2] > 1 and stride[-2] != t.shape[-1]):
+    if stride[-1] != 1 or (stride[-2] != row and t.shape[-2] > 1):
         raise ValueError("the heads of a token of %s must be contiguous" % name)
     return t.data_ptr(), stride[0], stride[1] if len(stride) == 4 else 0
 
@@ -296,32 +300,37 @@ def puzzle_kv_append_rope(desc: LayerDesc, view: KVView, rope: Rope, q: Optional
     of a wider array along the heads; q_out: bf16 [batch][n_new][Hq][D] contiguous, may be q; q None: k and v only."""
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
-    lead = tuple(k_new.shape[:-2])
-    if len(lead) not in (1, 2):
+    row, shape = desc.head_dim, k_new.shape
+    if len(shape) not in (3, 4):
         raise ValueError("k_new must be [batch][n_new][heads][D] or [batch][heads][D]")
-    kv_shape, q_shape = (*lead, desc.num_kv_heads, desc.head_dim), (*lead, desc.num_q_heads, desc.head_dim)
-    for name, t, shape in (("k_new", k_new, kv_shape), ("v_new", v_new, kv_shape), ("q", q, q_shape), ("q_out", q_out, q_shape)):
-        if t is not None and t.shape != shape:
-            raise ValueError("%s must be %s, got %s" % (name, shape, tuple(t.shape)))
-    k, v, qr = _rows(k_new, "k_new"), _rows(v_new, "v_new"), _rows(q, "q")
-    qkv = QKV(qr[0], k[0], v[0], qr[1], qr[2], k[1], k[2], v[1], v[2])
-    _check(_load().puzzle_kv_append_rope(ctypes.byref(desc), ctypes.byref(view), ctypes.byref(rope), ctypes.byref(qkv),
+    batch, n_new = shape[0], shape[1] if len(shape) == 4 else 1
+    lead = (batch, n_new) if len(shape) == 4 else (batch,)
+    kv_shape, q_shape = (*lead, desc.num_kv_heads, row), (*lead, desc.num_q_heads, row)
+    for name, t, want in (("k_new", k_new, kv_shape), ("v_new", v_new, kv_shape), ("q", q, q_shape), ("q_out", q_out, q_shape)):
+        if t is not None and t.shape != want:
+            raise ValueError("%s must be %s, got %s" % (name, want, tuple(t.shape)))
+    kp, ks, kt = _rows(k_new, "k_new", row)
+    vp, vs, vt = _rows(v_new, "v_new", row)
+    qp, qs, qt = _rows(q, "q", row) if q is not None else (None, 0, 0)
+    _check(_load().puzzle_kv_append_rope(ctypes.byref(desc), ctypes.byref(view), ctypes.byref(rope),
+                                         ctypes.byref(QKV(qp, kp, vp, qs, qt, ks, kt, vs, vt)),
                                          _p(q_out, torch.bfloat16, "q_out"), _p(new_lens, torch.int32, "new_lens"),
-                                         lead[0], lead[1] if len(lead) == 2 else 1, _p(dev_status, torch.int32),
-                                         _stream(stream)), "puzzle_kv_append_rope")
+                                         batch, n_new, _p(dev_status, torch.int32), _stream(stream, k_new)),
+           "puzzle_kv_append_rope")
 
 
 def puzzle_kv_read_tokens(desc: LayerDesc, view: KVView, k_out: torch.Tensor, v_out: torch.Tensor,
                           read_lens: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
                           stream=None) -> None:
     """k_out, v_out: bf16 [batch][n_read][Hkv][D]; read_lens: int32 [batch] or None (n_read tokens of every sequence)."""
-    for name, t in (("k_out", k_out), ("v_out", v_out)):
-        if t.dim() != 4 or t.shape[:2] != k_out.shape[:2] or tuple(t.shape[2:]) != (desc.num_kv_heads, desc.head_dim):
-            raise ValueError("%s must be [batch][n_read][%d][%d]" % (name, desc.num_kv_heads, desc.head_dim))
-    batch, n_read = k_out.shape[0], k_out.shape[1]
+    shape = k_out.shape
+    if len(shape) != 4 or shape[2] != desc.num_kv_heads or shape[3] != desc.head_dim or v_out.shape != shape:
+        raise ValueError("k_out and v_out must be [batch][n_read][%d][%d], got %s and %s"
+                         % (desc.num_kv_heads, desc.head_dim, tuple(shape), tuple(v_out.shape)))
+    batch, n_read = shape[0], shape[1]
     _check(_load().puzzle_kv_read_tokens(ctypes.byref(desc), ctypes.byref(view), _p(k_out, torch.bfloat16, "k_out"),
                                          _p(v_out, torch.bfloat16, "v_out"), _p(read_lens, torch.int32, "read_lens"),
-                                         batch, n_read, _p(dev_status, torch.int32), _stream(stream)),
+                                         batch, n_read, _p(dev_status, torch.int32), _stream(stream, k_out)),
            "puzzle_kv_read_tokens")
 
 
@@ -348,7 +357,8 @@ def puzzle_decode_attn_tokens(desc: LayerDesc, view: KVView, q: torch.Tensor, si
                                              _p(q_lens, torch.int32, "q_lens"), _p(sinks, torch.float32, "sinks"),
                                              _p(out, torch.bfloat16, "out"), _p(lse_out, torch.float32, "lse_out"),
                                              batch, n_q, _p(workspace), workspace.numel() * workspace.element_size(),
-                                             _p(dev_status, torch.int32), _stream(stream)), "puzzle_decode_attn_tokens")
+                                             _p(dev_status, torch.int32), _stream(stream, q)),
+           "puzzle_decode_attn_tokens")
 
 
 def puzzle_decode_attn_workspace_bytes(desc: LayerDesc, batch: int, num_splits: int = 0) -> int:
@@ -370,7 +380,7 @@ def _decode_attn(name: str, desc: LayerDesc, view: KVView, q, sinks, out, lse_ou
                                   _p(sinks, torch.float32, "sinks"), _p(out, torch.bfloat16, "out"),
                                   _p(lse_out, torch.float32, "lse_out"), batch, int(num_splits), _p(workspace),
                                   workspace.numel() * workspace.element_size(), _p(dev_status, torch.int32),
-                                  _stream(stream)), name)
+                                  _stream(stream, q)), name)
 
 
 def puzzle_decode_attn(desc: LayerDesc, view: KVView, q: torch.Tensor, sinks: Optional[torch.Tensor],

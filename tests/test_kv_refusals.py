@@ -106,3 +106,15 @@ def test_more_heads_than_a_grid_dimension_holds_are_refused(n_new):
     assert lib.puzzle_kv_append(desc, kv, 0x6000, 0x7000, 4, None, None) == UNSUPPORTED
     assert lib.puzzle_kv_append_tokens(desc, kv, 0x6000, 0x7000, None, 4, n_new, None, None) == UNSUPPORTED
     assert lib.puzzle_kv_read_tokens(desc, kv, 0x9000, 0xA000, None, 4, n_new, None, None) == UNSUPPORTED
+
+
+def test_binding_refuses_tensors_of_another_device(monkeypatch):
+    """A kernel is launched on the current device; the memory of another one is not its to read."""
+    from paper_2602_11937_b200 import binding as B
+
+    class Elsewhere:
+        def get_device(self):
+            return 1
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
+    with pytest.raises(ValueError, match="the tensors are on cuda:1, the current device is cuda:0"):
+        B._stream(None, Elsewhere())
