@@ -1,7 +1,10 @@
-"""ctypes binding of the C ABI: same entry-point names, argument marshalling only."""
+"""Binding of the C ABI: same entry-point names, argument marshalling only (ctypes; the entry points a decode step or a
+prompt chunk calls go through a small native module, csrc/call.cpp, because a microsecond of host time counts there)."""
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 from typing import Optional
 
@@ -9,7 +12,9 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "lib", "libpuzzle_attn.so")
+_CALL_PATH = os.path.join(_HERE, "lib", "_puzzle_call.so")
 _lib = None
+_call = None
 
 KV_FP8_E4M3 = 0
 KV_BF16 = 1
@@ -145,8 +150,36 @@ def _load():
         lib.puzzle_launch_count.argtypes = []
         lib.puzzle_decode_attn_kernel_name.restype = ctypes.c_char_p
         lib.puzzle_decode_attn_kernel_name.argtypes = [vp, vp, i32, i32]
+        _bind(lib)
         _lib = lib
     return _lib
+
+
+# The entry points of the native module, in the order of its Entries.
+_CALLS = ("puzzle_kv_append", "puzzle_kv_append_tokens", "puzzle_kv_append_rope", "puzzle_kv_read_tokens",
+          "puzzle_decode_attn", "puzzle_decode_attn_tcgen05", "puzzle_decode_attn_tokens")
+
+
+def _bind(lib):
+    """Loads the native module and gives it the addresses of the library's entry points."""
+    global _call
+    if _call is None:
+        if not os.path.exists(_CALL_PATH):
+            raise RuntimeError("%s is missing: build it with `python -m paper_2602_11937_b200.build`" % _CALL_PATH)
+        loader = importlib.machinery.ExtensionFileLoader("_puzzle_call", _CALL_PATH)
+        spec = importlib.util.spec_from_file_location("_puzzle_call", _CALL_PATH, loader=loader)
+        module = importlib.util.module_from_spec(spec)
+        loader.exec_module(module)
+    else:
+        module = _call
+    module.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _CALLS))
+    _call = module
+
+
+def _native():
+    if _lib is None:
+        _load()
+    return _call
 
 
 def _p(t: Optional[torch.Tensor], dtype=None, name="tensor"):
@@ -229,10 +262,7 @@ def _check(code: int, where: str):
 
 def puzzle_kv_append(desc: LayerDesc, view: KVView, k_new: torch.Tensor, v_new: torch.Tensor,
                      dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
-    batch = k_new.shape[0]
-    _check(_load().puzzle_kv_append(ctypes.byref(desc), ctypes.byref(view), _p(k_new, torch.bfloat16, "k_new"),
-                                    _p(v_new, torch.bfloat16, "v_new"), batch, _p(dev_status, torch.int32),
-                                    _stream(stream, k_new)), "puzzle_kv_append")
+    _check(_native().kv_append(desc, view, k_new, v_new, dev_status, stream), "puzzle_kv_append")
 
 
 def puzzle_kv_amax_update(x: torch.Tensor, amax: torch.Tensor, stream=None) -> None:
@@ -240,7 +270,7 @@ def puzzle_kv_amax_update(x: torch.Tensor, amax: torch.Tensor, stream=None) -> N
     hkv, d = x.shape[-2], x.shape[-1]
     n_tokens = x.numel() // (hkv * d) if x.numel() else 0
     _check(_load().puzzle_kv_amax_update(_p(x, torch.bfloat16, "x"), n_tokens, hkv, d, _p(amax, torch.float32, "amax"),
-                                         _stream(stream)), "puzzle_kv_amax_update")
+                                         _stream(stream, x)), "puzzle_kv_amax_update")
 
 
 def puzzle_kv_scales_from_amax(amax: torch.Tensor, scale_out: torch.Tensor, pow2: bool = False, stream=None) -> None:
@@ -264,11 +294,7 @@ def puzzle_kv_append_tokens(desc: LayerDesc, view: KVView, k_new: torch.Tensor, 
                             new_lens: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
                             stream=None) -> None:
     """k_new, v_new: bf16 [batch][n_new][Hkv][D]; new_lens: int32 [batch] or None (all n_new tokens are real)."""
-    batch, n_new = k_new.shape[0], k_new.shape[1]
-    _check(_load().puzzle_kv_append_tokens(ctypes.byref(desc), ctypes.byref(view), _p(k_new, torch.bfloat16, "k_new"),
-                                           _p(v_new, torch.bfloat16, "v_new"), _p(new_lens, torch.int32, "new_lens"),
-                                           batch, n_new, _p(dev_status, torch.int32), _stream(stream, k_new)),
-           "puzzle_kv_append_tokens")
+    _check(_native().kv_append_tokens(desc, view, k_new, v_new, new_lens, dev_status, stream), "puzzle_kv_append_tokens")
 
 
 def rope_view(cos_sin: torch.Tensor, interleaved: bool = False, pos_offset: Optional[torch.Tensor] = None) -> Rope:
@@ -282,40 +308,13 @@ def rope_view(cos_sin: torch.Tensor, interleaved: bool = False, pos_offset: Opti
     return r
 
 
-def _rows(t: torch.Tensor, name: str, row: int):
-    """Pointer, sequence stride and token stride of new tokens' rows [batch][n_new][heads][row] or [batch][heads][row]."""
-    if not t.is_cuda or t.dtype is not torch.bfloat16:
-        raise ValueError("%s must be a bf16 CUDA tensor" % name)
-    stride = t.stride()
-    if stride[-1] != 1 or (stride[-2] != row and t.shape[-2] > 1):
-        raise ValueError("the heads of a token of %s must be contiguous" % name)
-    return t.data_ptr(), stride[0], stride[1] if len(stride) == 4 else 0
-
-
 def puzzle_kv_append_rope(desc: LayerDesc, view: KVView, rope: Rope, q: Optional[torch.Tensor], k_new: torch.Tensor,
                           v_new: torch.Tensor, q_out: Optional[torch.Tensor] = None,
                           new_lens: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
                           stream=None) -> None:
     """q, k_new, v_new: bf16 [batch][n_new][heads][D] (or [batch][heads][D] for one token each), contiguous or slices
     of a wider array along the heads; q_out: bf16 [batch][n_new][Hq][D] contiguous, may be q; q None: k and v only."""
-    if (q is None) != (q_out is None):
-        raise ValueError("q and q_out go together")
-    row, shape = desc.head_dim, k_new.shape
-    if len(shape) not in (3, 4):
-        raise ValueError("k_new must be [batch][n_new][heads][D] or [batch][heads][D]")
-    batch, n_new = shape[0], shape[1] if len(shape) == 4 else 1
-    lead = (batch, n_new) if len(shape) == 4 else (batch,)
-    kv_shape, q_shape = (*lead, desc.num_kv_heads, row), (*lead, desc.num_q_heads, row)
-    for name, t, want in (("k_new", k_new, kv_shape), ("v_new", v_new, kv_shape), ("q", q, q_shape), ("q_out", q_out, q_shape)):
-        if t is not None and t.shape != want:
-            raise ValueError("%s must be %s, got %s" % (name, want, tuple(t.shape)))
-    kp, ks, kt = _rows(k_new, "k_new", row)
-    vp, vs, vt = _rows(v_new, "v_new", row)
-    qp, qs, qt = _rows(q, "q", row) if q is not None else (None, 0, 0)
-    _check(_load().puzzle_kv_append_rope(ctypes.byref(desc), ctypes.byref(view), ctypes.byref(rope),
-                                         ctypes.byref(QKV(qp, kp, vp, qs, qt, ks, kt, vs, vt)),
-                                         _p(q_out, torch.bfloat16, "q_out"), _p(new_lens, torch.int32, "new_lens"),
-                                         batch, n_new, _p(dev_status, torch.int32), _stream(stream, k_new)),
+    _check(_native().kv_append_rope(desc, view, rope, q, k_new, v_new, q_out, new_lens, dev_status, stream),
            "puzzle_kv_append_rope")
 
 
@@ -323,15 +322,7 @@ def puzzle_kv_read_tokens(desc: LayerDesc, view: KVView, k_out: torch.Tensor, v_
                           read_lens: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
                           stream=None) -> None:
     """k_out, v_out: bf16 [batch][n_read][Hkv][D]; read_lens: int32 [batch] or None (n_read tokens of every sequence)."""
-    shape = k_out.shape
-    if len(shape) != 4 or shape[2] != desc.num_kv_heads or shape[3] != desc.head_dim or v_out.shape != shape:
-        raise ValueError("k_out and v_out must be [batch][n_read][%d][%d], got %s and %s"
-                         % (desc.num_kv_heads, desc.head_dim, tuple(shape), tuple(v_out.shape)))
-    batch, n_read = shape[0], shape[1]
-    _check(_load().puzzle_kv_read_tokens(ctypes.byref(desc), ctypes.byref(view), _p(k_out, torch.bfloat16, "k_out"),
-                                         _p(v_out, torch.bfloat16, "v_out"), _p(read_lens, torch.int32, "read_lens"),
-                                         batch, n_read, _p(dev_status, torch.int32), _stream(stream, k_out)),
-           "puzzle_kv_read_tokens")
+    _check(_native().kv_read_tokens(desc, view, k_out, v_out, read_lens, dev_status, stream), "puzzle_kv_read_tokens")
 
 
 def puzzle_decode_attn_tokens_workspace_bytes(desc: LayerDesc, batch: int, n_q: int) -> int:
@@ -352,12 +343,7 @@ def puzzle_decode_attn_tokens(desc: LayerDesc, view: KVView, q: torch.Tensor, si
     """q, out: bf16 [batch][n_q][Hq][D]; q_lens: int32 [batch] or None; see include/puzzle_attn.h."""
     if workspace is None:
         raise ValueError("a workspace tensor is required (see puzzle_decode_attn_tokens_workspace_bytes)")
-    batch, n_q = q.shape[0], q.shape[1]
-    _check(_load().puzzle_decode_attn_tokens(ctypes.byref(desc), ctypes.byref(view), _p(q, torch.bfloat16, "q"),
-                                             _p(q_lens, torch.int32, "q_lens"), _p(sinks, torch.float32, "sinks"),
-                                             _p(out, torch.bfloat16, "out"), _p(lse_out, torch.float32, "lse_out"),
-                                             batch, n_q, _p(workspace), workspace.numel() * workspace.element_size(),
-                                             _p(dev_status, torch.int32), _stream(stream, q)),
+    _check(_native().decode_attn_tokens(desc, view, q, q_lens, sinks, out, lse_out, workspace, dev_status, stream),
            "puzzle_decode_attn_tokens")
 
 
@@ -371,23 +357,14 @@ def puzzle_decode_attn_workspace_init(desc: LayerDesc, batch: int, workspace: to
            "puzzle_decode_attn_workspace_init")
 
 
-def _decode_attn(name: str, desc: LayerDesc, view: KVView, q, sinks, out, lse_out, num_splits, workspace, dev_status,
-                 stream) -> None:
-    batch = q.shape[0]
-    if workspace is None:
-        raise ValueError("workspace is required (size it with puzzle_decode_attn_workspace_bytes)")
-    _check(getattr(_load(), name)(ctypes.byref(desc), ctypes.byref(view), _p(q, torch.bfloat16, "q"),
-                                  _p(sinks, torch.float32, "sinks"), _p(out, torch.bfloat16, "out"),
-                                  _p(lse_out, torch.float32, "lse_out"), batch, int(num_splits), _p(workspace),
-                                  workspace.numel() * workspace.element_size(), _p(dev_status, torch.int32),
-                                  _stream(stream, q)), name)
-
-
 def puzzle_decode_attn(desc: LayerDesc, view: KVView, q: torch.Tensor, sinks: Optional[torch.Tensor],
                        out: torch.Tensor, lse_out: Optional[torch.Tensor] = None, num_splits: int = 0,
                        workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
                        stream=None) -> None:
-    _decode_attn("puzzle_decode_attn", desc, view, q, sinks, out, lse_out, num_splits, workspace, dev_status, stream)
+    if workspace is None:
+        raise ValueError("workspace is required (size it with puzzle_decode_attn_workspace_bytes)")
+    _check(_native().decode_attn(desc, view, q, sinks, out, lse_out, num_splits, workspace, dev_status, stream),
+           "puzzle_decode_attn")
 
 
 def puzzle_decode_attn_tcgen05(desc: LayerDesc, view: KVView, q: torch.Tensor, sinks: Optional[torch.Tensor],
@@ -395,8 +372,10 @@ def puzzle_decode_attn_tcgen05(desc: LayerDesc, view: KVView, q: torch.Tensor, s
                                workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
                                stream=None) -> None:
     """puzzle_decode_attn computed by the tcgen05 / tensor-memory kernel (FP8 caches only)."""
-    _decode_attn("puzzle_decode_attn_tcgen05", desc, view, q, sinks, out, lse_out, num_splits, workspace, dev_status,
-                 stream)
+    if workspace is None:
+        raise ValueError("workspace is required (size it with puzzle_decode_attn_workspace_bytes)")
+    _check(_native().decode_attn_tcgen05(desc, view, q, sinks, out, lse_out, num_splits, workspace, dev_status, stream),
+           "puzzle_decode_attn_tcgen05")
 
 
 def puzzle_decode_attn_static(desc: LayerDesc, view: KVView, q: torch.Tensor, sinks: Optional[torch.Tensor],
@@ -408,7 +387,7 @@ def puzzle_decode_attn_static(desc: LayerDesc, view: KVView, q: torch.Tensor, si
     _check(_load().puzzle_decode_attn_static(ctypes.byref(desc), ctypes.byref(view), _p(q, torch.bfloat16, "q"),
                                              _p(sinks, torch.float32, "sinks"), _p(out, torch.bfloat16, "out"),
                                              _p(lse_out, torch.float32, "lse_out"), q.shape[0], int(num_splits),
-                                             _p(dev_status, torch.int32), _stream(stream)),
+                                             _p(dev_status, torch.int32), _stream(stream, q)),
            "puzzle_decode_attn_static")
 
 
@@ -434,7 +413,7 @@ def puzzle_decode_step_host(desc: LayerDesc, view: KVView, q_host: torch.Tensor,
                                            q_host.shape[0], int(num_splits), _p(staging),
                                            staging.numel() * staging.element_size(), _p(workspace),
                                            workspace.numel() * workspace.element_size(), _p(dev_status, torch.int32),
-                                           _stream(stream)), "puzzle_decode_step_host")
+                                           _stream(stream, workspace)), "puzzle_decode_step_host")
 
 
 def puzzle_decode_attn_partial(desc: LayerDesc, view: KVView, q: torch.Tensor, o_part: torch.Tensor,
@@ -447,7 +426,7 @@ def puzzle_decode_attn_partial(desc: LayerDesc, view: KVView, q: torch.Tensor, o
                                               _p(o_part, torch.float32, "o_part"),
                                               _p(lse_part, torch.float32, "lse_part"), q.shape[0], int(num_splits),
                                               _p(workspace), workspace.numel() * workspace.element_size(),
-                                              _p(dev_status, torch.int32), _stream(stream)),
+                                              _p(dev_status, torch.int32), _stream(stream, q)),
            "puzzle_decode_attn_partial")
 
 

@@ -1,18 +1,23 @@
-"""In-tree build of the CUDA library: nvcc for sm_100a, one shared object, no torch involved.
+"""In-tree build: the CUDA library (nvcc for sm_100a, one shared object, no torch involved) and the small Python module
+through which the binding calls its hot entry points (g++, torch's headers).
 
-``python -m paper_2602_11937_b200.build`` rebuilds when a source is newer than the library.
+``python -m paper_2602_11937_b200.build`` rebuilds when a source is newer than the library made from it.
 """
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIB_DIR, "libpuzzle_attn.so")
+CALL_SRC = os.path.join(CSRC, "call.cpp")
+CALL_LIB = os.path.join(LIB_DIR, "_puzzle_call.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
          "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
@@ -27,15 +32,35 @@ def _deps():
         glob.glob(os.path.join(HERE, "..", "include", "*.h")) + [os.path.abspath(__file__)]
 
 
+def _older(lib: str, deps) -> bool:
+    return not os.path.exists(lib) or any(os.path.getmtime(p) > os.path.getmtime(lib) for p in deps)
+
+
 def is_stale() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(p) > t for p in _deps())
+    return _older(LIB, _deps())
+
+
+def build_call(force: bool = False) -> str:
+    """Compile csrc/call.cpp into lib/_puzzle_call.so.  torch has to be imported before it."""
+    deps = [CALL_SRC, os.path.abspath(__file__)] + glob.glob(os.path.join(HERE, "..", "include", "*.h"))
+    if not force and not _older(CALL_LIB, deps):
+        return CALL_LIB
+    os.makedirs(LIB_DIR, exist_ok=True)
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    include = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include"),
+               os.path.join(HERE, "..", "include")]
+    tmp = CALL_LIB + ".tmp%d" % os.getpid()
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-w",
+                           *["-I" + i for i in include], CALL_SRC, "-o", tmp,
+                           "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+    os.replace(tmp, CALL_LIB)
+    return CALL_LIB
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ for sm_100a and link lib/libpuzzle_attn.so."""
+    """Compile every .cu under csrc/ for sm_100a, link lib/libpuzzle_attn.so, and build the Python module beside it."""
+    build_call(force)
     if not force and not is_stale():
         return LIB
     os.makedirs(LIB_DIR, exist_ok=True)

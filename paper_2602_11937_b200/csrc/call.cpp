@@ -1,0 +1,317 @@
+// The Python binding's way into the entry points that a decode step or a prompt chunk calls: tensors to pointers, sizes and
+// strides, checked, and the current stream.  A small call costs the GPU 2 to 6 us; the same marshalling through ctypes took
+// 4 to 5 us of host time beside the launch's own 3, this takes about half a microsecond.  The entry points themselves stay
+// plain C and know nothing of torch: this module is given their addresses.
+#include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAStream.h>
+
+#include <cstring>
+#include <string>
+
+#include "puzzle_attn.h"
+
+namespace {
+
+struct Entries {
+  decltype(&puzzle_kv_append) kv_append;
+  decltype(&puzzle_kv_append_tokens) kv_append_tokens;
+  decltype(&puzzle_kv_append_rope) kv_append_rope;
+  decltype(&puzzle_kv_read_tokens) kv_read_tokens;
+  decltype(&puzzle_decode_attn) decode_attn;
+  decltype(&puzzle_decode_attn_tcgen05) decode_attn_tcgen05;
+  decltype(&puzzle_decode_attn_tokens) decode_attn_tokens;
+} entry;
+constexpr Py_ssize_t kEntries = sizeof(Entries) / sizeof(void*);
+
+struct PythonError {};   // an exception is set
+
+[[noreturn]] void refuse(const std::string& what) {
+  PyErr_SetString(PyExc_ValueError, what.c_str());
+  throw PythonError();
+}
+
+const at::Tensor& tensor(PyObject* o, const char* name) {
+  if (!THPVariable_CheckExact(o) && !THPVariable_Check(o)) {
+    PyErr_Format(PyExc_TypeError, "%s must be a tensor, got %s", name, Py_TYPE(o)->tp_name);
+    throw PythonError();
+  }
+  return THPVariable_Unpack(o);
+}
+
+const char* type_name(at::ScalarType t) {
+  switch (t) {
+    case at::kBFloat16: return "torch.bfloat16";
+    case at::kFloat: return "torch.float32";
+    case at::kInt: return "torch.int32";
+    default: return c10::toString(t);
+  }
+}
+
+std::string shape_text(at::IntArrayRef s) {
+  std::string t = "(";
+  for (size_t i = 0; i < s.size(); ++i) t += (i ? ", " : "") + std::to_string(s[i]);
+  return t + (s.size() == 1 ? ",)" : ")");
+}
+
+// Device pointer of a contiguous CUDA tensor (None: NULL).
+void* pointer(PyObject* o, const char* name, at::ScalarType type) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o, name);
+  if (!t.is_cuda()) refuse(std::string(name) + " must be a CUDA tensor");
+  if (!t.is_contiguous()) refuse(std::string(name) + " must be contiguous");
+  if (type != at::kByte && t.scalar_type() != type)   // kByte: any type
+    refuse(std::string(name) + " must be " + type_name(type) + ", got " + type_name(t.scalar_type()));
+  return t.data_ptr();
+}
+template <typename T>
+T* pointer_to(PyObject* o, const char* name, at::ScalarType type) { return static_cast<T*>(pointer(o, name, type)); }
+
+// A ctypes structure's bytes.
+template <typename T>
+T structure(PyObject* o) {
+  Py_buffer b;
+  if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) throw PythonError();
+  T v;
+  const bool fits = b.len == (Py_ssize_t)sizeof(T);
+  if (fits) std::memcpy(&v, b.buf, sizeof(T));
+  PyBuffer_Release(&b);
+  if (!fits) refuse("a descriptor has the wrong size");
+  return v;
+}
+
+// The stream's handle (None: the current one).  Kernels are launched on the current device, so `t` has to lie there.
+void* stream_of(PyObject* stream, const at::Tensor& t) {
+  const int device = c10::cuda::current_device();
+  if (t.get_device() != device)
+    refuse("the tensors are on cuda:" + std::to_string(t.get_device()) + ", the current device is cuda:" +
+           std::to_string(device));
+  if (stream == Py_None) return c10::cuda::getCurrentCUDAStream(device).stream();
+  PyObject* h = PyObject_GetAttrString(stream, "cuda_stream");
+  if (!h) throw PythonError();
+  void* s = PyLong_AsVoidPtr(h);
+  Py_DECREF(h);
+  if (PyErr_Occurred()) throw PythonError();
+  return s;
+}
+
+int integer(PyObject* o) {
+  const long v = PyLong_AsLong(o);
+  if (v == -1 && PyErr_Occurred()) throw PythonError();
+  if (v < INT_MIN || v > INT_MAX) refuse("an integer argument does not fit 32 bits");
+  return (int)v;
+}
+
+// Batches and token counts are 32-bit in the C interface.
+int extent(const at::Tensor& t, int dim) {
+  const int64_t n = t.size(dim);
+  if (n > INT_MAX) refuse("a dimension does not fit 32 bits");
+  return (int)n;
+}
+
+template <typename F>
+PyObject* call(const char* name, Py_ssize_t given, Py_ssize_t wanted, F&& body) {
+  HANDLE_TH_ERRORS
+  if (given != wanted) {
+    PyErr_Format(PyExc_TypeError, "%s takes %zd arguments, got %zd", name, wanted, given);
+    return nullptr;
+  }
+  if (!entry.kv_append) {
+    PyErr_SetString(PyExc_RuntimeError, "the entry points have not been bound");
+    return nullptr;
+  }
+  try {
+    return PyLong_FromLong(body());
+  } catch (const PythonError&) {
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+// The C call itself, without Python's lock.
+template <typename F>
+int unlocked(F&& f) {
+  PyThreadState* ts = PyEval_SaveThread();
+  const int code = f();
+  PyEval_RestoreThread(ts);
+  return code;
+}
+
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != kEntries) {
+    PyErr_Format(PyExc_TypeError, "bind takes %zd addresses", kEntries);
+    return nullptr;
+  }
+  void* p[kEntries];
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  std::memcpy(&entry, p, sizeof entry);
+  Py_RETURN_NONE;
+}
+
+// desc, view, k_new, v_new, dev_status, stream
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call("kv_append", n, 6, [&] {
+    const auto desc = structure<puzzle_layer_desc>(a[0]);
+    const auto view = structure<puzzle_kv_view>(a[1]);
+    const at::Tensor& t = tensor(a[2], "k_new");
+    void* k = pointer(a[2], "k_new", at::kBFloat16);
+    void* v = pointer(a[3], "v_new", at::kBFloat16);
+    int32_t* status = pointer_to<int32_t>(a[4], "dev_status", at::kInt);
+    const int batch = extent(t, 0);
+    void* s = stream_of(a[5], t);
+    return unlocked([&] { return entry.kv_append(&desc, &view, k, v, batch, status, s); });
+  });
+}
+
+// desc, view, k_new, v_new, new_lens, dev_status, stream
+PyObject* kv_append_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call("kv_append_tokens", n, 7, [&] {
+    const auto desc = structure<puzzle_layer_desc>(a[0]);
+    const auto view = structure<puzzle_kv_view>(a[1]);
+    const at::Tensor& t = tensor(a[2], "k_new");
+    void* k = pointer(a[2], "k_new", at::kBFloat16);
+    void* v = pointer(a[3], "v_new", at::kBFloat16);
+    int32_t* lens = pointer_to<int32_t>(a[4], "new_lens", at::kInt);
+    int32_t* status = pointer_to<int32_t>(a[5], "dev_status", at::kInt);
+    const int batch = extent(t, 0), n_new = extent(t, 1);
+    void* s = stream_of(a[6], t);
+    return unlocked([&] { return entry.kv_append_tokens(&desc, &view, k, v, lens, batch, n_new, status, s); });
+  });
+}
+
+// Rows [batch][n_new][heads][D] or [batch][heads][D] of new tokens: every dimension as expected.
+void check_rows(const at::Tensor& t, const char* name, const at::Tensor& like, int heads, int row) {
+  const auto s = t.sizes(), l = like.sizes();
+  const size_t d = l.size();
+  if (s.size() == d && s[0] == l[0] && (d == 3 || s[1] == l[1]) && s[d - 2] == heads && s[d - 1] == row) return;
+  auto want = l.vec();
+  want[d - 2] = heads;
+  want[d - 1] = row;
+  refuse(std::string(name) + " must be " + shape_text(want) + ", got " + shape_text(s));
+}
+struct Rows {
+  void* p;
+  int64_t seq_stride, token_stride;
+};
+Rows rows(const at::Tensor& t, const char* name, int row) {
+  if (!t.is_cuda() || t.scalar_type() != at::kBFloat16) refuse(std::string(name) + " must be a bf16 CUDA tensor");
+  const auto st = t.strides();
+  const size_t d = st.size();
+  if (st[d - 1] != 1 || (st[d - 2] != row && t.size(d - 2) > 1))
+    refuse("the heads of a token of " + std::string(name) + " must be contiguous");
+  return {t.data_ptr(), st[0], d == 4 ? st[1] : 0};
+}
+
+// desc, view, rope, q, k_new, v_new, q_out, new_lens, dev_status, stream
+PyObject* kv_append_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call("kv_append_rope", n, 10, [&] {
+    const auto desc = structure<puzzle_layer_desc>(a[0]);
+    const auto view = structure<puzzle_kv_view>(a[1]);
+    const auto rope = structure<puzzle_rope>(a[2]);
+    const bool with_q = a[3] != Py_None;
+    if (with_q != (a[6] != Py_None)) refuse("q and q_out go together");
+    const at::Tensor &k = tensor(a[4], "k_new"), &v = tensor(a[5], "v_new");
+    if (k.dim() != 3 && k.dim() != 4) refuse("k_new must be [batch][n_new][heads][D] or [batch][heads][D]");
+    check_rows(k, "k_new", k, desc.num_kv_heads, desc.head_dim);
+    check_rows(v, "v_new", k, desc.num_kv_heads, desc.head_dim);
+    if (with_q) {
+      check_rows(tensor(a[3], "q"), "q", k, desc.num_q_heads, desc.head_dim);
+      check_rows(tensor(a[6], "q_out"), "q_out", k, desc.num_q_heads, desc.head_dim);
+    }
+    const Rows kr = rows(k, "k_new", desc.head_dim), vr = rows(v, "v_new", desc.head_dim);
+    const Rows qr = with_q ? rows(tensor(a[3], "q"), "q", desc.head_dim) : Rows{nullptr, 0, 0};
+    const puzzle_qkv qkv = {qr.p,          kr.p,            vr.p,          qr.seq_stride,  qr.token_stride,
+                            kr.seq_stride, kr.token_stride, vr.seq_stride, vr.token_stride};
+    void* q_out = pointer(a[6], "q_out", at::kBFloat16);
+    int32_t* lens = pointer_to<int32_t>(a[7], "new_lens", at::kInt);
+    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt);
+    const int batch = extent(k, 0), n_new = k.dim() == 4 ? extent(k, 1) : 1;
+    void* s = stream_of(a[9], k);
+    return unlocked([&] {
+      return entry.kv_append_rope(&desc, &view, &rope, &qkv, q_out, lens, batch, n_new, status, s);
+    });
+  });
+}
+
+// desc, view, k_out, v_out, read_lens, dev_status, stream
+PyObject* kv_read_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call("kv_read_tokens", n, 7, [&] {
+    const auto desc = structure<puzzle_layer_desc>(a[0]);
+    const auto view = structure<puzzle_kv_view>(a[1]);
+    const at::Tensor &k = tensor(a[2], "k_out"), &v = tensor(a[3], "v_out");
+    if (k.dim() != 4 || k.size(2) != desc.num_kv_heads || k.size(3) != desc.head_dim || v.sizes() != k.sizes())
+      refuse("k_out and v_out must be [batch][n_read][" + std::to_string(desc.num_kv_heads) + "][" +
+             std::to_string(desc.head_dim) + "], got " + shape_text(k.sizes()) + " and " + shape_text(v.sizes()));
+    void* kp = pointer(a[2], "k_out", at::kBFloat16);
+    void* vp = pointer(a[3], "v_out", at::kBFloat16);
+    int32_t* lens = pointer_to<int32_t>(a[4], "read_lens", at::kInt);
+    int32_t* status = pointer_to<int32_t>(a[5], "dev_status", at::kInt);
+    const int batch = extent(k, 0), n_read = extent(k, 1);
+    void* s = stream_of(a[6], k);
+    return unlocked([&] { return entry.kv_read_tokens(&desc, &view, kp, vp, lens, batch, n_read, status, s); });
+  });
+}
+
+// desc, view, q, sinks, out, lse_out, num_splits, workspace, dev_status, stream
+PyObject* decode(const char* name, decltype(&puzzle_decode_attn) f, PyObject* const* a, Py_ssize_t n) {
+  return call(name, n, 10, [&] {
+    const auto desc = structure<puzzle_layer_desc>(a[0]);
+    const auto view = structure<puzzle_kv_view>(a[1]);
+    const at::Tensor &t = tensor(a[2], "q"), &w = tensor(a[7], "workspace");
+    void* q = pointer(a[2], "q", at::kBFloat16);
+    const float* sinks = pointer_to<float>(a[3], "sinks", at::kFloat);
+    void* out = pointer(a[4], "out", at::kBFloat16);
+    float* lse = pointer_to<float>(a[5], "lse_out", at::kFloat);
+    const int splits = integer(a[6]);
+    void* workspace = pointer(a[7], "workspace", at::kByte);
+    const size_t bytes = w.nbytes();
+    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt);
+    const int batch = extent(t, 0);
+    void* s = stream_of(a[9], t);
+    return unlocked([&] { return f(&desc, &view, q, sinks, out, lse, batch, splits, workspace, bytes, status, s); });
+  });
+}
+PyObject* decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return decode("decode_attn", entry.decode_attn, a, n);
+}
+PyObject* decode_attn_tcgen05(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return decode("decode_attn_tcgen05", entry.decode_attn_tcgen05, a, n);
+}
+
+// desc, view, q, q_lens, sinks, out, lse_out, workspace, dev_status, stream
+PyObject* decode_attn_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call("decode_attn_tokens", n, 10, [&] {
+    const auto desc = structure<puzzle_layer_desc>(a[0]);
+    const auto view = structure<puzzle_kv_view>(a[1]);
+    const at::Tensor &t = tensor(a[2], "q"), &w = tensor(a[7], "workspace");
+    void* q = pointer(a[2], "q", at::kBFloat16);
+    const int32_t* lens = pointer_to<int32_t>(a[3], "q_lens", at::kInt);
+    const float* sinks = pointer_to<float>(a[4], "sinks", at::kFloat);
+    void* out = pointer(a[5], "out", at::kBFloat16);
+    float* lse = pointer_to<float>(a[6], "lse_out", at::kFloat);
+    void* workspace = pointer(a[7], "workspace", at::kByte);
+    const size_t bytes = w.nbytes();
+    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt);
+    const int batch = extent(t, 0), n_q = extent(t, 1);
+    void* s = stream_of(a[9], t);
+    return unlocked([&] {
+      return entry.decode_attn_tokens(&desc, &view, q, lens, sinks, out, lse, batch, n_q, workspace, bytes, status, s);
+    });
+  });
+}
+
+using Fast = PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t);
+#define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(static_cast<Fast>(name))), METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {METHOD(bind),           METHOD(kv_append),   METHOD(kv_append_tokens),    METHOD(kv_append_rope),
+                         METHOD(kv_read_tokens), METHOD(decode_attn), METHOD(decode_attn_tcgen05), METHOD(decode_attn_tokens),
+                         {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_puzzle_call", nullptr, -1, methods};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__puzzle_call() { return PyModule_Create(&module); }
