@@ -6,7 +6,7 @@
 // q to bf16 and k, v to the cache's type as in kv_append.cu.  Reading and writing every byte once is all there is to
 // do: a chunk is bound by HBM, a decode step by the chain of dependent loads (length -> table row, block -> store).
 // Measured: 16 x 2048 tokens with 64 query and 8 KV heads 103 us into a bf16 cache (6.6 TB/s of read and written bytes),
-// 108 E4M3 (6.0), 116 4-bit (5.4: sixteen-channel maxima, corrected quotients, byte-wide scale stores); one token for 16
+// 102 E4M3 (6.3), 111 4-bit (5.7: sixteen-channel maxima, corrected quotients, byte-wide scale stores); one token for 16
 // sequences 2.2 us, for 64 into the 4-bit cache 3.4.  Fewer heads per warp re-read the table's rows: 4 heads 5 % slower.
 //
 // Eight lanes hold a row, eight adjacent channels each: 16-byte loads, the rotation partner of the half-split form is
@@ -226,8 +226,10 @@ constexpr int kHeadsPerWarp = 8;
 
 }  // namespace
 
+// Four blocks of 64 registers per SM where the codes are computed (three of 80: 108.5 against 102.4 us into the E4M3 cache,
+// 116 against 111 into the 4-bit one); the bf16 copy has its loads in flight with three (103.5 against 104.7).
 template <int KV, int ROT>
-__global__ void __launch_bounds__(256) kv_append_chunk_kernel(const AppendParams P) {
+__global__ void __launch_bounds__(256, KV == PUZZLE_KV_BF16 ? 3 : 4) kv_append_chunk_kernel(const AppendParams P) {
   grid_dependency_wait();   // no early release, for the reason given in kv_append_kernel
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, o = lane & 7;
   const int b = blockIdx.z;
