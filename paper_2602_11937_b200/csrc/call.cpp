@@ -56,18 +56,30 @@ std::string shape_text(at::IntArrayRef s) {
   return t + (s.size() == 1 ? ",)" : ")");
 }
 
-// Device pointer of a contiguous CUDA tensor (None: NULL).
-void* pointer(PyObject* o, const char* name, at::ScalarType type) {
+// Device pointer of a contiguous CUDA tensor (None: NULL) of at least `need` elements: what the call reads or writes.
+void* pointer(PyObject* o, const char* name, at::ScalarType type, int64_t need) {
   if (o == Py_None) return nullptr;
   const at::Tensor& t = tensor(o, name);
   if (!t.is_cuda()) refuse(std::string(name) + " must be a CUDA tensor");
   if (!t.is_contiguous()) refuse(std::string(name) + " must be contiguous");
   if (type != at::kByte && t.scalar_type() != type)   // kByte: any type
     refuse(std::string(name) + " must be " + type_name(type) + ", got " + type_name(t.scalar_type()));
+  if (t.numel() < need)
+    refuse(std::string(name) + " has " + std::to_string(t.numel()) + " elements, the call needs " + std::to_string(need));
   return t.data_ptr();
 }
 template <typename T>
-T* pointer_to(PyObject* o, const char* name, at::ScalarType type) { return static_cast<T*>(pointer(o, name, type)); }
+T* pointer_to(PyObject* o, const char* name, at::ScalarType type, int64_t need) {
+  return static_cast<T*>(pointer(o, name, type, need));
+}
+// Elements of a token, for descriptors that the library takes; others need nothing here, because it refuses them itself with
+// a code that says why.
+bool taken(const puzzle_layer_desc& d) {
+  return d.num_kv_heads > 0 && d.head_dim == 64 && d.num_q_heads == 8 * (int64_t)d.num_kv_heads;
+}
+int64_t q_heads(const puzzle_layer_desc& d) { return taken(d) ? d.num_q_heads : 0; }
+int64_t q_row(const puzzle_layer_desc& d) { return q_heads(d) * d.head_dim; }
+int64_t kv_row(const puzzle_layer_desc& d) { return taken(d) ? (int64_t)d.num_kv_heads * d.head_dim : 0; }
 
 // A ctypes structure's bytes.
 template <typename T>
@@ -159,10 +171,10 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor& t = tensor(a[2], "k_new");
-    void* k = pointer(a[2], "k_new", at::kBFloat16);
-    void* v = pointer(a[3], "v_new", at::kBFloat16);
-    int32_t* status = pointer_to<int32_t>(a[4], "dev_status", at::kInt);
     const int batch = extent(t, 0);
+    void* k = pointer(a[2], "k_new", at::kBFloat16, batch * kv_row(desc));
+    void* v = pointer(a[3], "v_new", at::kBFloat16, batch * kv_row(desc));
+    int32_t* status = pointer_to<int32_t>(a[4], "dev_status", at::kInt, 1);
     void* s = stream_of(a[5], t);
     return unlocked([&] { return entry.kv_append(&desc, &view, k, v, batch, status, s); });
   });
@@ -174,11 +186,11 @@ PyObject* kv_append_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor& t = tensor(a[2], "k_new");
-    void* k = pointer(a[2], "k_new", at::kBFloat16);
-    void* v = pointer(a[3], "v_new", at::kBFloat16);
-    int32_t* lens = pointer_to<int32_t>(a[4], "new_lens", at::kInt);
-    int32_t* status = pointer_to<int32_t>(a[5], "dev_status", at::kInt);
     const int batch = extent(t, 0), n_new = extent(t, 1);
+    void* k = pointer(a[2], "k_new", at::kBFloat16, (int64_t)batch * n_new * kv_row(desc));
+    void* v = pointer(a[3], "v_new", at::kBFloat16, (int64_t)batch * n_new * kv_row(desc));
+    int32_t* lens = pointer_to<int32_t>(a[4], "new_lens", at::kInt, batch);
+    int32_t* status = pointer_to<int32_t>(a[5], "dev_status", at::kInt, 1);
     void* s = stream_of(a[6], t);
     return unlocked([&] { return entry.kv_append_tokens(&desc, &view, k, v, lens, batch, n_new, status, s); });
   });
@@ -227,10 +239,10 @@ PyObject* kv_append_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Rows qr = with_q ? rows(tensor(a[3], "q"), "q", desc.head_dim) : Rows{nullptr, 0, 0};
     const puzzle_qkv qkv = {qr.p,          kr.p,            vr.p,          qr.seq_stride,  qr.token_stride,
                             kr.seq_stride, kr.token_stride, vr.seq_stride, vr.token_stride};
-    void* q_out = pointer(a[6], "q_out", at::kBFloat16);
-    int32_t* lens = pointer_to<int32_t>(a[7], "new_lens", at::kInt);
-    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt);
     const int batch = extent(k, 0), n_new = k.dim() == 4 ? extent(k, 1) : 1;
+    void* q_out = pointer(a[6], "q_out", at::kBFloat16, 0);   // its shape has been checked
+    int32_t* lens = pointer_to<int32_t>(a[7], "new_lens", at::kInt, batch);
+    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt, 1);
     void* s = stream_of(a[9], k);
     return unlocked([&] {
       return entry.kv_append_rope(&desc, &view, &rope, &qkv, q_out, lens, batch, n_new, status, s);
@@ -247,11 +259,11 @@ PyObject* kv_read_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (k.dim() != 4 || k.size(2) != desc.num_kv_heads || k.size(3) != desc.head_dim || v.sizes() != k.sizes())
       refuse("k_out and v_out must be [batch][n_read][" + std::to_string(desc.num_kv_heads) + "][" +
              std::to_string(desc.head_dim) + "], got " + shape_text(k.sizes()) + " and " + shape_text(v.sizes()));
-    void* kp = pointer(a[2], "k_out", at::kBFloat16);
-    void* vp = pointer(a[3], "v_out", at::kBFloat16);
-    int32_t* lens = pointer_to<int32_t>(a[4], "read_lens", at::kInt);
-    int32_t* status = pointer_to<int32_t>(a[5], "dev_status", at::kInt);
     const int batch = extent(k, 0), n_read = extent(k, 1);
+    void* kp = pointer(a[2], "k_out", at::kBFloat16, 0);   // their shapes have been checked
+    void* vp = pointer(a[3], "v_out", at::kBFloat16, 0);
+    int32_t* lens = pointer_to<int32_t>(a[4], "read_lens", at::kInt, batch);
+    int32_t* status = pointer_to<int32_t>(a[5], "dev_status", at::kInt, 1);
     void* s = stream_of(a[6], k);
     return unlocked([&] { return entry.kv_read_tokens(&desc, &view, kp, vp, lens, batch, n_read, status, s); });
   });
@@ -263,15 +275,15 @@ PyObject* decode(const char* name, decltype(&puzzle_decode_attn) f, PyObject* co
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor &t = tensor(a[2], "q"), &w = tensor(a[7], "workspace");
-    void* q = pointer(a[2], "q", at::kBFloat16);
-    const float* sinks = pointer_to<float>(a[3], "sinks", at::kFloat);
-    void* out = pointer(a[4], "out", at::kBFloat16);
-    float* lse = pointer_to<float>(a[5], "lse_out", at::kFloat);
-    const int splits = integer(a[6]);
-    void* workspace = pointer(a[7], "workspace", at::kByte);
-    const size_t bytes = w.nbytes();
-    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt);
     const int batch = extent(t, 0);
+    void* q = pointer(a[2], "q", at::kBFloat16, batch * q_row(desc));
+    const float* sinks = pointer_to<float>(a[3], "sinks", at::kFloat, q_heads(desc));
+    void* out = pointer(a[4], "out", at::kBFloat16, batch * q_row(desc));
+    float* lse = pointer_to<float>(a[5], "lse_out", at::kFloat, batch * q_heads(desc));
+    const int splits = integer(a[6]);
+    void* workspace = pointer(a[7], "workspace", at::kByte, 0);   // the library checks its size
+    const size_t bytes = w.nbytes();
+    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt, 1);
     void* s = stream_of(a[9], t);
     return unlocked([&] { return f(&desc, &view, q, sinks, out, lse, batch, splits, workspace, bytes, status, s); });
   });
@@ -289,15 +301,16 @@ PyObject* decode_attn_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor &t = tensor(a[2], "q"), &w = tensor(a[7], "workspace");
-    void* q = pointer(a[2], "q", at::kBFloat16);
-    const int32_t* lens = pointer_to<int32_t>(a[3], "q_lens", at::kInt);
-    const float* sinks = pointer_to<float>(a[4], "sinks", at::kFloat);
-    void* out = pointer(a[5], "out", at::kBFloat16);
-    float* lse = pointer_to<float>(a[6], "lse_out", at::kFloat);
-    void* workspace = pointer(a[7], "workspace", at::kByte);
-    const size_t bytes = w.nbytes();
-    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt);
     const int batch = extent(t, 0), n_q = extent(t, 1);
+    const int64_t tokens = (int64_t)batch * n_q;
+    void* q = pointer(a[2], "q", at::kBFloat16, tokens * q_row(desc));
+    const int32_t* lens = pointer_to<int32_t>(a[3], "q_lens", at::kInt, batch);
+    const float* sinks = pointer_to<float>(a[4], "sinks", at::kFloat, q_heads(desc));
+    void* out = pointer(a[5], "out", at::kBFloat16, tokens * q_row(desc));
+    float* lse = pointer_to<float>(a[6], "lse_out", at::kFloat, tokens * q_heads(desc));
+    void* workspace = pointer(a[7], "workspace", at::kByte, 0);   // the library checks its size
+    const size_t bytes = w.nbytes();
+    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt, 1);
     void* s = stream_of(a[9], t);
     return unlocked([&] {
       return entry.decode_attn_tokens(&desc, &view, q, lens, sinks, out, lse, batch, n_q, workspace, bytes, status, s);

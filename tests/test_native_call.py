@@ -97,3 +97,36 @@ def test_tensors_that_the_calls_refuse():
         P.puzzle_kv_append(d, view, k, k, stream=object())
     torch.cuda.synchronize()
     assert int(cache.sum()) == 0
+
+
+@pytest.mark.gpu
+def test_tensors_too_small_for_the_call_are_refused():
+    """Nothing is launched: the kernels would read or write past their ends."""
+    import paper_2602_11937_b200 as P
+    z = lambda *shape, dtype=torch.bfloat16: torch.zeros(*shape, dtype=dtype, device="cuda")
+    d = P.layer_desc(kv_dtype=P.KV_FP4_E2M1)
+    cache, lens = z(4, 8, 576, dtype=torch.uint8), torch.ones(2, dtype=torch.int32, device="cuda")
+    view = P.kv_view(cache, cache.clone(), lens, max_blocks_per_seq=2)
+    q, k, f32, i32 = z(2, 64, 64), z(2, 8, 64), torch.float32, torch.int32
+    before = P.puzzle_launch_count()
+    ws = z(P.puzzle_decode_attn_workspace_bytes(d, 2), dtype=torch.uint8)
+    good = dict(q=q, sinks=z(64, dtype=f32), out=z(2, 64, 64), lse_out=z(2, 64, dtype=f32), workspace=ws,
+                dev_status=z(1, dtype=i32))
+    for name, t in dict(q=z(2, 63, 64), sinks=z(63, dtype=f32), out=z(1, 64, 64), lse_out=z(2, 63, dtype=f32),
+                        dev_status=z(0, dtype=i32)).items():
+        with pytest.raises(ValueError, match="%s has [0-9]+ elements, the call needs [0-9]+" % name):
+            P.puzzle_decode_attn(d, view, **{**good, name: t})
+    q3, ws3 = z(2, 3, 64, 64), z(P.puzzle_decode_attn_tokens_workspace_bytes(d, 2, 3), dtype=torch.uint8)
+    good = dict(q=q3, sinks=None, out=z(2, 3, 64, 64), lse_out=None, q_lens=lens, workspace=ws3)
+    for name, t in dict(out=z(2, 2, 64, 64), lse_out=z(2, 2, 64, dtype=f32), q_lens=z(1, dtype=i32)).items():
+        with pytest.raises(ValueError, match="%s has" % name):
+            P.puzzle_decode_attn_tokens(d, view, **{**good, name: t})
+    with pytest.raises(ValueError, match="v_new has 512 elements, the call needs 1024"):
+        P.puzzle_kv_append(d, view, k, k[:1])
+    with pytest.raises(ValueError, match="k_new has 1024 elements, the call needs 2048"):
+        P.puzzle_kv_append_tokens(d, view, k.view(2, 2, 4, 64), z(2, 2, 8, 64))
+    with pytest.raises(ValueError, match="new_lens has 1 elements"):
+        P.puzzle_kv_append_rope(d, view, P.rope_view(P.rope_table(8).cuda()), None, k, k, new_lens=lens[:1])
+    with pytest.raises(ValueError, match="read_lens has 1 elements"):
+        P.puzzle_kv_read_tokens(d, view, z(2, 1, 8, 64), z(2, 1, 8, 64), read_lens=lens[:1])
+    assert P.puzzle_launch_count() == before
