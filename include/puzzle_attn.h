@@ -282,6 +282,9 @@ PUZZLE_API puzzle_status puzzle_decode_attn_workspace_init(const puzzle_layer_de
  *     not overlap on the GPU.  Besides partials and counters it keeps the CTA speeds between calls:
  *     they change how the next launch is cut, never its result beyond rounding;
  *   dev_status: optional int32 device word (see PUZZLE_DEV_*).
+ * Softmax weights e^(s_j - M) of the numerator: FP8 and bf16 caches hold them in two 16-bit terms; the 4-bit cache in f16,
+ *     rounded once (2^-11 of a weight, 2^-37 of the largest one for those 2^-26 and more below it), which changes an output
+ *     by at most an eighth of its own rounding to bf16 where values do not cancel.  Z and lse: float32, every cache.
  * An empty context gives out = 0 and lse = sink (-inf without a sink). */
 PUZZLE_API puzzle_status puzzle_decode_attn(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const void* q,
                                  const float* sinks, void* out, float* lse_out, int32_t batch,

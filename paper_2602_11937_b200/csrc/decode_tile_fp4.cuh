@@ -9,10 +9,14 @@
 //    With 0.56 bytes per value the instruction stream, not HBM, is the nearer limit, so that is what the layout serves.
 //  * The softmax weights then have to change sides: a lane holds P[token g][heads 2c, 2c+1] and needs P[tokens 2c,
 //    2c+1][head g].  As packed f16 pairs that is one 8x8 transpose (movmatrix) per eight tokens.
-//  * P is rounded to f16 once (2^-11 relative, weights below 2^-14 of the reference maximum to 2^-25 absolute), an
-//    eighth of the bf16 output's own rounding and independent from key to key.  The sum takes the float32 weights.
-//  * The running maximum is only raised (a reduction over the lanes, accumulators rescaled) when some lane sees a logit
-//    more than 2^8 above it: one vote per tile otherwise.
+//  * P is rounded to f16 once: 2^-11 relative, an eighth of the bf16 output's own rounding and independent from key to
+//    key.  A second term for the remainder, as the other caches have it, is 16 more MMAs a tile and what feeds them: 112 to
+//    125 us at 16 x 64K, 152 to 190 for two tokens.  The sum takes the float32 weights, so the lse has their accuracy.
+//  * Weights are formed against a reference 2^12 below the largest one seen when it was set and reach 2^15 of it, so that
+//    f16's range lies where it is needed: weights down to 2^-26 of the largest keep all eleven bits, those below are off by
+//    2^-37 of the largest at most.  (With the reference at the maximum a long tail 2^-24 below one key was lost or off by a
+//    third.)  The reference is only raised (a reduction over the lanes, accumulators rescaled) when some lane sees a weight
+//    beyond 2^15: one vote per tile otherwise.
 //  * A block arrives as it lies in HBM; every shared-memory read of a tile (8 bytes per lane of K and
 //    V, 2 and 4 of the scales) is conflict free because the format's order is the fragments' order.
 #pragma once
@@ -151,6 +155,9 @@ __device__ __forceinline__ void fp4_v_fragments(uint32_t block, const Fp4Lanes& 
   }
 }
 
+constexpr float kFp4TopLog2 = 15.f;   // weights stay below 2^15 of the reference (f16 ends at 65504) ...
+constexpr float kFp4RefLog2 = 12.f;   // ... which is set 2^12 below the largest one seen
+
 // Running state of one warp over the tiles of one (sequence, KV head) for one query token: heads 2c and 2c + 1 are this
 // lane's columns.  O[i]: channels 8g + 2i (first two) and 8g + 2i + 1 (last two) of those heads.
 struct Fp4State {
@@ -200,16 +207,17 @@ struct Fp4State {
     alpha[0] = __shfl_sync(0xffffffffu, a, 8 * c);
     alpha[1] = __shfl_sync(0xffffffffu, a, 8 * c + 4);
   }
-  // Raises the reference maxima where a head's logits (mx: this lane's largest, code units) exceed them by 2^8.
+  // Raises the references where a head's logits (mx: this lane's largest, code units) exceed them by 2^kFp4TopLog2.
   __device__ __forceinline__ void raise(float (&mx)[2]) {
     const float t0 = mx[0] * alpha[0], t1 = mx[1] * alpha[1];
-    if (!__any_sync(0xffffffffu, t0 > m_ref[0] + kLazyLog2 || t1 > m_ref[1] + kLazyLog2)) return;
+    if (!__any_sync(0xffffffffu, t0 > m_ref[0] + kFp4TopLog2 || t1 > m_ref[1] + kFp4TopLog2)) return;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       float m = e ? t1 : t0;
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-      if (m > m_ref[e] + kLazyLog2) {
+      if (m > m_ref[e] + kFp4TopLog2) {
+        m -= kFp4RefLog2;
         const float corr = ex2(m_ref[e] - m);   // 0 on the first visible tile
         if (e) l_run.y *= corr; else l_run.x *= corr;
 #pragma unroll
@@ -218,12 +226,13 @@ struct Fp4State {
       }
     }
   }
-  // Weights of one block's logits s[4] (token g: heads 2c, 2c+1; token g + 8) as the B operand of O^T += V^T P^T.
-  __device__ __forceinline__ void weights(const float (&s)[4], float2 neg, uint32_t& b0, uint32_t& b1) {
+  // Weights of one block's logits s[4] (token g: heads 2c, 2c+1; token g + 8) as the B operand of O^T += V^T P^T.  They are
+  // added up over a tile's blocks before they join l_run, which rounds a long tail below one key a quarter as often.
+  __device__ __forceinline__ void weights(const float (&s)[4], float2 neg, bool first, float2& sum, uint32_t& b0, uint32_t& b1) {
     const float2 al = make_float2(alpha[0], alpha[1]);
     const float2 t0 = fma2(make_float2(s[0], s[1]), al, neg), t1 = fma2(make_float2(s[2], s[3]), al, neg);
     const float2 p0 = make_float2(ex2(t0.x), ex2(t0.y)), p1 = make_float2(ex2(t1.x), ex2(t1.y));
-    l_run = add2(l_run, add2(p0, p1));
+    sum = first ? add2(p0, p1) : add2(sum, add2(p0, p1));
     b0 = transpose8x8(f32x2_to_f16x2(p0.x, p0.y));
     b1 = transpose8x8(f32x2_to_f16x2(p1.x, p1.y));
   }
@@ -296,14 +305,16 @@ struct Fp4Tile {
     }
     st.raise(mx);
     const float2 neg = st.negated();
+    float2 sum;
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) {
       uint32_t b0, b1, a[4][4];
-      st.weights(s[blk], neg, b0, b1);
+      st.weights(s[blk], neg, blk == 0, sum, b0, b1);
       fp4_v_fragments<EDGE>(vbase + blk * kFp4BlockBytes, at, tok0 + kBlock * blk + 2 * c, lo, L, a);
 #pragma unroll
       for (int i = 0; i < 4; ++i) mma_f16(st.O[i], a[i][0], a[i][1], a[i][2], a[i][3], b0, b1);
     }
+    st.l_run = add2(st.l_run, sum);
   }
   // The state of head g on the four lanes of g, as the kernels combine and store it: lane c of the four gets channels
   // 16c + j in o[j][0] and 16c + 8 + j in o[j][1].

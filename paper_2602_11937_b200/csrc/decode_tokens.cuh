@@ -120,7 +120,7 @@ struct Fp4Pair {
           if (tk < lo || tk >= L) s[1][blk][2 * e] = s[1][blk][2 * e + 1] = -INFINITY;
         }
     }
-    float2 neg[2];
+    float2 neg[2], sum[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       float mx[2] = {-INFINITY, -INFINITY};
@@ -136,13 +136,15 @@ struct Fp4Pair {
     for (int blk = 0; blk < NB; ++blk) {
       uint32_t b[2][2], a[4][4];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) st.t[t].weights(s[t][blk], neg[t], b[t][0], b[t][1]);
+      for (int t = 0; t < 2; ++t) st.t[t].weights(s[t][blk], neg[t], blk == 0, sum[t], b[t][0], b[t][1]);
       fp4_v_fragments<EDGE>(vbase + blk * kFp4BlockBytes, at, tok0 + kBlock * blk + 2 * c, loA, L, a);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int t = 0; t < 2; ++t) mma_f16(st.t[t].O[i], a[i][0], a[i][1], a[i][2], a[i][3], b[t][0], b[t][1]);
     }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) st.t[t].l_run = add2(st.t[t].l_run, sum[t]);
   }
   static __device__ __forceinline__ void finish(const State& st, int tok, float& m, float& l, float (&o)[8][2], int lane) {
     Fp4Tile::finish(st.t[tok], m, l, o, lane);
