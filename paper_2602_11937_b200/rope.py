@@ -18,11 +18,12 @@ def rope_table(num_positions: int, rotary_dim: int = 64, theta: float = 10000.0,
     divided by the factor, those between are blended linearly in i, and cosines and sines carry the factor
     0.1 ln(factor) + 1.  The two ends of the blend are rounded outwards to whole i (truncate=True, the method's first
     implementation and most models since) or taken as they are (truncate=False: the gpt-oss family, with theta 150000,
-    factor 32 and 4096 original positions); a model needs the table it was trained with, the two differ by up to 76 % there.  Angles are formed in 64 bits: at position 100000 a float32 angle is off by up to 4e-3."""
+    factor 32 and 4096 original positions); a model needs the table it was trained with, the two differ by up to 76 %
+    there.  Angles are formed in 64 bits: at position 100000 a float32 angle is off by up to 4e-3."""
     if rotary_dim <= 0 or rotary_dim % 2 or num_positions < 1 or factor < 1.0:
         raise ValueError("rotary_dim must be even and positive, num_positions at least 1, factor at least 1")
-    if factor > 1.0 and (theta <= 1.0 or original_positions < 1 or not 0.0 < beta_slow < beta_fast):
-        raise ValueError("a stretched table needs theta above 1, original_positions at least 1 and 0 < beta_slow < beta_fast")
+    if factor > 1.0 and (theta <= 1.0 or original_positions < 1 or not 0.0 < beta_slow <= beta_fast):
+        raise ValueError("a stretched table needs theta above 1, original_positions at least 1 and 0 < beta_slow <= beta_fast")
     i = torch.arange(rotary_dim // 2, dtype=torch.float64, device=device)
     freq = theta ** (-2.0 * i / rotary_dim)
     gain = 1.0
