@@ -56,11 +56,27 @@ std::string shape_text(at::IntArrayRef s) {
   return t + (s.size() == 1 ? ",)" : ")");
 }
 
+// Kernels are launched on the current device, so everything they are given has to lie there.
+void check_place(const char* name, int64_t device, int64_t current) {
+  if (device != current)
+    refuse(std::string(name) + " is on cuda:" + std::to_string(device) + ", the current device is cuda:" + std::to_string(current));
+}
+// The current device, asked for once in a call (a call whose arguments are no CUDA tensors never asks).
+struct Here {
+  int device = -1;
+  int get() {
+    if (device < 0) device = c10::cuda::current_device();
+    return device;
+  }
+  void check(const char* name, const at::Tensor& t) { check_place(name, t.get_device(), get()); }
+};
+
 // Device pointer of a contiguous CUDA tensor (None: NULL) of at least `need` elements: what the call reads or writes.
-void* pointer(PyObject* o, const char* name, at::ScalarType type, int64_t need) {
+void* pointer(Here& here, PyObject* o, const char* name, at::ScalarType type, int64_t need) {
   if (o == Py_None) return nullptr;
   const at::Tensor& t = tensor(o, name);
   if (!t.is_cuda()) refuse(std::string(name) + " must be a CUDA tensor");
+  here.check(name, t);
   if (!t.is_contiguous()) refuse(std::string(name) + " must be contiguous");
   if (type != at::kByte && t.scalar_type() != type)   // kByte: any type
     refuse(std::string(name) + " must be " + type_name(type) + ", got " + type_name(t.scalar_type()));
@@ -69,8 +85,8 @@ void* pointer(PyObject* o, const char* name, at::ScalarType type, int64_t need) 
   return t.data_ptr();
 }
 template <typename T>
-T* pointer_to(PyObject* o, const char* name, at::ScalarType type, int64_t need) {
-  return static_cast<T*>(pointer(o, name, type, need));
+T* pointer_to(Here& here, PyObject* o, const char* name, at::ScalarType type, int64_t need) {
+  return static_cast<T*>(pointer(here, o, name, type, need));
 }
 // Elements of a token, for descriptors that the library takes; others need nothing here, because it refuses them itself with
 // a code that says why.
@@ -94,13 +110,9 @@ T structure(PyObject* o) {
   return v;
 }
 
-// The stream's handle (None: the current one).  Kernels are launched on the current device, so `t` has to lie there.
-void* stream_of(PyObject* stream, const at::Tensor& t) {
-  const int device = c10::cuda::current_device();
-  if (t.get_device() != device)
-    refuse("the tensors are on cuda:" + std::to_string(t.get_device()) + ", the current device is cuda:" +
-           std::to_string(device));
-  if (stream == Py_None) return c10::cuda::getCurrentCUDAStream(device).stream();
+// The stream's handle (None: the current one).
+void* stream_of(Here& here, PyObject* stream) {
+  if (stream == Py_None) return c10::cuda::getCurrentCUDAStream(here.get()).stream();
   PyObject* h = PyObject_GetAttrString(stream, "cuda_stream");
   if (!h) throw PythonError();
   void* s = PyLong_AsVoidPtr(h);
@@ -135,7 +147,8 @@ PyObject* call(const char* name, Py_ssize_t given, Py_ssize_t wanted, F&& body) 
     return nullptr;
   }
   try {
-    return PyLong_FromLong(body());
+    Here here;
+    return PyLong_FromLong(body(here));
   } catch (const PythonError&) {
     return nullptr;
   }
@@ -167,31 +180,31 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // desc, view, k_new, v_new, dev_status, stream
 PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return call("kv_append", n, 6, [&] {
+  return call("kv_append", n, 6, [&](Here& here) {
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor& t = tensor(a[2], "k_new");
     const int batch = extent(t, 0);
-    void* k = pointer(a[2], "k_new", at::kBFloat16, batch * kv_row(desc));
-    void* v = pointer(a[3], "v_new", at::kBFloat16, batch * kv_row(desc));
-    int32_t* status = pointer_to<int32_t>(a[4], "dev_status", at::kInt, 1);
-    void* s = stream_of(a[5], t);
+    void* k = pointer(here, a[2], "k_new", at::kBFloat16, batch * kv_row(desc));
+    void* v = pointer(here, a[3], "v_new", at::kBFloat16, batch * kv_row(desc));
+    int32_t* status = pointer_to<int32_t>(here, a[4], "dev_status", at::kInt, 1);
+    void* s = stream_of(here, a[5]);
     return unlocked([&] { return entry.kv_append(&desc, &view, k, v, batch, status, s); });
   });
 }
 
 // desc, view, k_new, v_new, new_lens, dev_status, stream
 PyObject* kv_append_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return call("kv_append_tokens", n, 7, [&] {
+  return call("kv_append_tokens", n, 7, [&](Here& here) {
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor& t = tensor(a[2], "k_new");
     const int batch = extent(t, 0), n_new = extent(t, 1);
-    void* k = pointer(a[2], "k_new", at::kBFloat16, (int64_t)batch * n_new * kv_row(desc));
-    void* v = pointer(a[3], "v_new", at::kBFloat16, (int64_t)batch * n_new * kv_row(desc));
-    int32_t* lens = pointer_to<int32_t>(a[4], "new_lens", at::kInt, batch);
-    int32_t* status = pointer_to<int32_t>(a[5], "dev_status", at::kInt, 1);
-    void* s = stream_of(a[6], t);
+    void* k = pointer(here, a[2], "k_new", at::kBFloat16, (int64_t)batch * n_new * kv_row(desc));
+    void* v = pointer(here, a[3], "v_new", at::kBFloat16, (int64_t)batch * n_new * kv_row(desc));
+    int32_t* lens = pointer_to<int32_t>(here, a[4], "new_lens", at::kInt, batch);
+    int32_t* status = pointer_to<int32_t>(here, a[5], "dev_status", at::kInt, 1);
+    void* s = stream_of(here, a[6]);
     return unlocked([&] { return entry.kv_append_tokens(&desc, &view, k, v, lens, batch, n_new, status, s); });
   });
 }
@@ -210,8 +223,9 @@ struct Rows {
   void* p;
   int64_t seq_stride, token_stride;
 };
-Rows rows(const at::Tensor& t, const char* name, int row) {
+Rows rows(Here& here, const at::Tensor& t, const char* name, int row) {
   if (!t.is_cuda() || t.scalar_type() != at::kBFloat16) refuse(std::string(name) + " must be a bf16 CUDA tensor");
+  here.check(name, t);
   const auto st = t.strides();
   const size_t d = st.size();
   if (st[d - 1] != 1 || (st[d - 2] != row && t.size(d - 2) > 1))
@@ -221,7 +235,7 @@ Rows rows(const at::Tensor& t, const char* name, int row) {
 
 // desc, view, rope, q, k_new, v_new, q_out, new_lens, dev_status, stream
 PyObject* kv_append_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return call("kv_append_rope", n, 10, [&] {
+  return call("kv_append_rope", n, 10, [&](Here& here) {
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     const auto rope = structure<puzzle_rope>(a[2]);
@@ -235,15 +249,15 @@ PyObject* kv_append_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
       check_rows(tensor(a[3], "q"), "q", k, desc.num_q_heads, desc.head_dim);
       check_rows(tensor(a[6], "q_out"), "q_out", k, desc.num_q_heads, desc.head_dim);
     }
-    const Rows kr = rows(k, "k_new", desc.head_dim), vr = rows(v, "v_new", desc.head_dim);
-    const Rows qr = with_q ? rows(tensor(a[3], "q"), "q", desc.head_dim) : Rows{nullptr, 0, 0};
+    const Rows kr = rows(here, k, "k_new", desc.head_dim), vr = rows(here, v, "v_new", desc.head_dim);
+    const Rows qr = with_q ? rows(here, tensor(a[3], "q"), "q", desc.head_dim) : Rows{nullptr, 0, 0};
     const puzzle_qkv qkv = {qr.p,          kr.p,            vr.p,          qr.seq_stride,  qr.token_stride,
                             kr.seq_stride, kr.token_stride, vr.seq_stride, vr.token_stride};
     const int batch = extent(k, 0), n_new = k.dim() == 4 ? extent(k, 1) : 1;
-    void* q_out = pointer(a[6], "q_out", at::kBFloat16, 0);   // its shape has been checked
-    int32_t* lens = pointer_to<int32_t>(a[7], "new_lens", at::kInt, batch);
-    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt, 1);
-    void* s = stream_of(a[9], k);
+    void* q_out = pointer(here, a[6], "q_out", at::kBFloat16, 0);   // its shape has been checked
+    int32_t* lens = pointer_to<int32_t>(here, a[7], "new_lens", at::kInt, batch);
+    int32_t* status = pointer_to<int32_t>(here, a[8], "dev_status", at::kInt, 1);
+    void* s = stream_of(here, a[9]);
     return unlocked([&] {
       return entry.kv_append_rope(&desc, &view, &rope, &qkv, q_out, lens, batch, n_new, status, s);
     });
@@ -252,7 +266,7 @@ PyObject* kv_append_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // desc, view, k_out, v_out, read_lens, dev_status, stream
 PyObject* kv_read_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return call("kv_read_tokens", n, 7, [&] {
+  return call("kv_read_tokens", n, 7, [&](Here& here) {
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor &k = tensor(a[2], "k_out"), &v = tensor(a[3], "v_out");
@@ -260,31 +274,31 @@ PyObject* kv_read_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
       refuse("k_out and v_out must be [batch][n_read][" + std::to_string(desc.num_kv_heads) + "][" +
              std::to_string(desc.head_dim) + "], got " + shape_text(k.sizes()) + " and " + shape_text(v.sizes()));
     const int batch = extent(k, 0), n_read = extent(k, 1);
-    void* kp = pointer(a[2], "k_out", at::kBFloat16, 0);   // their shapes have been checked
-    void* vp = pointer(a[3], "v_out", at::kBFloat16, 0);
-    int32_t* lens = pointer_to<int32_t>(a[4], "read_lens", at::kInt, batch);
-    int32_t* status = pointer_to<int32_t>(a[5], "dev_status", at::kInt, 1);
-    void* s = stream_of(a[6], k);
+    void* kp = pointer(here, a[2], "k_out", at::kBFloat16, 0);   // their shapes have been checked
+    void* vp = pointer(here, a[3], "v_out", at::kBFloat16, 0);
+    int32_t* lens = pointer_to<int32_t>(here, a[4], "read_lens", at::kInt, batch);
+    int32_t* status = pointer_to<int32_t>(here, a[5], "dev_status", at::kInt, 1);
+    void* s = stream_of(here, a[6]);
     return unlocked([&] { return entry.kv_read_tokens(&desc, &view, kp, vp, lens, batch, n_read, status, s); });
   });
 }
 
 // desc, view, q, sinks, out, lse_out, num_splits, workspace, dev_status, stream
 PyObject* decode(const char* name, decltype(&puzzle_decode_attn) f, PyObject* const* a, Py_ssize_t n) {
-  return call(name, n, 10, [&] {
+  return call(name, n, 10, [&](Here& here) {
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor &t = tensor(a[2], "q"), &w = tensor(a[7], "workspace");
     const int batch = extent(t, 0);
-    void* q = pointer(a[2], "q", at::kBFloat16, batch * q_row(desc));
-    const float* sinks = pointer_to<float>(a[3], "sinks", at::kFloat, q_heads(desc));
-    void* out = pointer(a[4], "out", at::kBFloat16, batch * q_row(desc));
-    float* lse = pointer_to<float>(a[5], "lse_out", at::kFloat, batch * q_heads(desc));
+    void* q = pointer(here, a[2], "q", at::kBFloat16, batch * q_row(desc));
+    const float* sinks = pointer_to<float>(here, a[3], "sinks", at::kFloat, q_heads(desc));
+    void* out = pointer(here, a[4], "out", at::kBFloat16, batch * q_row(desc));
+    float* lse = pointer_to<float>(here, a[5], "lse_out", at::kFloat, batch * q_heads(desc));
     const int splits = integer(a[6]);
-    void* workspace = pointer(a[7], "workspace", at::kByte, 0);   // the library checks its size
+    void* workspace = pointer(here, a[7], "workspace", at::kByte, 0);   // the library checks its size
     const size_t bytes = w.nbytes();
-    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt, 1);
-    void* s = stream_of(a[9], t);
+    int32_t* status = pointer_to<int32_t>(here, a[8], "dev_status", at::kInt, 1);
+    void* s = stream_of(here, a[9]);
     return unlocked([&] { return f(&desc, &view, q, sinks, out, lse, batch, splits, workspace, bytes, status, s); });
   });
 }
@@ -297,24 +311,34 @@ PyObject* decode_attn_tcgen05(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // desc, view, q, q_lens, sinks, out, lse_out, workspace, dev_status, stream
 PyObject* decode_attn_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return call("decode_attn_tokens", n, 10, [&] {
+  return call("decode_attn_tokens", n, 10, [&](Here& here) {
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor &t = tensor(a[2], "q"), &w = tensor(a[7], "workspace");
     const int batch = extent(t, 0), n_q = extent(t, 1);
     const int64_t tokens = (int64_t)batch * n_q;
-    void* q = pointer(a[2], "q", at::kBFloat16, tokens * q_row(desc));
-    const int32_t* lens = pointer_to<int32_t>(a[3], "q_lens", at::kInt, batch);
-    const float* sinks = pointer_to<float>(a[4], "sinks", at::kFloat, q_heads(desc));
-    void* out = pointer(a[5], "out", at::kBFloat16, tokens * q_row(desc));
-    float* lse = pointer_to<float>(a[6], "lse_out", at::kFloat, tokens * q_heads(desc));
-    void* workspace = pointer(a[7], "workspace", at::kByte, 0);   // the library checks its size
+    void* q = pointer(here, a[2], "q", at::kBFloat16, tokens * q_row(desc));
+    const int32_t* lens = pointer_to<int32_t>(here, a[3], "q_lens", at::kInt, batch);
+    const float* sinks = pointer_to<float>(here, a[4], "sinks", at::kFloat, q_heads(desc));
+    void* out = pointer(here, a[5], "out", at::kBFloat16, tokens * q_row(desc));
+    float* lse = pointer_to<float>(here, a[6], "lse_out", at::kFloat, tokens * q_heads(desc));
+    void* workspace = pointer(here, a[7], "workspace", at::kByte, 0);   // the library checks its size
     const size_t bytes = w.nbytes();
-    int32_t* status = pointer_to<int32_t>(a[8], "dev_status", at::kInt, 1);
-    void* s = stream_of(a[9], t);
+    int32_t* status = pointer_to<int32_t>(here, a[8], "dev_status", at::kInt, 1);
+    void* s = stream_of(here, a[9]);
     return unlocked([&] {
       return entry.decode_attn_tokens(&desc, &view, q, lens, sinks, out, lse, batch, n_q, workspace, bytes, status, s);
     });
+  });
+}
+
+// name, device of a tensor, current device: the check every tensor of every call goes through, for tests without two GPUs.
+PyObject* check_device(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call("check_device", n, 3, [&](Here&) {
+    const char* name = PyUnicode_AsUTF8(a[0]);
+    if (!name) throw PythonError();
+    check_place(name, integer(a[1]), integer(a[2]));
+    return 0;
   });
 }
 
@@ -322,6 +346,7 @@ using Fast = PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t);
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(static_cast<Fast>(name))), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind),           METHOD(kv_append),   METHOD(kv_append_tokens),    METHOD(kv_append_rope),
                          METHOD(kv_read_tokens), METHOD(decode_attn), METHOD(decode_attn_tcgen05), METHOD(decode_attn_tokens),
+                         METHOD(check_device),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_puzzle_call", nullptr, -1, methods};
 
