@@ -70,11 +70,14 @@ class KVView(ctypes.Structure):
     _fields_ = [("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p), ("num_blocks", ctypes.c_int64),
                 ("block_table", ctypes.c_void_p), ("max_blocks_per_seq", ctypes.c_int32),
                 ("seq_lens", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+    # What the tensors behind the pointers hold, noted by kv_view: device, sequences, scales, bytes of the smaller cache.
+    _held = None
 
 
 class Rope(ctypes.Structure):
     _fields_ = [("cos_sin", ctypes.c_void_p), ("num_positions", ctypes.c_int64), ("rotary_dim", ctypes.c_int32),
                 ("interleaved", ctypes.c_int32), ("pos_offset", ctypes.c_void_p)]
+    _held = None    # noted by rope_view: device, sequences that have an offset
 
 
 class QKV(ctypes.Structure):
@@ -195,6 +198,16 @@ def _p(t: Optional[torch.Tensor], dtype=None, name="tensor"):
     return t.data_ptr()
 
 
+_ANY = 1 << 62    # as many as a call may want
+
+
+def _device_of(what: str, *tensors) -> int:
+    devices = {t.get_device() for t in tensors if t is not None and t.is_cuda}
+    if len(devices) > 1:
+        raise ValueError("the tensors of %s lie on several devices" % what)
+    return devices.pop() if devices else -1
+
+
 # The current stream's handle without a Stream object around it: a decode step's call is a few microseconds of host time.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
@@ -239,6 +252,9 @@ def kv_view(k_cache: torch.Tensor, v_cache: torch.Tensor, seq_lens: torch.Tensor
     v.seq_lens = _p(seq_lens, torch.int32, "seq_lens")
     v.k_scale = _p(k_scale, torch.float32, "k_scale")
     v.v_scale = _p(v_scale, torch.float32, "v_scale")
+    v._held = (_device_of("a cache view", k_cache, v_cache, seq_lens, block_table, k_scale, v_scale),
+               min(seq_lens.numel(), _ANY if block_table is None else block_table.shape[0]),
+               min(_ANY if t is None else t.numel() for t in (k_scale, v_scale)), min(k_cache.nbytes, v_cache.nbytes))
     return v
 
 
@@ -305,6 +321,7 @@ def rope_view(cos_sin: torch.Tensor, interleaved: bool = False, pos_offset: Opti
     r.num_positions, r.rotary_dim = cos_sin.shape
     r.interleaved = int(bool(interleaved))
     r.pos_offset = _p(pos_offset, torch.int32, "pos_offset")
+    r._held = (_device_of("a rotation", cos_sin, pos_offset), _ANY if pos_offset is None else pos_offset.numel())
     return r
 
 

@@ -71,13 +71,17 @@ struct Here {
   void check(const char* name, const at::Tensor& t) { check_place(name, t.get_device(), get()); }
 };
 
+void check_contiguous(const char* name, const at::Tensor& t) {
+  if (!t.is_contiguous()) refuse(std::string(name) + " must be contiguous");
+}
+
 // Device pointer of a contiguous CUDA tensor (None: NULL) of at least `need` elements: what the call reads or writes.
 void* pointer(Here& here, PyObject* o, const char* name, at::ScalarType type, int64_t need) {
   if (o == Py_None) return nullptr;
   const at::Tensor& t = tensor(o, name);
   if (!t.is_cuda()) refuse(std::string(name) + " must be a CUDA tensor");
   here.check(name, t);
-  if (!t.is_contiguous()) refuse(std::string(name) + " must be contiguous");
+  check_contiguous(name, t);
   if (type != at::kByte && t.scalar_type() != type)   // kByte: any type
     refuse(std::string(name) + " must be " + type_name(type) + ", got " + type_name(t.scalar_type()));
   if (t.numel() < need)
@@ -108,6 +112,48 @@ T structure(PyObject* o) {
   PyBuffer_Release(&b);
   if (!fits) refuse("a descriptor has the wrong size");
   return v;
+}
+
+// The numbers that the binding notes on a descriptor it made from tensors (attribute _held: a tuple, or None on a descriptor
+// that was filled in by hand): what the tensors hold, which the pointers in the structure do not say.
+template <size_t N>
+bool held(PyObject* o, int64_t (&v)[N]) {
+  static PyObject* const name = PyUnicode_InternFromString("_held");
+  PyObject* t = PyObject_GetAttr(o, name);
+  if (!t) {
+    PyErr_Clear();
+    return false;
+  }
+  bool known = PyTuple_Check(t) && PyTuple_GET_SIZE(t) == (Py_ssize_t)N;
+  for (size_t i = 0; known && i < N; ++i) v[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
+  Py_DECREF(t);
+  if (PyErr_Occurred()) throw PythonError();
+  return known;
+}
+
+int64_t block_bytes(const puzzle_layer_desc& d) {   // of one (block, KV head), K or V
+  return d.kv_dtype == PUZZLE_KV_FP4_E2M1 ? PUZZLE_FP4_BLOCK_BYTES : d.kv_dtype == PUZZLE_KV_BF16 ? 16 * 64 * 2 : 16 * 64;
+}
+// Whether what a view points to has room for this descriptor and this many sequences.
+void check_view(Here& here, PyObject* view, const puzzle_layer_desc& d, const puzzle_kv_view& v, int batch) {
+  int64_t h[4];   // device, sequences, scales, bytes of the smaller cache
+  if (!held(view, h)) return;
+  if (h[1] < batch)
+    refuse("the cache view has " + std::to_string(h[1]) + " sequences, the call needs " + std::to_string(batch));
+  if (taken(d) && h[2] < d.num_kv_heads && d.kv_dtype != PUZZLE_KV_BF16)
+    refuse("the cache view has " + std::to_string(h[2]) + " scales, the call needs " + std::to_string(d.num_kv_heads));
+  const int64_t need = taken(d) ? v.num_blocks * d.num_kv_heads * block_bytes(d) : 0;
+  if (h[3] < need)
+    refuse("the cache has " + std::to_string(h[3]) + " bytes, the descriptor's " + std::to_string(v.num_blocks) + " blocks need " +
+           std::to_string(need));
+  check_place("the cache view", h[0], here.get());
+}
+void check_rope(Here& here, PyObject* rope, int batch) {
+  int64_t h[2];   // device, sequences that have an offset
+  if (!held(rope, h)) return;
+  if (h[1] < batch)
+    refuse("the rotation has offsets for " + std::to_string(h[1]) + " sequences, the call needs " + std::to_string(batch));
+  check_place("the rotation", h[0], here.get());
 }
 
 // The stream's handle (None: the current one).
@@ -185,6 +231,8 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor& t = tensor(a[2], "k_new");
     const int batch = extent(t, 0);
+    check_contiguous("k_new", t);   // or its first dimension need not be the batch
+    check_view(here, a[1], desc, view, batch);
     void* k = pointer(here, a[2], "k_new", at::kBFloat16, batch * kv_row(desc));
     void* v = pointer(here, a[3], "v_new", at::kBFloat16, batch * kv_row(desc));
     int32_t* status = pointer_to<int32_t>(here, a[4], "dev_status", at::kInt, 1);
@@ -200,6 +248,8 @@ PyObject* kv_append_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor& t = tensor(a[2], "k_new");
     const int batch = extent(t, 0), n_new = extent(t, 1);
+    check_contiguous("k_new", t);
+    check_view(here, a[1], desc, view, batch);
     void* k = pointer(here, a[2], "k_new", at::kBFloat16, (int64_t)batch * n_new * kv_row(desc));
     void* v = pointer(here, a[3], "v_new", at::kBFloat16, (int64_t)batch * n_new * kv_row(desc));
     int32_t* lens = pointer_to<int32_t>(here, a[4], "new_lens", at::kInt, batch);
@@ -243,6 +293,9 @@ PyObject* kv_append_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (with_q != (a[6] != Py_None)) refuse("q and q_out go together");
     const at::Tensor &k = tensor(a[4], "k_new"), &v = tensor(a[5], "v_new");
     if (k.dim() != 3 && k.dim() != 4) refuse("k_new must be [batch][n_new][heads][D] or [batch][heads][D]");
+    const int batch = extent(k, 0), n_new = k.dim() == 4 ? extent(k, 1) : 1;
+    check_view(here, a[1], desc, view, batch);
+    check_rope(here, a[2], batch);
     check_rows(k, "k_new", k, desc.num_kv_heads, desc.head_dim);
     check_rows(v, "v_new", k, desc.num_kv_heads, desc.head_dim);
     if (with_q) {
@@ -253,7 +306,6 @@ PyObject* kv_append_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Rows qr = with_q ? rows(here, tensor(a[3], "q"), "q", desc.head_dim) : Rows{nullptr, 0, 0};
     const puzzle_qkv qkv = {qr.p,          kr.p,            vr.p,          qr.seq_stride,  qr.token_stride,
                             kr.seq_stride, kr.token_stride, vr.seq_stride, vr.token_stride};
-    const int batch = extent(k, 0), n_new = k.dim() == 4 ? extent(k, 1) : 1;
     void* q_out = pointer(here, a[6], "q_out", at::kBFloat16, 0);   // its shape has been checked
     int32_t* lens = pointer_to<int32_t>(here, a[7], "new_lens", at::kInt, batch);
     int32_t* status = pointer_to<int32_t>(here, a[8], "dev_status", at::kInt, 1);
@@ -274,6 +326,7 @@ PyObject* kv_read_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
       refuse("k_out and v_out must be [batch][n_read][" + std::to_string(desc.num_kv_heads) + "][" +
              std::to_string(desc.head_dim) + "], got " + shape_text(k.sizes()) + " and " + shape_text(v.sizes()));
     const int batch = extent(k, 0), n_read = extent(k, 1);
+    check_view(here, a[1], desc, view, batch);
     void* kp = pointer(here, a[2], "k_out", at::kBFloat16, 0);   // their shapes have been checked
     void* vp = pointer(here, a[3], "v_out", at::kBFloat16, 0);
     int32_t* lens = pointer_to<int32_t>(here, a[4], "read_lens", at::kInt, batch);
@@ -290,6 +343,8 @@ PyObject* decode(const char* name, decltype(&puzzle_decode_attn) f, PyObject* co
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor &t = tensor(a[2], "q"), &w = tensor(a[7], "workspace");
     const int batch = extent(t, 0);
+    check_contiguous("q", t);   // or its first dimension need not be the batch
+    check_view(here, a[1], desc, view, batch);
     void* q = pointer(here, a[2], "q", at::kBFloat16, batch * q_row(desc));
     const float* sinks = pointer_to<float>(here, a[3], "sinks", at::kFloat, q_heads(desc));
     void* out = pointer(here, a[4], "out", at::kBFloat16, batch * q_row(desc));
@@ -317,6 +372,8 @@ PyObject* decode_attn_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor &t = tensor(a[2], "q"), &w = tensor(a[7], "workspace");
     const int batch = extent(t, 0), n_q = extent(t, 1);
     const int64_t tokens = (int64_t)batch * n_q;
+    check_contiguous("q", t);
+    check_view(here, a[1], desc, view, batch);
     void* q = pointer(here, a[2], "q", at::kBFloat16, tokens * q_row(desc));
     const int32_t* lens = pointer_to<int32_t>(here, a[3], "q_lens", at::kInt, batch);
     const float* sinks = pointer_to<float>(here, a[4], "sinks", at::kFloat, q_heads(desc));
