@@ -226,6 +226,62 @@ def _stream(stream, tensor=None):
     return torch.cuda.current_stream().cuda_stream
 
 
+def _arg(t: Optional[torch.Tensor], dtype=None, name="tensor", need: int = 0):
+    """Device pointer (None -> NULL) of a tensor that a call is given: contiguous, on the current device, with at least
+    `need` elements."""
+    p = _p(t, dtype, name)
+    if t is None:
+        return p
+    _same_device(name, t.get_device())
+    if t.numel() < need:
+        raise ValueError("%s has %d elements, the call needs %d" % (name, t.numel(), need))
+    return p
+
+
+def _same_device(name: str, device: int):
+    if device != _current_device():
+        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, device, _current_device()))
+
+
+def _reach(t: torch.Tensor, dtype, name: str, need: int):
+    """_arg of a tensor that names the first of `need` elements of its storage."""
+    p = _arg(t, dtype, name)
+    if p is not None and t.untyped_storage().nbytes() // t.element_size() - t.storage_offset() < need:
+        raise ValueError("%s reaches fewer than the %d elements that the call needs" % (name, need))
+    return p
+
+
+_BLOCK_BYTES = {KV_FP8_E4M3: 16 * 64, KV_BF16: 16 * 64 * 2, KV_FP4_E2M1: FP4_BLOCK_BYTES}
+
+
+def _taken(desc) -> bool:
+    """Whether the library takes this descriptor; others it refuses itself, with a code that says why."""
+    return desc.num_kv_heads > 0 and desc.head_dim == 64 and desc.num_q_heads == 8 * desc.num_kv_heads
+
+
+def _check_view(desc, view, batch: int):
+    """Whether what a view points to has room for this descriptor and this many sequences (as in csrc/call.cpp)."""
+    if view._held is None:
+        return
+    device, sequences, scales, cache_bytes = view._held
+    if sequences < batch:
+        raise ValueError("the cache view has %d sequences, the call needs %d" % (sequences, batch))
+    if _taken(desc):
+        if scales < desc.num_kv_heads and desc.kv_dtype != KV_BF16:
+            raise ValueError("the cache view has %d scales, the call needs %d" % (scales, desc.num_kv_heads))
+        need = view.num_blocks * desc.num_kv_heads * _BLOCK_BYTES.get(desc.kv_dtype, 0)
+        if cache_bytes < need:
+            raise ValueError("the cache has %d bytes, the descriptor's %d blocks need %d" % (cache_bytes, view.num_blocks, need))
+    _same_device("the cache view", device)
+
+
+def _rows(desc, batch: int):
+    """Elements of q or out, of their heads, and of k_new or v_new, for `batch` tokens."""
+    if not _taken(desc):
+        return 0, 0, 0
+    return batch * desc.num_q_heads * 64, batch * desc.num_q_heads, batch * desc.num_kv_heads * 64
+
+
 def layer_desc(window: int = 0, kv_dtype: int = KV_FP8_E4M3, num_q_heads: int = 64, num_kv_heads: int = 8,
                head_dim: int = 64, block_size: int = 16, sm_scale: Optional[float] = None) -> LayerDesc:
     return LayerDesc(num_q_heads, num_kv_heads, head_dim, block_size, int(window), int(kv_dtype),
@@ -285,13 +341,13 @@ def puzzle_kv_amax_update(x: torch.Tensor, amax: torch.Tensor, stream=None) -> N
     """x: bf16 [n_tokens][Hkv][D] (any leading dims, flattened); amax: float32 [Hkv], raised in place."""
     hkv, d = x.shape[-2], x.shape[-1]
     n_tokens = x.numel() // (hkv * d) if x.numel() else 0
-    _check(_load().puzzle_kv_amax_update(_p(x, torch.bfloat16, "x"), n_tokens, hkv, d, _p(amax, torch.float32, "amax"),
+    _check(_load().puzzle_kv_amax_update(_arg(x, torch.bfloat16, "x"), n_tokens, hkv, d, _arg(amax, torch.float32, "amax", hkv),
                                          _stream(stream, x)), "puzzle_kv_amax_update")
 
 
 def puzzle_kv_scales_from_amax(amax: torch.Tensor, scale_out: torch.Tensor, pow2: bool = False, stream=None) -> None:
-    _check(_load().puzzle_kv_scales_from_amax(_p(amax, torch.float32, "amax"), amax.numel(), int(bool(pow2)),
-                                              _p(scale_out, torch.float32, "scale_out"), _stream(stream)),
+    _check(_load().puzzle_kv_scales_from_amax(_arg(amax, torch.float32, "amax"), amax.numel(), int(bool(pow2)),
+                                              _arg(scale_out, torch.float32, "scale_out", amax.numel()), _stream(stream)),
            "puzzle_kv_scales_from_amax")
 
 
@@ -348,7 +404,7 @@ def puzzle_decode_attn_tokens_workspace_bytes(desc: LayerDesc, batch: int, n_q: 
 
 def puzzle_decode_attn_tokens_workspace_init(desc: LayerDesc, batch: int, n_q: int, workspace: torch.Tensor,
                                              stream=None) -> None:
-    _check(_load().puzzle_decode_attn_tokens_workspace_init(ctypes.byref(desc), int(batch), int(n_q), _p(workspace),
+    _check(_load().puzzle_decode_attn_tokens_workspace_init(ctypes.byref(desc), int(batch), int(n_q), _arg(workspace, None, "workspace"),
                                                             workspace.numel() * workspace.element_size(),
                                                             _stream(stream)), "puzzle_decode_attn_tokens_workspace_init")
 
@@ -369,7 +425,7 @@ def puzzle_decode_attn_workspace_bytes(desc: LayerDesc, batch: int, num_splits: 
 
 
 def puzzle_decode_attn_workspace_init(desc: LayerDesc, batch: int, workspace: torch.Tensor, stream=None) -> None:
-    _check(_load().puzzle_decode_attn_workspace_init(ctypes.byref(desc), int(batch), _p(workspace),
+    _check(_load().puzzle_decode_attn_workspace_init(ctypes.byref(desc), int(batch), _arg(workspace, None, "workspace"),
                                                      workspace.numel() * workspace.element_size(), _stream(stream)),
            "puzzle_decode_attn_workspace_init")
 
@@ -401,10 +457,14 @@ def puzzle_decode_attn_static(desc: LayerDesc, view: KVView, q: torch.Tensor, si
     """puzzle_decode_attn on the library's built-in 8 MiB scratch: for callers that cannot allocate device
     memory (no workspace tensor is involved, and nothing is allocated on the way).  Calls that share a
     device must not overlap on the GPU; make the first call on a device outside any stream capture."""
-    _check(_load().puzzle_decode_attn_static(ctypes.byref(desc), ctypes.byref(view), _p(q, torch.bfloat16, "q"),
-                                             _p(sinks, torch.float32, "sinks"), _p(out, torch.bfloat16, "out"),
-                                             _p(lse_out, torch.float32, "lse_out"), q.shape[0], int(num_splits),
-                                             _p(dev_status, torch.int32), _stream(stream, q)),
+    batch = q.shape[0]
+    _check_view(desc, view, batch)
+    n, heads, _ = _rows(desc, batch)
+    _check(_load().puzzle_decode_attn_static(ctypes.byref(desc), ctypes.byref(view), _arg(q, torch.bfloat16, "q", n),
+                                             _arg(sinks, torch.float32, "sinks", heads // batch if batch else 0),
+                                             _arg(out, torch.bfloat16, "out", n),
+                                             _arg(lse_out, torch.float32, "lse_out", heads), batch, int(num_splits),
+                                             _arg(dev_status, torch.int32, "dev_status", 1), _stream(stream, q)),
            "puzzle_decode_attn_static")
 
 
@@ -412,9 +472,11 @@ def puzzle_decode_step_host_staging_bytes(desc: LayerDesc, batch: int) -> int:
     return int(_load().puzzle_decode_step_host_staging_bytes(ctypes.byref(desc), int(batch)))
 
 
-def _host_ptr(t: torch.Tensor, name: str):
+def _host_ptr(t: torch.Tensor, name: str, need: int):
     if t.is_cuda or not t.is_contiguous() or t.dtype != torch.bfloat16:
         raise ValueError("%s must be a contiguous bf16 host tensor" % name)
+    if t.numel() < need:
+        raise ValueError("%s has %d elements, the call needs %d" % (name, t.numel(), need))
     return t.data_ptr()
 
 
@@ -424,13 +486,18 @@ def puzzle_decode_step_host(desc: LayerDesc, view: KVView, q_host: torch.Tensor,
                             dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """Append + attention of one layer with q, k_new, v_new and out in host memory (pinned for asynchronous copies);
     staging and workspace are device tensors.  Synchronise the stream before reading out_host."""
-    _check(_load().puzzle_decode_step_host(ctypes.byref(desc), ctypes.byref(view), _host_ptr(q_host, "q_host"),
-                                           _host_ptr(k_new_host, "k_new_host"), _host_ptr(v_new_host, "v_new_host"),
-                                           _p(sinks, torch.float32, "sinks"), _host_ptr(out_host, "out_host"),
-                                           q_host.shape[0], int(num_splits), _p(staging),
-                                           staging.numel() * staging.element_size(), _p(workspace),
-                                           workspace.numel() * workspace.element_size(), _p(dev_status, torch.int32),
-                                           _stream(stream, workspace)), "puzzle_decode_step_host")
+    batch = q_host.shape[0]
+    n, heads, kn = _rows(desc, batch)
+    q, k, v, out = (_host_ptr(t, name, need) for t, name, need in (
+        (q_host, "q_host", n), (k_new_host, "k_new_host", kn), (v_new_host, "v_new_host", kn), (out_host, "out_host", n)))
+    _check_view(desc, view, batch)
+    _check(_load().puzzle_decode_step_host(ctypes.byref(desc), ctypes.byref(view), q, k, v,
+                                           _arg(sinks, torch.float32, "sinks", heads // batch if batch else 0), out, batch,
+                                           int(num_splits), _arg(staging, None, "staging"),
+                                           staging.numel() * staging.element_size(), _arg(workspace, None, "workspace"),
+                                           workspace.numel() * workspace.element_size(),
+                                           _arg(dev_status, torch.int32, "dev_status", 1), _stream(stream, workspace)),
+           "puzzle_decode_step_host")
 
 
 def puzzle_decode_attn_partial(desc: LayerDesc, view: KVView, q: torch.Tensor, o_part: torch.Tensor,
@@ -439,11 +506,14 @@ def puzzle_decode_attn_partial(desc: LayerDesc, view: KVView, q: torch.Tensor, o
     """This device's float32 partial (o, lse) over the keys its view holds, no sink: see the header."""
     if workspace is None:
         raise ValueError("workspace is required (size it with puzzle_decode_attn_workspace_bytes)")
-    _check(_load().puzzle_decode_attn_partial(ctypes.byref(desc), ctypes.byref(view), _p(q, torch.bfloat16, "q"),
-                                              _p(o_part, torch.float32, "o_part"),
-                                              _p(lse_part, torch.float32, "lse_part"), q.shape[0], int(num_splits),
-                                              _p(workspace), workspace.numel() * workspace.element_size(),
-                                              _p(dev_status, torch.int32), _stream(stream, q)),
+    batch = q.shape[0]
+    _check_view(desc, view, batch)
+    n, heads, _ = _rows(desc, batch)
+    _check(_load().puzzle_decode_attn_partial(ctypes.byref(desc), ctypes.byref(view), _arg(q, torch.bfloat16, "q", n),
+                                              _arg(o_part, torch.float32, "o_part", n),
+                                              _arg(lse_part, torch.float32, "lse_part", heads), batch, int(num_splits),
+                                              _arg(workspace, None, "workspace"), workspace.numel() * workspace.element_size(),
+                                              _arg(dev_status, torch.int32, "dev_status", 1), _stream(stream, q)),
            "puzzle_decode_attn_partial")
 
 
@@ -453,24 +523,30 @@ def puzzle_attn_merge_strided(part_o: torch.Tensor, part_lse: torch.Tensor, o_ro
                               lse_out: Optional[torch.Tensor] = None, stream=None) -> None:
     """part_o / part_lse: float32 tensors whose first elements are part 0 of row 0 (strides in floats)."""
     batch, hq, d = out.shape
-    _check(_load().puzzle_attn_merge_strided(_p(part_o, torch.float32, "part_o"), _p(part_lse, torch.float32, "part_lse"),
-                                             int(o_row_stride), int(o_part_stride), int(lse_row_stride),
-                                             int(lse_part_stride), _p(num_parts, torch.int32, "num_parts"),
-                                             _p(sinks, torch.float32, "sinks"), _p(out, torch.bfloat16, "out"),
-                                             _p(lse_out, torch.float32, "lse_out"), batch, hq, d, int(num_parts_max),
-                                             _stream(stream)), "puzzle_attn_merge_strided")
+    # with num_parts given, how many parts there are is known on the device alone: one is asked for
+    last, parts = max(batch * hq - 1, 0), max(int(num_parts_max) - 1, 0) if num_parts is None else 0
+    _check(_load().puzzle_attn_merge_strided(
+        _reach(part_o, torch.float32, "part_o", last * int(o_row_stride) + parts * int(o_part_stride) + d),
+        _reach(part_lse, torch.float32, "part_lse", last * int(lse_row_stride) + parts * int(lse_part_stride) + 1),
+        int(o_row_stride), int(o_part_stride), int(lse_row_stride), int(lse_part_stride),
+        _arg(num_parts, torch.int32, "num_parts", batch), _arg(sinks, torch.float32, "sinks", hq),
+        _arg(out, torch.bfloat16, "out"), _arg(lse_out, torch.float32, "lse_out", batch * hq), batch, hq, d,
+        int(num_parts_max), _stream(stream)), "puzzle_attn_merge_strided")
 
 
 def puzzle_attn_merge(part_o: torch.Tensor, part_lse: torch.Tensor, num_parts: Optional[torch.Tensor],
                       sinks: Optional[torch.Tensor], out: torch.Tensor, lse_out: Optional[torch.Tensor] = None,
                       stream=None) -> None:
     batch, hq, s, d = part_o.shape
-    _check(_load().puzzle_attn_merge(_p(part_o, torch.float32, "part_o"), _p(part_lse, torch.float32, "part_lse"),
-                                     _p(num_parts, torch.int32, "num_parts"), _p(sinks, torch.float32, "sinks"),
-                                     _p(out, torch.bfloat16, "out"), _p(lse_out, torch.float32, "lse_out"),
-                                     batch, hq, d, s, _stream(stream)), "puzzle_attn_merge")
+    _check(_load().puzzle_attn_merge(_arg(part_o, torch.float32, "part_o"),
+                                     _arg(part_lse, torch.float32, "part_lse", batch * hq * s),
+                                     _arg(num_parts, torch.int32, "num_parts", batch), _arg(sinks, torch.float32, "sinks", hq),
+                                     _arg(out, torch.bfloat16, "out", batch * hq * d),
+                                     _arg(lse_out, torch.float32, "lse_out", batch * hq), batch, hq, d, s, _stream(stream)),
+           "puzzle_attn_merge")
 
 
 def puzzle_hbm_read_probe(buf: torch.Tensor, sink: torch.Tensor, stream=None) -> None:
-    _check(_load().puzzle_hbm_read_probe(_p(buf), buf.numel() * buf.element_size(), _p(sink), _stream(stream)),
+    _check(_load().puzzle_hbm_read_probe(_arg(buf, None, "buf"), buf.numel() * buf.element_size(),
+                                         _arg(sink, None, "sink", -(-8 // sink.element_size())), _stream(stream)),
            "puzzle_hbm_read_probe")
