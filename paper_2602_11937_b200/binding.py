@@ -371,13 +371,14 @@ def puzzle_kv_append_tokens(desc: LayerDesc, view: KVView, k_new: torch.Tensor, 
 
 def rope_view(cos_sin: torch.Tensor, interleaved: bool = False, pos_offset: Optional[torch.Tensor] = None) -> Rope:
     """Describe a rotation table: float32 [num_positions][rotary_dim], the cosines of a position and then its sines
-    (``rope_table`` makes one); pos_offset: int32 [batch] or None.  Keep the tensors alive while the view is in use."""
+    (``rope_table`` makes one); pos_offset: int32 [batch] or None.  The description keeps both tensors alive."""
     r = Rope()
     r.cos_sin = _p(cos_sin, torch.float32, "cos_sin")
     r.num_positions, r.rotary_dim = cos_sin.shape
     r.interleaved = int(bool(interleaved))
     r.pos_offset = _p(pos_offset, torch.int32, "pos_offset")
     r._held = (_device_of("a rotation", cos_sin, pos_offset), _ANY if pos_offset is None else pos_offset.numel())
+    r._tensors = (cos_sin, pos_offset)
     return r
 
 

@@ -21,8 +21,9 @@ class DecodeStack:
                  k_scales: Sequence[Optional[torch.Tensor]], v_scales: Sequence[Optional[torch.Tensor]],
                  sinks: Sequence[Optional[torch.Tensor]], kv_dtype: int = B.KV_FP8_E4M3, num_splits: int = 0,
                  rope: Optional[B.Rope] = None):
-        """rope: q and k of ``step`` arrive unrotated and are rotated on their way (one table for all layers; keep its
-        tensors alive); None: they arrive rotated."""
+        """rope: q and k of ``step`` arrive unrotated and are rotated on their way (one table for all layers); None: they
+        arrive rotated.  A sequence that a layer skips (longer than its table row, or at a position the rotation does not
+        have: ``status`` says so) has no valid output in that step."""
         n = len(windows)
         assert all(len(x) == n for x in (k_caches, v_caches, block_tables, k_scales, v_scales, sinks))
         self.windows = list(windows)

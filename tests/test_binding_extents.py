@@ -124,3 +124,16 @@ def test_strided_merge(B):
         call(buf, parts=3)
     with pytest.raises(ValueError, match="num_parts has 1 elements"):
         call(buf, num_parts=Pretend(1, dtype=I32))
+
+
+def test_a_rotation_keeps_its_tensors(B):
+    """rope_view(rope_table(n).cuda()): the table lives as long as the description that points to it."""
+    import weakref
+    table, offset = Pretend(8, 64, dtype=F32), Pretend(2, dtype=I32)
+    alive = weakref.ref(table), weakref.ref(offset)
+    rope = B.rope_view(table, pos_offset=offset)
+    del table, offset
+    assert alive[0]() is not None and alive[1]() is not None
+    assert rope.cos_sin == alive[0]().t.data_ptr()
+    del rope
+    assert alive[0]() is None and alive[1]() is None
