@@ -6,6 +6,7 @@ import ctypes
 import importlib.machinery
 import importlib.util
 import os
+import platform
 from typing import Optional
 
 import torch
@@ -173,6 +174,11 @@ def _bind(lib):
         spec = importlib.util.spec_from_file_location("_puzzle_call", _CALL_PATH, loader=loader)
         module = importlib.util.module_from_spec(spec)
         loader.exec_module(module)
+        here = "python %s torch %s" % (".".join(platform.python_version_tuple()[:2]), torch.__version__)
+        built_for = getattr(module, "built_for", "an unknown version")
+        if built_for != here:
+            raise RuntimeError("%s was built for %s, this is %s: build it again with `python -m paper_2602_11937_b200.build`"
+                               % (_CALL_PATH, built_for, here))
     else:
         module = _call
     module.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _CALLS))

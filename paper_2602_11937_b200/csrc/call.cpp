@@ -409,4 +409,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_puzzle_call", nullptr, -1, method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__puzzle_call() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__puzzle_call() {
+  PyObject* m = PyModule_Create(&module);
+  // the binding compares it with what it runs in: the interfaces used here change between versions
+  if (m && PyModule_AddStringConstant(m, "built_for", PUZZLE_BUILT_FOR) != 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}
