@@ -134,15 +134,17 @@ bool held(PyObject* o, int64_t (&v)[N]) {
 int64_t block_bytes(const puzzle_layer_desc& d) {   // of one (block, KV head), K or V
   return d.kv_dtype == PUZZLE_KV_FP4_E2M1 ? PUZZLE_FP4_BLOCK_BYTES : d.kv_dtype == PUZZLE_KV_BF16 ? 16 * 64 * 2 : 16 * 64;
 }
-// Whether what a view points to has room for this descriptor and this many sequences.
-void check_view(Here& here, PyObject* view, const puzzle_layer_desc& d, const puzzle_kv_view& v, int batch) {
+// Whether what a view points to has room for this descriptor and this many sequences.  type_taken: the entry point has this
+// cache type (others it refuses itself, with a code that says why).
+void check_view(Here& here, PyObject* view, const puzzle_layer_desc& d, const puzzle_kv_view& v, int batch,
+                bool type_taken = true) {
   int64_t h[4];   // device, sequences, scales, bytes of the smaller cache
   if (!held(view, h)) return;
   if (h[1] < batch)
     refuse("the cache view has " + std::to_string(h[1]) + " sequences, the call needs " + std::to_string(batch));
   if (taken(d) && h[2] < d.num_kv_heads && d.kv_dtype != PUZZLE_KV_BF16)
     refuse("the cache view has " + std::to_string(h[2]) + " scales, the call needs " + std::to_string(d.num_kv_heads));
-  const int64_t need = taken(d) ? v.num_blocks * d.num_kv_heads * block_bytes(d) : 0;
+  const int64_t need = taken(d) && type_taken ? v.num_blocks * d.num_kv_heads * block_bytes(d) : 0;
   if (h[3] < need)
     refuse("the cache has " + std::to_string(h[3]) + " bytes, the descriptor's " + std::to_string(v.num_blocks) + " blocks need " +
            std::to_string(need));
@@ -337,14 +339,14 @@ PyObject* kv_read_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // desc, view, q, sinks, out, lse_out, num_splits, workspace, dev_status, stream
-PyObject* decode(const char* name, decltype(&puzzle_decode_attn) f, PyObject* const* a, Py_ssize_t n) {
+PyObject* decode(const char* name, decltype(&puzzle_decode_attn) f, bool fp8_only, PyObject* const* a, Py_ssize_t n) {
   return call(name, n, 10, [&](Here& here) {
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     const at::Tensor &t = tensor(a[2], "q"), &w = tensor(a[7], "workspace");
     const int batch = extent(t, 0);
     check_contiguous("q", t);   // or its first dimension need not be the batch
-    check_view(here, a[1], desc, view, batch);
+    check_view(here, a[1], desc, view, batch, !fp8_only || desc.kv_dtype == PUZZLE_KV_FP8_E4M3);
     void* q = pointer(here, a[2], "q", at::kBFloat16, batch * q_row(desc));
     const float* sinks = pointer_to<float>(here, a[3], "sinks", at::kFloat, q_heads(desc));
     void* out = pointer(here, a[4], "out", at::kBFloat16, batch * q_row(desc));
@@ -358,10 +360,10 @@ PyObject* decode(const char* name, decltype(&puzzle_decode_attn) f, PyObject* co
   });
 }
 PyObject* decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return decode("decode_attn", entry.decode_attn, a, n);
+  return decode("decode_attn", entry.decode_attn, false, a, n);
 }
 PyObject* decode_attn_tcgen05(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return decode("decode_attn_tcgen05", entry.decode_attn_tcgen05, a, n);
+  return decode("decode_attn_tcgen05", entry.decode_attn_tcgen05, true, a, n);
 }
 
 // desc, view, q, q_lens, sinks, out, lse_out, workspace, dev_status, stream
@@ -373,7 +375,7 @@ PyObject* decode_attn_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int batch = extent(t, 0), n_q = extent(t, 1);
     const int64_t tokens = (int64_t)batch * n_q;
     check_contiguous("q", t);
-    check_view(here, a[1], desc, view, batch);
+    check_view(here, a[1], desc, view, batch, desc.kv_dtype != PUZZLE_KV_BF16);
     void* q = pointer(here, a[2], "q", at::kBFloat16, tokens * q_row(desc));
     const int32_t* lens = pointer_to<int32_t>(here, a[3], "q_lens", at::kInt, batch);
     const float* sinks = pointer_to<float>(here, a[4], "sinks", at::kFloat, q_heads(desc));
