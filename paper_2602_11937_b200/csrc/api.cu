@@ -189,7 +189,7 @@ size_t counter_bytes(int batch, int Hkv) {
 long long tiles_per_pair_bound(const puzzle_layer_desc* d, const puzzle_kv_view* kv) {
   const int tt = tile_tokens(d->kv_dtype);
   long long per_pair = ((long long)kv->max_blocks_per_seq * kBlock + tt - 1) / tt;
-  if (d->window > 0) per_pair = std::min<long long>(per_pair, (d->window + tt - 1) / tt + 1);
+  if (d->window > 0) per_pair = std::min<long long>(per_pair, ((long long)d->window + tt - 1) / tt + 1);
   return per_pair;
 }
 

@@ -1,0 +1,70 @@
+"""Sizes at the ends of what the descriptors can say: windows as long as an int32 goes, table rows whose tokens an int32 cannot
+count, more KV heads than a grid dimension holds."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+OK, SHAPE, UNSUPPORTED = 0, 2, 3
+WIDEST = [2 ** 31 - 1, 2 ** 31 - 63, 2 ** 31 - 32, 2 ** 30]
+
+
+def _view(blocks=1 << 16, row=1 << 12):
+    from paper_2602_11937_b200 import binding as B
+    kv = B.KVView()
+    kv.k_cache, kv.v_cache, kv.seq_lens, kv.block_table = 0x1000, 0x2000, 0x3000, 0x4000
+    kv.num_blocks, kv.max_blocks_per_seq = blocks, row
+    return kv
+
+
+@pytest.mark.parametrize("kv_dtype", [0, 1, 2])
+@pytest.mark.parametrize("batch", [1, 16, 300])
+def test_a_window_beyond_every_context_is_no_window(kv_dtype, batch):
+    """The kernel is chosen by the tiles that a sequence can have: as for a layer without a window."""
+    import paper_2602_11937_b200 as P
+    want = P.puzzle_decode_attn_kernel_name(P.layer_desc(kv_dtype=kv_dtype), _view(), batch)
+    assert want != "decode_attn_small_kernel"
+    for window in WIDEST:
+        assert P.puzzle_decode_attn_kernel_name(P.layer_desc(window=window, kv_dtype=kv_dtype), _view(), batch) == want
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kv_dtype", [0, 1, 2])
+def test_the_widest_windows_see_every_key(kv_dtype):
+    import paper_2602_11937_b200 as P
+    n, batch = 5000, 3
+    blocks = -(-n // 16)
+    g = torch.Generator().manual_seed(kv_dtype)
+    k, v = (torch.randn(batch, n, 8, 64, generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    lens = torch.tensor([n, 700, 1], dtype=torch.int32, device="cuda")
+    shape = {0: (16, 64), 1: (16, 64), 2: (576,)}[kv_dtype]
+    caches = [torch.zeros(batch * blocks, 8, *shape, dtype=torch.bfloat16 if kv_dtype == 1 else torch.uint8, device="cuda")
+              for _ in range(2)]
+    view = P.kv_view(*caches, lens, max_blocks_per_seq=blocks)
+    P.puzzle_kv_append_tokens(P.layer_desc(kv_dtype=kv_dtype), view, k, v, new_lens=lens)
+    q = torch.randn(batch, 2, 64, 64, generator=g).to(torch.bfloat16).cuda()
+    q1 = q[:, 0].contiguous()
+    want, lse = None, None
+    for window in [0] + WIDEST:
+        d = P.layer_desc(window=window, kv_dtype=kv_dtype)
+        ws = torch.empty(P.puzzle_decode_attn_workspace_bytes(d, batch), dtype=torch.uint8, device="cuda")
+        P.puzzle_decode_attn_workspace_init(d, batch, ws)
+        got, got_lse = [torch.empty_like(q1)], [torch.empty(batch, 64, device="cuda")]
+        P.puzzle_decode_attn(d, view, q1, None, got[0], got_lse[0], workspace=ws)
+        if kv_dtype != 1:
+            wt = torch.empty(P.puzzle_decode_attn_tokens_workspace_bytes(d, batch, 2), dtype=torch.uint8, device="cuda")
+            P.puzzle_decode_attn_tokens_workspace_init(d, batch, 2, wt)
+            got.append(torch.empty_like(q))
+            got_lse.append(torch.empty(batch, 2, 64, device="cuda"))
+            P.puzzle_decode_attn_tokens(d, view, q, None, got[1], got_lse[1], workspace=wt)
+        torch.cuda.synchronize()
+        if want is None:
+            want, lse = got, got_lse
+            continue
+        # the same kernel and the same weights, float32 sums in another order at most: one bf16 step, and for outputs near
+        # zero 5000 * 2^-24 of the weighted mean of |v| (below 1)
+        for a, b, c, e in zip(got, want, got_lse, lse):
+            assert torch.allclose(a.float(), b.float(), rtol=2.0 ** -7, atol=5000 * 2.0 ** -24)
+            finite = torch.isfinite(e)                       # the earlier token of the one-token sequence sees no key
+            assert torch.equal(torch.isfinite(c), finite) and torch.allclose(c[finite], e[finite], rtol=0, atol=1e-5)
