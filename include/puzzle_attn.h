@@ -44,7 +44,8 @@
  *     table row) set a bit in *dev_status, skip the access and never trap.
  *   - Shapes supported by this version: head_dim 64, block_size 16,
  *     num_q_heads == 8 * num_kv_heads, batch <= 4096 (num_kv_heads <= 4096 for
- *     puzzle_kv_append_rope, puzzle_kv_read_tokens and appends to a 4-bit cache).
+ *     puzzle_kv_append_rope, puzzle_kv_read_tokens and appends to a 4-bit cache),
+ *     max_blocks_per_seq <= 2^26.
  *
  * Cache layout (both K and V):  [num_blocks][num_kv_heads][block_size][head_dim]
  *   elements u8 (E4M3 codes) or bf16; one (block, KV head) is 1 KiB (FP8) or

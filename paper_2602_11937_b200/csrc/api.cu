@@ -61,6 +61,7 @@ puzzle_status check_view(const puzzle_layer_desc* d, const puzzle_kv_view* kv, i
   if (!kv || !kv->k_cache || !kv->v_cache || !kv->seq_lens) return PUZZLE_ERR_NULL;
   if (batch <= 0 || kv->num_blocks <= 0 || kv->max_blocks_per_seq <= 0) return PUZZLE_ERR_SHAPE;
   if (batch > kMaxBatch) return PUZZLE_ERR_UNSUPPORTED;
+  if (kv->max_blocks_per_seq > (1 << 26)) return PUZZLE_ERR_UNSUPPORTED;   // tokens are counted in 32 bits, rounded up to tiles
   if ((reinterpret_cast<uintptr_t>(kv->k_cache) & 15) || (reinterpret_cast<uintptr_t>(kv->v_cache) & 15))
     return PUZZLE_ERR_SHAPE;
   // rows of the 2-D view of the cache must fit a signed 32-bit TMA coordinate

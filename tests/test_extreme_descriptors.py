@@ -68,3 +68,23 @@ def test_the_widest_windows_see_every_key(kv_dtype):
             assert torch.allclose(a.float(), b.float(), rtol=2.0 ** -7, atol=5000 * 2.0 ** -24)
             finite = torch.isfinite(e)                       # the earlier token of the one-token sequence sees no key
             assert torch.equal(torch.isfinite(c), finite) and torch.allclose(c[finite], e[finite], rtol=0, atol=1e-5)
+
+
+@pytest.mark.parametrize("kv_dtype", [0, 1, 2])
+def test_table_rows_whose_tokens_an_int32_cannot_count(kv_dtype):
+    """From 2^27 blocks of 16 tokens on every length counted as too long for its row."""
+    from paper_2602_11937_b200 import binding as B
+    lib, d = B._load(), B.layer_desc(kv_dtype=kv_dtype)
+    ref = ctypes.byref
+    for row in ((1 << 26) + 1, 1 << 27, 2 ** 31 - 1):
+        kv = _view(row=row)
+        assert lib.puzzle_decode_attn(ref(d), ref(kv), 0x5000, None, 0x8000, None, 4, 0, 0x10000, 1 << 30, None, None) == UNSUPPORTED
+        assert lib.puzzle_decode_attn_tokens(ref(d), ref(kv), 0x5000, None, None, 0x8000, None, 4, 2, 0x10000, 1 << 30, None,
+                                             None) == UNSUPPORTED
+        assert lib.puzzle_kv_append(ref(d), ref(kv), 0x6000, 0x7000, 4, None, None) == UNSUPPORTED
+        assert lib.puzzle_kv_append_tokens(ref(d), ref(kv), 0x6000, 0x7000, None, 4, 2, None, None) == UNSUPPORTED
+        assert lib.puzzle_kv_read_tokens(ref(d), ref(kv), 0x9000, 0xA000, None, 4, 2, None, None) == UNSUPPORTED
+        rope, qkv = B.Rope(0x4000, 1024, 64, 0, None), B.QKV(None, 0x6000, 0x7000, 0, 0, 512, 512, 512, 512)
+        assert lib.puzzle_kv_append_rope(ref(d), ref(kv), ref(rope), ref(qkv), None, None, 4, 1, None, None) == UNSUPPORTED
+    kv = _view(row=1 << 26)
+    assert lib.puzzle_decode_attn(ref(d), ref(kv), 0x5000, None, 0x8000, None, 4, 0, None, 0, None, None) == 4   # the workspace
