@@ -584,6 +584,7 @@ puzzle_status puzzle_decode_step_host(const puzzle_layer_desc* desc, const puzzl
   // every host-visible error of the two device calls is found before the first copy is enqueued
   puzzle_status st = check_decode_attn_args(desc, kv, dq, dout, batch, num_splits, false);
   if (st != PUZZLE_OK) return st;
+  if (desc->kv_dtype == PUZZLE_KV_FP4_E2M1 && desc->num_kv_heads > kMaxAppendHeads) return PUZZLE_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < puzzle_decode_attn_workspace_bytes(desc, batch, num_splits) ||
       (reinterpret_cast<uintptr_t>(workspace) & 15))
     return PUZZLE_ERR_WORKSPACE;

@@ -2,7 +2,6 @@
 count, more KV heads than a grid dimension holds."""
 import ctypes
 
-import numpy as np
 import pytest
 import torch
 
@@ -88,3 +87,15 @@ def test_table_rows_whose_tokens_an_int32_cannot_count(kv_dtype):
         assert lib.puzzle_kv_append_rope(ref(d), ref(kv), ref(rope), ref(qkv), None, None, 4, 1, None, None) == UNSUPPORTED
     kv = _view(row=1 << 26)
     assert lib.puzzle_decode_attn(ref(d), ref(kv), 0x5000, None, 0x8000, None, 4, 0, None, 0, None, None) == 4   # the workspace
+
+
+def test_a_step_from_host_memory_refuses_before_it_copies():
+    """More KV heads than an append to a 4-bit cache takes: found before the first copy is enqueued (here there is no device to
+    copy to, so a copy would show as a CUDA error)."""
+    from paper_2602_11937_b200 import binding as B
+    lib, d = B._load(), B.layer_desc(kv_dtype=B.KV_FP4_E2M1, num_q_heads=8 * 4097, num_kv_heads=4097)
+    kv = _view(blocks=1 << 10)
+    staging = lib.puzzle_decode_step_host_staging_bytes(ctypes.byref(d), 2)
+    ws = lib.puzzle_decode_attn_workspace_bytes(ctypes.byref(d), 2, 0)
+    assert lib.puzzle_decode_step_host(ctypes.byref(d), ctypes.byref(kv), 0x100, 0x200, 0x300, None, 0x400, 2, 0, 0x10000, staging,
+                                       0x10000, ws, None, None) == UNSUPPORTED
