@@ -202,6 +202,11 @@ typedef struct {
  *   tokens of one call must land in different cache slots: over a ring of R blocks, at most 16 (R - 1) of a sequence at a
  *     time, and no two sequences into one block (in a 4-bit block two tokens share V's bytes, which is why appends to it
  *     read them: the other token's half is kept).
+ *   a context dealt to several devices: a device whose slice does not get the token skips the sequence, its query included, so
+ *     devices that need the rotated query and the device that stores the token make two calls: one for q, with k and v into a
+ *     scratch cache of one block per sequence (seq_lens 1, pos_offset the position), one with q NULL for the slice
+ *     (pos_offset the position minus the place in the slice).  A chunk's positions are place + offset within one block only:
+ *     give it in pieces that end with a block, or rotated, to puzzle_kv_append_tokens.
  * n_new == 1 runs a kernel laid out for latency, chunks one laid out for bandwidth; the results are the same. */
 PUZZLE_API puzzle_status puzzle_kv_append_rope(const puzzle_layer_desc* desc, const puzzle_kv_view* kv,
                                  const puzzle_rope* rope, const puzzle_qkv* qkv, void* q_out, const int32_t* new_lens,

@@ -42,6 +42,11 @@ def context_slice(seq_lens: torch.Tensor, rank: int, world: int, block: int = 16
     * ``append_lens``: ``local_lens`` where ``rank`` owns the block of the newest token, else 0 (its ``seq_lens``
       for ``puzzle_kv_append``, which skips sequences of length 0): the new token is always the last token of its
       owner's slice.
+
+    ``puzzle_kv_append_rope`` skips the query of a sequence of length 0 too, but every rank needs it.  A step with rotation is
+    therefore two calls on each rank: one for the queries, with k and v into a scratch cache of one block per sequence
+    (``seq_lens`` 1, ``pos_offset`` = global length - 1), and one without q into the rank's slice (``seq_lens`` = append_lens,
+    ``pos_offset`` = global length - append_lens).
     """
     L = seq_lens.to(torch.int64)
     full, tail = L // block, L % block
