@@ -83,7 +83,7 @@ struct Producer {
         if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
       }
     }
-    F::template load_tile<NB>(P, stage_addr, row, bar, lane, [] {});
+    F::template load_tile<NB>(P, stage_addr, row, bar);
     if (++seg.t == seg.t_end) {
       ok = next_segment<TT>(cur, seg, P, cum, lens, w);
       skip_empty(P, cum, lens, w);
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_attn_kernel(const __grid_co
       // ---- refill this stage with the tile NS ahead
       __syncwarp();
       if (prod.template issue<F>(P, cum, lens, w, lane, kbase, bars + 8 * stage)) ++inflight;
-        if (++stage == NS) { stage = 0; phase ^= 1u; }
+      if (++stage == NS) { stage = 0; phase ^= 1u; }
     }
     if (failed) break;
 

@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(Q::kWarps * 32, 1) decode_attn_group_kernel(co
         row = phys * P.Hkv + it.kvh;   // the maps have one row per block and head
       else if (phys != INT_MIN && P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
     }
-    F::template load_tile<NB>(P, pipe + st * STAGE_BYTES, row, bars + 8 * st, lane, [] {});
+    F::template load_tile<NB>(P, pipe + st * STAGE_BYTES, row, bars + 8 * st);
     t_issue += GW;
     lookup();
   };
@@ -438,9 +438,11 @@ static cudaError_t launch_group_variant(const DecodeParams& P, int ctas, cudaStr
 
 template <bool CUT>
 static cudaError_t launch_one(const DecodeParams& P, int warps, int ctas, cudaStream_t s, int* smem_limit) {
+  if constexpr (!CUT) {   // cut launches have groups of four warps or more
+    if (warps == 1) return launch_group_variant<1, OneToken, CUT>(P, ctas, s, smem_limit[0]);
+    if (warps == 2) return launch_group_variant<2, OneToken, CUT>(P, ctas, s, smem_limit[1]);
+  }
   switch (warps) {
-    case 1: return launch_group_variant<1, OneToken, CUT>(P, ctas, s, smem_limit[0]);
-    case 2: return launch_group_variant<2, OneToken, CUT>(P, ctas, s, smem_limit[1]);
     case 4: return launch_group_variant<4, OneToken, CUT>(P, ctas, s, smem_limit[2]);
     case 8: return launch_group_variant<8, OneToken, CUT>(P, ctas, s, smem_limit[3]);
     default: return launch_group_variant<16, OneToken, CUT>(P, ctas, s, smem_limit[4]);
@@ -452,9 +454,11 @@ cudaError_t launch_decode_attn_group(const DecodeParams& P, int warps, bool cut,
 
 template <bool CUT>
 static cudaError_t launch_pair(const DecodeParams& P, int warps, int ctas, cudaStream_t s, int* smem_limit) {
+  if constexpr (!CUT) {
+    if (warps == 1) return launch_group_variant<1, TokenPair, CUT>(P, ctas, s, smem_limit[0]);
+    if (warps == 2) return launch_group_variant<2, TokenPair, CUT>(P, ctas, s, smem_limit[1]);
+  }
   switch (warps) {
-    case 1: return launch_group_variant<1, TokenPair, CUT>(P, ctas, s, smem_limit[0]);
-    case 2: return launch_group_variant<2, TokenPair, CUT>(P, ctas, s, smem_limit[1]);
     case 4: return launch_group_variant<4, TokenPair, CUT>(P, ctas, s, smem_limit[2]);
     case 6: return launch_group_variant<6, TokenPair, CUT>(P, ctas, s, smem_limit[3]);
     default: return launch_group_variant<12, TokenPair, CUT>(P, ctas, s, smem_limit[4]);

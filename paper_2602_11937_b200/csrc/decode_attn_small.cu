@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kSmallWarps * 32, 1) decode_attn_small_kernel(
           else if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
         }
       }
-      F::template load_tile<NB>(P, stage, row, bar, lane, [] {});
+      F::template load_tile<NB>(P, stage, row, bar);
       // ---- query, scales and sink while the tile is in flight
       F::load_query(st, P.q + ((size_t)b * (P.Hkv * kGroup) + kvh * kGroup + g) * kHeadDim,
                     P.k_scale && F::kScaled ? P.k_scale[kvh] : 1.f, P.sm_scale_log2e, lane);

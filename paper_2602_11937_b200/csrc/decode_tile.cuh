@@ -327,7 +327,6 @@ template <bool FP8>
 struct SwizzledTile {
   static constexpr int kBlockBytes = kBlock * kHeadDim * (FP8 ? 1 : 2);   // one (block, KV head) of K or of V
   static constexpr bool kScaled = FP8;
-  static constexpr int kAlign = 1024;   // of the stages in shared memory: the swizzle repeats every 1 KiB
   using Lanes = LaneOffsets<FP8>;
   using State = TileState;
 
@@ -336,17 +335,15 @@ struct SwizzledTile {
     tma_prefetch_desc(&P.tmV);
   }
   // Starts the copies of a tile of NB blocks into `stage`; all lanes call it.  row, in lane i < NB: first row of block i
-  // in the tensor maps (P.oob_row: the block is fetched as zeros).  note(): run by one lane on the way.
-  template <int NB, typename Note>
-  static __device__ __forceinline__ void load_tile(const DecodeParams& P, uint32_t stage, int row, uint32_t bar, int,
-                                                   Note note) {
+  // in the tensor maps (P.oob_row: the block is fetched as zeros).
+  template <int NB>
+  static __device__ __forceinline__ void load_tile(const DecodeParams& P, uint32_t stage, int row, uint32_t bar) {
     // the copies are issued by one lane, which collects the row coordinates first: a TMA instruction takes
     // warp-uniform operands, so issuing from several lanes would be serialised lane by lane anyway
     int rows[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) rows[i] = __shfl_sync(0xffffffffu, row, i);
     if (elect_one()) {
-      note();
       mbar_arrive_expect_tx(bar, 2 * NB * kBlockBytes);
 #pragma unroll
       for (int i = 0; i < NB; ++i) tma_load_2d(stage + i * kBlockBytes, &P.tmK, 0, rows[i], bar);

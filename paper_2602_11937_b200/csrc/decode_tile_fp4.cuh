@@ -254,15 +254,13 @@ struct Fp4Tile {
     tma_prefetch_desc(&P.tmV);
   }
   // One gather of four rows brings the K (V) blocks of 64 tokens, wherever they are: the tensor maps' rows are blocks.
-  template <int NB, typename Note>
-  static __device__ __forceinline__ void load_tile(const DecodeParams& P, uint32_t stage, int row, uint32_t bar, int,
-                                                   Note note) {
+  template <int NB>
+  static __device__ __forceinline__ void load_tile(const DecodeParams& P, uint32_t stage, int row, uint32_t bar) {
     static_assert(NB % 4 == 0, "whole gathers");
     int rows[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) rows[i] = __shfl_sync(0xffffffffu, row, i);
     if (elect_one()) {
-      note();
       mbar_arrive_expect_tx(bar, 2 * NB * kBlockBytes);
 #pragma unroll
       for (int i = 0; i < NB; i += 4) {

@@ -146,9 +146,6 @@ struct Fp4Pair {
 #pragma unroll
     for (int t = 0; t < 2; ++t) st.t[t].l_run = add2(st.t[t].l_run, sum[t]);
   }
-  static __device__ __forceinline__ void finish(const State& st, int tok, float& m, float& l, float (&o)[8][2], int lane) {
-    Fp4Tile::finish(st.t[tok], m, l, o, lane);
-  }
 };
 
 }  // namespace
