@@ -341,8 +341,8 @@ PUZZLE_API puzzle_status puzzle_decode_attn_partial(const puzzle_layer_desc* des
  *   q_host: host bf16 [batch][num_q_heads][head_dim];  k_new_host, v_new_host: host bf16 [batch][num_kv_heads][head_dim];
  *   out_host: host bf16 [batch][num_q_heads][head_dim].  Pinned (page-locked) host memory keeps the copies
  *     asynchronous; pageable memory works but serialises with the host.  When k_new_host follows q_host and
- *     v_new_host follows k_new_host directly in memory (and the sizes are multiples of 256 bytes) the three travel
- *     as one copy;
+ *     v_new_host follows k_new_host directly in one page-locked allocation (and the sizes are multiples of 256 bytes)
+ *     the three travel as one copy;
  *   staging: device scratch of at least puzzle_decode_step_host_staging_bytes(desc, batch) bytes, 256-byte
  *     aligned, owned by the caller (the library allocates nothing); not to be shared by steps that overlap;
  *   num_splits, workspace, dev_status: as puzzle_decode_attn.

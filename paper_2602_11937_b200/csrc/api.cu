@@ -30,6 +30,27 @@ EncodeTiledFn encode_tiled() {
   return fn;
 }
 
+// Whether the `bytes` bytes at p lie in one page-locked allocation.  Allocations of their own can follow each other without a
+// gap, and a copy may not cross from one into the next.  Pageable memory: false.
+bool one_pinned_range(const void* p, size_t bytes) {
+  typedef CUresult (*Attributes)(unsigned int, CUpointer_attribute*, void**, CUdeviceptr);
+  static Attributes get = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPoint("cuPointerGetAttributes", &f, cudaEnableDefault, &qres) != cudaSuccess ||
+        qres != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return reinterpret_cast<Attributes>(f);
+  }();
+  if (!get) return false;
+  CUdeviceptr start = 0;
+  size_t size = 0;
+  CUpointer_attribute what[2] = {CU_POINTER_ATTRIBUTE_RANGE_START_ADDR, CU_POINTER_ATTRIBUTE_RANGE_SIZE};
+  void* into[2] = {&start, &size};
+  const CUdeviceptr at = reinterpret_cast<CUdeviceptr>(p);
+  return get(2, what, into, at) == CUDA_SUCCESS && size != 0 && start <= at && at + bytes <= start + size;
+}
+
 struct DeviceInfo {
   int sm_count = 0;
   // dynamic shared-memory limits already set per kernel and cache type; 0 = not raised yet
@@ -592,8 +613,8 @@ puzzle_status puzzle_decode_step_host(const puzzle_layer_desc* desc, const puzzl
   const size_t qb = qn * sizeof(__nv_bfloat16), kb = kn * sizeof(__nv_bfloat16);
   const char* hq = static_cast<const char*>(q_host);
   if (static_cast<const char*>(k_new_host) == hq + qb && static_cast<const char*>(v_new_host) == hq + qb + kb &&
-      qb % 256 == 0 && kb % 256 == 0) {
-    // the three inputs follow each other in host memory as they do in the staging area: one copy
+      qb % 256 == 0 && kb % 256 == 0 && one_pinned_range(hq, qb + 2 * kb)) {
+    // the three inputs follow each other in one pinned buffer as they do in the staging area: one copy
     if (cudaMemcpyAsync(dq, q_host, qb + 2 * kb, cudaMemcpyHostToDevice, s) != cudaSuccess) return PUZZLE_ERR_CUDA;
   } else if (cudaMemcpyAsync(dq, q_host, qb, cudaMemcpyHostToDevice, s) != cudaSuccess ||
              cudaMemcpyAsync(dk, k_new_host, kb, cudaMemcpyHostToDevice, s) != cudaSuccess ||
