@@ -144,7 +144,7 @@ PUZZLE_API puzzle_status puzzle_kv_scales_from_amax(const float* amax, int32_t n
  * "4-bit cache" above.  The token
  * lands at logical position seq_lens[b]-1 through the block table.  This is
  * the FP8 KV quantisation of Section "KV Quantization" applied at decode time.
- *   k_new, v_new: bf16 [batch][num_kv_heads][head_dim].
+ *   k_new, v_new: bf16 [batch][num_kv_heads][head_dim]; 16-byte aligned for a 4-bit cache.
  *   dev_status: optional int32 device word, bits OR-ed in on device-side errors. */
 PUZZLE_API puzzle_status puzzle_kv_append(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const void* k_new,
                                const void* v_new, int32_t batch, int32_t* dev_status, void* stream);
@@ -288,7 +288,8 @@ PUZZLE_API puzzle_status puzzle_decode_attn_workspace_init(const puzzle_layer_de
  *     not overlap on the GPU.  Besides partials and counters it keeps the CTA speeds between calls:
  *     they change how the next launch is cut, never its result beyond rounding;
  *   dev_status: optional int32 device word (see PUZZLE_DEV_*).
- * Softmax weights e^(s_j - M) of the numerator: FP8 and bf16 caches hold them in two 16-bit terms; the 4-bit cache in f16,
+ * Softmax weights e^(s_j - M) of the numerator: a bf16 cache's are held in two bf16 terms, an FP8 cache's in two f16 terms
+ *     (2^-25 of the largest weight is their end); a 4-bit cache's in f16,
  *     rounded once (2^-11 of a weight, 2^-37 of the largest one for those 2^-26 and more below it), which changes an output
  *     by at most an eighth of its own rounding to bf16 where values do not cancel.  Z and lse: float32, every cache.
  * An empty context gives out = 0 and lse = sink (-inf without a sink). */
@@ -370,7 +371,7 @@ PUZZLE_API puzzle_status puzzle_decode_step_host(const puzzle_layer_desc* desc, 
  *     prepared once by puzzle_decode_attn_tokens_workspace_init (zero-fills its arrival counters; every completed
  *     call leaves them at zero); not to be shared with calls that overlap on the GPU;
  *   a token whose position would be negative (q_lens[b] > seq_lens[b]) sees no key: out = 0, lse = sink.
- * FP8 caches only (PUZZLE_ERR_UNSUPPORTED for bf16: give puzzle_decode_attn one batch row per query token instead);
+ * FP8 and 4-bit caches (PUZZLE_ERR_UNSUPPORTED for bf16: give puzzle_decode_attn one batch row per query token instead);
  * batch * ceil(n_q / 2) <= 8192 (PUZZLE_ERR_SHAPE).  Errors and dev_status as puzzle_decode_attn. */
 PUZZLE_API size_t puzzle_decode_attn_tokens_workspace_bytes(const puzzle_layer_desc* desc, int32_t batch, int32_t n_q);
 PUZZLE_API puzzle_status puzzle_decode_attn_tokens_workspace_init(const puzzle_layer_desc* desc, int32_t batch,

@@ -54,8 +54,10 @@ struct MergeParams {
 // warp and tokens per tile (the unit of the schedule and of one pipeline stage).
 constexpr int kDecodeWarpsFp8 = 12, kDecodeStagesFp8 = 2, kTileFp8 = 64;
 constexpr int kDecodeWarpsBf16 = 12, kDecodeStagesBf16 = 2, kTileBf16 = 32;
-// 16 warps of 64-token tiles (128 registers, a few words spilled outside the tile loop): 122 us at 256 x 4096 against
-// 132 with 12 warps and no spill.
+// 4-bit cache: explicit splits and the pinned warp schedule only, its default is the group kernel.  16 warps of 64-token tiles
+// (128 registers, a few words spilled outside the tile loop) against 12 without a spill: 256 x 4096 tokens pinned 123 / 131
+// us, 16 x 65536 pinned 123 / 126, 64 x 4096 in 4 splits 42 / 55; but 16 x 65536 in 8 splits 246 / 166, because 1024 splits
+// dealt to 16 x 148 warps at even distances fall on the same 64 SMs again and again.
 constexpr int kDecodeWarpsFp4 = 16, kDecodeStagesFp4 = 2, kTileFp4 = 64;
 // The CTA-balanced kernel keeps its schedule arrays beside the TMA rings and the deposit buffers in shared memory,
 // which bounds the batch it takes.  Launches with at least kCtaRateMinTiles tiles per CTA note the speed of every

@@ -5,14 +5,16 @@
 // there are GW times fewer partials; compared with tiles handed out inside a CTA (decode_attn_cta.cu) nothing is
 // claimed or recorded per tile.  Both weigh more here than on the E4M3 cache: a 4-bit tile has half the bytes of an E4M3
 // tile and as many instructions, so what a tile costs besides its arithmetic decides (CTA-balanced kernel 123 us at 16 x
-// 64K, 143 at 37 x 32K; this one 117 and 130).
+// 64K, 143 at 37 x 32K; this one 117 and 130).  Comparisons in this file are of launches without pause on one box; these run at
+// the power cap, and what the codes are decides with: 16 x 64K takes 112 us over normally distributed values, 128 over
+// uniformly random codes.
 //  * Whole pairs: a launch that fills the SMs evenly needs no cutting.  No schedule is built, nothing but inputs and
 //    outputs touches global memory, and the end of a pair is one barrier of its group.  4 x 1024 tokens 6.1 us (evenly cut
 //    over all warps 13.9), 16 x 4096 11.7 (20.2), 16 x 16384 34.5 (44).
 //  * CUT: the tile space of all pairs is cut evenly over the groups; a run that is not a whole pair leaves one float32
 //    partial, and a small second kernel merges them.
-// The tile loop of one token takes 122 registers without spilling, so sixteen warps fit; a pair of tokens 164, twelve warps.
-// At 16 x 64K the kernel reads 5.2 TB/s.  Bare copies of the same blocks in the same order run at 5.9 (6.5 when the blocks of
+// The tile loop of one token takes 122 registers without spilling, so sixteen warps fit; a pair of tokens 162 to 166, twelve.
+// At 16 x 64K the kernel reads 5.2 to 5.4 TB/s.  Bare copies of the same blocks in the same order run at 5.9 (6.5 when the blocks of
 // two heads are fetched together: a block of one head is 576 bytes); the rest is the arithmetic, which alone would take
 // about 105 us, and 10 us of set-up, first tile and merge.
 #include <cuda.h>
@@ -204,8 +206,8 @@ __global__ void __launch_bounds__(Q::kWarps * 32, 1) decode_attn_group_kernel(co
   auto lookup = [&]() {
     phys = INT_MIN;
     const int j = t_issue * NB + lane;
-    // The same range, with what a run has in common worked out at its start: 123.5 to 120.5 us at 16 x 64K, 137 to 132 at
-    // 37 x 32K.  For a pair of tokens the registers it takes cost more (twelve-warp groups: 155 to 169 us at 16 x 64K).
+    // The same range, with what a run has in common worked out at its start: 2.4 % less time at 16 x 64K, 3.6 % at 37 x 32K
+    // (123.5 to 120.5 us, 137 to 132).  For a pair of tokens the registers it takes cost more (twelve-warp groups: 155 to 169 us at 16 x 64K).
     if constexpr (Q::kTokens == 1) {
       if (lane < NB && (unsigned)(j - j_lo) < (unsigned)j_n) phys = table ? table[j] : it.b * P.max_blocks_per_seq + j;
     } else {
