@@ -58,7 +58,8 @@
  *   x ~ code * scale * k_scale[h] (v_scale[h]), so the calibrated scales of the FP8 cache serve it too.  An append
  *   computes, with y the float32 quotient x / k_scale[h], scale = E4M3(max |y| / 6) over the group (float32 quotient,
  *   to nearest even, saturating at 448) and code = E2M1(y / scale) (to nearest even, saturating at 6); a group whose
- *   scale is zero holds zeros, one with a NaN has the scale 0x7F (and so reads as NaN).
+ *   scale is zero holds zeros, one with a NaN has the scale 0x7F (and so reads as NaN).  Two tokens share a byte of V, so
+ *   appends that run at the same time, and sequences of one call, must not write into the same block.
  */
 #ifndef PUZZLE_ATTN_H_
 #define PUZZLE_ATTN_H_
@@ -156,7 +157,8 @@ PUZZLE_API puzzle_status puzzle_kv_append(const puzzle_layer_desc* desc, const p
  *   k_new, v_new: device bf16 [batch][n_new][num_kv_heads][head_dim], 16-byte aligned;
  *   new_lens: device int32 [batch], tokens of each row that are real (clamped to [0, n_new]; the rest of
  *     the row is ignored), or NULL = n_new for every sequence.  Tokens that would land before position
- *     0 (new_lens[b] > seq_lens[b]) are skipped.
+ *     0 (new_lens[b] > seq_lens[b]) are skipped.  Tokens of one call must land in different cache slots: over a
+ *     ring of R blocks, at most 16 (R - 1) of a sequence at a time.
  * Errors and dev_status as puzzle_kv_append. */
 PUZZLE_API puzzle_status puzzle_kv_append_tokens(const puzzle_layer_desc* desc, const puzzle_kv_view* kv,
                                  const void* k_new, const void* v_new, const int32_t* new_lens, int32_t batch,

@@ -5,7 +5,7 @@
 // there are GW times fewer partials; compared with tiles handed out inside a CTA (decode_attn_cta.cu) nothing is
 // claimed or recorded per tile.  Both weigh more here than on the E4M3 cache: a 4-bit tile has half the bytes of an E4M3
 // tile and as many instructions, so what a tile costs besides its arithmetic decides (CTA-balanced kernel 123 us at 16 x
-// 64K, 143 at 37 x 32K; this one 117 and 130).  Comparisons in this file are of launches without pause on one box; these run at
+// 64K, 143 at 37 x 32K; this one 117 and 130).  Comparisons in this file are of launches without pause on one GPU; these run at
 // the power cap, and what the codes are decides with: 16 x 64K takes 112 us over normally distributed values, 128 over
 // uniformly random codes.
 //  * Whole pairs: a launch that fills the SMs evenly needs no cutting.  No schedule is built, nothing but inputs and
