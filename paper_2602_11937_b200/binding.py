@@ -67,18 +67,28 @@ class LayerDesc(ctypes.Structure):
                 ("sm_scale", ctypes.c_float)]
 
 
-class KVView(ctypes.Structure):
+class _Pointers(ctypes.Structure):
+    """A descriptor of pointers, with a note (_held) of what the tensors behind them hold.  A field set by hand may lead to
+    other tensors: the note ends with it."""
+    _held = None
+
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        if name[0] != "_":
+            super().__setattr__("_held", None)
+
+
+class KVView(_Pointers):
     _fields_ = [("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p), ("num_blocks", ctypes.c_int64),
                 ("block_table", ctypes.c_void_p), ("max_blocks_per_seq", ctypes.c_int32),
                 ("seq_lens", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
-    # What the tensors behind the pointers hold, noted by kv_view: device, sequences, scales, bytes of the smaller cache.
-    _held = None
+    # _held, noted by kv_view: device, sequences, scales, bytes of the smaller cache
 
 
-class Rope(ctypes.Structure):
+class Rope(_Pointers):
     _fields_ = [("cos_sin", ctypes.c_void_p), ("num_positions", ctypes.c_int64), ("rotary_dim", ctypes.c_int32),
                 ("interleaved", ctypes.c_int32), ("pos_offset", ctypes.c_void_p)]
-    _held = None    # noted by rope_view: device, sequences that have an offset
+    # _held, noted by rope_view: device, sequences that have an offset
 
 
 class QKV(ctypes.Structure):

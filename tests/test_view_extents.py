@@ -94,3 +94,18 @@ def test_what_a_view_notes():
     with pytest.raises(ValueError, match="the rotation has offsets for 1 sequences"):
         P.puzzle_kv_append_rope(P.layer_desc(kv_dtype=P.KV_FP4_E2M1), view, r, None, x, x)
     assert P.puzzle_launch_count() == before
+
+
+def test_a_field_set_by_hand_ends_what_was_noted():
+    """The pointers may lead to other tensors then; nothing is known of those, and the call is not held to the old ones."""
+    import paper_2602_11937_b200 as P
+    for name in ("seq_lens", "block_table", "k_cache", "num_blocks", "k_scale"):
+        v = _view()
+        setattr(v, name, 64)
+        assert v._held is None
+        with pytest.raises(ValueError, match="k_new must be a CUDA tensor"):
+            _calls(P, batch=3)["append"](P.layer_desc(), v)
+    r = P.Rope()
+    r._held = (0, 1)
+    r.pos_offset = 64
+    assert r._held is None
