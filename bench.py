@@ -492,8 +492,8 @@ NCU_CAPTURE = {
     "source": "profiles/decode_attn_cta_fp8_c3_64k_ncu_full.md (one launch, ncu --set full --clock-control none)",
     "workload": 3, "kernel": "mma", "splits": 0,
     "sources": ("decode_attn_cta.cu", "decode_tile.cuh", "decode_sched.cuh", "common.cuh", "decode_attn.cuh"),
-    "sha256": "fa7bf900555a45a71b76e1a1db1b4a468348c8ecb623b44d30f43b561de503ba",
-    "dram_bytes_per_launch": 1075441000 + 4546048,
+    "sha256": "88124c170b8fca62530c7d8ebada642bccee0742d3375bd3e5a6b6f20cda471b",
+    "dram_bytes_per_launch": 1075479000 + 4624128,
 }
 
 

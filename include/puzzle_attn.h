@@ -291,9 +291,8 @@ PUZZLE_API puzzle_status puzzle_decode_attn_workspace_init(const puzzle_layer_de
  *     they change how the next launch is cut, never its result beyond rounding;
  *   dev_status: optional int32 device word (see PUZZLE_DEV_*).
  * Softmax weights e^(s_j - M) of the numerator: a bf16 cache's are held in two bf16 terms, an FP8 cache's in two f16 terms
- *     (2^-25 of the largest weight is their end); a 4-bit cache's in f16,
- *     rounded once (2^-11 of a weight, 2^-37 of the largest one for those 2^-26 and more below it), which changes an output
- *     by at most an eighth of its own rounding to bf16 where values do not cancel.  Z and lse: float32, every cache.
+ *     (off by 2^-37 of the largest weight at most), a 4-bit cache's in one f16 (off by 2^-11 of themselves besides, which
+ *     changes an output by at most an eighth of its own rounding to bf16 where values do not cancel).  Z and lse: float32.
  * An empty context gives out = 0 and lse = sink (-inf without a sink). */
 PUZZLE_API puzzle_status puzzle_decode_attn(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const void* q,
                                  const float* sinks, void* out, float* lse_out, int32_t batch,
@@ -304,7 +303,7 @@ PUZZLE_API puzzle_status puzzle_decode_attn(const puzzle_layer_desc* desc, const
  * results within the same tolerance), computed by a second kernel that feeds the E4M3 codes of the
  * cache straight to the 5th-generation tensor cores (tcgen05 MMA, accumulators in tensor memory):
  * S = K Q^T with the bf16 query split exactly into two E4M3 terms, O^T += V^T P with the softmax
- * weights split into four E4M3 terms.  FP8 caches only: a bf16 cache returns
+ * weights split into four E4M3 terms (off by 2^-22 of the largest at most).  FP8 caches only: a bf16 cache returns
  * PUZZLE_ERR_UNSUPPORTED and nothing is launched.  Tiles are 128 tokens (num_splits >= 1 cuts the
  * context into runs of 128-token tiles).  It is the slower of the two kernels on the workloads
  * measured so far and is kept as a validated alternative; puzzle_decode_attn is the default path.

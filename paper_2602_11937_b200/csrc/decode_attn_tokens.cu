@@ -160,8 +160,9 @@ struct TileState2 {
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
       mx *= alpha[t];
-      if (mx > m_ref[t] + kLazyLog2 || m_ref[t] == -INFINITY) {
+      if (mx > m_ref[t] + kTopLog2 || m_ref[t] == -INFINITY) {
         if (mx != -INFINITY) {
+          mx -= kRefLog2;
           const float corr = ex2(m_ref[t] - mx);
           l_run[t] *= corr;
 #pragma unroll

@@ -12,8 +12,10 @@
 //    computes are exactly the A-fragment registers of the P.V product: no shuffle or shared-memory round trip
 //    between the two products.  Rows 0-7 of P carry the high and rows 8-15 the low half of an exact two-term
 //    split of each float32 weight, so P.V keeps more than 16 significant bits at no extra MMA.
-//  * The running maximum is only raised (and the accumulators rescaled) when a tile exceeds it by more than 2^8;
-//    between such events a tile costs no accumulator traffic at all.
+//  * Weights are formed against a reference 2^12 below the largest one seen when it was set.  It is only raised (and the
+//    accumulators rescaled) when a tile's largest weight passes 2^15 of it; between such events a tile costs no
+//    accumulator traffic at all.  f16's range then lies where it is needed: weights are off by 2^-37 of the largest at
+//    most (with the reference at the maximum a long tail 2^-24 below one key was off by a third).
 #pragma once
 
 #include "common.cuh"
@@ -22,7 +24,8 @@
 namespace puzzle {
 namespace {
 
-constexpr float kLazyLog2 = 8.0f;  // weights stay below 2^8 relative to the reference maximum
+constexpr float kTopLog2 = 15.f;   // weights stay below 2^15 of the reference (f16 ends at 65504) ...
+constexpr float kRefLog2 = 12.f;   // ... which is set 2^12 below the largest one seen
 
 // E4M3 -> f16 of the four codes in `r`: lo = codes 0,1; hi = codes 2,3.
 __device__ __forceinline__ void e4m3x4_to_f16x2x2(uint32_t r, uint32_t& lo, uint32_t& hi) {
@@ -221,15 +224,16 @@ struct TileState {
           if (tk + e < lo || tk + e >= L) sr[nt][e] = -INFINITY;
       }
     }
-    // ---- online softmax in base 2 against a lazily raised reference maximum
+    // ---- online softmax in base 2 against a lazily raised reference
     float mx = -INFINITY;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) mx = fmaxf(mx, fmaxf(sr[nt][0], sr[nt][1]));
     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
     mx *= alpha;
-    if (mx > m_ref + kLazyLog2 || m_ref == -INFINITY) {
+    if (mx > m_ref + kTopLog2 || m_ref == -INFINITY) {
       if (mx != -INFINITY) {
+        mx -= kRefLog2;
         const float corr = ex2(m_ref - mx);  // 0 on the first visible tile
         l_run *= corr;
 #pragma unroll

@@ -12,11 +12,9 @@
 //  * P is rounded to f16 once: 2^-11 relative, an eighth of the bf16 output's own rounding and independent from key to
 //    key.  A second term for the remainder, as the other caches have it, is 16 more MMAs a tile and what feeds them: 112 to
 //    125 us at 16 x 64K, 152 to 190 for two tokens.  The sum takes the float32 weights, so the lse has their accuracy.
-//  * Weights are formed against a reference 2^12 below the largest one seen when it was set and reach 2^15 of it, so that
-//    f16's range lies where it is needed: weights down to 2^-26 of the largest keep all eleven bits, those below are off by
-//    2^-37 of the largest at most.  (With the reference at the maximum a long tail 2^-24 below one key was lost or off by a
-//    third.)  The reference is only raised (a reduction over the lanes, accumulators rescaled) when some lane sees a weight
-//    beyond 2^15: one vote per tile otherwise.
+//  * The reference of the weights is decode_tile.cuh's: weights down to 2^-26 of the largest keep all eleven bits, those
+//    below are off by 2^-37 of the largest at most.  One vote per tile says whether some lane sees a weight beyond 2^15 of
+//    it; only then it is raised (a reduction over the lanes, accumulators rescaled).
 //  * A block arrives as it lies in HBM; every shared-memory read of a tile (8 bytes per lane of K and
 //    V, 2 and 4 of the scales) is conflict free because the format's order is the fragments' order.
 #pragma once
@@ -155,9 +153,6 @@ __device__ __forceinline__ void fp4_v_fragments(uint32_t block, const Fp4Lanes& 
   }
 }
 
-constexpr float kFp4TopLog2 = 15.f;   // weights stay below 2^15 of the reference (f16 ends at 65504) ...
-constexpr float kFp4RefLog2 = 12.f;   // ... which is set 2^12 below the largest one seen
-
 // Running state of one warp over the tiles of one (sequence, KV head) for one query token: heads 2c and 2c + 1 are this
 // lane's columns.  O[i]: channels 8g + 2i (first two) and 8g + 2i + 1 (last two) of those heads.
 struct Fp4State {
@@ -207,17 +202,17 @@ struct Fp4State {
     alpha[0] = __shfl_sync(0xffffffffu, a, 8 * c);
     alpha[1] = __shfl_sync(0xffffffffu, a, 8 * c + 4);
   }
-  // Raises the references where a head's logits (mx: this lane's largest, code units) exceed them by 2^kFp4TopLog2.
+  // Raises the references where a head's logits (mx: this lane's largest, code units) exceed them by 2^kTopLog2.
   __device__ __forceinline__ void raise(float (&mx)[2]) {
     const float t0 = mx[0] * alpha[0], t1 = mx[1] * alpha[1];
-    if (!__any_sync(0xffffffffu, t0 > m_ref[0] + kFp4TopLog2 || t1 > m_ref[1] + kFp4TopLog2)) return;
+    if (!__any_sync(0xffffffffu, t0 > m_ref[0] + kTopLog2 || t1 > m_ref[1] + kTopLog2)) return;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       float m = e ? t1 : t0;
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-      if (m > m_ref[e] + kFp4TopLog2) {
-        m -= kFp4RefLog2;
+      if (m > m_ref[e] + kTopLog2) {
+        m -= kRefLog2;
         const float corr = ex2(m_ref[e] - m);   // 0 on the first visible tile
         if (e) l_run.y *= corr; else l_run.x *= corr;
 #pragma unroll
