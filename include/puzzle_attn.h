@@ -94,6 +94,7 @@ typedef enum { PUZZLE_KV_FP8_E4M3 = 0, PUZZLE_KV_BF16 = 1, PUZZLE_KV_FP4_E2M1 = 
 #define PUZZLE_DEV_SEQ_TOO_LONG 2u /* seq_len > max_blocks_per_seq * block_size (clamped) */
 #define PUZZLE_DEV_WAIT_EXPIRED 4u /* a bounded wait on a copy ran out; results invalid */
 #define PUZZLE_DEV_BAD_POSITION 8u /* a token's position outside the rotation table (the token is skipped) */
+#define PUZZLE_DEV_BAD_STARTS 16u  /* a sequence's rows of a packed array are not inside it, or end before they start (it is skipped) */
 
 /* One per layer: the layer's attention choice (host struct). */
 typedef struct {
@@ -213,6 +214,60 @@ typedef struct {
 PUZZLE_API puzzle_status puzzle_kv_append_rope(const puzzle_layer_desc* desc, const puzzle_kv_view* kv,
                                  const puzzle_rope* rope, const puzzle_qkv* qkv, void* q_out, const int32_t* new_lens,
                                  int32_t batch, int32_t n_new, int32_t* dev_status, void* stream);
+
+/* Packed tokens (puzzle_kv_append_packed, puzzle_prompt_attn, puzzle_chunk_attn): the tokens of several sequences behind each
+ * other, one row each, as a serving batch of prompts of different lengths holds them.  starts: device int32 [batch + 1];
+ * sequence b has rows starts[b] .. starts[b + 1] - 1 of the total_tokens rows of every packed array, which may be none.
+ * Rows that belong to no sequence are neither read for a result nor written.  A sequence whose rows are not inside the array,
+ * or end before they start, is skipped (PUZZLE_DEV_BAD_STARTS); no two sequences may share rows.  Row i of head h of an input
+ * lies at base + i * token_stride + h * head_dim: strides in elements, multiples of 8 that rows do not overlap with, without
+ * meaning for a single row; q, k and v may be slices of one [total_tokens][Hq + 2 Hkv][head_dim] array.  Outputs are contiguous.
+ * total_tokens <= 2^30; 0 is legal and launches nothing.  Pointers of bf16 rows are 16-byte aligned. */
+
+/* puzzle_kv_append_rope for packed tokens (same passages, same arithmetic, the same bytes in the cache), with the rotated keys
+ * given out as bf16 too, for the attention of a prompt over its own keys.  Token i of sequence b lands at place
+ * seq_lens[b] - n_b + i of its cache, n_b = starts[b + 1] - starts[b], seq_lens counted AFTER the append.
+ *   rope: NULL for tokens that arrive rotated, or of a model without: then qkv->q, q_out and k_out have to be NULL;
+ *   q_out: device bf16 [total_tokens][num_q_heads][head_dim], required when qkv->q is given; may be qkv->q itself if that is
+ *     contiguous.  k_out: device bf16 [total_tokens][num_kv_heads][head_dim] or NULL; likewise.  A bad block-table entry
+ *     skips the token in the cache only; tokens that are skipped altogether (see puzzle_kv_append_rope) leave their rows as they were;
+ *   the sequence strides of qkv mean nothing.  Errors and dev_status as puzzle_kv_append_rope. */
+PUZZLE_API puzzle_status puzzle_kv_append_packed(const puzzle_layer_desc* desc, const puzzle_kv_view* kv,
+                                 const puzzle_rope* rope, const puzzle_qkv* qkv, void* q_out, void* k_out,
+                                 const int32_t* starts, int32_t batch, int32_t total_tokens, int32_t* dev_status,
+                                 void* stream);
+
+/* Attention of whole prompts over their own packed keys and values: token i of sequence b is one decode step of
+ * puzzle_decode_attn (same formula, sinks and window) over the tokens [i + 1 - min(W, i + 1), i] of its sequence (all of [0, i]
+ * when window == 0), which are read as they are, in bf16, not from a cache.  (Paper: the input half of the fixed-length
+ * scenarios, Section "Optimized Scenarios"; window layers, Section "Window attention for long-context inference".)  Computed on
+ * the 5th-generation tensor cores in one pass, softmax weights rounded to bf16 and everything else held in float32; bound by
+ * the exponentials.
+ *   qkv: packed rows; sinks: float32 [num_q_heads] or NULL; out: bf16 [total_tokens][num_q_heads][head_dim]; lse_out: float32
+ *   [total_tokens][num_q_heads] or NULL.  desc->kv_dtype has no meaning here.  Unlike the balanced schedules, two calls on the same
+ *   inputs give the same bits. */
+PUZZLE_API puzzle_status puzzle_prompt_attn(const puzzle_layer_desc* desc, const puzzle_qkv* qkv, const int32_t* starts,
+                                 const float* sinks, void* out, float* lse_out, int32_t batch, int32_t total_tokens,
+                                 int32_t* dev_status, void* stream);
+
+/* Attention of chunks of new tokens over the paged cache (E4M3, bf16 or 4-bit), after their append: pieces of long prompts,
+ * drafted tokens, single tokens, in any mixture.  The n_b packed tokens of sequence b are its last ones: token i sits at
+ * position p = seq_lens[b] - n_b + i and sees the keys [p + 1 - min(W, p + 1), p], as in puzzle_decode_attn_tokens, which
+ * is the better call for up to four tokens per sequence over an E4M3 or 4-bit cache; this one shares a pass over the cache
+ * among 16 or 32 tokens and has no bound on them.  (Same passages as puzzle_prompt_attn and puzzle_decode_attn_tokens.)
+ *   q: packed rows of bf16, stride q_token_stride; out, lse_out, sinks as puzzle_prompt_attn;
+ *   workspace: at least puzzle_chunk_attn_workspace_bytes(...) bytes, 16-byte aligned; it needs no preparation, its size is the
+ *     same for every batch and total_tokens, and nothing in it lasts from call to call.  Calls that share one must not overlap on
+ *     the GPU;
+ *   a token whose position is negative sees no key: out = 0, lse = sink.  A sequence longer than its table row is clamped to it
+ *   (PUZZLE_DEV_SEQ_TOO_LONG); keys behind a bad block-table entry count as zeros (PUZZLE_DEV_BAD_BLOCK).
+ * Softmax weights are held in bf16 over a bf16 cache (off by 2^-8 of themselves at most) and in f16 over the others (2^-11, down to
+ * 2^-25 of the largest, 2^-36 of that below).  Two calls on the same inputs give the same bits. */
+PUZZLE_API size_t puzzle_chunk_attn_workspace_bytes(const puzzle_layer_desc* desc, int32_t batch, int32_t total_tokens);
+PUZZLE_API puzzle_status puzzle_chunk_attn(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const void* q,
+                                 int64_t q_token_stride, const int32_t* starts, const float* sinks, void* out,
+                                 float* lse_out, int32_t batch, int32_t total_tokens, void* workspace,
+                                 size_t workspace_bytes, int32_t* dev_status, void* stream);
 
 /* Cached tokens back as bf16, dequantised: the last read_lens[b] tokens of every sequence, token i from place
  * seq_lens[b] - read_lens[b] + i.  For the attention of a prompt chunk over its own rounded keys and values, for a cache

@@ -25,6 +25,7 @@ DEV_BAD_BLOCK = 1
 DEV_SEQ_TOO_LONG = 2
 DEV_WAIT_EXPIRED = 4
 DEV_BAD_POSITION = 8
+DEV_BAD_STARTS = 16
 STATIC_SCRATCH_BYTES = 8 << 20
 SCHED_AUTO, SCHED_CTA, SCHED_WARP = 0, -1, -2      # num_splits values that select the balanced schedule
 
@@ -34,6 +35,10 @@ EXPORTS = (
     "puzzle_kv_append",
     "puzzle_kv_append_tokens",
     "puzzle_kv_append_rope",
+    "puzzle_kv_append_packed",
+    "puzzle_prompt_attn",
+    "puzzle_chunk_attn",
+    "puzzle_chunk_attn_workspace_bytes",
     "puzzle_kv_read_tokens",
     "puzzle_decode_attn_workspace_bytes",
     "puzzle_decode_attn_workspace_init",
@@ -124,6 +129,16 @@ def _load():
         lib.puzzle_kv_read_tokens.restype = ctypes.c_int
         lib.puzzle_kv_read_tokens.argtypes = [ctypes.POINTER(LayerDesc), ctypes.POINTER(KVView), vp, vp, vp, i32, i32,
                                               vp, vp]
+        lib.puzzle_kv_append_packed.restype = ctypes.c_int
+        lib.puzzle_kv_append_packed.argtypes = [ctypes.POINTER(LayerDesc), ctypes.POINTER(KVView), ctypes.POINTER(Rope),
+                                                ctypes.POINTER(QKV), vp, vp, vp, i32, i32, vp, vp]
+        lib.puzzle_prompt_attn.restype = ctypes.c_int
+        lib.puzzle_prompt_attn.argtypes = [ctypes.POINTER(LayerDesc), ctypes.POINTER(QKV), vp, vp, vp, vp, i32, i32, vp, vp]
+        lib.puzzle_chunk_attn_workspace_bytes.restype = sz
+        lib.puzzle_chunk_attn_workspace_bytes.argtypes = [ctypes.POINTER(LayerDesc), i32, i32]
+        lib.puzzle_chunk_attn.restype = ctypes.c_int
+        lib.puzzle_chunk_attn.argtypes = [ctypes.POINTER(LayerDesc), ctypes.POINTER(KVView), vp, ctypes.c_int64, vp, vp, vp, vp,
+                                          i32, i32, vp, sz, vp, vp]
         lib.puzzle_decode_attn_workspace_bytes.restype = sz
         lib.puzzle_decode_attn_workspace_bytes.argtypes = [ctypes.POINTER(LayerDesc), i32, i32]
         lib.puzzle_decode_attn_workspace_init.restype = ctypes.c_int
@@ -171,7 +186,8 @@ def _load():
 
 # The entry points of the native module, in the order of its Entries.
 _CALLS = ("puzzle_kv_append", "puzzle_kv_append_tokens", "puzzle_kv_append_rope", "puzzle_kv_read_tokens",
-          "puzzle_decode_attn", "puzzle_decode_attn_tcgen05", "puzzle_decode_attn_tokens")
+          "puzzle_decode_attn", "puzzle_decode_attn_tcgen05", "puzzle_decode_attn_tokens", "puzzle_kv_append_packed",
+          "puzzle_prompt_attn", "puzzle_chunk_attn")
 
 
 def _bind(lib):
@@ -413,6 +429,39 @@ def puzzle_kv_read_tokens(desc: LayerDesc, view: KVView, k_out: torch.Tensor, v_
                           stream=None) -> None:
     """k_out, v_out: bf16 [batch][n_read][Hkv][D]; read_lens: int32 [batch] or None (n_read tokens of every sequence)."""
     _check(_native().kv_read_tokens(desc, view, k_out, v_out, read_lens, dev_status, stream), "puzzle_kv_read_tokens")
+
+
+def puzzle_kv_append_packed(desc: LayerDesc, view: KVView, rope: Optional[Rope], q: Optional[torch.Tensor],
+                            k_new: torch.Tensor, v_new: torch.Tensor, starts: torch.Tensor,
+                            q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                            dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """q, k_new, v_new: bf16 [tokens][heads][D], the tokens of all sequences behind each other, contiguous or slices of a
+    wider array along the heads; starts: int32 [batch + 1]; q_out, k_out: the rotated rows, bf16, contiguous; rope None: k and v
+    go into the cache as they are, and q, q_out and k_out have to be None."""
+    _check(_native().kv_append_packed(desc, view, rope, q, k_new, v_new, starts, q_out, k_out, dev_status, stream),
+           "puzzle_kv_append_packed")
+
+
+def puzzle_prompt_attn(desc: LayerDesc, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor,
+                       sinks: Optional[torch.Tensor], out: torch.Tensor, lse_out: Optional[torch.Tensor] = None,
+                       dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Causal attention of whole prompts over their own keys.  q, k, v: bf16 [tokens][heads][D] as for
+    puzzle_kv_append_packed; starts: int32 [batch + 1]; out: bf16 [tokens][Hq][D]; lse_out: float32 [tokens][Hq] or None."""
+    _check(_native().prompt_attn(desc, q, k, v, starts, sinks, out, lse_out, dev_status, stream), "puzzle_prompt_attn")
+
+
+def puzzle_chunk_attn_workspace_bytes(desc: LayerDesc, batch: int, total_tokens: int) -> int:
+    return int(_load().puzzle_chunk_attn_workspace_bytes(ctypes.byref(desc), int(batch), int(total_tokens)))
+
+
+def puzzle_chunk_attn(desc: LayerDesc, view: KVView, q: torch.Tensor, starts: torch.Tensor, sinks: Optional[torch.Tensor],
+                      out: torch.Tensor, lse_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Causal attention of the last tokens of every sequence over its cache.  q: bf16 [tokens][Hq][D], packed; starts: int32
+    [batch + 1]; out, lse_out as for puzzle_prompt_attn; see include/puzzle_attn.h."""
+    if workspace is None:
+        raise ValueError("a workspace tensor is required (see puzzle_chunk_attn_workspace_bytes)")
+    _check(_native().chunk_attn(desc, view, q, starts, sinks, out, lse_out, workspace, dev_status, stream), "puzzle_chunk_attn")
 
 
 def puzzle_decode_attn_tokens_workspace_bytes(desc: LayerDesc, batch: int, n_q: int) -> int:

@@ -6,6 +6,7 @@
 
 #include "common.cuh"
 #include "decode_attn.cuh"
+#include "prompt_attn.cuh"
 
 namespace puzzle {
 
@@ -56,6 +57,7 @@ struct DeviceInfo {
   // dynamic shared-memory limits already set per kernel and cache type; 0 = not raised yet
   int smem_warp[3] = {}, smem_cta[2] = {}, smem_small[3] = {};
   int smem_tc = 0, smem_tokens = 0, smem_group[10] = {}, smem_tokens_group[10] = {};
+  int smem_prompt[4] = {};
 };
 DeviceInfo& device_info() {
   static DeviceInfo info[64];
@@ -298,6 +300,57 @@ size_t pair_parts_bytes(size_t pairs, int kv_dtype) { return kv_dtype == PUZZLE_
 
 }  // namespace
 
+namespace {
+
+// Rows [tokens][heads][64] of bf16 as the prompt kernel fetches them: box of `box_heads` heads of `box_tokens` tokens, 128 bytes
+// a row, 128-byte swizzle; rows behind the last token read as zeros.
+bool make_rows_map(CUtensorMap* m, const void* base, int heads, int tokens, int64_t token_stride, int box_heads, int box_tokens) {
+  EncodeTiledFn enc = encode_tiled();
+  if (!enc) return false;
+  const cuuint64_t dims[3] = {kHeadDim, (cuuint64_t)heads, (cuuint64_t)tokens};
+  const int64_t stride = tokens > 1 ? token_stride : (int64_t)heads * kHeadDim;   // without meaning for one token
+  const cuuint64_t strides[2] = {kHeadDim * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[3] = {kHeadDim, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int kMaxPacked = 1 << 30;   // rows of a packed array
+// Stride between the packed rows of `heads` heads: rows do not overlap and are fetched 16 bytes at a time.
+bool packed_stride_ok(int64_t stride, int heads, int total) {
+  return total <= 1 || (stride >= (int64_t)heads * kHeadDim && stride % 8 == 0 && stride < (1ll << 38));
+}
+puzzle_status check_packed(const puzzle_layer_desc* d, const int32_t* starts, int batch, int total) {
+  const puzzle_status st = check_desc(d);
+  if (st != PUZZLE_OK) return st;
+  if (!starts) return PUZZLE_ERR_NULL;
+  if (batch <= 0 || total < 0 || total > kMaxPacked) return PUZZLE_ERR_SHAPE;
+  return batch > kMaxBatch ? PUZZLE_ERR_UNSUPPORTED : PUZZLE_OK;
+}
+
+// What both kinds of prompt attention are given.
+PromptParams prompt_params(const puzzle_layer_desc* d, const int32_t* starts, const float* sinks, void* out, float* lse_out,
+                           int batch, int total, int32_t* dev_status) {
+  PromptParams P;
+  std::memset(&P, 0, sizeof P);
+  P.starts = starts;
+  P.sinks = sinks;
+  P.out = static_cast<__nv_bfloat16*>(out);
+  P.lse_out = lse_out;
+  P.dev_status = dev_status;
+  P.batch = batch;
+  P.total = total;
+  P.Hkv = d->num_kv_heads;
+  P.window = std::min(d->window, 1 << 30);   // no position is beyond that
+  P.splits = 1;
+  P.sm_scale_log2e = d->sm_scale * 1.4426950408889634f;
+  return P;
+}
+
+}  // namespace
+
 // Everything about a decode-attention call that the host can check, short of the workspace.
 puzzle_status check_decode_attn_args(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const void* q,
                                      const void* out, int batch, int num_splits, bool tcgen05) {
@@ -476,6 +529,122 @@ puzzle_status puzzle_kv_read_tokens(const puzzle_layer_desc* desc, const puzzle_
   R.max_blocks_per_seq = kv->max_blocks_per_seq;
   const cudaError_t e = launch_read_tokens(R, desc->kv_dtype, static_cast<cudaStream_t>(stream));
   count_launch();
+  return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
+}
+
+puzzle_status puzzle_kv_append_packed(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const puzzle_rope* rope,
+                                      const puzzle_qkv* qkv, void* q_out, void* k_out, const int32_t* starts, int32_t batch,
+                                      int32_t total_tokens, int32_t* dev_status, void* stream) {
+  puzzle_status st = check_packed(desc, starts, batch, total_tokens);
+  if (st != PUZZLE_OK) return st;
+  st = check_view(desc, kv, batch);
+  if (st != PUZZLE_OK) return st;
+  if (!qkv || (rope && !rope->cos_sin)) return PUZZLE_ERR_NULL;
+  if (!rope && (qkv->q || q_out || k_out)) return PUZZLE_ERR_SHAPE;   // what is not rotated needs no other place
+  if (rope) {
+    if (rope->num_positions <= 0 || rope->rotary_dim <= 0 || rope->rotary_dim > desc->head_dim) return PUZZLE_ERR_SHAPE;
+    if (rope->rotary_dim % 16) return PUZZLE_ERR_UNSUPPORTED;
+    if (!aligned16(rope->cos_sin)) return PUZZLE_ERR_SHAPE;
+  }
+  if (desc->num_kv_heads > kMaxAppendHeads) return PUZZLE_ERR_UNSUPPORTED;
+  if (total_tokens == 0) return PUZZLE_OK;
+  if (!qkv->k || !qkv->v || (qkv->q && !q_out)) return PUZZLE_ERR_NULL;
+  if (!aligned16(qkv->q) || !aligned16(qkv->k) || !aligned16(qkv->v) || (qkv->q && !aligned16(q_out)) || !aligned16(k_out))
+    return PUZZLE_ERR_SHAPE;
+  const int Hq = desc->num_q_heads, Hkv = desc->num_kv_heads;
+  if (!packed_stride_ok(qkv->k_token_stride, Hkv, total_tokens) || !packed_stride_ok(qkv->v_token_stride, Hkv, total_tokens) ||
+      (qkv->q && !packed_stride_ok(qkv->q_token_stride, Hq, total_tokens)))
+    return PUZZLE_ERR_SHAPE;
+  // in place: every row has to lie where its rotated form goes, or one row would overwrite another before it is read
+  if (total_tokens > 1 && ((qkv->q && q_out == qkv->q && qkv->q_token_stride != (int64_t)Hq * kHeadDim) ||
+                           (k_out == qkv->k && qkv->k_token_stride != (int64_t)Hkv * kHeadDim)))
+    return PUZZLE_ERR_SHAPE;
+  AppendParams A = append_params(desc, kv, batch, 0, nullptr, dev_status);
+  A.q = static_cast<const __nv_bfloat16*>(qkv->q);
+  A.k = static_cast<const __nv_bfloat16*>(qkv->k);
+  A.v = static_cast<const __nv_bfloat16*>(qkv->v);
+  A.q_token_stride = qkv->q_token_stride;
+  A.k_token_stride = qkv->k_token_stride;
+  A.v_token_stride = qkv->v_token_stride;
+  A.q_out = static_cast<__nv_bfloat16*>(q_out);
+  A.k_out = static_cast<__nv_bfloat16*>(k_out);
+  A.starts = starts;
+  A.total = total_tokens;
+  if (rope) {
+    A.pos_offset = rope->pos_offset;
+    A.cos_sin = rope->cos_sin;
+    A.num_positions = rope->num_positions;
+    A.rotary = rope->rotary_dim;
+  }
+  const cudaError_t e =
+      launch_append(A, desc->kv_dtype, rope != nullptr, rope && rope->interleaved != 0, static_cast<cudaStream_t>(stream));
+  count_launch();
+  return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
+}
+
+puzzle_status puzzle_prompt_attn(const puzzle_layer_desc* desc, const puzzle_qkv* qkv, const int32_t* starts,
+                                 const float* sinks, void* out, float* lse_out, int32_t batch, int32_t total_tokens,
+                                 int32_t* dev_status, void* stream) {
+  const puzzle_status st = check_packed(desc, starts, batch, total_tokens);
+  if (st != PUZZLE_OK) return st;
+  if (!qkv) return PUZZLE_ERR_NULL;
+  if (total_tokens == 0) return PUZZLE_OK;
+  if (!qkv->q || !qkv->k || !qkv->v || !out) return PUZZLE_ERR_NULL;
+  if (!aligned16(qkv->q) || !aligned16(qkv->k) || !aligned16(qkv->v) || !aligned16(out)) return PUZZLE_ERR_SHAPE;
+  const int Hq = desc->num_q_heads, Hkv = desc->num_kv_heads;
+  if (!packed_stride_ok(qkv->q_token_stride, Hq, total_tokens) || !packed_stride_ok(qkv->k_token_stride, Hkv, total_tokens) ||
+      !packed_stride_ok(qkv->v_token_stride, Hkv, total_tokens))
+    return PUZZLE_ERR_SHAPE;
+  PromptParams P = prompt_params(desc, starts, sinks, out, lse_out, batch, total_tokens, dev_status);
+  P.v = static_cast<const __nv_bfloat16*>(qkv->v);
+  P.v_token_stride = qkv->v_token_stride;
+  if (!make_rows_map(&P.tmQ, qkv->q, Hq, total_tokens, qkv->q_token_stride, kGroup, 16) ||
+      !make_rows_map(&P.tmK, qkv->k, Hkv, total_tokens, qkv->k_token_stride, 1, 128) ||
+      !make_rows_map(&P.tmV, qkv->v, Hkv, total_tokens, qkv->v_token_stride, 1, 128))
+    return PUZZLE_ERR_CUDA;
+  P.narrow = prompt_plan(batch, total_tokens, Hkv, 0, false, grid_ctas()).narrow;
+  const cudaError_t e = launch_prompt_attn(P, kSrcPacked, grid_ctas(), static_cast<cudaStream_t>(stream), device_info().smem_prompt);
+  return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
+}
+
+size_t puzzle_chunk_attn_workspace_bytes(const puzzle_layer_desc* desc, int32_t batch, int32_t total_tokens) {
+  if (check_desc(desc) != PUZZLE_OK || batch <= 0 || batch > kMaxBatch || total_tokens < 0 || total_tokens > kMaxPacked) return 0;
+  return prompt_partial_bytes(grid_ctas(), desc->num_kv_heads);
+}
+
+puzzle_status puzzle_chunk_attn(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const void* q, int64_t q_token_stride,
+                                const int32_t* starts, const float* sinks, void* out, float* lse_out, int32_t batch,
+                                int32_t total_tokens, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                                void* stream) {
+  puzzle_status st = check_packed(desc, starts, batch, total_tokens);
+  if (st != PUZZLE_OK) return st;
+  st = check_view(desc, kv, batch);
+  if (st != PUZZLE_OK) return st;
+  if (!workspace || workspace_bytes < puzzle_chunk_attn_workspace_bytes(desc, batch, total_tokens) || !aligned16(workspace))
+    return PUZZLE_ERR_WORKSPACE;
+  if (total_tokens == 0) return PUZZLE_OK;
+  if (!q || !out) return PUZZLE_ERR_NULL;
+  if (!aligned16(q) || !aligned16(out) || !packed_stride_ok(q_token_stride, desc->num_q_heads, total_tokens))
+    return PUZZLE_ERR_SHAPE;
+  PromptParams P = prompt_params(desc, starts, sinks, out, lse_out, batch, total_tokens, dev_status);
+  P.k_cache = kv->k_cache;
+  P.v_cache = kv->v_cache;
+  P.block_table = kv->block_table;
+  P.seq_lens = kv->seq_lens;
+  P.k_scale = kv->k_scale;
+  P.v_scale = kv->v_scale;
+  P.num_blocks = kv->num_blocks;
+  P.max_blocks_per_seq = kv->max_blocks_per_seq;
+  if (!make_rows_map(&P.tmQ, q, desc->num_q_heads, total_tokens, q_token_stride, kGroup, 16)) return PUZZLE_ERR_CUDA;
+  long long keys = (long long)kv->max_blocks_per_seq * kBlock;
+  if (desc->window > 0) keys = std::min<long long>(keys, (long long)desc->window + 2 * kBlock);
+  const PromptPlan plan = prompt_plan(batch, total_tokens, P.Hkv, keys, true, grid_ctas());
+  P.narrow = plan.narrow;
+  P.splits = plan.splits;
+  P.part_o = static_cast<float*>(workspace);
+  P.part_lse = P.part_o + (size_t)plan.splits * total_tokens * desc->num_q_heads * kHeadDim;
+  const PromptSource src = desc->kv_dtype == PUZZLE_KV_FP8_E4M3 ? kSrcFp8 : (desc->kv_dtype == PUZZLE_KV_BF16 ? kSrcBf16 : kSrcFp4);
+  const cudaError_t e = launch_prompt_attn(P, src, grid_ctas(), static_cast<cudaStream_t>(stream), device_info().smem_prompt);
   return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
 }
 

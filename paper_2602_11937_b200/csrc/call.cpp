@@ -23,6 +23,9 @@ struct Entries {
   decltype(&puzzle_decode_attn) decode_attn;
   decltype(&puzzle_decode_attn_tcgen05) decode_attn_tcgen05;
   decltype(&puzzle_decode_attn_tokens) decode_attn_tokens;
+  decltype(&puzzle_kv_append_packed) kv_append_packed;
+  decltype(&puzzle_prompt_attn) prompt_attn;
+  decltype(&puzzle_chunk_attn) chunk_attn;
 } entry;
 constexpr Py_ssize_t kEntries = sizeof(Entries) / sizeof(void*);
 
@@ -391,6 +394,113 @@ PyObject* decode_attn_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Packed rows [tokens][heads][D]: every dimension as expected (all inputs of a call before any pointer is taken).
+void check_packed(PyObject* o, const char* name, int64_t tokens, int heads, int row) {
+  const at::Tensor& t = tensor(o, name);
+  if (t.dim() != 3 || t.size(0) != tokens || t.size(1) != heads || t.size(2) != row)
+    refuse(std::string(name) + " must be " + shape_text({tokens, heads, row}) + ", got " + shape_text(t.sizes()));
+}
+// Pointer and token stride of an input's packed rows.
+Rows packed_rows(Here& here, PyObject* o, const char* name, int row) {
+  Rows r = rows(here, tensor(o, name), name, row);
+  r.token_stride = r.seq_stride;
+  r.seq_stride = 0;
+  return r;
+}
+// A contiguous packed array [tokens][heads][D].
+void* packed_out(Here& here, PyObject* o, const char* name, int64_t tokens, int heads, int row) {
+  if (o == Py_None) return nullptr;
+  check_packed(o, name, tokens, heads, row);
+  return pointer(here, o, name, at::kBFloat16, 0);
+}
+int packed_batch(const at::Tensor& starts) {
+  if (starts.dim() != 1 || starts.size(0) < 2) refuse("starts must have one element more than there are sequences");
+  if (starts.size(0) - 1 > INT_MAX) refuse("a dimension does not fit 32 bits");
+  return (int)(starts.size(0) - 1);
+}
+
+// desc, view, rope, q, k_new, v_new, starts, q_out, k_out, dev_status, stream
+PyObject* kv_append_packed(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call("kv_append_packed", n, 11, [&](Here& here) {
+    const auto desc = structure<puzzle_layer_desc>(a[0]);
+    const auto view = structure<puzzle_kv_view>(a[1]);
+    puzzle_rope rope = {};
+    const bool rotate = a[2] != Py_None, with_q = a[3] != Py_None;
+    if (rotate) rope = structure<puzzle_rope>(a[2]);
+    if (with_q != (a[7] != Py_None)) refuse("q and q_out go together");
+    const at::Tensor& k = tensor(a[4], "k_new");
+    if (k.dim() != 3) refuse("k_new must be [tokens][heads][D]");
+    const int tokens = extent(k, 0), batch = packed_batch(tensor(a[6], "starts"));
+    check_view(here, a[1], desc, view, batch);
+    if (rotate) check_rope(here, a[2], batch);
+    check_packed(a[4], "k_new", tokens, desc.num_kv_heads, desc.head_dim);
+    check_packed(a[5], "v_new", tokens, desc.num_kv_heads, desc.head_dim);
+    if (with_q) check_packed(a[3], "q", tokens, desc.num_q_heads, desc.head_dim);
+    const Rows kr = packed_rows(here, a[4], "k_new", desc.head_dim), vr = packed_rows(here, a[5], "v_new", desc.head_dim);
+    const Rows qr = with_q ? packed_rows(here, a[3], "q", desc.head_dim) : Rows{nullptr, 0, 0};
+    const puzzle_qkv qkv = {qr.p, kr.p, vr.p, 0, qr.token_stride, 0, kr.token_stride, 0, vr.token_stride};
+    const int32_t* starts = pointer_to<int32_t>(here, a[6], "starts", at::kInt, 2);
+    void* q_out = packed_out(here, a[7], "q_out", tokens, desc.num_q_heads, desc.head_dim);
+    void* k_out = packed_out(here, a[8], "k_out", tokens, desc.num_kv_heads, desc.head_dim);
+    int32_t* status = pointer_to<int32_t>(here, a[9], "dev_status", at::kInt, 1);
+    void* s = stream_of(here, a[10]);
+    return unlocked([&] {
+      return entry.kv_append_packed(&desc, &view, rotate ? &rope : nullptr, &qkv, q_out, k_out, starts, batch, tokens, status, s);
+    });
+  });
+}
+
+// desc, q, k, v, starts, sinks, out, lse_out, dev_status, stream
+PyObject* prompt_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call("prompt_attn", n, 10, [&](Here& here) {
+    const auto desc = structure<puzzle_layer_desc>(a[0]);
+    const at::Tensor& t = tensor(a[1], "q");
+    if (t.dim() != 3) refuse("q must be [tokens][heads][D]");
+    const int tokens = extent(t, 0), batch = packed_batch(tensor(a[4], "starts"));
+    check_packed(a[1], "q", tokens, desc.num_q_heads, desc.head_dim);
+    check_packed(a[2], "k", tokens, desc.num_kv_heads, desc.head_dim);
+    check_packed(a[3], "v", tokens, desc.num_kv_heads, desc.head_dim);
+    const Rows qr = packed_rows(here, a[1], "q", desc.head_dim), kr = packed_rows(here, a[2], "k", desc.head_dim);
+    const Rows vr = packed_rows(here, a[3], "v", desc.head_dim);
+    const puzzle_qkv qkv = {qr.p, kr.p, vr.p, 0, qr.token_stride, 0, kr.token_stride, 0, vr.token_stride};
+    const int32_t* starts = pointer_to<int32_t>(here, a[4], "starts", at::kInt, 2);
+    const float* sinks = pointer_to<float>(here, a[5], "sinks", at::kFloat, q_heads(desc));
+    if (a[6] == Py_None) refuse("out is required");
+    void* out = packed_out(here, a[6], "out", tokens, desc.num_q_heads, desc.head_dim);
+    float* lse = pointer_to<float>(here, a[7], "lse_out", at::kFloat, tokens * q_heads(desc));
+    int32_t* status = pointer_to<int32_t>(here, a[8], "dev_status", at::kInt, 1);
+    void* s = stream_of(here, a[9]);
+    return unlocked([&] { return entry.prompt_attn(&desc, &qkv, starts, sinks, out, lse, batch, tokens, status, s); });
+  });
+}
+
+// desc, view, q, starts, sinks, out, lse_out, workspace, dev_status, stream
+PyObject* chunk_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call("chunk_attn", n, 10, [&](Here& here) {
+    const auto desc = structure<puzzle_layer_desc>(a[0]);
+    const auto view = structure<puzzle_kv_view>(a[1]);
+    const at::Tensor &t = tensor(a[2], "q"), &w = tensor(a[7], "workspace");
+    if (t.dim() != 3) refuse("q must be [tokens][heads][D]");
+    const int tokens = extent(t, 0), batch = packed_batch(tensor(a[3], "starts"));
+    check_view(here, a[1], desc, view, batch);
+    check_packed(a[2], "q", tokens, desc.num_q_heads, desc.head_dim);
+    const Rows qr = packed_rows(here, a[2], "q", desc.head_dim);
+    const int32_t* starts = pointer_to<int32_t>(here, a[3], "starts", at::kInt, 2);
+    const float* sinks = pointer_to<float>(here, a[4], "sinks", at::kFloat, q_heads(desc));
+    if (a[5] == Py_None) refuse("out is required");
+    void* out = packed_out(here, a[5], "out", tokens, desc.num_q_heads, desc.head_dim);
+    float* lse = pointer_to<float>(here, a[6], "lse_out", at::kFloat, tokens * q_heads(desc));
+    void* workspace = pointer(here, a[7], "workspace", at::kByte, 0);   // the library checks its size
+    const size_t bytes = w.nbytes();
+    int32_t* status = pointer_to<int32_t>(here, a[8], "dev_status", at::kInt, 1);
+    void* s = stream_of(here, a[9]);
+    return unlocked([&] {
+      return entry.chunk_attn(&desc, &view, qr.p, qr.token_stride, starts, sinks, out, lse, batch, tokens, workspace, bytes,
+                              status, s);
+    });
+  });
+}
+
 // name, device of a tensor, current device: the check every tensor of every call goes through, for tests without two GPUs.
 PyObject* check_device(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call("check_device", n, 3, [&](Here&) {
@@ -405,7 +515,7 @@ using Fast = PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t);
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(static_cast<Fast>(name))), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind),           METHOD(kv_append),   METHOD(kv_append_tokens),    METHOD(kv_append_rope),
                          METHOD(kv_read_tokens), METHOD(decode_attn), METHOD(decode_attn_tcgen05), METHOD(decode_attn_tokens),
-                         METHOD(check_device),
+                         METHOD(kv_append_packed), METHOD(prompt_attn), METHOD(chunk_attn), METHOD(check_device),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_puzzle_call", nullptr, -1, methods};
 

@@ -129,6 +129,10 @@ struct AppendParams {
   int32_t* dev_status;
   long long num_blocks, num_positions;
   int batch, n_new, Hq, Hkv, max_blocks_per_seq, rotary;
+  // packed tokens (n_new and the sequence strides mean nothing then)
+  const int32_t* starts;
+  __nv_bfloat16* k_out;
+  int total;
 };
 cudaError_t launch_append(const AppendParams& P, int kv_dtype, bool rotate, bool adjacent, cudaStream_t s);
 

@@ -16,6 +16,8 @@
 //    aligned to four so that the two tokens that share V's bytes in a 4-bit block are in one warp.
 //  * step kernel (one token per sequence): a group of eight lanes takes one (sequence, head), nothing is shared, the
 //    launch is one chain of loads.
+#include <algorithm>
+
 #include "common.cuh"
 #include "decode_attn.cuh"
 #include "kv_fp4.cuh"
@@ -146,10 +148,9 @@ struct Span {
   int first, count;
   bool ok;
 };
-__device__ __forceinline__ Span span_of(const AppendParams& P, int b, bool reporter) {
+__device__ __forceinline__ Span span_from(const AppendParams& P, int len, int count, int b, bool reporter) {
   Span sp;
-  const int len = P.seq_lens[b];
-  sp.count = P.new_lens ? min(max(P.new_lens[b], 0), P.n_new) : P.n_new;
+  sp.count = count;
   sp.first = len - sp.count;
   sp.ok = len > 0 && sp.count > 0;
   if (len > P.max_blocks_per_seq * kBlock) {
@@ -157,6 +158,44 @@ __device__ __forceinline__ Span span_of(const AppendParams& P, int b, bool repor
     sp.ok = false;
   }
   return sp;
+}
+__device__ __forceinline__ Span span_of(const AppendParams& P, int b, bool reporter) {
+  return span_from(P, P.seq_lens[b], P.new_lens ? min(max(P.new_lens[b], 0), P.n_new) : P.n_new, b, reporter);
+}
+
+// Packed tokens: sequence b has (tokens + 34) / 32 groups of 32 places (up to three of them before its first token, so that
+// groups start at a multiple of four places).  The sequence of group `at`, its first row and its tokens; false: there is none.
+// All lanes of the warp call it.
+__device__ __forceinline__ bool find_packed(const AppendParams& P, int at, int& b, int& group, int& start, int& count,
+                                            bool reporter) {
+  const int lane = threadIdx.x & 31;
+  for (int b0 = 0, before = 0; b0 < P.batch; b0 += 32) {
+    int st = 0, n = 0;
+    if (b0 + lane < P.batch) {
+      st = P.starts[b0 + lane];
+      const int en = P.starts[b0 + lane + 1];
+      if (st >= 0 && en >= st && en <= P.total) n = en - st;
+      else if (P.dev_status && reporter) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_STARTS);
+    }
+    const int groups = n > 0 ? (n + 34) / 32 : 0;
+    int upto = groups;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += u;
+    }
+    const uint32_t behind = __ballot_sync(0xffffffffu, before + upto > at);
+    if (behind) {
+      const int src = __ffs(behind) - 1;
+      b = b0 + src;
+      group = at - before - __shfl_sync(0xffffffffu, upto - groups, src);
+      start = __shfl_sync(0xffffffffu, st, src);
+      count = __shfl_sync(0xffffffffu, n, src);
+      return true;
+    }
+    before += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  return false;
 }
 
 // The table row of position `pos` of sequence b, or null (flagged) when the table has none.
@@ -228,11 +267,14 @@ constexpr int kHeadsPerWarp = 8;
 
 // Four blocks of 64 registers per SM where the codes are computed (three of 80: 108.5 against 102.4 us into the E4M3 cache,
 // 116 against 111 into the 4-bit one); the bf16 copy has its loads in flight with three (103.5 against 104.7).
-template <int KV, int ROT>
+// PACKED: the tokens of all sequences lie behind each other (starts), a block finds the sequence of its 32 tokens itself.
+template <int KV, int ROT, bool PACKED>
 __global__ void __launch_bounds__(256, KV == PUZZLE_KV_BF16 ? 3 : 4) kv_append_chunk_kernel(const AppendParams P) {
   grid_dependency_wait();   // no early release, for the reason given in kv_append_kernel
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, o = lane & 7;
-  const int b = blockIdx.z;
+  int b = blockIdx.z, group = blockIdx.x;
+  long long first_row = 0;   // packed: row of the sequence's first token
+  Span sp;
   const int kv_jobs = (P.Hkv + kHeadsPerWarp - 1) / kHeadsPerWarp;
   // keys, then values, then the query heads: the last blocks of the launch are quick ones (4 % at 16 x 2048 tokens)
   int job = blockIdx.y;
@@ -240,9 +282,16 @@ __global__ void __launch_bounds__(256, KV == PUZZLE_KV_BF16 ? 3 : 4) kv_append_c
   job -= is_q ? 2 * kv_jobs : (is_v ? kv_jobs : 0);
   const bool reporter = o == 0 && blockIdx.y == 0;
 
-  const Span sp = span_of(P, b, reporter);
+  if constexpr (PACKED) {
+    int start = 0, count = 0;
+    if (!find_packed(P, group, b, group, start, count, blockIdx.y == 0 && warp == 0)) return;
+    first_row = start;
+    sp = span_from(P, P.seq_lens[b], count, b, reporter);
+  } else {
+    sp = span_of(P, b, reporter);
+  }
   if (!sp.ok) return;
-  const int pos = (max(sp.first, 0) & ~3) + (blockIdx.x * 8 + warp) * 4 + (lane >> 3);
+  const int pos = (max(sp.first, 0) & ~3) + (group * 8 + warp) * 4 + (lane >> 3);
   const int tok = pos - sp.first;
   bool on = pos >= sp.first && tok < sp.count;
   if (!__any_sync(0xffffffffu, on)) return;
@@ -253,16 +302,18 @@ __global__ void __launch_bounds__(256, KV == PUZZLE_KV_BF16 ? 3 : 4) kv_append_c
     if (!is_v) turn.load(on ? row : P.cos_sin, P.rotary, lane);
   }
   const int h0 = job * kHeadsPerWarp, heads = min(kHeadsPerWarp, (is_q ? P.Hq : P.Hkv) - h0);
-  const __nv_bfloat16* src = is_q ? P.q + b * P.q_seq_stride + tok * P.q_token_stride
-                                  : (is_v ? P.v + b * P.v_seq_stride + tok * P.v_token_stride
-                                          : P.k + b * P.k_seq_stride + tok * P.k_token_stride);
+  const long long row_in = PACKED ? first_row + tok : tok, seq_in = PACKED ? 0 : b;
+  const __nv_bfloat16* src = is_q ? P.q + seq_in * P.q_seq_stride + row_in * P.q_token_stride
+                                  : (is_v ? P.v + seq_in * P.v_seq_stride + row_in * P.v_token_stride
+                                          : P.k + seq_in * P.k_seq_stride + row_in * P.k_token_stride);
   const uint4* in = reinterpret_cast<const uint4*>(src + h0 * kHeadDim) + o;
   uint4 raw[kHeadsPerWarp];
 #pragma unroll
   for (int j = 0; j < kHeadsPerWarp; ++j)
     raw[j] = on && j < heads ? __ldcs(in + j * (kHeadDim / 8)) : make_uint4(0, 0, 0, 0);
+  const long long row_out = PACKED ? first_row + tok : (long long)b * P.n_new + tok;
   if (is_q) {
-    uint4* out = reinterpret_cast<uint4*>(P.q_out + (((long long)b * P.n_new + tok) * P.Hq + h0) * kHeadDim) + o;
+    uint4* out = reinterpret_cast<uint4*>(P.q_out + (row_out * P.Hq + h0) * kHeadDim) + o;
 #pragma unroll
     for (int j = 0; j < kHeadsPerWarp; ++j) {
       float x[8];
@@ -271,6 +322,7 @@ __global__ void __launch_bounds__(256, KV == PUZZLE_KV_BF16 ? 3 : 4) kv_append_c
     }
     return;
   }
+  [[maybe_unused]] const bool real = on;   // rotated keys go out whatever the block table says
   long long blk = 0;
   if (on) {
     blk = block_of(P, b, pos, o == 0 && !is_v && job == 0);
@@ -294,6 +346,8 @@ __global__ void __launch_bounds__(256, KV == PUZZLE_KV_BF16 ? 3 : 4) kv_append_c
       if (j >= heads) break;
       float x[8];
       turn.apply(raw[j], x);
+      if constexpr (PACKED && ROT != kNoRotation)
+        if (P.k_out && real) reinterpret_cast<uint4*>(P.k_out + (row_out * P.Hkv + h0 + j) * kHeadDim)[o] = pack8(x);
       Divisor div;
       div.set(KV != PUZZLE_KV_BF16 && P.k_scale ? P.k_scale[h0 + j] : 1.f);
       store8<KV, false, true>(P.k_cache, blk * P.Hkv + h0 + j, slot, o, raw[j], x, div, ROT != kNoRotation, on, pair_on);
@@ -361,22 +415,37 @@ __global__ void __launch_bounds__(128) kv_append_step_kernel(const AppendParams 
   }
 }
 
+// More than the groups of packed tokens are, whatever the lengths: the last block looks at every sequence and finds none.
+static long long packed_groups(const AppendParams& P) { return (P.total + 34ll * std::min(P.batch, P.total)) / 32 + 1; }
+
 template <int KV, int ROT>
 static cudaError_t launch_append_variant(const AppendParams& P, cudaStream_t s) {
   const int hq = P.q ? P.Hq : 0;
+  const int jobs = (hq + kHeadsPerWarp - 1) / kHeadsPerWarp + 2 * ((P.Hkv + kHeadsPerWarp - 1) / kHeadsPerWarp);
+  if (P.starts)
+    return launch_dependent(kv_append_chunk_kernel<KV, ROT, true>, dim3((unsigned)packed_groups(P), (unsigned)jobs), dim3(256), 0,
+                            s, P);
   if (P.n_new == 1) {
     const long long threads = (long long)P.batch * (hq + 2 * P.Hkv) * 8;
     return launch_dependent(kv_append_step_kernel<KV, ROT>, dim3((unsigned)((threads + 127) / 128)), dim3(128), 0, s, P);
   }
-  const int jobs = (hq + kHeadsPerWarp - 1) / kHeadsPerWarp + 2 * ((P.Hkv + kHeadsPerWarp - 1) / kHeadsPerWarp);
   const dim3 grid((unsigned)((P.n_new + 3 + 31) / 32), (unsigned)jobs, (unsigned)P.batch);
-  return launch_dependent(kv_append_chunk_kernel<KV, ROT>, grid, dim3(256), 0, s, P);
+  return launch_dependent(kv_append_chunk_kernel<KV, ROT, false>, grid, dim3(256), 0, s, P);
+}
+
+template <int KV>
+static cudaError_t launch_append_plain_packed(const AppendParams& P, cudaStream_t s) {
+  const int jobs = 2 * ((P.Hkv + kHeadsPerWarp - 1) / kHeadsPerWarp);
+  return launch_dependent(kv_append_chunk_kernel<KV, kNoRotation, true>, dim3((unsigned)packed_groups(P), (unsigned)jobs),
+                          dim3(256), 0, s, P);
 }
 
 template <int KV>
 static cudaError_t launch_append_kv(const AppendParams& P, bool rotate, bool adjacent, cudaStream_t s) {
-  if constexpr (KV == PUZZLE_KV_FP4_E2M1)   // the other types' plain appends are kv_append.cu's
-    if (!rotate) return launch_append_variant<KV, kNoRotation>(P, s);
+  if (!rotate) {
+    if constexpr (KV == PUZZLE_KV_FP4_E2M1) return launch_append_variant<KV, kNoRotation>(P, s);
+    else return launch_append_plain_packed<KV>(P, s);   // rectangles of the other types are kv_append.cu's
+  }
   return adjacent ? launch_append_variant<KV, kAdjacent>(P, s) : launch_append_variant<KV, kHalves>(P, s);
 }
 

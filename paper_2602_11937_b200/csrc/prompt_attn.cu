@@ -1,0 +1,1071 @@
+// Attention of many new tokens per sequence, on the 5th-generation tensor cores: whole prompts over their own packed keys and
+// values, and chunks of new tokens over the paged cache (E4M3, bf16 or 4-bit codes).  Causal, with a window or without,
+// sink logit per query head (paper, Sections "Window attention for long-context inference" and "Optimized Scenarios").
+//
+//     s_j = sm_scale k_scale (q . k_j),  M = max(max_j s_j, sink),  Z = e^(sink - M) + sum_j e^(s_j - M),
+//     out = v_scale sum_j e^(s_j - M) v_j / Z,    j over the keys [p + 1 - W, p] of the token at position p
+//
+// in one pass over the keys with a running maximum and sum.  A tile of rows is 16 tokens x the 8 query heads of one KV head
+// (128 rows, so that one tile of keys serves all of them and a window wastes at most 16 tokens of it), a tile of keys 128.
+//
+//  * Two softmax warpgroups own one tile of rows each: thread = row.  S = Q K^T (128 x 128) goes to tensor memory, the thread
+//    reads its row, and writes the weights P back to tensor memory as the A operand of O += P V, which stays in tensor memory
+//    as well: 2 x (128 columns S, 64 P, 64 O) = all 512 columns.  P has columns of its own, so that the next S is computed
+//    while a row is exponentiated.
+//  * One warp per warpgroup issues its MMAs, one plans the work and loads queries (and packed keys and values) by TMA, one
+//    looks at the values of tiles that not every row sees (below).  Over a cache four more warps fetch the blocks of a tile
+//    through the block table and convert the codes: K to bf16, V to f16, both exact for E4M3 and for E2M1 times its scale.
+//  * Wide groups: 32 tokens, 16 per warpgroup, both reading the same tiles of keys.  Narrow ones (few tokens, or few groups):
+//    16 tokens, the warpgroups take the tiles in turn and join at the end through tensor memory.
+//  * The weights of a bf16 V are bf16 (half a step, 2^-8 of each, the rounding of the output itself); those of a converted V
+//    are f16 (2^-11), scaled by 2^11 so that weights down to 2^-25 of the reference keep all their bits.  The reference is
+//    raised, and O rescaled, only when a row's maximum exceeds it by more than 2^4.  Sums are float32.
+//  * 0 x NaN: a tile of V that some row of the group does not see is searched for infinities and NaN before its product.  They
+//    are replaced by zero, and the rows that do see them get them added at the end, read again from where they come from.
+//
+// Every wait is bounded: one that runs out sets PUZZLE_DEV_WAIT_EXPIRED and a flag upon which every role leaves its loop.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "kv_fp4.cuh"
+#include "prompt_attn.cuh"
+
+namespace puzzle {
+namespace {
+
+constexpr int kRowTokens = 16;              // tokens of a tile of rows
+constexpr int TK = 128;                     // keys of a tile
+constexpr int NBLK = TK / kBlock;
+constexpr int kTileBytes = TK * kHeadDim * 2;
+constexpr int kRing = 4;                    // work records in flight
+constexpr unsigned kFull = 0xffffffffu;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// tensor memory of a warpgroup: S, P, O
+constexpr int kTmemS = 0, kTmemP = 256, kTmemO = 384;
+
+template <int SRC>
+struct Cfg {
+  static constexpr bool kPaged = SRC != kSrcPacked;
+  static constexpr bool kCodes = SRC == kSrcFp8 || SRC == kSrcFp4;
+  static constexpr int kThreads = kPaged ? 512 : 384;
+  static constexpr int kStages = kCodes ? 3 : 5;             // tiles of K and V in the form the MMAs read
+  static constexpr int kBlockBytes = SRC == kSrcFp8 ? kBlock * kHeadDim : (SRC == kSrcFp4 ? kFp4BlockBytes : 0);
+  static constexpr int kCodeTile = 2 * NBLK * kBlockBytes;   // codes of K and V of a tile as they lie in the cache
+  // tiles whose copies are in flight; a bf16 tile is copied to where the MMAs read it, and has to leave two of these places
+  static constexpr int kCopySlots = SRC == kSrcFp8 ? 5 : (SRC == kSrcFp4 ? 8 : 3);
+  static constexpr int kCodeStages = kCodes ? kCopySlots : 0;
+  static constexpr int kFullArrivals = kPaged ? 4 : 1;
+  // register shares of the softmax warpgroups and of the others; launch: 65536 / threads rounded down to 8
+  static constexpr int kRegsSoftmax = 208, kRegsOther = kPaged ? 48 : 88;
+  // shares of f16 weights lie at 2^11, of bf16 weights at 1
+  static constexpr float kShift = kCodes ? 11.f : 0.f;
+  static constexpr float kRaise = 4.f;
+  static constexpr int kSmem = 2 * kTileBytes + 2 * kStages * kTileBytes + kCodeStages * kCodeTile;
+};
+
+struct Record {
+  int on, b, kvh, row0, ntok, pos0, kb0, kb_end, part, bad_v;
+};
+struct Ctl {
+  uint64_t rec_full[kRing], rec_empty[kRing];
+  uint64_t q_full[2], q_empty[2];
+  uint64_t k_full[5], k_empty[5], v_full[5], v_empty[5], v_ok[5];
+  uint64_t s_full[2], s_empty[2], p_full[2], pv_done[2], o_empty[2];
+  uint64_t join_full, join_empty;
+  uint64_t copied[4][8];
+  Record rec[kRing];
+  float join[128][2];
+  uint32_t tmem;
+  volatile int abort;
+};
+
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// Matrix descriptor of a tile with 128-byte rows and the 128-byte swizzle, eight rows every 1024 bytes.
+__device__ __forceinline__ uint64_t desc128(uint32_t saddr) {
+  return (uint64_t)((saddr >> 4) & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)64 << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+#define PZ_R32(r, b) \
+  "=r"(r[b + 0]), "=r"(r[b + 1]), "=r"(r[b + 2]), "=r"(r[b + 3]), "=r"(r[b + 4]), "=r"(r[b + 5]), "=r"(r[b + 6]), \
+      "=r"(r[b + 7]), "=r"(r[b + 8]), "=r"(r[b + 9]), "=r"(r[b + 10]), "=r"(r[b + 11]), "=r"(r[b + 12]), "=r"(r[b + 13]), \
+      "=r"(r[b + 14]), "=r"(r[b + 15]), "=r"(r[b + 16]), "=r"(r[b + 17]), "=r"(r[b + 18]), "=r"(r[b + 19]), "=r"(r[b + 20]), \
+      "=r"(r[b + 21]), "=r"(r[b + 22]), "=r"(r[b + 23]), "=r"(r[b + 24]), "=r"(r[b + 25]), "=r"(r[b + 26]), "=r"(r[b + 27]), \
+      "=r"(r[b + 28]), "=r"(r[b + 29]), "=r"(r[b + 30]), "=r"(r[b + 31])
+#define PZ_V32(r) \
+  "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), \
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), \
+      "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), \
+      "r"(r[31])
+// 32 columns of the warp's 32 lanes.
+#define PZ_LIST32 \
+  "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}"
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 " PZ_LIST32 ", [%32];" : PZ_R32(r, 0) : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], " PZ_LIST32 ";" ::PZ_V32(r), "r"(taddr) : "memory");
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+      : "memory");
+}
+// 16 bytes from global to shared memory, zeros if !on.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+// One arrival of this thread once its copies so far have landed (the barrier's count includes it).
+__device__ __forceinline__ void cp_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cp_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void regs_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+__device__ __forceinline__ void st_shared16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+// Two f16 values, both exact in bf16.
+__device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t h) { return f32x2_to_bf16x2(f16_lo_to_f32(h), f16_hi_to_f32(h)); }
+
+// Waits by whole warps: one decision for the 32 lanes.
+struct Waiter {
+  Ctl* C;
+  int32_t* status;
+  __device__ __forceinline__ bool operator()(const uint64_t& bar, uint32_t parity) const {
+    const uint32_t a = smem_u32(&bar);
+    bool ok = mbar_try_wait(a, parity);
+    if (__all_sync(kFull, ok)) return true;
+    return slow(a, parity);
+  }
+  __device__ __forceinline__ bool slow(uint32_t a, uint32_t parity) const {
+    bool ok = false;
+    for (uint32_t i = 0; i < (1u << 22); ++i) {
+      if (mbar_try_wait(a, parity)) { ok = true; break; }
+      if (C->abort) break;
+      if (i > 64) __nanosleep(32);
+    }
+    ok = __all_sync(kFull, ok);
+    if (!ok && !C->abort) {
+      if (status) atomicOr(status, (int)PUZZLE_DEV_WAIT_EXPIRED);
+      C->abort = 1;
+    }
+    return ok;
+  }
+};
+
+// What a warpgroup does of a record: its tokens, the tiles [t0, t1) in steps of `step`, and where its keys end.
+struct Share {
+  int pos, ntok, t0, t1, step, kb_hi, nt;
+  __device__ __forceinline__ Share(const Record& r, int w, int narrow, int window) {
+    const int first = narrow ? 0 : kRowTokens * w;
+    pos = r.pos0 + first;
+    ntok = min(max(r.ntok - first, 0), kRowTokens);
+    const int hi = pos + ntok;                                              // behind the last key that one of them sees
+    const int lo = window > 0 ? max(pos - window + 1, 0) : 0;
+    kb_hi = min(r.kb_end, hi > 0 ? (hi + kBlock - 1) / kBlock : 0);
+    nt = (r.kb_end - r.kb0 + NBLK - 1) / NBLK;
+    t0 = max(lo / kBlock - r.kb0, 0) / NBLK;
+    t1 = ntok > 0 && kb_hi > r.kb0 ? (kb_hi - r.kb0 + NBLK - 1) / NBLK : 0;
+    step = 1;
+    if (narrow) {
+      step = 2;
+      t0 += (t0 ^ w) & 1;
+    }
+    if (t0 >= t1) t0 = t1 = 0;
+  }
+  __device__ __forceinline__ bool on() const { return t1 > t0; }
+  __device__ __forceinline__ bool mine(int t) const { return t >= t0 && t < t1 && (t - t0) % step == 0; }
+  __device__ __forceinline__ int blocks(const Record& r, int t) const { return min(kb_hi - r.kb0 - t * NBLK, NBLK); }
+};
+
+// Value d of key `key` of a record's sequence and head, in units of v_scale; for the rows that see an infinity or a NaN.
+template <int SRC>
+__device__ __forceinline__ float value_at(const PromptParams& P, int b, int kvh, long long first_row, int key, int d) {
+  if constexpr (SRC == kSrcPacked) {
+    return __bfloat162float(P.v[(first_row + key) * P.v_token_stride + kvh * kHeadDim + d]);
+  } else {
+    const long long blk = P.block_table ? (long long)P.block_table[(size_t)b * P.max_blocks_per_seq + key / kBlock]
+                                        : (long long)b * P.max_blocks_per_seq + key / kBlock;
+    if (blk < 0 || blk >= P.num_blocks) return 0.f;
+    const long long row = blk * P.Hkv + kvh;
+    const int t = key % kBlock;
+    if constexpr (SRC == kSrcBf16) {
+      return __bfloat162float(static_cast<const __nv_bfloat16*>(P.v_cache)[(row * kBlock + t) * kHeadDim + d]);
+    } else if constexpr (SRC == kSrcFp8) {
+      return f16_lo_to_f32(e4m3x2_to_f16x2(static_cast<const uint8_t*>(P.v_cache)[(row * kBlock + t) * kHeadDim + d]));
+    } else {   // only its scale can be a NaN
+      const uint8_t* base = static_cast<const uint8_t*>(P.v_cache) + row * kFp4BlockBytes;
+      return f16_lo_to_f32(e4m3x2_to_f16x2(base[fp4_v_scale_at(t, d >> 4)]));
+    }
+  }
+}
+
+// Whether every token of the record sees every key of tile t.
+__device__ __forceinline__ bool all_see(const Record& r, int t, int window) {
+  const int k0 = (r.kb0 + t * NBLK) * kBlock;
+  return k0 + TK <= r.pos0 + 1 && (window == 0 || k0 >= r.pos0 + r.ntok - window);
+}
+
+}  // namespace
+
+template <int SRC>
+__global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(const __grid_constant__ PromptParams P) {
+  using K = Cfg<SRC>;
+  constexpr int NS = K::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  Ctl* C = reinterpret_cast<Ctl*>(smem + K::kSmem);
+  const uint32_t q_at = smem_u32(smem), k_at = q_at + 2 * kTileBytes, v_at = k_at + NS * kTileBytes;
+  [[maybe_unused]] const uint32_t code_at = v_at + NS * kTileBytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int narrow = P.narrow, window = P.window;
+  const Waiter wait{C, P.dev_status};
+
+  if (threadIdx.x == 0) {
+    const int users = narrow ? 1 : 2;   // warpgroups that read a tile of keys
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(smem_u32(&C->rec_full[i]), 1);
+      mbar_init(smem_u32(&C->rec_empty[i]), 8 + 3 + (K::kPaged ? 4 : 0));
+    }
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(smem_u32(&C->k_full[i]), K::kFullArrivals);
+      mbar_init(smem_u32(&C->v_full[i]), K::kFullArrivals);
+      mbar_init(smem_u32(&C->k_empty[i]), users);
+      mbar_init(smem_u32(&C->v_empty[i]), users);
+      mbar_init(smem_u32(&C->v_ok[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&C->q_full[i]), 1);
+      mbar_init(smem_u32(&C->q_empty[i]), 1);
+      mbar_init(smem_u32(&C->s_full[i]), 1);
+      mbar_init(smem_u32(&C->s_empty[i]), 4);
+      mbar_init(smem_u32(&C->p_full[i]), 4);
+      mbar_init(smem_u32(&C->pv_done[i]), 1);
+      mbar_init(smem_u32(&C->o_empty[i]), 4);
+    }
+    for (int i = 0; i < 4 * 8; ++i) mbar_init(smem_u32(&C->copied[0][0] + i), 32);
+    mbar_init(smem_u32(&C->join_full), 4);
+    mbar_init(smem_u32(&C->join_empty), 4);
+    C->abort = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&P.tmQ);
+    if constexpr (!K::kPaged) {
+      tma_prefetch_desc(&P.tmK);
+      tma_prefetch_desc(&P.tmV);
+    }
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&C->tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_before();
+  __syncthreads();
+  tc_after();
+  const uint32_t tmem = C->tmem;
+  grid_dependency_wait();
+
+  // The record of item n, copied; the slot is let go at once by those that do not need it later (release()).
+  auto get_record = [&](int n, Record& r) -> bool {
+    const int s = n % kRing;
+    if (!wait(C->rec_full[s], (uint32_t)(n / kRing) & 1u)) return false;
+    r = C->rec[s];
+    return r.on != 0;
+  };
+  auto release = [&](int n) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&C->rec_empty[n % kRing]));
+  };
+
+  if (warp >= 8) {
+    regs_down<K::kRegsOther>();
+    if (warp < 10) {
+      // ================================================================= MMA issue, one warp per softmax warpgroup
+      const int w = warp - 8;
+      constexpr uint32_t kFmt = K::kCodes ? 0u : 1u;   // P and V: f16 or bf16
+      constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);
+      constexpr uint32_t kIdescPV = (1u << 4) | (kFmt << 7) | (kFmt << 10) | (1u << 16) | (8u << 17) | (8u << 24);
+      const uint32_t ts = tmem + kTmemS + 128 * w, tp = tmem + kTmemP + 64 * w, to = tmem + kTmemO + 64 * w;
+      const uint32_t qa = q_at + w * kTileBytes;
+      int kt = 0, n = 0, items = 0;   // tiles of all items, tiles and items of this warpgroup
+      int pend = -1, pend_nb = 0, pend_first = 0;
+      Record r;
+      auto product = [&]() -> bool {   // O (+)= P V of the pending tile
+        const int s = pend % NS;
+        if (!wait(C->v_full[s], (uint32_t)(pend / NS) & 1u) || !wait(C->v_ok[s], (uint32_t)(pend / NS) & 1u)) return false;
+        if (pend_first && !wait(C->o_empty[w], ((uint32_t)items & 1u) ^ 1u)) return false;
+        if (!wait(C->p_full[w], (uint32_t)(n - 1) & 1u)) return false;
+        tc_after();
+        if (elect_one()) {
+          for (int ks = 0; ks < pend_nb; ++ks)   // a block of 16 keys each
+            umma_ts(to, tp + 8 * ks, desc128(v_at + s * kTileBytes + 2048 * ks), kIdescPV, !(pend_first && ks == 0));
+          umma_commit(smem_u32(&C->pv_done[w]));
+          umma_commit(smem_u32(&C->v_empty[s]));
+        }
+        __syncwarp();
+        pend = -1;
+        return true;
+      };
+      bool ok = true;
+      for (int it = 0; ok && get_record(it, r); ++it) {
+        release(it);
+        const Share sh(r, w, narrow, window);
+        if (sh.on()) ok = wait(C->q_full[w], (uint32_t)items & 1u);
+        for (int t = 0; ok && t < sh.nt; ++t, ++kt) {
+          const int s = kt % NS;
+          const uint32_t par = (uint32_t)(kt / NS) & 1u;
+          if (sh.mine(t)) {
+            const int nb = sh.blocks(r, t);
+            ok = wait(C->k_full[s], par) && wait(C->s_empty[w], ((uint32_t)n & 1u) ^ 1u);
+            if (!ok) break;
+            tc_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int ks = 0; ks < 4; ++ks)
+                umma_ss(ts, desc128(qa + 32 * ks), desc128(k_at + s * kTileBytes + 32 * ks), kIdescQK | (uint32_t)(2 * nb) << 17,
+                        ks);
+              umma_commit(smem_u32(&C->s_full[w]));
+              umma_commit(smem_u32(&C->k_empty[s]));
+              if (t + sh.step >= sh.t1) umma_commit(smem_u32(&C->q_empty[w]));
+            }
+            __syncwarp();
+            if (pend >= 0) ok = product();
+            ++n;
+            pend = kt;
+            pend_nb = nb;
+            pend_first = t == sh.t0;
+          } else if (!narrow) {   // the other warpgroup's tile alone: let go of it
+            if (pend >= 0) ok = product();
+            ok = ok && wait(C->k_full[s], par) && wait(C->v_full[s], par) && wait(C->v_ok[s], par);
+            if (ok && elect_one()) {
+              mbar_arrive(smem_u32(&C->k_empty[s]));
+              mbar_arrive(smem_u32(&C->v_empty[s]));
+            }
+            __syncwarp();
+          }
+        }
+        if (ok && pend >= 0) ok = product();
+        if (sh.on()) ++items;
+      }
+    } else if (warp == 10) {
+      // ================================================================= work records, queries, packed keys and values
+      const int T = narrow ? kRowTokens : 2 * kRowTokens;
+      const int per_tile = P.Hkv * P.splits;
+      int b0 = 0, before = 0;           // a window of 32 sequences and the tiles of those before it
+      int cnt = 0, upto = 0, st = 0, len = 0, ntok = 0;
+      auto load_window = [&]() {
+        const int b = b0 + lane;
+        cnt = st = len = ntok = 0;
+        if (b < P.batch) {
+          st = P.starts[b];
+          const int en = P.starts[b + 1];
+          if (st >= 0 && en >= st && en <= P.total) ntok = en - st;
+          else if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_STARTS);
+          len = ntok;
+          if constexpr (K::kPaged) {
+            if (ntok > 0) {
+              len = P.seq_lens[b];
+              const int most = P.max_blocks_per_seq * kBlock;
+              if (len > most) {
+                len = most;
+                if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_SEQ_TOO_LONG);
+              }
+              len = max(len, 0);
+            }
+          }
+          cnt = (ntok + T - 1) / T;
+        }
+        upto = cnt;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int u = __shfl_up_sync(kFull, upto, d);
+          if (lane >= d) upto += u;
+        }
+      };
+      load_window();
+      int kt = 0, q_n[2] = {0, 0};
+      bool ok = true;
+      for (int it = 0;; ++it) {
+        // items in rounds of one per CTA, every other round backwards: long and short ones even out
+        const long long item = (long long)it * gridDim.x + ((it & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+        const long long tile = item / per_tile;
+        const int rest = (int)(item - tile * per_tile);
+        while (b0 < P.batch && before + __shfl_sync(kFull, upto, 31) <= tile) {
+          before += __shfl_sync(kFull, upto, 31);
+          b0 += 32;
+          if (b0 < P.batch) load_window();
+        }
+        Record r;
+        r.on = b0 < P.batch;
+        r.b = r.kvh = r.row0 = r.ntok = r.pos0 = r.kb0 = r.kb_end = r.part = r.bad_v = 0;
+        if (r.on) {
+          const int src = __ffs(__ballot_sync(kFull, before + upto > tile)) - 1;
+          const int s_cnt = __shfl_sync(kFull, cnt, src), s_upto = __shfl_sync(kFull, upto, src);
+          const int s_st = __shfl_sync(kFull, st, src), s_len = __shfl_sync(kFull, len, src);
+          const int s_n = __shfl_sync(kFull, ntok, src);
+          const int i = s_cnt - 1 - (int)(tile - (before + s_upto - s_cnt));   // a sequence's last tokens first
+          r.b = b0 + src;
+          r.kvh = rest % P.Hkv;
+          r.part = rest / P.Hkv;
+          r.row0 = s_st + i * T;
+          r.ntok = min(T, s_n - i * T);
+          r.pos0 = s_len - s_n + i * T;
+          const int hi = max(r.pos0 + r.ntok, 0), lo = window > 0 ? max(r.pos0 - window + 1, 0) : 0;
+          const int kb_hi = (hi + kBlock - 1) / kBlock, kb_lo = hi > 0 ? lo / kBlock : 0;
+          const int nt = (kb_hi - kb_lo + NBLK - 1) / NBLK;
+          const int parts = min(P.splits, max(nt, 1));
+          if (r.part < parts) {
+            r.kb0 = kb_lo + (int)((long long)nt * r.part / parts) * NBLK;
+            r.kb_end = min(kb_lo + (int)((long long)nt * (r.part + 1) / parts) * NBLK, kb_hi);
+          }
+        }
+        const int slot = it % kRing;
+        ok = wait(C->rec_empty[slot], ((uint32_t)(it / kRing) & 1u) ^ 1u);
+        if (!ok) break;
+        if (lane == 0) {
+          C->rec[slot] = r;
+          mbar_arrive(smem_u32(&C->rec_full[slot]));
+        }
+        __syncwarp();
+        if (!r.on) break;
+        const Share a(r, 0, narrow, window), c(r, 1, narrow, window);
+        auto load_q = [&](const Share& sh, int w) {
+          if (!ok || !sh.on()) return;
+          ok = wait(C->q_empty[w], ((uint32_t)q_n[w] & 1u) ^ 1u);
+          ++q_n[w];
+          if (ok && elect_one()) {
+            const uint32_t bar = smem_u32(&C->q_full[w]);
+            mbar_arrive_expect_tx(bar, kTileBytes);
+            tma_load_3d(q_at + w * kTileBytes, &P.tmQ, 0, r.kvh * kGroup, r.row0 + (narrow ? 0 : kRowTokens * w), bar);
+          }
+          __syncwarp();
+        };
+        load_q(a, 0);
+        load_q(c, 1);
+        if constexpr (!K::kPaged) {
+          const int first = r.row0 - r.pos0;   // the sequence's first row
+          for (int t = 0; ok && t < a.nt; ++t, ++kt) {
+            const int s = kt % NS;
+            const uint32_t par = ((uint32_t)(kt / NS) & 1u) ^ 1u;
+            const int row = first + (r.kb0 + t * NBLK) * kBlock;
+            ok = wait(C->k_empty[s], par);
+            if (ok && elect_one()) {
+              const uint32_t bar = smem_u32(&C->k_full[s]);
+              mbar_arrive_expect_tx(bar, kTileBytes);
+              tma_load_3d(k_at + s * kTileBytes, &P.tmK, 0, r.kvh, row, bar);
+            }
+            __syncwarp();
+            ok = ok && wait(C->v_empty[s], par);
+            if (ok && elect_one()) {
+              const uint32_t bar = smem_u32(&C->v_full[s]);
+              mbar_arrive_expect_tx(bar, kTileBytes);
+              tma_load_3d(v_at + s * kTileBytes, &P.tmV, 0, r.kvh, row, bar);
+            }
+            __syncwarp();
+          }
+        }
+        if (!ok) break;
+      }
+      if (C->abort) {   // the copies in flight end before the shared memory is given back
+        for (int w = 0; w < 2; ++w)
+          if (q_n[w] > 0) mbar_wait_bounded(smem_u32(&C->q_full[w]), (uint32_t)(q_n[w] - 1) & 1u);
+        for (int i = max(kt - NS, 0); i < kt; ++i) {
+          mbar_wait_bounded(smem_u32(&C->k_full[i % NS]), (uint32_t)(i / NS) & 1u);
+          mbar_wait_bounded(smem_u32(&C->v_full[i % NS]), (uint32_t)(i / NS) & 1u);
+        }
+      }
+    } else if (warp == 11) {
+      // ================================================================= infinities and NaN among values not all rows see
+      constexpr uint32_t kInf = K::kCodes ? 0x7c007c00u : 0x7f807f80u;
+      int kt = 0;
+      Record r;
+      bool ok = true;
+      for (int it = 0; ok && get_record(it, r); ++it) {
+        const int nt = (r.kb_end - r.kb0 + NBLK - 1) / NBLK;
+        for (int t = 0; t < nt; ++t, ++kt) {
+          const int s = kt % NS;
+          ok = wait(C->v_full[s], (uint32_t)(kt / NS) & 1u);
+          if (!ok) break;
+          if (!all_see(r, t, window)) {
+            const int nb = min(r.kb_end - r.kb0 - t * NBLK, NBLK);
+            const uint32_t base = v_at + s * kTileBytes + 16 * lane;
+            bool bad = false;
+#pragma unroll 8
+            for (int i = 0; i < nb * 4; ++i) {   // 512 bytes, four tokens each
+              uint4 v = ld_shared16(base + 512 * i);
+              const uint32_t x = __vcmpeq2(v.x & kInf, kInf), y = __vcmpeq2(v.y & kInf, kInf), z = __vcmpeq2(v.z & kInf, kInf),
+                             u = __vcmpeq2(v.w & kInf, kInf);
+              if (x | y | z | u) {
+                bad = true;
+                st_shared16(base + 512 * i, v.x & ~x, v.y & ~y, v.z & ~z, v.w & ~u);
+              }
+            }
+            if (bad) {
+              *reinterpret_cast<volatile int*>(&C->rec[it % kRing].bad_v) = 1;
+              __threadfence_block();
+              fence_proxy_async();
+            }
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&C->v_ok[s]));
+        }
+        release(it);
+      }
+    } else if constexpr (K::kPaged) {
+      // ================================================================= blocks of the cache, four warps
+      // Warp lw has blocks lw and lw + 4 of every tile, K and V, from the copy to the converted form: nothing is shared with
+      // the other three.  Places in the cache are looked up for 16 tiles at a time, lane = 2 tile + block.
+      const int lw = warp - 12;
+      constexpr int kSlots = K::kCopySlots;
+      auto lookup = [&](const Record& r, int t_first) -> int {   // row (block, KV head) of the cache, -1: none
+        const int j = r.kb0 + (t_first + (lane >> 1)) * NBLK + lw + 4 * (lane & 1);
+        if (j >= r.kb_end) return -1;
+        const long long blk = P.block_table ? (long long)P.block_table[(size_t)r.b * P.max_blocks_per_seq + j]
+                                            : (long long)r.b * P.max_blocks_per_seq + j;
+        if (blk >= 0 && blk < P.num_blocks) return (int)(blk * P.Hkv + r.kvh);
+        if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
+        return -1;
+      };
+      bool ok = true;
+      // The next tile to copy.  Records of items that nothing is copied of yet are taken only as they come: their being
+      // published can depend on tiles that this warp has still to hand on.
+      Record r;
+      int it = -1, t = 0, nt = 0, ent = -1;
+      bool more = true;
+      auto have_tile = [&](bool block) -> bool {
+        while (more && t == nt) {
+          const int s = (it + 1) % kRing;
+          const uint32_t par = (uint32_t)((it + 1) / kRing) & 1u;
+          if (!block && !__all_sync(kFull, mbar_try_wait(smem_u32(&C->rec_full[s]), par))) return false;
+          more = get_record(it + 1, r);
+          if (!more) return false;
+          release(++it);
+          t = 0;
+          nt = (r.kb_end - r.kb0 + NBLK - 1) / NBLK;
+          if (nt > 0) ent = lookup(r, 0);
+        }
+        return more;
+      };
+      int in = 0, out = 0;                         // tiles whose copies are begun, tiles handed on
+      auto begin_copy = [&]() {
+        const int row0 = __shfl_sync(kFull, ent, 2 * (t & 15)), row1 = __shfl_sync(kFull, ent, 2 * (t & 15) + 1);
+        if constexpr (SRC == kSrcBf16) {
+          const int s = in % NS;
+          const uint32_t par = ((uint32_t)(in / NS) & 1u) ^ 1u;
+          ok = wait(C->k_empty[s], par) && wait(C->v_empty[s], par);
+          if (!ok) return;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int row = h ? row1 : row0;
+            const size_t at = (size_t)max(row, 0) * (kBlock * kHeadDim * 2);
+            const char* ks = static_cast<const char*>(P.k_cache) + at;
+            const char* vs = static_cast<const char*>(P.v_cache) + at;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int cidx = lane + 32 * i, tok = (lw + 4 * h) * kBlock + (cidx >> 3);
+              const uint32_t dst = (uint32_t)(s * kTileBytes + tok * 128 + (((cidx & 7) ^ (tok & 7)) << 4));
+              cp_async16(k_at + dst, ks + 16 * cidx, row >= 0);
+              cp_async16(v_at + dst, vs + 16 * cidx, row >= 0);
+            }
+          }
+        } else {
+          const uint32_t dst = code_at + (in % kSlots) * K::kCodeTile;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int row = h ? row1 : row0;
+            const size_t at = (size_t)max(row, 0) * K::kBlockBytes;
+            const char* ks = static_cast<const char*>(P.k_cache) + at;
+            const char* vs = static_cast<const char*>(P.v_cache) + at;
+            const uint32_t kd = dst + (lw + 4 * h) * K::kBlockBytes, vd = kd + NBLK * K::kBlockBytes;
+            for (int i = lane; i < K::kBlockBytes / 16; i += 32) {
+              cp_async16(kd + 16 * i, ks + 16 * i, row >= 0);
+              cp_async16(vd + 16 * i, vs + 16 * i, row >= 0);
+            }
+          }
+        }
+        cp_arrive(smem_u32(&C->copied[lw][in % kSlots]));
+        ++in;
+        if (++t < nt && (t & 15) == 0) ent = lookup(r, t);
+      };
+      // Codes of a tile -> bf16 keys and f16 values in the swizzled rows that the MMAs read.
+      auto convert = [&](uint32_t src, uint32_t dst, bool is_v) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int blk = lw + 4 * h;
+          const uint32_t cb = src + blk * K::kBlockBytes;
+          if constexpr (SRC == kSrcFp8) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int cidx = lane + 32 * i, tok = blk * kBlock + (cidx >> 2), o = 2 * (cidx & 3);
+              const uint4 w4 = ld_shared16(cb + 16 * cidx);
+              const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+              uint32_t x[8];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                x[2 * k] = e4m3x2_to_f16x2(w[k] & 0xffffu);
+                x[2 * k + 1] = e4m3x2_to_f16x2(w[k] >> 16);
+              }
+              if (!is_v)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = f16x2_to_bf16x2(x[k]);
+              const uint32_t row = dst + tok * 128;
+              st_shared16(row + ((o ^ (tok & 7)) << 4), x[0], x[1], x[2], x[3]);
+              st_shared16(row + (((o + 1) ^ (tok & 7)) << 4), x[4], x[5], x[6], x[7]);
+            }
+          } else if constexpr (SRC == kSrcFp4) {
+            const uint4 w4 = ld_shared16(cb + 16 * lane);
+            const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+            auto scale2 = [&](int at) -> __half2 {   // the E4M3 scale at this byte of the block, twice
+              uint32_t sc;
+              asm volatile("ld.shared.u8 %0, [%1];" : "=r"(sc) : "r"(cb + at) : "memory");
+              const uint32_t hh = e4m3x2_to_f16x2(sc | (sc << 8));
+              return *reinterpret_cast<const __half2*>(&hh);
+            };
+            auto times = [](uint32_t a, __half2 s) -> uint32_t {
+              const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&a), s);
+              return *reinterpret_cast<const uint32_t*>(&p);
+            };
+            if (!is_v) {   // token lane / 2, channels 32 (lane % 2) ..
+              const int t = lane >> 1, tok = blk * kBlock + t, g = 2 * (lane & 1);
+              const uint32_t row = dst + tok * 128;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {   // eight channels
+                const __half2 sc = scale2(fp4_k_scale_at(t, g + (k >> 1)));
+                uint32_t x0, x1, x2, x3;
+                e2m1x8_to_f16x2x4(w[k], x0, x1, x2, x3);
+                st_shared16(row + (((2 * g + k) ^ (tok & 7)) << 4), f16x2_to_bf16x2(times(x0, sc)), f16x2_to_bf16x2(times(x1, sc)),
+                            f16x2_to_bf16x2(times(x2, sc)), f16x2_to_bf16x2(times(x3, sc)));
+              }
+            } else {       // tokens 2 tp and 2 tp + 1, channels 32 (lane / 16) + 16 (lane % 2) ..
+              const int tp = (lane & 15) >> 1, g = 2 * (lane >> 4) + (lane & 1), tok = blk * kBlock + 2 * tp;
+              const __half2 s0 = scale2(fp4_v_scale_at(2 * tp, g)), s1 = scale2(fp4_v_scale_at(2 * tp + 1, g));
+              const uint32_t row = dst + tok * 128;
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {   // eight channels of both tokens
+                uint32_t e[4], o[4];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                  uint32_t x0, x1, x2, x3;   // (even token, odd token) of four channels
+                  e2m1x8_to_f16x2x4(w[2 * k + m], x0, x1, x2, x3);
+                  e[2 * m] = times(prmt(x0, x1, 0x5410), s0);
+                  e[2 * m + 1] = times(prmt(x2, x3, 0x5410), s0);
+                  o[2 * m] = times(prmt(x0, x1, 0x7632), s1);
+                  o[2 * m + 1] = times(prmt(x2, x3, 0x7632), s1);
+                }
+                st_shared16(row + (((2 * g + k) ^ (tok & 7)) << 4), e[0], e[1], e[2], e[3]);
+                st_shared16(row + 128 + (((2 * g + k) ^ ((tok + 1) & 7)) << 4), o[0], o[1], o[2], o[3]);
+              }
+            }
+          }
+        }
+      };
+      auto signal = [&](const uint64_t& bar) {
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bar));
+      };
+      while (ok) {
+        while (ok && in - out < kSlots && have_tile(in == out)) begin_copy();
+        if (!ok || in == out) break;
+        ok = wait(C->copied[lw][out % kSlots], (uint32_t)(out / kSlots) & 1u);
+        if (!ok) break;
+        const int s = out % NS;
+        if constexpr (SRC == kSrcBf16) {
+          signal(C->k_full[s]);
+          signal(C->v_full[s]);
+        } else {
+          const uint32_t par = ((uint32_t)(out / NS) & 1u) ^ 1u;
+          const uint32_t src = code_at + (out % kSlots) * K::kCodeTile;
+          ok = wait(C->k_empty[s], par);
+          if (!ok) break;
+          convert(src, k_at + s * kTileBytes, false);
+          signal(C->k_full[s]);
+          ok = wait(C->v_empty[s], par);
+          if (!ok) break;
+          convert(src + NBLK * K::kBlockBytes, v_at + s * kTileBytes, true);
+          signal(C->v_full[s]);
+        }
+        ++out;
+      }
+      cp_wait_all();   // none is in flight when the shared memory is given back
+    }
+  } else {
+    // =================================================================== softmax, two warpgroups, thread = row
+    regs_up<K::kRegsSoftmax>();
+    const int w = warp >> 2, wq = warp & 3, row = 32 * wq + lane, head = row & 7;
+    const uint32_t quad = (uint32_t)(32 * wq) << 16;
+    const uint32_t ts = tmem + kTmemS + 128 * w + quad, tp = tmem + kTmemP + 64 * w + quad, to = tmem + kTmemO + quad;
+    int n = 0, joins = 0;   // tiles of this warpgroup, joined items
+    Record r;
+    bool ok = true;
+    for (int it = 0; ok && get_record(it, r); ++it) {
+      const Share sh(r, w, narrow, window);
+      const float ks = K::kCodes && P.k_scale ? P.k_scale[r.kvh] : 1.f;
+      float c = P.sm_scale_log2e * ks;
+      const bool odd = !(c > 0.f && c < INFINITY);   // then logits are scaled before their maximum is taken
+      const float pre = c;
+      if (odd) c = 1.f;
+      const int p = sh.pos + (row >> 3);                       // this row's position; it sees [lo, hi)
+      const int hi = p + 1, lo = window > 0 ? p - window + 1 : 0;
+      float m = -INFINITY, ref = -K::kShift, l = 0.f;          // weights are 2^(c s - ref), ref = c m - shift
+      for (int t = sh.t0; t < sh.t1; t += sh.step, ++n) {
+        const int nb = sh.blocks(r, t), k0 = (r.kb0 + t * NBLK) * kBlock;
+        ok = wait(C->s_full[w], (uint32_t)n & 1u);
+        if (!ok) break;
+        tc_after();
+        uint32_t u[128];
+        float* s = reinterpret_cast<float*>(u);
+        const int chunks = (nb + 1) >> 1;                      // of 32 columns
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (q < chunks) tmem_ld32(ts + 32 * q, u + 32 * q);
+          else
+#pragma unroll
+            for (int j = 0; j < 32; ++j) s[32 * q + j] = -INFINITY;
+        }
+        tmem_wait_ld();
+        tc_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&C->s_empty[w]));
+        if (odd)
+#pragma unroll
+          for (int j = 0; j < 128; ++j) s[j] *= pre;
+        // do all tokens of this warp see all keys?
+        const int p0 = sh.pos + 4 * wq;
+        if (k0 + TK > p0 + 1 || (window > 0 && k0 < p0 + 3 - window + 1)) {
+          const int jlo = lo - k0, wide = hi - lo;
+#pragma unroll
+          for (int j = 0; j < 128; ++j)
+            if ((unsigned)(j - jlo) >= (unsigned)max(wide, 0)) s[j] = -INFINITY;
+        }
+        float x[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int j = 4; j < 128; j += 4) {
+          x[0] = fmaxf(x[0], s[j]);
+          x[1] = fmaxf(x[1], s[j + 1]);
+          x[2] = fmaxf(x[2], s[j + 2]);
+          x[3] = fmaxf(x[3], s[j + 3]);
+        }
+        const float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+        const bool first = t == sh.t0;
+        const bool raise = top > m && (top - m) * c > K::kRaise;   // m = -inf: any finite top
+        if (__any_sync(kFull, raise)) {
+          float alpha = 1.f;
+          if (raise) {
+            const float now = top * c - K::kShift;
+            alpha = m == -INFINITY ? 0.f : ex2(ref - now);
+            m = top;
+            ref = now;
+          }
+          l *= alpha;
+          if (!first) {
+            ok = wait(C->pv_done[w], (uint32_t)(n - 1) & 1u);
+            if (!ok) break;
+            tc_after();
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              uint32_t o[32];
+              tmem_ld32(to + 64 * w + 32 * q, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+              tmem_st32(to + 64 * w + 32 * q, o);
+            }
+          }
+        }
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (q < chunks) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float e0 = ex2(fmaf(s[32 * q + j], c, -ref)), e1 = ex2(fmaf(s[32 * q + j + 1], c, -ref));
+              sum[j & 2] += e0;
+              sum[(j & 2) + 1] += e1;
+              u[16 * q + (j >> 1)] = K::kCodes ? f32x2_to_f16x2(e0, e1) : f32x2_to_bf16x2(e0, e1);
+            }
+          }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        if (n > 0) {   // P of the tile before has been read
+          ok = wait(C->pv_done[w], (uint32_t)(n - 1) & 1u);
+          if (!ok) break;
+          tc_after();
+        }
+        tmem_st32(tp, u);
+        if (chunks > 2) tmem_st32(tp + 32, u + 32);
+        tmem_wait_st();
+        tc_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&C->p_full[w]));
+      }
+      if (!ok) break;
+      // ---- the item's end: O of this warpgroup, joined with the other's in narrow groups, by warpgroup 0
+      if (sh.on()) {
+        ok = wait(C->pv_done[w], (uint32_t)(n - 1) & 1u);
+        if (!ok) break;
+        tc_after();
+      }
+      const Share other(r, 1, narrow, window);
+      const bool join = narrow && other.on();
+      if (narrow && w == 1) {
+        if (join) {
+          ok = wait(C->join_empty, ((uint32_t)joins & 1u) ^ 1u);
+          if (!ok) break;
+          C->join[row][0] = m == -INFINITY ? -INFINITY : ref;
+          C->join[row][1] = l;
+          tc_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&C->join_full));
+          ++joins;
+        }
+        release(it);
+        continue;
+      }
+      uint32_t u[64];
+      float* o = reinterpret_cast<float*>(u);
+      if (m == -INFINITY) ref = -INFINITY;   // no logit above -inf; l is 0, or a NaN
+      if (sh.on()) {
+        tmem_ld32(to + 64 * w, u);
+        tmem_ld32(to + 64 * w + 32, u + 32);
+        tmem_wait_ld();
+      } else {
+#pragma unroll
+        for (int j = 0; j < 64; ++j) o[j] = 0.f;
+      }
+      if (join) {
+        ok = wait(C->join_full, (uint32_t)joins & 1u);
+        if (!ok) break;
+        tc_after();
+        const float ref1 = C->join[row][0], l1 = C->join[row][1];
+        const float both = fmaxf(ref, ref1), zero = both == -INFINITY ? 0.f : both;
+        const float a0 = ex2(ref - zero), a1 = ex2(ref1 - zero);
+        l = l * a0 + l1 * a1;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          uint32_t o1[32];
+          tmem_ld32(to + 64 + 32 * q, o1);
+          tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) o[32 * q + j] = o[32 * q + j] * a0 + __uint_as_float(o1[j]) * a1;
+        }
+        ref = both;
+        tc_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&C->join_empty));
+          mbar_arrive(smem_u32(&C->o_empty[1]));
+        }
+        ++joins;
+      }
+      if (sh.on()) {
+        tc_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&C->o_empty[w]));
+      }
+      const bool real = (row >> 3) < sh.ntok;
+      if (real && *reinterpret_cast<volatile int*>(&C->rec[it % kRing].bad_v)) {
+        const int from = max(max(lo, 0), r.kb0 * kBlock), to_key = min(hi, r.kb_end * kBlock);
+        const long long first_row = (long long)r.row0 - r.pos0;
+        for (int key = from; key < to_key; ++key) {
+          const int t = (key / kBlock - r.kb0) / NBLK;
+          if (all_see(r, t, window)) {          // the product has them
+            key = (r.kb0 + (t + 1) * NBLK) * kBlock - 1;
+            continue;
+          }
+#pragma unroll 1
+          for (int d = 0; d < kHeadDim; ++d) {
+            const float v = value_at<SRC>(P, r.b, r.kvh, first_row, key, d);
+            if (!(fabsf(v) < INFINITY)) {
+#pragma unroll
+              for (int j = 0; j < 64; ++j)
+                if (j == d) o[j] += v;
+            }
+          }
+        }
+      }
+      release(it);
+      if (real) {
+        const int g = r.kvh * kGroup + head;
+        const long long token = r.row0 + (narrow ? 0 : kRowTokens * w) + (row >> 3);
+        const long long at = token * (P.Hkv * kGroup) + g;
+        const float vs = K::kCodes && P.v_scale ? P.v_scale[r.kvh] : 1.f;
+        float z = l, big = ref;
+        if (P.splits == 1 && P.sinks) {
+          const float sk = P.sinks[g] * kLog2e;
+          big = sk > ref ? sk : ref;             // a NaN sink is not above; it comes in through z
+          const float base = big == -INFINITY ? 0.f : big;
+          z = l * ex2(ref - base) + ex2(sk - base);
+        }
+        const float base = big == -INFINITY ? 0.f : big;
+        float f = ex2(ref - base) * vs / z;
+        float lse = (base + lg2(z)) * kLn2;
+        if (P.splits > 1) {
+          if (l == 0.f) lse = -INFINITY;         // no key in this part, or none above -inf
+          const size_t to_row = (size_t)r.part * ((size_t)P.total * (P.Hkv * kGroup)) + at;
+          P.part_lse[to_row] = lse;
+          if (lse != -INFINITY) {
+            float4* dst = reinterpret_cast<float4*>(P.part_o + to_row * kHeadDim);
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              dst[j] = make_float4(o[4 * j] * f, o[4 * j + 1] * f, o[4 * j + 2] * f, o[4 * j + 3] * f);
+          }
+        } else {
+          if (z == 0.f) {                        // nothing seen: zeros; nothing but logits of -inf: 0 / 0
+            f = hi > 0 ? NAN : 0.f;
+            lse = hi > 0 ? NAN : -INFINITY;
+          }
+          uint4* dst = reinterpret_cast<uint4*>(P.out + at * kHeadDim);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            dst[j] = make_uint4(f32x2_to_bf16x2(o[8 * j] * f, o[8 * j + 1] * f), f32x2_to_bf16x2(o[8 * j + 2] * f, o[8 * j + 3] * f),
+                                f32x2_to_bf16x2(o[8 * j + 4] * f, o[8 * j + 5] * f), f32x2_to_bf16x2(o[8 * j + 6] * f, o[8 * j + 7] * f));
+          if (P.lse_out) P.lse_out[at] = lse;
+        }
+      }
+      __syncwarp();
+    }
+  }
+  __syncthreads();
+  if (warp == 8) {
+    tc_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+namespace {
+
+// Partials of the parts of a row -> its output; 16 lanes a row.
+__global__ void __launch_bounds__(256) prompt_merge_kernel(const __grid_constant__ PromptParams P) {
+  const int Hq = P.Hkv * kGroup;
+  const size_t rows = (size_t)P.total * Hq;
+  const size_t at = ((size_t)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
+  const int o = threadIdx.x & 15;
+  grid_dependency_wait();
+  if (at >= rows) return;
+  const int token = (int)(at / Hq), g = (int)(at % Hq);
+  int lo = 0, hi = P.batch;             // the last sequence that starts at this row or before
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (P.starts[mid] <= token) lo = mid;
+    else hi = mid;
+  }
+  const int st = P.starts[lo], en = P.starts[lo + 1];
+  if (st < 0 || en > P.total || token < st || token >= en) return;   // no sequence's row
+  const int len = min(max(P.seq_lens[lo], 0), P.max_blocks_per_seq * kBlock);
+  const bool sees = len - (en - token) >= 0;
+  const float* lse = P.part_lse + at;
+  float top = P.sinks ? P.sinks[g] : -INFINITY;
+  const float sk = top;
+  for (int p = 0; p < P.splits; ++p) top = fmaxf(top, lse[p * rows]);
+  const float base = top == -INFINITY ? 0.f : top;
+  float z = P.sinks ? ex2((sk - base) * kLog2e) : 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p = 0; p < P.splits; ++p) {
+    const float e = lse[p * rows];
+    if (e == -INFINITY) continue;
+    const float wgt = ex2((e - base) * kLog2e);
+    const float4 v = reinterpret_cast<const float4*>(P.part_o + (p * rows + at) * kHeadDim)[o];
+    z += wgt;
+    acc.x += wgt * v.x;
+    acc.y += wgt * v.y;
+    acc.z += wgt * v.z;
+    acc.w += wgt * v.w;
+  }
+  float f = 1.f / z, out_lse = base + lg2(z) * kLn2;
+  if (z == 0.f) {
+    f = sees ? NAN : 0.f;
+    out_lse = sees ? NAN : -INFINITY;
+  }
+  reinterpret_cast<uint2*>(P.out + at * kHeadDim)[o] = make_uint2(f32x2_to_bf16x2(acc.x * f, acc.y * f), f32x2_to_bf16x2(acc.z * f, acc.w * f));
+  if (P.lse_out && o == 0) P.lse_out[at] = out_lse;
+}
+
+template <int SRC>
+cudaError_t launch(const PromptParams& P, int sm_count, cudaStream_t s, int* smem_limit) {
+  const int need = Cfg<SRC>::kSmem + (int)sizeof(Ctl) + 1024;
+  if (*smem_limit == 0) {
+    const cudaError_t e = cudaFuncSetAttribute(prompt_attn_kernel<SRC>, cudaFuncAttributeMaxDynamicSharedMemorySize, need);
+    if (e != cudaSuccess) return e;
+    *smem_limit = need;
+  }
+  const int T = P.narrow ? kRowTokens : 2 * kRowTokens;
+  const long long tiles = P.total / T + std::min(P.batch, P.total);   // no more than these, whatever the lengths
+  const long long items = tiles * P.Hkv * P.splits;
+  cudaError_t e = launch_dependent(prompt_attn_kernel<SRC>, dim3((unsigned)std::min<long long>(items, sm_count)),
+                                   dim3(Cfg<SRC>::kThreads), need, s, P);
+  count_launch();
+  if (e == cudaSuccess && P.splits > 1) {
+    const size_t threads = (size_t)P.total * P.Hkv * kGroup * 16;
+    e = launch_dependent(prompt_merge_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, P);
+    count_launch();
+  }
+  return e;
+}
+
+}  // namespace
+
+PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool may_split, int sm_count) {
+  const long long seqs = std::min(batch, total);
+  PromptPlan plan;
+  const long long wide = std::max<long long>((total + 2 * kRowTokens - 1) / (2 * kRowTokens), seqs) * Hkv;
+  plan.narrow = total <= kRowTokens * seqs || wide < sm_count;
+  const long long items = plan.narrow ? std::max<long long>((total + kRowTokens - 1) / kRowTokens, seqs) * Hkv : wide;
+  plan.splits = 1;
+  if (may_split && items < sm_count) {
+    const long long tiles = (key_bound + TK - 1) / TK;
+    plan.splits = (int)std::max<long long>(1, std::min<long long>(sm_count / items, tiles / 4));
+  }
+  return plan;
+}
+
+// Keys are cut only where groups are fewer than the SMs, and into no more parts than these leave room for: parts x rows is at
+// most the rows of that many groups.
+size_t prompt_partial_bytes(int sm_count, int Hkv) {
+  return (size_t)(sm_count + Hkv) * kRowTokens * kGroup * (kHeadDim + 1) * sizeof(float);
+}
+
+cudaError_t launch_prompt_attn(const PromptParams& P, PromptSource src, int sm_count, cudaStream_t s, int* smem_limit) {
+  switch (src) {
+    case kSrcPacked: return launch<kSrcPacked>(P, sm_count, s, smem_limit + 0);
+    case kSrcBf16: return launch<kSrcBf16>(P, sm_count, s, smem_limit + 1);
+    case kSrcFp8: return launch<kSrcFp8>(P, sm_count, s, smem_limit + 2);
+    default: return launch<kSrcFp4>(P, sm_count, s, smem_limit + 3);
+  }
+}
+
+}  // namespace puzzle

@@ -1,0 +1,38 @@
+// Attention of many query tokens per sequence (whole prompts, chunks over the cache): parameters and launch.
+#pragma once
+
+#include <cuda.h>
+
+#include "common.cuh"
+
+namespace puzzle {
+
+// Where keys and values come from.
+enum PromptSource { kSrcPacked = 0, kSrcBf16 = 1, kSrcFp8 = 2, kSrcFp4 = 3 };
+
+struct PromptParams {
+  CUtensorMap tmQ;            // [total][Hq][64] bf16, box = 16 tokens of one KV head's 8 query heads
+  CUtensorMap tmK, tmV;       // packed keys and values [total][Hkv][64]: box = 128 tokens of one head (kSrcPacked only)
+  const void *k_cache, *v_cache;
+  const __nv_bfloat16* v;     // packed values
+  long long v_token_stride;   // in elements
+  const int32_t *block_table, *seq_lens, *starts;
+  const float *k_scale, *v_scale, *sinks;
+  __nv_bfloat16* out;
+  float *lse_out, *part_o, *part_lse;
+  int32_t* dev_status;
+  long long num_blocks;
+  int batch, total, Hkv, max_blocks_per_seq, window, splits, narrow;
+  float sm_scale_log2e;
+};
+
+// splits: parts that the keys of a group of tokens are cut into (1: the kernel writes the output, else partials that a second
+// kernel merges).  narrow: groups of 16 tokens instead of 32.
+struct PromptPlan {
+  int splits, narrow;
+};
+PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool may_split, int sm_count);
+size_t prompt_partial_bytes(int sm_count, int Hkv);   // of the partials of any call
+cudaError_t launch_prompt_attn(const PromptParams& P, PromptSource src, int sm_count, cudaStream_t s, int* smem_limit);
+
+}  // namespace puzzle
