@@ -8,18 +8,28 @@
 // in one pass over the keys with a running maximum and sum.  A tile of rows is 16 tokens x the 8 query heads of one KV head
 // (128 rows, so that one tile of keys serves all of them and a window wastes at most 16 tokens of it), a tile of keys 128.
 //
-//  * Two softmax warpgroups own one tile of rows each: thread = row.  S = Q K^T (128 x 128) goes to tensor memory, the thread
-//    reads its row, and writes the weights P back to tensor memory as the A operand of O += P V, which stays in tensor memory
-//    as well: 2 x (128 columns S, 64 P, 64 O) = all 512 columns.  P has columns of its own, so that the next S is computed
-//    while a row is exponentiated.
-//  * One warp per warpgroup issues its MMAs, one plans the work and loads queries (and packed keys and values) by TMA, one
-//    looks at the values of tiles that not every row sees (below).  Over a cache four more warps fetch the blocks of a tile
-//    through the block table and convert the codes: K to bf16, V to f16, both exact for E4M3 and for E2M1 times its scale.
-//  * Wide groups: 32 tokens, 16 per warpgroup, both reading the same tiles of keys.  Narrow ones (few tokens, or few groups):
-//    16 tokens, the warpgroups take the tiles in turn and join at the end through tensor memory.
-//  * The weights of a bf16 V are bf16 (half a step, 2^-8 of each, the rounding of the output itself); those of a converted V
-//    are f16 (2^-11), scaled by 2^11 so that weights down to 2^-25 of the reference keep all their bits.  The reference is
-//    raised, and O rescaled, only when a row's maximum exceeds it by more than 2^4.  Sums are float32.
+//  * Four streams, each with a warpgroup for the softmax (thread = row) and a warp that issues its MMAs.  A stream computes
+//    S = Q K^T (128 rows x 64 keys: half a tile) into 64 columns of tensor memory, its threads read their rows, write the weights
+//    P over them as the A operand of O += P V, and O stays in 64 columns of its own: 4 x (64 + 64) = all 512 columns.  Streams
+//    share nothing until their rows are done; then they join through tensor memory, each for a part of the channels.  The two
+//    halves of a tile are two streams, not one of twice the width, so that every scheduler has four softmax warps: the special
+//    function unit, which bounds the kernel (16 exponentials a clock and SM), is fed while others wait for loads and products.
+//    Measured on a prompt of 8192 tokens: 707 us, the unit busy for 72 % of the time; two streams of 128 keys, with S and P apart
+//    so that the next S is computed early, 966; the same with two threads to a row 802.
+//  * Wide groups: 32 tokens, two streams for each half of them, all reading the same tiles of keys.  Narrow ones (few tokens, or
+//    few groups): 16 tokens, two streams take the even tiles of keys, two the odd ones.
+//  * One warp plans the work and loads queries (and packed keys and values) by TMA, one looks at the values of tiles that not
+//    every row sees (below).  Over a cache four more warps fetch the blocks of a tile through the block table and convert the
+//    codes: K to bf16, V to f16, both exact for E4M3 and for E2M1 times its scale.
+//  * The weights of a bf16 V are bf16 (half a step, 2^-8 of each, the rounding of the output itself); they have float32's range,
+//    so the reference that they are relative to is taken from a row's first keys and looked at again only where their sum exceeds
+//    2^40 (no maximum in the usual tile: 740 -> 707 us).  Those of a converted V are f16 (2^-11), scaled by 2^11 so that weights
+//    down to 2^-25 of the reference keep all their bits; it is raised, and O rescaled, where a maximum exceeds it by more than 2^4.
+//    Sums are float32.
+//  * Work comes by request (cluster launch control): a CTA asks for the next block of the grid while it works on one.  Blocks are
+//    ordered long ones first within a sequence.
+//  * MMAs and copies are issued by one elected lane out of a converged warp, with operands that the compiler knows to be uniform
+//    (broadcast by a shuffle): otherwise every MMA costs 75 to 150 clocks to issue, which alone took 200 us of 950.
 //  * 0 x NaN: a tile of V that some row of the group does not see is searched for infinities and NaN before its product.  They
 //    are replaced by zero, and the rows that do see them get them added at the end, read again from where they come from.
 //
@@ -38,17 +48,19 @@ constexpr int kRowTokens = 16;              // tokens of a tile of rows
 constexpr int TK = 128;                     // keys of a tile
 constexpr int NBLK = TK / kBlock;
 constexpr int kTileBytes = TK * kHeadDim * 2;
-constexpr int kRing = 4;                    // work records in flight
+constexpr int kRing = 2;                    // work records: the one being worked on and the next
 constexpr unsigned kFull = 0xffffffffu;
+constexpr float kMuch = 1.1e12f;           // 2^40: weights that call for another reference
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// tensor memory of a warpgroup: S, P, O
-constexpr int kTmemS = 0, kTmemP = 256, kTmemO = 384;
+constexpr int kHalf = NBLK / 2;             // blocks of a stream's half of a tile
+// tensor memory: S (and P over it) of the four streams, then O
+constexpr int kTmemS = 0, kTmemO = 256;
 
 template <int SRC>
 struct Cfg {
   static constexpr bool kPaged = SRC != kSrcPacked;
   static constexpr bool kCodes = SRC == kSrcFp8 || SRC == kSrcFp4;
-  static constexpr int kThreads = kPaged ? 512 : 384;
+  static constexpr int kThreads = kPaged ? 896 : 768;
   static constexpr int kStages = kCodes ? 3 : 5;             // tiles of K and V in the form the MMAs read
   static constexpr int kBlockBytes = SRC == kSrcFp8 ? kBlock * kHeadDim : (SRC == kSrcFp4 ? kFp4BlockBytes : 0);
   static constexpr int kCodeTile = 2 * NBLK * kBlockBytes;   // codes of K and V of a tile as they lie in the cache
@@ -56,8 +68,10 @@ struct Cfg {
   static constexpr int kCopySlots = SRC == kSrcFp8 ? 5 : (SRC == kSrcFp4 ? 8 : 3);
   static constexpr int kCodeStages = kCodes ? kCopySlots : 0;
   static constexpr int kFullArrivals = kPaged ? 4 : 1;
-  // register shares of the softmax warpgroups and of the others; launch: 65536 / threads rounded down to 8
-  static constexpr int kRegsSoftmax = 208, kRegsOther = kPaged ? 48 : 88;
+  // Register shares of the softmax warpgroups and of the others.  They come out of what the launch has: 65536 / threads rounded
+  // down to 8 each, 72 x 896 and 80 x 768.
+  static constexpr int kRegsSoftmax = 96, kRegsOther = kPaged ? 40 : 48;
+  static_assert(512 * kRegsSoftmax + (kThreads - 512) * kRegsOther <= kThreads * (65536 / kThreads / 8 * 8), "more than there are");
   // shares of f16 weights lie at 2^11, of bf16 weights at 1
   static constexpr float kShift = kCodes ? 11.f : 0.f;
   static constexpr float kRaise = 4.f;
@@ -71,11 +85,13 @@ struct Ctl {
   uint64_t rec_full[kRing], rec_empty[kRing];
   uint64_t q_full[2], q_empty[2];
   uint64_t k_full[5], k_empty[5], v_full[5], v_empty[5], v_ok[5];
-  uint64_t s_full[2], s_empty[2], p_full[2], pv_done[2], o_empty[2];
-  uint64_t join_full, join_empty;
+  uint64_t s_full[4], p_full[4], o_full[4], o_empty[4];   // of the streams
+  uint64_t join_full[2];
+  uint64_t next_full;
+  alignas(16) uint4 next;   // answer to a request for work
   uint64_t copied[4][8];
   Record rec[kRing];
-  float join[128][2];
+  float2 join[2][4][128];   // by turns: reference and sum of a stream's rows
   uint32_t tmem;
   volatile int abort;
 };
@@ -86,10 +102,10 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// Matrix descriptor of a tile with 128-byte rows and the 128-byte swizzle, eight rows every 1024 bytes.
-__device__ __forceinline__ uint64_t desc128(uint32_t saddr) {
-  return (uint64_t)((saddr >> 4) & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)64 << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+// Matrix descriptor of a tile with 128-byte rows and the 128-byte swizzle, eight rows every 1024 bytes.  `lo`: its address in units
+// of 16 bytes, plus kDescLo.
+constexpr uint32_t kDescLo = 1u << 16, kDescHi = 64u | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint64_t desc128(uint32_t lo) { return (uint64_t)kDescHi << 32 | lo; }
 __device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -128,6 +144,42 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], " PZ_LIST32 ";" ::PZ_V32(r), "r"(taddr) : "memory");
 }
 
+#define PZ_LIST16 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}"
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 " PZ_LIST16 ", [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                 "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], " PZ_LIST16 ";" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
+               "r"(r[14]), "r"(r[15]), "r"(taddr)
+               : "memory");
+}
+
+// Pairs of floats, one instruction for both.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
@@ -162,6 +214,27 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
 // Two f16 values, both exact in bf16.
 __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t h) { return f32x2_to_bf16x2(f16_lo_to_f32(h), f16_hi_to_f32(h)); }
 
+// Work by request: a CTA asks for a block of the grid that has not been started, and works in its place.  The answer goes to 16
+// bytes of shared memory.
+__device__ __forceinline__ void request_block(uint32_t dst, uint32_t bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(dst), "r"(bar)
+               : "memory");
+}
+// The block's index, -1: there is none left.
+__device__ __forceinline__ int granted_block(uint32_t src) {
+  uint32_t ok, x;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 a;\n\t"
+      "ld.shared.b128 a, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, a;\n\t}"
+      : "=r"(ok), "=r"(x)
+      : "r"(src)
+      : "memory");
+  return ok ? (int)x : -1;
+}
+
 // Waits by whole warps: one decision for the 32 lanes.
 struct Waiter {
   Ctl* C;
@@ -188,19 +261,18 @@ struct Waiter {
   }
 };
 
-// What a warpgroup does of a record: its tokens, the tiles [t0, t1) in steps of `step`, and where its keys end.
+// What stream (w, h) does of a record: its tokens, the tiles [t0, t1) in steps of `step` (half h of each), where its keys end.
 struct Share {
-  int pos, ntok, t0, t1, step, kb_hi, nt;
-  __device__ __forceinline__ Share(const Record& r, int w, int narrow, int window) {
+  int pos, ntok, t0, t1, step, end;
+  __device__ __forceinline__ Share(const Record& r, int w, int h, int narrow, int window) {
     const int first = narrow ? 0 : kRowTokens * w;
     pos = r.pos0 + first;
     ntok = min(max(r.ntok - first, 0), kRowTokens);
     const int hi = pos + ntok;                                              // behind the last key that one of them sees
-    const int lo = window > 0 ? max(pos - window + 1, 0) : 0;
-    kb_hi = min(r.kb_end, hi > 0 ? (hi + kBlock - 1) / kBlock : 0);
-    nt = (r.kb_end - r.kb0 + NBLK - 1) / NBLK;
-    t0 = max(lo / kBlock - r.kb0, 0) / NBLK;
-    t1 = ntok > 0 && kb_hi > r.kb0 ? (kb_hi - r.kb0 + NBLK - 1) / NBLK : 0;
+    const int lo = (window > 0 ? max(pos - window + 1, 0) : 0) / kBlock - r.kb0 - kHalf * h;
+    end = ntok > 0 ? min(r.kb_end, hi > 0 ? (hi + kBlock - 1) / kBlock : 0) - r.kb0 - kHalf * h : 0;   // blocks, counted from half h
+    t0 = lo >= kHalf ? (lo - kHalf) / NBLK + 1 : 0;
+    t1 = end > 0 ? (end + NBLK - 1) / NBLK : 0;
     step = 1;
     if (narrow) {
       step = 2;
@@ -209,9 +281,11 @@ struct Share {
     if (t0 >= t1) t0 = t1 = 0;
   }
   __device__ __forceinline__ bool on() const { return t1 > t0; }
-  __device__ __forceinline__ bool mine(int t) const { return t >= t0 && t < t1 && (t - t0) % step == 0; }
-  __device__ __forceinline__ int blocks(const Record& r, int t) const { return min(kb_hi - r.kb0 - t * NBLK, NBLK); }
+  __device__ __forceinline__ bool mine(int t) const { return t >= t0 && t < t1 && ((t - t0) & (step - 1)) == 0; }
+  __device__ __forceinline__ bool last(int t) const { return t + step >= t1; }
+  __device__ __forceinline__ int blocks(int t) const { return min(end - t * NBLK, kHalf); }
 };
+__device__ __forceinline__ int tiles_of(const Record& r) { return (r.kb_end - r.kb0 + NBLK - 1) / NBLK; }
 
 // Value d of key `key` of a record's sequence and head, in units of v_scale; for the rows that see an infinity or a NaN.
 template <int SRC>
@@ -253,15 +327,15 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
   Ctl* C = reinterpret_cast<Ctl*>(smem + K::kSmem);
   const uint32_t q_at = smem_u32(smem), k_at = q_at + 2 * kTileBytes, v_at = k_at + NS * kTileBytes;
   [[maybe_unused]] const uint32_t code_at = v_at + NS * kTileBytes;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // (uniform, as the compiler sees it)
   const int narrow = P.narrow, window = P.window;
   const Waiter wait{C, P.dev_status};
 
   if (threadIdx.x == 0) {
-    const int users = narrow ? 1 : 2;   // warpgroups that read a tile of keys
+    const int users = narrow ? 2 : 4;   // streams that read a tile of keys
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&C->rec_full[i]), 1);
-      mbar_init(smem_u32(&C->rec_empty[i]), 8 + 3 + (K::kPaged ? 4 : 0));
+      mbar_init(smem_u32(&C->rec_empty[i]), 16 + 4 + 1 + 1 + (K::kPaged ? 4 : 0));
     }
     for (int i = 0; i < NS; ++i) {
       mbar_init(smem_u32(&C->k_full[i]), K::kFullArrivals);
@@ -272,16 +346,17 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&C->q_full[i]), 1);
-      mbar_init(smem_u32(&C->q_empty[i]), 1);
-      mbar_init(smem_u32(&C->s_full[i]), 1);
-      mbar_init(smem_u32(&C->s_empty[i]), 4);
-      mbar_init(smem_u32(&C->p_full[i]), 4);
-      mbar_init(smem_u32(&C->pv_done[i]), 1);
-      mbar_init(smem_u32(&C->o_empty[i]), 4);
+      mbar_init(smem_u32(&C->q_empty[i]), 2);
+      mbar_init(smem_u32(&C->join_full[i]), narrow ? 16 : 8);
     }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(smem_u32(&C->s_full[i]), 1);
+      mbar_init(smem_u32(&C->p_full[i]), 4);
+      mbar_init(smem_u32(&C->o_full[i]), 1);
+      mbar_init(smem_u32(&C->o_empty[i]), narrow ? 16 : 8);   // the warps that join
+    }
+    mbar_init(smem_u32(&C->next_full), 1);
     for (int i = 0; i < 4 * 8; ++i) mbar_init(smem_u32(&C->copied[0][0] + i), 32);
-    mbar_init(smem_u32(&C->join_full), 4);
-    mbar_init(smem_u32(&C->join_empty), 4);
     C->abort = 0;
     fence_mbar_init();
     tma_prefetch_desc(&P.tmQ);
@@ -290,21 +365,31 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
       tma_prefetch_desc(&P.tmV);
     }
   }
-  if (warp == 8) {
+  if (warp == 16) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&C->tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_before();
   __syncthreads();
   tc_after();
-  const uint32_t tmem = C->tmem;
+  const uint32_t tmem = __shfl_sync(kFull, C->tmem, 0);
   grid_dependency_wait();
 
   // The record of item n, copied; the slot is let go at once by those that do not need it later (release()).
   auto get_record = [&](int n, Record& r) -> bool {
     const int s = n % kRing;
     if (!wait(C->rec_full[s], (uint32_t)(n / kRing) & 1u)) return false;
-    r = C->rec[s];
+    // the same in all lanes, and known to be: operands of MMAs and copies that come of it stay in uniform registers
+    const Record& c = C->rec[s];
+    r.on = __shfl_sync(kFull, c.on, 0);
+    r.b = __shfl_sync(kFull, c.b, 0);
+    r.kvh = __shfl_sync(kFull, c.kvh, 0);
+    r.row0 = __shfl_sync(kFull, c.row0, 0);
+    r.ntok = __shfl_sync(kFull, c.ntok, 0);
+    r.pos0 = __shfl_sync(kFull, c.pos0, 0);
+    r.kb0 = __shfl_sync(kFull, c.kb0, 0);
+    r.kb_end = __shfl_sync(kFull, c.kb_end, 0);
+    r.part = __shfl_sync(kFull, c.part, 0);
     return r.on != 0;
   };
   auto release = [&](int n) {
@@ -312,77 +397,75 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
     if (lane == 0) mbar_arrive(smem_u32(&C->rec_empty[n % kRing]));
   };
 
-  if (warp >= 8) {
+  if (warp >= 16) {
     regs_down<K::kRegsOther>();
-    if (warp < 10) {
-      // ================================================================= MMA issue, one warp per softmax warpgroup
-      const int w = warp - 8;
+    if (warp < 20) {
+      // ================================================================= MMA issue, one warp per stream
+      const int st = warp - 16, w = st >> 1, h = st & 1;
       constexpr uint32_t kFmt = K::kCodes ? 0u : 1u;   // P and V: f16 or bf16
       constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);
       constexpr uint32_t kIdescPV = (1u << 4) | (kFmt << 7) | (kFmt << 10) | (1u << 16) | (8u << 17) | (8u << 24);
-      const uint32_t ts = tmem + kTmemS + 128 * w, tp = tmem + kTmemP + 64 * w, to = tmem + kTmemO + 64 * w;
-      const uint32_t qa = q_at + w * kTileBytes;
-      int kt = 0, n = 0, items = 0;   // tiles of all items, tiles and items of this warpgroup
-      int pend = -1, pend_nb = 0, pend_first = 0;
+      const uint32_t ts = tmem + kTmemS + 64 * st, to = tmem + kTmemO + 64 * st;
+      const uint32_t q_lo = ((q_at + w * kTileBytes) >> 4) + kDescLo, k_lo = ((k_at + h * (kTileBytes / 2)) >> 4) + kDescLo,
+                     v_lo = ((v_at + h * (kTileBytes / 2)) >> 4) + kDescLo;
+      int kt = 0, n = 0, items = 0, queries = 0;   // tiles of all items; tiles, items and query tiles of this stream
       Record r;
-      auto product = [&]() -> bool {   // O (+)= P V of the pending tile
-        const int s = pend % NS;
-        if (!wait(C->v_full[s], (uint32_t)(pend / NS) & 1u) || !wait(C->v_ok[s], (uint32_t)(pend / NS) & 1u)) return false;
-        if (pend_first && !wait(C->o_empty[w], ((uint32_t)items & 1u) ^ 1u)) return false;
-        if (!wait(C->p_full[w], (uint32_t)(n - 1) & 1u)) return false;
-        tc_after();
-        if (elect_one()) {
-          for (int ks = 0; ks < pend_nb; ++ks)   // a block of 16 keys each
-            umma_ts(to, tp + 8 * ks, desc128(v_at + s * kTileBytes + 2048 * ks), kIdescPV, !(pend_first && ks == 0));
-          umma_commit(smem_u32(&C->pv_done[w]));
-          umma_commit(smem_u32(&C->v_empty[s]));
-        }
-        __syncwarp();
-        pend = -1;
-        return true;
-      };
       bool ok = true;
       for (int it = 0; ok && get_record(it, r); ++it) {
         release(it);
-        const Share sh(r, w, narrow, window);
-        if (sh.on()) ok = wait(C->q_full[w], (uint32_t)items & 1u);
-        for (int t = 0; ok && t < sh.nt; ++t, ++kt) {
+        const Share sh(r, w, h, narrow, window);
+        const bool with_q = sh.on() || Share(r, w, h ^ 1, narrow, window).on();
+        if (with_q) {
+          ok = wait(C->q_full[w], (uint32_t)queries & 1u);
+          ++queries;
+          if (ok && !sh.on() && lane == 0) mbar_arrive(smem_u32(&C->q_empty[w]));
+        }
+        const int nt = tiles_of(r);
+        for (int t = 0; ok && t < nt; ++t, ++kt) {
           const int s = kt % NS;
           const uint32_t par = (uint32_t)(kt / NS) & 1u;
           if (sh.mine(t)) {
-            const int nb = sh.blocks(r, t);
-            ok = wait(C->k_full[s], par) && wait(C->s_empty[w], ((uint32_t)n & 1u) ^ 1u);
+            // The P that this S overwrites has been read: products of one CTA run in the order of their issue.
+            const int nb = sh.blocks(t);
+            ok = wait(C->k_full[s], par);
             if (!ok) break;
             tc_after();
             if (elect_one()) {
 #pragma unroll
               for (int ks = 0; ks < 4; ++ks)
-                umma_ss(ts, desc128(qa + 32 * ks), desc128(k_at + s * kTileBytes + 32 * ks), kIdescQK | (uint32_t)(2 * nb) << 17,
-                        ks);
-              umma_commit(smem_u32(&C->s_full[w]));
+                umma_ss(ts, desc128(q_lo + 2 * ks), desc128(k_lo + s * (kTileBytes / 16) + 2 * ks),
+                        kIdescQK | (uint32_t)(2 * nb) << 17, ks);
+              umma_commit(smem_u32(&C->s_full[st]));
               umma_commit(smem_u32(&C->k_empty[s]));
-              if (t + sh.step >= sh.t1) umma_commit(smem_u32(&C->q_empty[w]));
+              if (sh.last(t)) umma_commit(smem_u32(&C->q_empty[w]));
             }
             __syncwarp();
-            if (pend >= 0) ok = product();
+            const bool first = t == sh.t0;
+            ok = wait(C->v_ok[s], par) &&
+                 (!first || wait(C->o_empty[st], ((uint32_t)items & 1u) ^ 1u)) && wait(C->p_full[st], (uint32_t)n & 1u);
+            if (!ok) break;
+            tc_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int ks = 0; ks < kHalf; ++ks)   // a block of 16 keys each
+                if (ks < nb) umma_ts(to, ts + 8 * ks, desc128(v_lo + s * (kTileBytes / 16) + 128 * ks), kIdescPV, !(first && ks == 0));
+              if (sh.last(t)) umma_commit(smem_u32(&C->o_full[st]));
+              umma_commit(smem_u32(&C->v_empty[s]));
+            }
+            __syncwarp();
             ++n;
-            pend = kt;
-            pend_nb = nb;
-            pend_first = t == sh.t0;
-          } else if (!narrow) {   // the other warpgroup's tile alone: let go of it
-            if (pend >= 0) ok = product();
-            ok = ok && wait(C->k_full[s], par) && wait(C->v_full[s], par) && wait(C->v_ok[s], par);
-            if (ok && elect_one()) {
+          } else if (!narrow || (t & 1) == w) {   // other streams' alone: let go of it
+            ok = wait(C->k_full[s], par) && wait(C->v_full[s], par) && wait(C->v_ok[s], par);
+            if (ok && lane == 0) {
               mbar_arrive(smem_u32(&C->k_empty[s]));
               mbar_arrive(smem_u32(&C->v_empty[s]));
             }
             __syncwarp();
           }
         }
-        if (ok && pend >= 0) ok = product();
         if (sh.on()) ++items;
       }
-    } else if (warp == 10) {
+    } else if (warp == 20) {
       // ================================================================= work records, queries, packed keys and values
       const int T = narrow ? kRowTokens : 2 * kRowTokens;
       const int per_tile = P.Hkv * P.splits;
@@ -418,13 +501,31 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         }
       };
       load_window();
-      int kt = 0, q_n[2] = {0, 0};
+      int kt = 0;
       bool ok = true;
       for (int it = 0;; ++it) {
-        // items in rounds of one per CTA, every other round backwards: long and short ones even out
-        const long long item = (long long)it * gridDim.x + ((it & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-        const long long tile = item / per_tile;
-        const int rest = (int)(item - tile * per_tile);
+        // blocks of the grid are items, long ones first; the next is asked for when the one before the last has been done with
+        int item = blockIdx.x;
+        const int slot = it % kRing;
+        ok = wait(C->rec_empty[slot], ((uint32_t)(it / kRing) & 1u) ^ 1u);
+        if (ok && it > 0) {
+          fence_proxy_async();
+          __syncwarp();
+          if (elect_one()) {
+            const uint32_t bar = smem_u32(&C->next_full);
+            mbar_arrive_expect_tx(bar, 16);
+            request_block(smem_u32(&C->next), bar);
+          }
+          __syncwarp();
+          ok = wait(C->next_full, (uint32_t)(it - 1) & 1u);
+          if (ok) item = granted_block(smem_u32(&C->next));
+        }
+        if (!ok) break;
+        const int tile = item >= 0 ? item / per_tile : 0x7fffffff, rest = item - tile * per_tile;
+        if (tile < before) {   // (blocks are granted in order; this does not rely on it)
+          b0 = before = 0;
+          load_window();
+        }
         while (b0 < P.batch && before + __shfl_sync(kFull, upto, 31) <= tile) {
           before += __shfl_sync(kFull, upto, 31);
           b0 += 32;
@@ -438,7 +539,7 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
           const int s_cnt = __shfl_sync(kFull, cnt, src), s_upto = __shfl_sync(kFull, upto, src);
           const int s_st = __shfl_sync(kFull, st, src), s_len = __shfl_sync(kFull, len, src);
           const int s_n = __shfl_sync(kFull, ntok, src);
-          const int i = s_cnt - 1 - (int)(tile - (before + s_upto - s_cnt));   // a sequence's last tokens first
+          const int i = s_cnt - 1 - (tile - (before + s_upto - s_cnt));   // a sequence's last tokens first
           r.b = b0 + src;
           r.kvh = rest % P.Hkv;
           r.part = rest / P.Hkv;
@@ -454,32 +555,16 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
             r.kb_end = min(kb_lo + (int)((long long)nt * (r.part + 1) / parts) * NBLK, kb_hi);
           }
         }
-        const int slot = it % kRing;
-        ok = wait(C->rec_empty[slot], ((uint32_t)(it / kRing) & 1u) ^ 1u);
-        if (!ok) break;
         if (lane == 0) {
           C->rec[slot] = r;
           mbar_arrive(smem_u32(&C->rec_full[slot]));
         }
         __syncwarp();
         if (!r.on) break;
-        const Share a(r, 0, narrow, window), c(r, 1, narrow, window);
-        auto load_q = [&](const Share& sh, int w) {
-          if (!ok || !sh.on()) return;
-          ok = wait(C->q_empty[w], ((uint32_t)q_n[w] & 1u) ^ 1u);
-          ++q_n[w];
-          if (ok && elect_one()) {
-            const uint32_t bar = smem_u32(&C->q_full[w]);
-            mbar_arrive_expect_tx(bar, kTileBytes);
-            tma_load_3d(q_at + w * kTileBytes, &P.tmQ, 0, r.kvh * kGroup, r.row0 + (narrow ? 0 : kRowTokens * w), bar);
-          }
-          __syncwarp();
-        };
-        load_q(a, 0);
-        load_q(c, 1);
         if constexpr (!K::kPaged) {
           const int first = r.row0 - r.pos0;   // the sequence's first row
-          for (int t = 0; ok && t < a.nt; ++t, ++kt) {
+          const int nt = tiles_of(r);
+          for (int t = 0; ok && t < nt; ++t, ++kt) {
             const int s = kt % NS;
             const uint32_t par = ((uint32_t)(kt / NS) & 1u) ^ 1u;
             const int row = first + (r.kb0 + t * NBLK) * kBlock;
@@ -502,21 +587,19 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         if (!ok) break;
       }
       if (C->abort) {   // the copies in flight end before the shared memory is given back
-        for (int w = 0; w < 2; ++w)
-          if (q_n[w] > 0) mbar_wait_bounded(smem_u32(&C->q_full[w]), (uint32_t)(q_n[w] - 1) & 1u);
         for (int i = max(kt - NS, 0); i < kt; ++i) {
           mbar_wait_bounded(smem_u32(&C->k_full[i % NS]), (uint32_t)(i / NS) & 1u);
           mbar_wait_bounded(smem_u32(&C->v_full[i % NS]), (uint32_t)(i / NS) & 1u);
         }
       }
-    } else if (warp == 11) {
+    } else if (warp == 21) {
       // ================================================================= infinities and NaN among values not all rows see
       constexpr uint32_t kInf = K::kCodes ? 0x7c007c00u : 0x7f807f80u;
       int kt = 0;
       Record r;
       bool ok = true;
       for (int it = 0; ok && get_record(it, r); ++it) {
-        const int nt = (r.kb_end - r.kb0 + NBLK - 1) / NBLK;
+        const int nt = tiles_of(r);
         for (int t = 0; t < nt; ++t, ++kt) {
           const int s = kt % NS;
           ok = wait(C->v_full[s], (uint32_t)(kt / NS) & 1u);
@@ -546,11 +629,35 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         }
         release(it);
       }
-    } else if constexpr (K::kPaged) {
+    } else if (warp == 22) {
+      // ================================================================= queries
+      int q_n[2] = {0, 0};
+      Record r;
+      bool ok = true;
+      for (int it = 0; ok && get_record(it, r); ++it) {
+        release(it);
+        for (int w = 0; w < 2; ++w) {
+          if (!Share(r, w, 0, narrow, window).on() && !Share(r, w, 1, narrow, window).on()) continue;
+          ok = ok && wait(C->q_empty[w], ((uint32_t)q_n[w] & 1u) ^ 1u);
+          if (!ok) break;
+          ++q_n[w];
+          if (elect_one()) {
+            const uint32_t bar = smem_u32(&C->q_full[w]);
+            mbar_arrive_expect_tx(bar, kTileBytes);
+            tma_load_3d(q_at + w * kTileBytes, &P.tmQ, 0, r.kvh * kGroup, r.row0 + (narrow ? 0 : kRowTokens * w), bar);
+          }
+          __syncwarp();
+        }
+      }
+      if (C->abort)   // the copies in flight end before the shared memory is given back
+        for (int w = 0; w < 2; ++w)
+          if (q_n[w] > 0) mbar_wait_bounded(smem_u32(&C->q_full[w]), (uint32_t)(q_n[w] - 1) & 1u);
+    } else if (K::kPaged && warp >= 24) {
+     if constexpr (K::kPaged) {
       // ================================================================= blocks of the cache, four warps
       // Warp lw has blocks lw and lw + 4 of every tile, K and V, from the copy to the converted form: nothing is shared with
       // the other three.  Places in the cache are looked up for 16 tiles at a time, lane = 2 tile + block.
-      const int lw = warp - 12;
+      const int lw = warp - 24;
       constexpr int kSlots = K::kCopySlots;
       auto lookup = [&](const Record& r, int t_first) -> int {   // row (block, KV head) of the cache, -1: none
         const int j = r.kb0 + (t_first + (lane >> 1)) * NBLK + lw + 4 * (lane & 1);
@@ -576,7 +683,7 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
           if (!more) return false;
           release(++it);
           t = 0;
-          nt = (r.kb_end - r.kb0 + NBLK - 1) / NBLK;
+          nt = tiles_of(r);
           if (nt > 0) ent = lookup(r, 0);
         }
         return more;
@@ -723,179 +830,154 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         ++out;
       }
       cp_wait_all();   // none is in flight when the shared memory is given back
+     }
     }
   } else {
-    // =================================================================== softmax, two warpgroups, thread = row
+    // =================================================================== softmax, four warpgroups, thread = row
     regs_up<K::kRegsSoftmax>();
-    const int w = warp >> 2, wq = warp & 3, row = 32 * wq + lane, head = row & 7;
+    const int st = warp >> 2, w = st >> 1, h = st & 1, wq = warp & 3, row = 32 * wq + lane;
     const uint32_t quad = (uint32_t)(32 * wq) << 16;
-    const uint32_t ts = tmem + kTmemS + 128 * w + quad, tp = tmem + kTmemP + 64 * w + quad, to = tmem + kTmemO + quad;
-    int n = 0, joins = 0;   // tiles of this warpgroup, joined items
+    const uint32_t ts = tmem + kTmemS + 64 * st + quad, to = tmem + kTmemO + quad;
+    int n = 0, items = 0;   // tiles and items of this stream
     Record r;
     bool ok = true;
     for (int it = 0; ok && get_record(it, r); ++it) {
-      const Share sh(r, w, narrow, window);
-      const float ks = K::kCodes && P.k_scale ? P.k_scale[r.kvh] : 1.f;
-      float c = P.sm_scale_log2e * ks;
+      const Share sh(r, w, h, narrow, window);
+      float c = P.sm_scale_log2e;
+      if (K::kCodes && P.k_scale) c *= P.k_scale[r.kvh];
       const bool odd = !(c > 0.f && c < INFINITY);   // then logits are scaled before their maximum is taken
       const float pre = c;
       if (odd) c = 1.f;
       const int p = sh.pos + (row >> 3);                       // this row's position; it sees [lo, hi)
       const int hi = p + 1, lo = window > 0 ? p - window + 1 : 0;
-      float m = -INFINITY, ref = -K::kShift, l = 0.f;          // weights are 2^(c s - ref), ref = c m - shift
+      float m = -INFINITY, ref = -1e30f, l = 0.f;   // weights are 2^(c s - ref), ref = c m - shift; none yet: any logit is far above
       for (int t = sh.t0; t < sh.t1; t += sh.step, ++n) {
-        const int nb = sh.blocks(r, t), k0 = (r.kb0 + t * NBLK) * kBlock;
-        ok = wait(C->s_full[w], (uint32_t)n & 1u);
+        const int nb = sh.blocks(t), k0 = (r.kb0 + t * NBLK + kHalf * h) * kBlock;
+        ok = wait(C->s_full[st], (uint32_t)n & 1u);
         if (!ok) break;
         tc_after();
-        uint32_t u[128];
+        uint32_t u[64];
         float* s = reinterpret_cast<float*>(u);
-        const int chunks = (nb + 1) >> 1;                      // of 32 columns
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (q < chunks) tmem_ld32(ts + 32 * q, u + 32 * q);
+        const int p0 = sh.pos + 4 * wq;
+        // do all tokens of this warp see all keys?
+        const bool edge = odd || k0 + TK / 2 > p0 + 1 || (window > 0 && k0 < p0 + 3 - window + 1);
+        float part = 0.f;
+        for (bool look = K::kCodes || t == sh.t0;; look = true) {
+          tmem_ld32(ts, u);
+          if (nb > 2) tmem_ld32(ts + 32, u + 32);
           else
 #pragma unroll
-            for (int j = 0; j < 32; ++j) s[32 * q + j] = -INFINITY;
-        }
-        tmem_wait_ld();
-        tc_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&C->s_empty[w]));
-        if (odd)
+            for (int j = 32; j < 64; ++j) s[j] = -INFINITY;
+          tmem_wait_ld();
+          if (edge) {
+            if (odd)
 #pragma unroll
-          for (int j = 0; j < 128; ++j) s[j] *= pre;
-        // do all tokens of this warp see all keys?
-        const int p0 = sh.pos + 4 * wq;
-        if (k0 + TK > p0 + 1 || (window > 0 && k0 < p0 + 3 - window + 1)) {
-          const int jlo = lo - k0, wide = hi - lo;
+              for (int j = 0; j < 64; ++j) s[j] *= pre;
+            const int jlo = lo - k0;
+            const unsigned wide = (unsigned)max(hi - lo, 0);
 #pragma unroll
-          for (int j = 0; j < 128; ++j)
-            if ((unsigned)(j - jlo) >= (unsigned)max(wide, 0)) s[j] = -INFINITY;
-        }
-        float x[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-        for (int j = 4; j < 128; j += 4) {
-          x[0] = fmaxf(x[0], s[j]);
-          x[1] = fmaxf(x[1], s[j + 1]);
-          x[2] = fmaxf(x[2], s[j + 2]);
-          x[3] = fmaxf(x[3], s[j + 3]);
-        }
-        const float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-        const bool first = t == sh.t0;
-        const bool raise = top > m && (top - m) * c > K::kRaise;   // m = -inf: any finite top
-        if (__any_sync(kFull, raise)) {
-          float alpha = 1.f;
-          if (raise) {
-            const float now = top * c - K::kShift;
-            alpha = m == -INFINITY ? 0.f : ex2(ref - now);
-            m = top;
-            ref = now;
+            for (int j = 0; j < 64; ++j)
+              if ((unsigned)(j - jlo) >= wide) s[j] = -INFINITY;
           }
-          l *= alpha;
-          if (!first) {
-            ok = wait(C->pv_done[w], (uint32_t)(n - 1) & 1u);
-            if (!ok) break;
-            tc_after();
+          if (look) {
+            float x[4] = {s[0], s[1], s[2], s[3]};   // NaN beats everything
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              uint32_t o[32];
-              tmem_ld32(to + 64 * w + 32 * q, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
-              tmem_st32(to + 64 * w + 32 * q, o);
+            for (int j = 0; j < 64; j += 8) {
+              x[0] = max3(x[0], s[j], s[j + 1]);
+              x[1] = max3(x[1], s[j + 2], s[j + 3]);
+              x[2] = max3(x[2], s[j + 4], s[j + 5]);
+              x[3] = max3(x[3], s[j + 6], s[j + 7]);
             }
-          }
-        }
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            const float top = max3(max3(x[0], x[1], x[2]), x[3], x[3]);
+            const bool raise = top > m && (top - m) * c > K::kRaise;   // m = -inf: any finite top
+            if (__any_sync(kFull, raise)) {
+              float alpha = 1.f;
+              if (raise) {
+                const float now = top * c - K::kShift;
+                alpha = m == -INFINITY ? 0.f : ex2(ref - now);
+                m = top;
+                ref = now;
+              }
+              l *= alpha;
+              if (t != sh.t0) {        // the product before has ended: this S was issued behind it
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (q < chunks) {
+                for (int q = 0; q < 4; ++q) {
+                  uint32_t o[16];
+                  tmem_ld16(to + 64 * st + 16 * q, o);
+                  tmem_wait_ld();
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float e0 = ex2(fmaf(s[32 * q + j], c, -ref)), e1 = ex2(fmaf(s[32 * q + j + 1], c, -ref));
-              sum[j & 2] += e0;
-              sum[(j & 2) + 1] += e1;
-              u[16 * q + (j >> 1)] = K::kCodes ? f32x2_to_f16x2(e0, e1) : f32x2_to_bf16x2(e0, e1);
+                  for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                  tmem_st16(to + 64 * st + 16 * q, o);
+                }
+              }
             }
+            // infinity - infinity, or a NaN: the whole row is NaN
+            if (!(top < INFINITY)) ref = NAN;
           }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        if (n > 0) {   // P of the tile before has been read
-          ok = wait(C->pv_done[w], (uint32_t)(n - 1) & 1u);
-          if (!ok) break;
-          tc_after();
+          const uint64_t c2 = pack2(c, c), r2 = pack2(-ref, -ref);
+          uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const uint64_t x2 = fma2(pack2(s[2 * j], s[2 * j + 1]), c2, r2);
+            float x0, x1;
+            unpack2(x2, x0, x1);
+            const float e0 = ex2(x0), e1 = ex2(x1);
+            sum[j & 1] = add2(sum[j & 1], pack2(e0, e1));
+            u[j] = K::kCodes ? f32x2_to_f16x2(e0, e1) : f32x2_to_bf16x2(e0, e1);
+          }
+          float a0, a1;
+          unpack2(add2(sum[0], sum[1]), a0, a1);
+          part = a0 + a1;
+          if (look || !__any_sync(kFull, !(part < kMuch))) break;
         }
-        tmem_st32(tp, u);
-        if (chunks > 2) tmem_st32(tp + 32, u + 32);
+        tmem_st32(ts, u);
         tmem_wait_st();
         tc_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&C->p_full[w]));
+        if (lane == 0) mbar_arrive(smem_u32(&C->p_full[st]));
+        l += part;
       }
       if (!ok) break;
-      // ---- the item's end: O of this warpgroup, joined with the other's in narrow groups, by warpgroup 0
+      // ---- the item's end: the streams of a tile of rows join, each for its part of the channels
       if (sh.on()) {
-        ok = wait(C->pv_done[w], (uint32_t)(n - 1) & 1u);
+        ok = wait(C->o_full[st], (uint32_t)items & 1u);
         if (!ok) break;
-        tc_after();
+        ++items;
       }
-      const Share other(r, 1, narrow, window);
-      const bool join = narrow && other.on();
-      if (narrow && w == 1) {
-        if (join) {
-          ok = wait(C->join_empty, ((uint32_t)joins & 1u) ^ 1u);
-          if (!ok) break;
-          C->join[row][0] = m == -INFINITY ? -INFINITY : ref;
-          C->join[row][1] = l;
+      if (m == -INFINITY) ref = -INFINITY;   // no logit above -inf: the sum is 0, or a NaN
+      C->join[it & 1][st][row] = make_float2(ref, l);
+      tc_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&C->join_full[narrow ? 0 : w]));
+      ok = wait(C->join_full[narrow ? 0 : w], (uint32_t)it & 1u);
+      if (!ok) break;
+      tc_after();
+      const int g0 = narrow ? 0 : 2 * w, parts = narrow ? 4 : 2, cols = 64 / parts, col0 = cols * (st - g0);
+      ref = -INFINITY;
+      for (int i = 0; i < parts; ++i) ref = fmaxf(ref, C->join[it & 1][g0 + i][row].x);
+      const float zero = ref == -INFINITY ? 0.f : ref;
+      l = 0.f;
+      float o[32];
+#pragma unroll
+      for (int j = 0; j < 32; ++j) o[j] = 0.f;
+      for (int i = 0; i < parts; ++i) {
+        const float2 side = C->join[it & 1][g0 + i][row];
+        const float a = ex2(side.x - zero);
+        l += side.y * a;
+        if (Share(r, narrow ? i >> 1 : w, i & 1, narrow, window).on()) {
+          uint32_t v[16];
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            if (16 * q < cols) {
+              tmem_ld16(to + 64 * (g0 + i) + col0 + 16 * q, v);
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[16 * q + j] += __uint_as_float(v[j]) * a;
+            }
           tc_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&C->join_full));
-          ++joins;
+          if (lane == 0) mbar_arrive(smem_u32(&C->o_empty[g0 + i]));
         }
-        release(it);
-        continue;
-      }
-      uint32_t u[64];
-      float* o = reinterpret_cast<float*>(u);
-      if (m == -INFINITY) ref = -INFINITY;   // no logit above -inf; l is 0, or a NaN
-      if (sh.on()) {
-        tmem_ld32(to + 64 * w, u);
-        tmem_ld32(to + 64 * w + 32, u + 32);
-        tmem_wait_ld();
-      } else {
-#pragma unroll
-        for (int j = 0; j < 64; ++j) o[j] = 0.f;
-      }
-      if (join) {
-        ok = wait(C->join_full, (uint32_t)joins & 1u);
-        if (!ok) break;
-        tc_after();
-        const float ref1 = C->join[row][0], l1 = C->join[row][1];
-        const float both = fmaxf(ref, ref1), zero = both == -INFINITY ? 0.f : both;
-        const float a0 = ex2(ref - zero), a1 = ex2(ref1 - zero);
-        l = l * a0 + l1 * a1;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          uint32_t o1[32];
-          tmem_ld32(to + 64 + 32 * q, o1);
-          tmem_wait_ld();
-#pragma unroll
-          for (int j = 0; j < 32; ++j) o[32 * q + j] = o[32 * q + j] * a0 + __uint_as_float(o1[j]) * a1;
-        }
-        ref = both;
-        tc_before();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(smem_u32(&C->join_empty));
-          mbar_arrive(smem_u32(&C->o_empty[1]));
-        }
-        ++joins;
-      }
-      if (sh.on()) {
-        tc_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&C->o_empty[w]));
       }
       const bool real = (row >> 3) < sh.ntok;
       if (real && *reinterpret_cast<volatile int*>(&C->rec[it % kRing].bad_v)) {
@@ -908,11 +990,11 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
             continue;
           }
 #pragma unroll 1
-          for (int d = 0; d < kHeadDim; ++d) {
-            const float v = value_at<SRC>(P, r.b, r.kvh, first_row, key, d);
+          for (int d = 0; d < cols; ++d) {
+            const float v = value_at<SRC>(P, r.b, r.kvh, first_row, key, col0 + d);
             if (!(fabsf(v) < INFINITY)) {
 #pragma unroll
-              for (int j = 0; j < 64; ++j)
+              for (int j = 0; j < 32; ++j)
                 if (j == d) o[j] += v;
             }
           }
@@ -920,7 +1002,7 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
       }
       release(it);
       if (real) {
-        const int g = r.kvh * kGroup + head;
+        const int g = r.kvh * kGroup + (row & 7);
         const long long token = r.row0 + (narrow ? 0 : kRowTokens * w) + (row >> 3);
         const long long at = token * (P.Hkv * kGroup) + g;
         const float vs = K::kCodes && P.v_scale ? P.v_scale[r.kvh] : 1.f;
@@ -937,31 +1019,32 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         if (P.splits > 1) {
           if (l == 0.f) lse = -INFINITY;         // no key in this part, or none above -inf
           const size_t to_row = (size_t)r.part * ((size_t)P.total * (P.Hkv * kGroup)) + at;
-          P.part_lse[to_row] = lse;
+          if (st == g0) P.part_lse[to_row] = lse;
           if (lse != -INFINITY) {
-            float4* dst = reinterpret_cast<float4*>(P.part_o + to_row * kHeadDim);
+            float4* dst = reinterpret_cast<float4*>(P.part_o + to_row * kHeadDim + col0);
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-              dst[j] = make_float4(o[4 * j] * f, o[4 * j + 1] * f, o[4 * j + 2] * f, o[4 * j + 3] * f);
+            for (int j = 0; j < 8; ++j)
+              if (4 * j < cols) dst[j] = make_float4(o[4 * j] * f, o[4 * j + 1] * f, o[4 * j + 2] * f, o[4 * j + 3] * f);
           }
         } else {
           if (z == 0.f) {                        // nothing seen: zeros; nothing but logits of -inf: 0 / 0
             f = hi > 0 ? NAN : 0.f;
             lse = hi > 0 ? NAN : -INFINITY;
           }
-          uint4* dst = reinterpret_cast<uint4*>(P.out + at * kHeadDim);
+          uint4* dst = reinterpret_cast<uint4*>(P.out + at * kHeadDim + col0);
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            dst[j] = make_uint4(f32x2_to_bf16x2(o[8 * j] * f, o[8 * j + 1] * f), f32x2_to_bf16x2(o[8 * j + 2] * f, o[8 * j + 3] * f),
-                                f32x2_to_bf16x2(o[8 * j + 4] * f, o[8 * j + 5] * f), f32x2_to_bf16x2(o[8 * j + 6] * f, o[8 * j + 7] * f));
-          if (P.lse_out) P.lse_out[at] = lse;
+          for (int j = 0; j < 4; ++j)
+            if (8 * j < cols)
+              dst[j] = make_uint4(f32x2_to_bf16x2(o[8 * j] * f, o[8 * j + 1] * f), f32x2_to_bf16x2(o[8 * j + 2] * f, o[8 * j + 3] * f),
+                                  f32x2_to_bf16x2(o[8 * j + 4] * f, o[8 * j + 5] * f), f32x2_to_bf16x2(o[8 * j + 6] * f, o[8 * j + 7] * f));
+          if (P.lse_out && st == g0) P.lse_out[at] = lse;
         }
       }
       __syncwarp();
     }
   }
   __syncthreads();
-  if (warp == 8) {
+  if (warp == 16) {
     tc_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
@@ -1026,7 +1109,8 @@ cudaError_t launch(const PromptParams& P, int sm_count, cudaStream_t s, int* sme
   const int T = P.narrow ? kRowTokens : 2 * kRowTokens;
   const long long tiles = P.total / T + std::min(P.batch, P.total);   // no more than these, whatever the lengths
   const long long items = tiles * P.Hkv * P.splits;
-  cudaError_t e = launch_dependent(prompt_attn_kernel<SRC>, dim3((unsigned)std::min<long long>(items, sm_count)),
+  if (items > 0x7fffffff) return cudaErrorInvalidValue;
+  cudaError_t e = launch_dependent(prompt_attn_kernel<SRC>, dim3((unsigned)items),
                                    dim3(Cfg<SRC>::kThreads), need, s, P);
   count_launch();
   if (e == cudaSuccess && P.splits > 1) {
