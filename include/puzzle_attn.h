@@ -256,13 +256,13 @@ PUZZLE_API puzzle_status puzzle_prompt_attn(const puzzle_layer_desc* desc, const
  * is the better call for up to four tokens per sequence over an E4M3 or 4-bit cache; this one shares a pass over the cache
  * among 16 or 32 tokens and has no bound on them.  (Same passages as puzzle_prompt_attn and puzzle_decode_attn_tokens.)
  *   q: packed rows of bf16, stride q_token_stride; out, lse_out, sinks as puzzle_prompt_attn;
- *   workspace: at least puzzle_chunk_attn_workspace_bytes(...) bytes, 16-byte aligned; it needs no preparation, its size is the
- *     same for every batch and total_tokens, and nothing in it lasts from call to call.  Calls that share one must not overlap on
- *     the GPU;
+ *   workspace: at least puzzle_chunk_attn_workspace_bytes(...) bytes for this batch and total_tokens, 16-byte aligned (below 90 MB
+ *     with 8 KV heads on 148 SMs, and next to nothing where there are many tokens); it needs no preparation, and nothing in it lasts
+ *     from call to call.  Calls that share one must not overlap on the GPU;
  *   a token whose position is negative sees no key: out = 0, lse = sink.  A sequence longer than its table row is clamped to it
  *   (PUZZLE_DEV_SEQ_TOO_LONG); keys behind a bad block-table entry count as zeros (PUZZLE_DEV_BAD_BLOCK).
  * Softmax weights are held in bf16 over a bf16 cache (off by 2^-8 of themselves at most) and in f16 over the others (2^-11, down to
- * 2^-25 of the largest, 2^-36 of that below).  Two calls on the same inputs give the same bits. */
+ * 2^-23 of the largest, 2^-34 of that below).  Two calls on the same inputs give the same bits. */
 PUZZLE_API size_t puzzle_chunk_attn_workspace_bytes(const puzzle_layer_desc* desc, int32_t batch, int32_t total_tokens);
 PUZZLE_API puzzle_status puzzle_chunk_attn(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const void* q,
                                  int64_t q_token_stride, const int32_t* starts, const float* sinks, void* out,

@@ -609,7 +609,8 @@ puzzle_status puzzle_prompt_attn(const puzzle_layer_desc* desc, const puzzle_qkv
 
 size_t puzzle_chunk_attn_workspace_bytes(const puzzle_layer_desc* desc, int32_t batch, int32_t total_tokens) {
   if (check_desc(desc) != PUZZLE_OK || batch <= 0 || batch > kMaxBatch || total_tokens < 0 || total_tokens > kMaxPacked) return 0;
-  return prompt_partial_bytes(grid_ctas(), desc->num_kv_heads);
+  return prompt_partial_bytes(total_tokens, desc->num_kv_heads,
+                              prompt_most_splits(batch, total_tokens, desc->num_kv_heads, grid_ctas()));
 }
 
 puzzle_status puzzle_chunk_attn(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const void* q, int64_t q_token_stride,

@@ -21,11 +21,11 @@
 //  * One warp plans the work and loads queries (and packed keys and values) by TMA, one looks at the values of tiles that not
 //    every row sees (below).  Over a cache four more warps fetch the blocks of a tile through the block table and convert the
 //    codes: K to bf16, V to f16, both exact for E4M3 and for E2M1 times its scale.
-//  * The weights of a bf16 V are bf16 (half a step, 2^-8 of each, the rounding of the output itself); they have float32's range,
-//    so the reference that they are relative to is taken from a row's first keys and looked at again only where their sum exceeds
-//    2^40 (no maximum in the usual tile: 740 -> 707 us).  Those of a converted V are f16 (2^-11), scaled by 2^11 so that weights
-//    down to 2^-25 of the reference keep all their bits; it is raised, and O rescaled, where a maximum exceeds it by more than 2^4.
-//    Sums are float32.
+//  * The reference that weights are relative to is the largest logit of a row's first 64 keys.  It is looked at again, and O
+//    rescaled, only where the weights of 64 keys sum to more than the type of P can take: usual tiles need no maximum (740 -> 707
+//    us).  The weights of a bf16 V are bf16 (half a step, 2^-8 of each, the rounding of the output itself) with float32's range: the
+//    limit is 2^40.  Those of a converted V are f16 (2^-11) and lie at 2^9 of their value, so that the sum of 64 at the reference
+//    stays below the limit, f16's largest number, and weights down to 2^-23 of the reference keep all their bits.  Sums are float32.
 //  * Work comes by request (cluster launch control): a CTA asks for the next block of the grid while it works on one.  Blocks are
 //    ordered long ones first within a sequence.
 //  * MMAs and copies are issued by one elected lane out of a converged warp, with operands that the compiler knows to be uniform
@@ -50,7 +50,6 @@ constexpr int NBLK = TK / kBlock;
 constexpr int kTileBytes = TK * kHeadDim * 2;
 constexpr int kRing = 2;                    // work records: the one being worked on and the next
 constexpr unsigned kFull = 0xffffffffu;
-constexpr float kMuch = 1.1e12f;           // 2^40: weights that call for another reference
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kHalf = NBLK / 2;             // blocks of a stream's half of a tile
 // tensor memory: S (and P over it) of the four streams, then O
@@ -65,16 +64,15 @@ struct Cfg {
   static constexpr int kBlockBytes = SRC == kSrcFp8 ? kBlock * kHeadDim : (SRC == kSrcFp4 ? kFp4BlockBytes : 0);
   static constexpr int kCodeTile = 2 * NBLK * kBlockBytes;   // codes of K and V of a tile as they lie in the cache
   // tiles whose copies are in flight; a bf16 tile is copied to where the MMAs read it, and has to leave two of these places
-  static constexpr int kCopySlots = SRC == kSrcFp8 ? 5 : (SRC == kSrcFp4 ? 8 : 3);
+  static constexpr int kCopySlots = SRC == kSrcFp8 ? 3 : (SRC == kSrcFp4 ? 6 : 3);
   static constexpr int kCodeStages = kCodes ? kCopySlots : 0;
   static constexpr int kFullArrivals = kPaged ? 4 : 1;
   // Register shares of the softmax warpgroups and of the others.  They come out of what the launch has: 65536 / threads rounded
   // down to 8 each, 72 x 896 and 80 x 768.
   static constexpr int kRegsSoftmax = 96, kRegsOther = kPaged ? 40 : 48;
   static_assert(512 * kRegsSoftmax + (kThreads - 512) * kRegsOther <= kThreads * (65536 / kThreads / 8 * 8), "more than there are");
-  // shares of f16 weights lie at 2^11, of bf16 weights at 1
-  static constexpr float kShift = kCodes ? 11.f : 0.f;
-  static constexpr float kRaise = 4.f;
+  static constexpr float kShift = kCodes ? 9.f : 0.f;                  // weights lie at 2^shift of their value
+  static constexpr float kMuch = kCodes ? 65000.f : 1.0995116e12f;     // sum of 64 weights that calls for another reference
   static constexpr int kSmem = 2 * kTileBytes + 2 * kStages * kTileBytes + kCodeStages * kCodeTile;
 };
 
@@ -862,7 +860,7 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         // do all tokens of this warp see all keys?
         const bool edge = odd || k0 + TK / 2 > p0 + 1 || (window > 0 && k0 < p0 + 3 - window + 1);
         float part = 0.f;
-        for (bool look = K::kCodes || t == sh.t0;; look = true) {
+        for (bool look = t == sh.t0;; look = true) {
           tmem_ld32(ts, u);
           if (nb > 2) tmem_ld32(ts + 32, u + 32);
           else
@@ -889,7 +887,7 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
               x[3] = max3(x[3], s[j + 6], s[j + 7]);
             }
             const float top = max3(max3(x[0], x[1], x[2]), x[3], x[3]);
-            const bool raise = top > m && (top - m) * c > K::kRaise;   // m = -inf: any finite top
+            const bool raise = top > m;
             if (__any_sync(kFull, raise)) {
               float alpha = 1.f;
               if (raise) {
@@ -928,7 +926,7 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
           float a0, a1;
           unpack2(add2(sum[0], sum[1]), a0, a1);
           part = a0 + a1;
-          if (look || !__any_sync(kFull, !(part < kMuch))) break;
+          if (look || !__any_sync(kFull, !(part < K::kMuch))) break;
         }
         tmem_st32(ts, u);
         tmem_wait_st();
@@ -1123,24 +1121,41 @@ cudaError_t launch(const PromptParams& P, int sm_count, cudaStream_t s, int* sme
 
 }  // namespace
 
+// Groups of 32 tokens unless sequences have 16 or fewer on average, or there are fewer such groups than SMs and no way to cut their
+// keys instead: the streams of a narrow group take the tiles of keys in turn, which fetches (and converts) twice as many for the
+// same rows (512 tokens over 64K E4M3 keys: narrow 1224 us, wide and cut 963).
+// Keys are cut into the number of parts that takes the SM with the most of them the fewest tiles, a part's own cost counted as five
+// tiles; none has fewer than four tiles, and there are at most 8 parts per SM, which bounds the partials.
 PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool may_split, int sm_count) {
   const long long seqs = std::min(batch, total);
   PromptPlan plan;
   const long long wide = std::max<long long>((total + 2 * kRowTokens - 1) / (2 * kRowTokens), seqs) * Hkv;
-  plan.narrow = total <= kRowTokens * seqs || wide < sm_count;
+  const long long tiles = (key_bound + TK - 1) / TK;
+  plan.narrow = total <= kRowTokens * seqs || (wide < sm_count && (!may_split || tiles < 16));
   const long long items = plan.narrow ? std::max<long long>((total + kRowTokens - 1) / kRowTokens, seqs) * Hkv : wide;
   plan.splits = 1;
-  if (may_split && items < sm_count) {
-    const long long tiles = (key_bound + TK - 1) / TK;
-    plan.splits = (int)std::max<long long>(1, std::min<long long>(sm_count / items, tiles / 4));
+  if (may_split) {
+    double best = 1e30;
+    for (long long n = 1; n == 1 || (n <= tiles / 4 && n * items <= 8ll * sm_count); ++n) {
+      const double cost = (double)((items * n + sm_count - 1) / sm_count) * ((double)tiles / n + 5);
+      if (cost < best * 0.98) {   // a little gain is not worth the partials
+        best = cost;
+        plan.splits = (int)n;
+      }
+    }
   }
   return plan;
 }
 
-// Keys are cut only where groups are fewer than the SMs, and into no more parts than these leave room for: parts x rows is at
-// most the rows of that many groups.
-size_t prompt_partial_bytes(int sm_count, int Hkv) {
-  return (size_t)(sm_count + Hkv) * kRowTokens * kGroup * (kHeadDim + 1) * sizeof(float);
+size_t prompt_partial_bytes(int total, int Hkv, int splits) {
+  return std::max<size_t>(16, splits > 1 ? (size_t)splits * total * Hkv * kGroup * (kHeadDim + 1) * sizeof(float) : 0);
+}
+// The most parts that prompt_plan cuts into, whatever the context's length.
+int prompt_most_splits(int batch, int total, int Hkv, int sm_count) {
+  const long long seqs = std::min(batch, total);
+  const long long wide = std::max<long long>((total + 2 * kRowTokens - 1) / (2 * kRowTokens), seqs) * Hkv;
+  const long long narrow = std::max<long long>((total + kRowTokens - 1) / kRowTokens, seqs) * Hkv;
+  return (int)std::max<long long>(1, 8ll * sm_count / std::max<long long>(1, total <= kRowTokens * seqs ? narrow : wide));
 }
 
 cudaError_t launch_prompt_attn(const PromptParams& P, PromptSource src, int sm_count, cudaStream_t s, int* smem_limit) {

@@ -32,7 +32,8 @@ struct PromptPlan {
   int splits, narrow;
 };
 PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool may_split, int sm_count);
-size_t prompt_partial_bytes(int sm_count, int Hkv);   // of the partials of any call
+int prompt_most_splits(int batch, int total, int Hkv, int sm_count);
+size_t prompt_partial_bytes(int total, int Hkv, int splits);
 cudaError_t launch_prompt_attn(const PromptParams& P, PromptSource src, int sm_count, cudaStream_t s, int* smem_limit);
 
 }  // namespace puzzle
