@@ -48,7 +48,8 @@ constexpr int kRowTokens = 16;              // tokens of a tile of rows
 constexpr int TK = 128;                     // keys of a tile
 constexpr int NBLK = TK / kBlock;
 constexpr int kTileBytes = TK * kHeadDim * 2;
-constexpr int kRing = 2;                    // work records: the one being worked on and the next
+constexpr int kRing = 4;                    // work records: of the item being worked on and the next ones
+constexpr int kShortTiles = 4;              // items of no more tiles are asked for that far ahead, longer ones one ahead
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kHalf = NBLK / 2;             // blocks of a stream's half of a tile
@@ -211,6 +212,9 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
 }
 // Two f16 values, both exact in bf16.
 __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t h) { return f32x2_to_bf16x2(f16_lo_to_f32(h), f16_hi_to_f32(h)); }
+
+// The lowest n of 32 bits.
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
 
 // Work by request: a CTA asks for a block of the grid that has not been started, and works in its place.  The answer goes to 16
 // bytes of shared memory.
@@ -499,13 +503,15 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         }
       };
       load_window();
-      int kt = 0;
+      int kt = 0, before_tiles = 0;
       bool ok = true;
       for (int it = 0;; ++it) {
-        // blocks of the grid are items, long ones first; the next is asked for when the one before the last has been done with
+        // blocks of the grid are items, long ones first; a long one is asked for when the one before the last has been done with
         int item = blockIdx.x;
         const int slot = it % kRing;
         ok = wait(C->rec_empty[slot], ((uint32_t)(it / kRing) & 1u) ^ 1u);
+        if (ok && it > 1 && before_tiles > kShortTiles)
+          ok = wait(C->rec_empty[(it - 2) % kRing], (uint32_t)((it - 2) / kRing) & 1u);
         if (ok && it > 0) {
           fence_proxy_async();
           __syncwarp();
@@ -553,6 +559,7 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
             r.kb_end = min(kb_lo + (int)((long long)nt * (r.part + 1) / parts) * NBLK, kb_hi);
           }
         }
+        before_tiles = tiles_of(r);
         if (lane == 0) {
           C->rec[slot] = r;
           mbar_arrive(smem_u32(&C->rec_full[slot]));
