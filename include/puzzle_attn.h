@@ -231,11 +231,14 @@ PUZZLE_API puzzle_status puzzle_kv_append_rope(const puzzle_layer_desc* desc, co
  *   q_out: device bf16 [total_tokens][num_q_heads][head_dim], required when qkv->q is given; may be qkv->q itself if that is
  *     contiguous.  k_out: device bf16 [total_tokens][num_kv_heads][head_dim] or NULL; likewise.  A bad block-table entry
  *     skips the token in the cache only; tokens that are skipped altogether (see puzzle_kv_append_rope) leave their rows as they were;
+ *   keep_last: how many tokens of a sequence go into the cache, counted from its end (0: all of them).  A window layer's later steps
+ *     never read more than the window, and a ring of R blocks takes at most 16 (R - 1) tokens of a sequence in one call; every
+ *     token's rotated rows are given out all the same;
  *   the sequence strides of qkv mean nothing.  Errors and dev_status as puzzle_kv_append_rope. */
 PUZZLE_API puzzle_status puzzle_kv_append_packed(const puzzle_layer_desc* desc, const puzzle_kv_view* kv,
                                  const puzzle_rope* rope, const puzzle_qkv* qkv, void* q_out, void* k_out,
-                                 const int32_t* starts, int32_t batch, int32_t total_tokens, int32_t* dev_status,
-                                 void* stream);
+                                 const int32_t* starts, int32_t batch, int32_t total_tokens, int32_t keep_last,
+                                 int32_t* dev_status, void* stream);
 
 /* Attention of whole prompts over their own packed keys and values: token i of sequence b is one decode step of
  * puzzle_decode_attn (same formula, sinks and window) over the tokens [i + 1 - min(W, i + 1), i] of its sequence (all of [0, i]

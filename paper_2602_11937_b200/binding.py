@@ -131,7 +131,7 @@ def _load():
                                               vp, vp]
         lib.puzzle_kv_append_packed.restype = ctypes.c_int
         lib.puzzle_kv_append_packed.argtypes = [ctypes.POINTER(LayerDesc), ctypes.POINTER(KVView), ctypes.POINTER(Rope),
-                                                ctypes.POINTER(QKV), vp, vp, vp, i32, i32, vp, vp]
+                                                ctypes.POINTER(QKV), vp, vp, vp, i32, i32, i32, vp, vp]
         lib.puzzle_prompt_attn.restype = ctypes.c_int
         lib.puzzle_prompt_attn.argtypes = [ctypes.POINTER(LayerDesc), ctypes.POINTER(QKV), vp, vp, vp, vp, i32, i32, vp, vp]
         lib.puzzle_chunk_attn_workspace_bytes.restype = sz
@@ -433,12 +433,13 @@ def puzzle_kv_read_tokens(desc: LayerDesc, view: KVView, k_out: torch.Tensor, v_
 
 def puzzle_kv_append_packed(desc: LayerDesc, view: KVView, rope: Optional[Rope], q: Optional[torch.Tensor],
                             k_new: torch.Tensor, v_new: torch.Tensor, starts: torch.Tensor,
-                            q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                            q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, keep_last: int = 0,
                             dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """q, k_new, v_new: bf16 [tokens][heads][D], the tokens of all sequences behind each other, contiguous or slices of a
     wider array along the heads; starts: int32 [batch + 1]; q_out, k_out: the rotated rows, bf16, contiguous; rope None: k and v
-    go into the cache as they are, and q, q_out and k_out have to be None."""
-    _check(_native().kv_append_packed(desc, view, rope, q, k_new, v_new, starts, q_out, k_out, dev_status, stream),
+    go into the cache as they are, and q, q_out and k_out have to be None; keep_last: only the last so many tokens of a sequence
+    go into the cache (0: all)."""
+    _check(_native().kv_append_packed(desc, view, rope, q, k_new, v_new, starts, q_out, k_out, keep_last, dev_status, stream),
            "puzzle_kv_append_packed")
 
 

@@ -534,12 +534,13 @@ puzzle_status puzzle_kv_read_tokens(const puzzle_layer_desc* desc, const puzzle_
 
 puzzle_status puzzle_kv_append_packed(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const puzzle_rope* rope,
                                       const puzzle_qkv* qkv, void* q_out, void* k_out, const int32_t* starts, int32_t batch,
-                                      int32_t total_tokens, int32_t* dev_status, void* stream) {
+                                      int32_t total_tokens, int32_t keep_last, int32_t* dev_status, void* stream) {
   puzzle_status st = check_packed(desc, starts, batch, total_tokens);
   if (st != PUZZLE_OK) return st;
   st = check_view(desc, kv, batch);
   if (st != PUZZLE_OK) return st;
   if (!qkv || (rope && !rope->cos_sin)) return PUZZLE_ERR_NULL;
+  if (keep_last < 0) return PUZZLE_ERR_SHAPE;
   if (!rope && (qkv->q || q_out || k_out)) return PUZZLE_ERR_SHAPE;   // what is not rotated needs no other place
   if (rope) {
     if (rope->num_positions <= 0 || rope->rotary_dim <= 0 || rope->rotary_dim > desc->head_dim) return PUZZLE_ERR_SHAPE;
@@ -570,6 +571,7 @@ puzzle_status puzzle_kv_append_packed(const puzzle_layer_desc* desc, const puzzl
   A.k_out = static_cast<__nv_bfloat16*>(k_out);
   A.starts = starts;
   A.total = total_tokens;
+  A.keep_last = keep_last;
   if (rope) {
     A.pos_offset = rope->pos_offset;
     A.cos_sin = rope->cos_sin;

@@ -419,9 +419,9 @@ int packed_batch(const at::Tensor& starts) {
   return (int)(starts.size(0) - 1);
 }
 
-// desc, view, rope, q, k_new, v_new, starts, q_out, k_out, dev_status, stream
+// desc, view, rope, q, k_new, v_new, starts, q_out, k_out, keep_last, dev_status, stream
 PyObject* kv_append_packed(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return call("kv_append_packed", n, 11, [&](Here& here) {
+  return call("kv_append_packed", n, 12, [&](Here& here) {
     const auto desc = structure<puzzle_layer_desc>(a[0]);
     const auto view = structure<puzzle_kv_view>(a[1]);
     puzzle_rope rope = {};
@@ -442,10 +442,12 @@ PyObject* kv_append_packed(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t* starts = pointer_to<int32_t>(here, a[6], "starts", at::kInt, 2);
     void* q_out = packed_out(here, a[7], "q_out", tokens, desc.num_q_heads, desc.head_dim);
     void* k_out = packed_out(here, a[8], "k_out", tokens, desc.num_kv_heads, desc.head_dim);
-    int32_t* status = pointer_to<int32_t>(here, a[9], "dev_status", at::kInt, 1);
-    void* s = stream_of(here, a[10]);
+    const int keep = integer(a[9]);
+    int32_t* status = pointer_to<int32_t>(here, a[10], "dev_status", at::kInt, 1);
+    void* s = stream_of(here, a[11]);
     return unlocked([&] {
-      return entry.kv_append_packed(&desc, &view, rotate ? &rope : nullptr, &qkv, q_out, k_out, starts, batch, tokens, status, s);
+      return entry.kv_append_packed(&desc, &view, rotate ? &rope : nullptr, &qkv, q_out, k_out, starts, batch, tokens, keep, status,
+                                    s);
     });
   });
 }

@@ -132,7 +132,7 @@ struct AppendParams {
   // packed tokens (n_new and the sequence strides mean nothing then)
   const int32_t* starts;
   __nv_bfloat16* k_out;
-  int total;
+  int total, keep_last;   // keep_last: tokens of a sequence that go into the cache, from its end; 0 = all
 };
 cudaError_t launch_append(const AppendParams& P, int kv_dtype, bool rotate, bool adjacent, cudaStream_t s);
 

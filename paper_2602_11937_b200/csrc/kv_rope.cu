@@ -322,7 +322,8 @@ __global__ void __launch_bounds__(256, KV == PUZZLE_KV_BF16 ? 3 : 4) kv_append_c
     }
     return;
   }
-  [[maybe_unused]] const bool real = on;   // rotated keys go out whatever the block table says
+  [[maybe_unused]] const bool real = on;   // rotated keys go out whether they go into the cache or not
+  if (PACKED && P.keep_last > 0 && tok < sp.count - P.keep_last) on = false;
   long long blk = 0;
   if (on) {
     blk = block_of(P, b, pos, o == 0 && !is_v && job == 0);

@@ -1,4 +1,4 @@
-"""Per-layer pattern driver: one decode step of the attention stack of a model whose layers are each
+"""Per-layer pattern driver: one decode step, or the prompts before it, of the attention stack of a model whose layers are each
 full-context or sliding-window (the per-layer choice the paper's architecture search makes, Section
 "Window attention for long-context inference").
 
@@ -61,6 +61,44 @@ class DecodeStack:
             B.puzzle_decode_attn(self.descs[i], self.views[i], q_i, self.sinks[i], out[i], None,
                                  num_splits=self.num_splits, workspace=self.workspace, dev_status=self.status,
                                  stream=stream)
+
+    def prefill(self, q: List[torch.Tensor], k_new: List[torch.Tensor], v_new: List[torch.Tensor], starts: torch.Tensor,
+                out: List[torch.Tensor], continued: bool = False, stream=None) -> None:
+        """Append + attention of the prompts' tokens for every layer.  q[i], k_new[i], v_new[i]: bf16 [tokens][heads][D] of layer
+        i, the tokens of all sequences behind each other (slices of one projection's output will do); starts: int32
+        [batch + 1], first row of every sequence and the end of the last; out[i]: bf16 [tokens][Hq][D].  The lengths that
+        the stack was made with count these tokens already.
+
+        continued False: every sequence begins with these tokens; they attend to one another's keys and values as they are, and of
+        a window layer only the tokens that a later step can see go into the cache (a ring of ``window_ring_blocks`` takes
+        them).  continued True: pieces behind earlier tokens attend to the cache.  A window layer's cache then has to
+        hold the window before the piece's first token together with the piece, which a ring of that size does for very
+        short pieces only.  Not for capture: buffers are allocated as needed."""
+        tokens = q[0].shape[0]
+        d0 = self.descs[0]
+        rotate = self.rope is not None
+        room = lambda heads: torch.empty(tokens, heads, d0.head_dim, dtype=torch.bfloat16, device=q[0].device)
+        q_rot, k_rot = (room(d0.num_q_heads), room(d0.num_kv_heads)) if rotate else (None, None)
+        workspace = None
+        if continued:
+            nbytes = B.puzzle_chunk_attn_workspace_bytes(d0, self.batch, tokens)
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q[0].device)
+        if stream is not None:                       # the buffers are used there, whatever stream they were made on
+            stream.wait_stream(torch.cuda.current_stream())
+            for t in (q_rot, k_rot, workspace):
+                if t is not None:
+                    t.record_stream(stream)
+        for i, w in enumerate(self.windows):
+            keep = 0 if continued or w == 0 else -(-w // d0.block_size) * d0.block_size
+            B.puzzle_kv_append_packed(self.descs[i], self.views[i], self.rope, q[i] if rotate else None, k_new[i], v_new[i], starts,
+                                      q_rot, k_rot, keep, dev_status=self.status, stream=stream)
+            q_i, k_i = (q_rot, k_rot) if rotate else (q[i], k_new[i])
+            if continued:
+                B.puzzle_chunk_attn(self.descs[i], self.views[i], q_i, starts, self.sinks[i], out[i], workspace=workspace,
+                                    dev_status=self.status, stream=stream)
+            else:
+                B.puzzle_prompt_attn(self.descs[i], q_i, k_i, v_new[i], starts, self.sinks[i], out[i], dev_status=self.status,
+                                     stream=stream)
 
     def capture(self, q, k_new, v_new, out) -> "torch.cuda.CUDAGraph":
         """Records one step (with these argument tensors) into a CUDA graph; replay with ``graph.replay()``."""

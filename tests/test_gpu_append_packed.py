@@ -39,13 +39,14 @@ class Case:
         k, v = caches or self.caches
         return P.kv_view(k, v, self.seq_lens, block_table=self.table, k_scale=self.scales[0], v_scale=self.scales[1])
 
-    def call(self, rotate=True, with_q=True, with_k=True):
+    def call(self, rotate=True, with_q=True, with_k=True, keep_last=0):
         q, k, v = self.parts()
         if rotate:
             P.puzzle_kv_append_packed(self.desc, self.view(), self.rope, q if with_q else None, k, v, self.starts,
-                                      self.q_out if with_q else None, self.k_out if with_k else None, dev_status=self.status)
+                                      self.q_out if with_q else None, self.k_out if with_k else None, keep_last,
+                                      dev_status=self.status)
         else:
-            P.puzzle_kv_append_packed(self.desc, self.view(), None, None, k, v, self.starts, dev_status=self.status)
+            P.puzzle_kv_append_packed(self.desc, self.view(), None, None, k, v, self.starts, keep_last=keep_last, dev_status=self.status)
         torch.cuda.synchronize()
 
     def rectangle(self, caches, rotate=True):
@@ -198,3 +199,36 @@ def test_no_tokens_at_all():
     P.puzzle_chunk_attn(c.desc, c.view(), c.parts()[0], c.starts, None, c.q_out, workspace=ws)
     torch.cuda.synchronize()
     assert same_bytes(c.caches, before)
+
+
+@pytest.mark.parametrize("kv", ALL)
+@pytest.mark.parametrize("keep", [1, 16, 31, 500])
+def test_only_the_last_tokens_are_kept(kv, keep):
+    c = Case(kv, [70, 1, 500, 33, 18], [70, 1, 130, 0, 5])
+    before = [x.clone() for x in c.caches]
+    c.rectangle(before)                          # all of them, then what was there before in the places that are left alone
+    was = [x.clone() for x in c.caches]
+    new, lens = list(c.new), list(c.lens)
+    for b, n in enumerate(new):                  # the same bytes by appending the tail alone
+        if n > keep:
+            for p in range(lens[b] - n, lens[b] - keep):
+                blk, t = c.table[b, p // BLOCK].item(), p % BLOCK
+                for x, y, is_v in zip(before, was, (False, True)):
+                    if kv != "fp4":
+                        x[blk, :, t] = y[blk, :, t]
+                        continue
+                    d = torch.arange(D, device="cuda")
+                    byte = 256 * (d // 32) + 32 * (t // 2) + d % 32 if is_v else 32 * t + d // 2
+                    odd = torch.full_like(d, t % 2) if is_v else d % 2
+                    for e in (0, 1):
+                        at, mask = byte[odd == e], (0xf0 if e else 0x0f)
+                        x[blk, :, at] = (x[blk, :, at] & (0xff ^ mask)) | (y[blk, :, at] & mask)
+                    g = torch.arange(4, device="cuda")
+                    at = 512 + 16 * g + (4 * (t % 8 // 2) + 2 * (t // 8) + t % 2 if is_v else 2 * (t % 8) + t // 8)
+                    x[blk, :, at] = y[blk, :, at]
+    c.call(keep_last=keep)
+    assert c.status.item() == 0 and same_bytes(c.caches, before)
+    for b, n in enumerate(new):
+        rows, pos = slice(c.at[b], c.at[b + 1]), torch.arange(lens[b] - n, lens[b], device="cuda")
+        assert torch.equal(c.k_out[rows], c.turned(c.parts()[1][rows], pos, c.hkv).bfloat16())
+        assert torch.equal(c.q_out[rows], c.turned(c.parts()[0][rows], pos, c.hq).bfloat16())

@@ -18,7 +18,7 @@ def _args(over):
     kv.num_blocks, kv.max_blocks_per_seq = 64, 16
     rope = B.Rope(0x4000, 1024, 64, 0, None)
     qkv = B.QKV(0x5000, 0x6000, 0x7000, 0, 4096, 0, 512, 0, 512)
-    d = dict(desc=desc, kv=kv, rope=rope, qkv=qkv, q_out=0x8000, k_out=0x9000, starts=0xA000, batch=4, total=9, out=0x8000,
+    d = dict(desc=desc, kv=kv, rope=rope, qkv=qkv, q_out=0x8000, k_out=0x9000, starts=0xA000, batch=4, total=9, keep=0, out=0x8000,
              workspace=0x10000, workspace_bytes=1 << 30, stride=4096)
     for k, v in over.items():
         where, _, field = k.partition("__")
@@ -45,12 +45,12 @@ COMMON = [
     (dict(k_out=0x9004), SHAPE), (dict(qkv__k_token_stride=508), SHAPE), (dict(qkv__v_token_stride=0), SHAPE),
     (dict(qkv__q_token_stride=4100), SHAPE), (dict(qkv__q_token_stride=-4096), SHAPE),
     (dict(q_out=0x5000, qkv__q_token_stride=5120), SHAPE), (dict(k_out=0x6000, qkv__k_token_stride=5120), SHAPE),
-    (dict(num_q_heads=8 * 4097, num_kv_heads=4097), UNSUPPORTED), (dict(total=0, qkv__k=None), OK),
+    (dict(num_q_heads=8 * 4097, num_kv_heads=4097), UNSUPPORTED), (dict(total=0, qkv__k=None), OK), (dict(keep=-1), SHAPE),
 ])
 def test_append_packed(over, want):
     lib, d = _args(dict(over))
     assert lib.puzzle_kv_append_packed(ref(d["desc"]), ref(d["kv"]), ref(d["rope"]), ref(d["qkv"]), d["q_out"], d["k_out"],
-                                       d["starts"], d["batch"], d["total"], None, None) == want
+                                       d["starts"], d["batch"], d["total"], d["keep"], None, None) == want
 
 
 @pytest.mark.parametrize("over, want", COMMON + [
