@@ -604,7 +604,9 @@ puzzle_status puzzle_prompt_attn(const puzzle_layer_desc* desc, const puzzle_qkv
       !make_rows_map(&P.tmK, qkv->k, Hkv, total_tokens, qkv->k_token_stride, 1, 128) ||
       !make_rows_map(&P.tmV, qkv->v, Hkv, total_tokens, qkv->v_token_stride, 1, 128))
     return PUZZLE_ERR_CUDA;
-  P.narrow = prompt_plan(batch, total_tokens, Hkv, 0, false, grid_ctas()).narrow;
+  long long keys = total_tokens / std::min(batch, total_tokens) / 2;   // on average, where lengths are alike
+  if (desc->window > 0) keys = std::min<long long>(keys, desc->window);
+  P.turns = prompt_plan(batch, total_tokens, Hkv, keys, false, 0.05, grid_ctas()).turns;
   const cudaError_t e = launch_prompt_attn(P, kSrcPacked, grid_ctas(), static_cast<cudaStream_t>(stream), device_info().smem_prompt);
   return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
 }
@@ -640,9 +642,9 @@ puzzle_status puzzle_chunk_attn(const puzzle_layer_desc* desc, const puzzle_kv_v
   P.max_blocks_per_seq = kv->max_blocks_per_seq;
   if (!make_rows_map(&P.tmQ, q, desc->num_q_heads, total_tokens, q_token_stride, kGroup, 16)) return PUZZLE_ERR_CUDA;
   long long keys = (long long)kv->max_blocks_per_seq * kBlock;
-  if (desc->window > 0) keys = std::min<long long>(keys, (long long)desc->window + 2 * kBlock);
-  const PromptPlan plan = prompt_plan(batch, total_tokens, P.Hkv, keys, true, grid_ctas());
-  P.narrow = plan.narrow;
+  if (desc->window > 0) keys = std::min<long long>(keys, (long long)desc->window);
+  const PromptPlan plan = prompt_plan(batch, total_tokens, P.Hkv, keys, true, desc->kv_dtype == PUZZLE_KV_BF16 ? 0.1 : 0.3, grid_ctas());
+  P.turns = plan.turns;
   P.splits = plan.splits;
   P.part_o = static_cast<float*>(workspace);
   P.part_lse = P.part_o + (size_t)plan.splits * total_tokens * desc->num_q_heads * kHeadDim;

@@ -16,8 +16,9 @@
 //    function unit, which bounds the kernel (16 exponentials a clock and SM), is fed while others wait for loads and products.
 //    Measured on a prompt of 8192 tokens: 707 us, the unit busy for 72 % of the time; two streams of 128 keys, with S and P apart
 //    so that the next S is computed early, 966; the same with two threads to a row 802.
-//  * Wide groups: 32 tokens, two streams for each half of them, all reading the same tiles of keys.  Narrow ones (few tokens, or
-//    few groups): 16 tokens, two streams take the even tiles of keys, two the odd ones.
+//  * A group of 64, 32 or 16 tokens is 4, 2 or 1 tiles of rows with 1, 2 or 4 streams each; these take the halves of the tiles of keys
+//    in turn and join at the end.  Large groups fetch (and convert) a tile of keys once for many rows and have nothing to join, small
+//    ones make more items of few tokens.
 //  * One warp plans the work and loads queries (and packed keys and values) by TMA, one looks at the values of tiles that not
 //    every row sees (below).  Over a cache four more warps fetch the blocks of a tile through the block table and convert the
 //    codes: K to bf16, V to f16, both exact for E4M3 and for E2M1 times its scale.
@@ -61,11 +62,11 @@ struct Cfg {
   static constexpr bool kPaged = SRC != kSrcPacked;
   static constexpr bool kCodes = SRC == kSrcFp8 || SRC == kSrcFp4;
   static constexpr int kThreads = kPaged ? 896 : 768;
-  static constexpr int kStages = kCodes ? 3 : 5;             // tiles of K and V in the form the MMAs read
+  static constexpr int kStages = kCodes ? 3 : 4;             // tiles of K and V in the form the MMAs read
   static constexpr int kBlockBytes = SRC == kSrcFp8 ? kBlock * kHeadDim : (SRC == kSrcFp4 ? kFp4BlockBytes : 0);
   static constexpr int kCodeTile = 2 * NBLK * kBlockBytes;   // codes of K and V of a tile as they lie in the cache
   // tiles whose copies are in flight; a bf16 tile is copied to where the MMAs read it, and has to leave two of these places
-  static constexpr int kCopySlots = SRC == kSrcFp8 ? 3 : (SRC == kSrcFp4 ? 6 : 3);
+  static constexpr int kCopySlots = SRC == kSrcFp8 ? 3 : (SRC == kSrcFp4 ? 5 : 3);
   static constexpr int kCodeStages = kCodes ? kCopySlots : 0;
   static constexpr int kFullArrivals = kPaged ? 4 : 1;
   // Register shares of the softmax warpgroups and of the others.  They come out of what the launch has: 65536 / threads rounded
@@ -74,7 +75,7 @@ struct Cfg {
   static_assert(512 * kRegsSoftmax + (kThreads - 512) * kRegsOther <= kThreads * (65536 / kThreads / 8 * 8), "more than there are");
   static constexpr float kShift = kCodes ? 9.f : 0.f;                  // weights lie at 2^shift of their value
   static constexpr float kMuch = kCodes ? 65000.f : 1.0995116e12f;     // sum of 64 weights that calls for another reference
-  static constexpr int kSmem = 2 * kTileBytes + 2 * kStages * kTileBytes + kCodeStages * kCodeTile;
+  static constexpr int kSmem = 4 * kTileBytes + 2 * kStages * kTileBytes + kCodeStages * kCodeTile;
 };
 
 struct Record {
@@ -82,10 +83,10 @@ struct Record {
 };
 struct Ctl {
   uint64_t rec_full[kRing], rec_empty[kRing];
-  uint64_t q_full[2], q_empty[2];
+  uint64_t q_full[4], q_empty[4];                         // of the tiles of rows
   uint64_t k_full[5], k_empty[5], v_full[5], v_empty[5], v_ok[5];
   uint64_t s_full[4], p_full[4], o_full[4], o_empty[4];   // of the streams
-  uint64_t join_full[2];
+  uint64_t join_full[4];
   uint64_t next_full;
   alignas(16) uint4 next;   // answer to a request for work
   uint64_t copied[4][8];
@@ -263,29 +264,26 @@ struct Waiter {
   }
 };
 
-// What stream (w, h) does of a record: its tokens, the tiles [t0, t1) in steps of `step` (half h of each), where its keys end.
+// What stream st does of a record, `turns` streams to a tile of rows: its tokens, and of the half tiles [j_lo, j_hi) that they see
+// those from j0 on, every turns-th.
 struct Share {
-  int pos, ntok, t0, t1, step, end;
-  __device__ __forceinline__ Share(const Record& r, int w, int h, int narrow, int window) {
-    const int first = narrow ? 0 : kRowTokens * w;
+  int pos, ntok, j_lo, j_hi, j0, turns, end;
+  __device__ __forceinline__ Share(const Record& r, int st, int turns_, int window) : turns(turns_) {
+    const int first = kRowTokens * (st / turns);
     pos = r.pos0 + first;
     ntok = min(max(r.ntok - first, 0), kRowTokens);
     const int hi = pos + ntok;                                              // behind the last key that one of them sees
-    const int lo = (window > 0 ? max(pos - window + 1, 0) : 0) / kBlock - r.kb0 - kHalf * h;
-    end = ntok > 0 ? min(r.kb_end, hi > 0 ? (hi + kBlock - 1) / kBlock : 0) - r.kb0 - kHalf * h : 0;   // blocks, counted from half h
-    t0 = lo >= kHalf ? (lo - kHalf) / NBLK + 1 : 0;
-    t1 = end > 0 ? (end + NBLK - 1) / NBLK : 0;
-    step = 1;
-    if (narrow) {
-      step = 2;
-      t0 += (t0 ^ w) & 1;
-    }
-    if (t0 >= t1) t0 = t1 = 0;
+    const int lo = window > 0 ? max(pos - window + 1, 0) : 0;
+    end = ntok > 0 ? min(r.kb_end, hi > 0 ? (hi + kBlock - 1) / kBlock : 0) - r.kb0 : 0;   // blocks
+    j_lo = max(lo / kBlock - r.kb0, 0) / kHalf;
+    j_hi = end > 0 ? (end + kHalf - 1) / kHalf : 0;
+    j0 = j_lo + ((st - j_lo) & (turns - 1));
   }
-  __device__ __forceinline__ bool on() const { return t1 > t0; }
-  __device__ __forceinline__ bool mine(int t) const { return t >= t0 && t < t1 && ((t - t0) & (step - 1)) == 0; }
-  __device__ __forceinline__ bool last(int t) const { return t + step >= t1; }
-  __device__ __forceinline__ int blocks(int t) const { return min(end - t * NBLK, kHalf); }
+  __device__ __forceinline__ bool any() const { return j_hi > j_lo; }      // one of the streams of these tokens
+  __device__ __forceinline__ bool on() const { return j_hi > j0; }
+  __device__ __forceinline__ bool mine(int j) const { return j >= j0 && j < j_hi; }   // j of this stream's turn
+  __device__ __forceinline__ bool last(int j) const { return j + turns >= j_hi; }
+  __device__ __forceinline__ int blocks(int j) const { return min(end - j * kHalf, kHalf); }
 };
 __device__ __forceinline__ int tiles_of(const Record& r) { return (r.kb_end - r.kb0 + NBLK - 1) / NBLK; }
 
@@ -327,14 +325,14 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
   const uint32_t raw = smem_u32(smem_raw);
   uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);
   Ctl* C = reinterpret_cast<Ctl*>(smem + K::kSmem);
-  const uint32_t q_at = smem_u32(smem), k_at = q_at + 2 * kTileBytes, v_at = k_at + NS * kTileBytes;
+  const uint32_t q_at = smem_u32(smem), k_at = q_at + 4 * kTileBytes, v_at = k_at + NS * kTileBytes;
   [[maybe_unused]] const uint32_t code_at = v_at + NS * kTileBytes;
   const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // (uniform, as the compiler sees it)
-  const int narrow = P.narrow, window = P.window;
+  const int turns = P.turns, window = P.window;
   const Waiter wait{C, P.dev_status};
 
   if (threadIdx.x == 0) {
-    const int users = narrow ? 2 : 4;   // streams that read a tile of keys
+    const int users = turns == 4 ? 2 : 4;   // streams that read a tile of keys
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&C->rec_full[i]), 1);
       mbar_init(smem_u32(&C->rec_empty[i]), 16 + 4 + 1 + 1 + (K::kPaged ? 4 : 0));
@@ -346,16 +344,14 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
       mbar_init(smem_u32(&C->v_empty[i]), users);
       mbar_init(smem_u32(&C->v_ok[i]), 1);
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&C->q_full[i]), 1);
-      mbar_init(smem_u32(&C->q_empty[i]), 2);
-      mbar_init(smem_u32(&C->join_full[i]), narrow ? 16 : 8);
-    }
     for (int i = 0; i < 4; ++i) {
+      mbar_init(smem_u32(&C->q_full[i]), 1);
+      mbar_init(smem_u32(&C->q_empty[i]), turns);
+      mbar_init(smem_u32(&C->join_full[i]), 4 * turns);
       mbar_init(smem_u32(&C->s_full[i]), 1);
       mbar_init(smem_u32(&C->p_full[i]), 4);
       mbar_init(smem_u32(&C->o_full[i]), 1);
-      mbar_init(smem_u32(&C->o_empty[i]), narrow ? 16 : 8);   // the warps that join
+      mbar_init(smem_u32(&C->o_empty[i]), 4 * turns);   // the warps that join
     }
     mbar_init(smem_u32(&C->next_full), 1);
     for (int i = 0; i < 4 * 8; ++i) mbar_init(smem_u32(&C->copied[0][0] + i), 32);
@@ -403,73 +399,78 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
     regs_down<K::kRegsOther>();
     if (warp < 20) {
       // ================================================================= MMA issue, one warp per stream
-      const int st = warp - 16, w = st >> 1, h = st & 1;
+      const int st = warp - 16, tile = st / turns;
       constexpr uint32_t kFmt = K::kCodes ? 0u : 1u;   // P and V: f16 or bf16
       constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);
       constexpr uint32_t kIdescPV = (1u << 4) | (kFmt << 7) | (kFmt << 10) | (1u << 16) | (8u << 17) | (8u << 24);
       const uint32_t ts = tmem + kTmemS + 64 * st, to = tmem + kTmemO + 64 * st;
-      const uint32_t q_lo = ((q_at + w * kTileBytes) >> 4) + kDescLo, k_lo = ((k_at + h * (kTileBytes / 2)) >> 4) + kDescLo,
-                     v_lo = ((v_at + h * (kTileBytes / 2)) >> 4) + kDescLo;
-      int kt = 0, n = 0, items = 0, queries = 0;   // tiles of all items; tiles, items and query tiles of this stream
+      const uint32_t q_lo = ((q_at + tile * kTileBytes) >> 4) + kDescLo, k_lo = (k_at >> 4) + kDescLo, v_lo = (v_at >> 4) + kDescLo;
+      int kt = 0, n = 0, items = 0, queries = 0;   // tiles of all items; half tiles, items and query tiles of this stream
       Record r;
       bool ok = true;
       for (int it = 0; ok && get_record(it, r); ++it) {
         release(it);
-        const Share sh(r, w, h, narrow, window);
-        const bool with_q = sh.on() || Share(r, w, h ^ 1, narrow, window).on();
-        if (with_q) {
-          ok = wait(C->q_full[w], (uint32_t)queries & 1u);
+        const Share sh(r, st, turns, window);
+        if (sh.any()) {
+          ok = wait(C->q_full[tile], (uint32_t)queries & 1u);
           ++queries;
-          if (ok && !sh.on() && lane == 0) mbar_arrive(smem_u32(&C->q_empty[w]));
+          if (ok && !sh.on() && lane == 0) mbar_arrive(smem_u32(&C->q_empty[tile]));
         }
         const int nt = tiles_of(r);
         for (int t = 0; ok && t < nt; ++t, ++kt) {
+          if (turns == 4 && (t & 1) != (st >> 1)) continue;   // two other streams' tile
           const int s = kt % NS;
           const uint32_t par = (uint32_t)(kt / NS) & 1u;
-          if (sh.mine(t)) {
+          // one stream to a tile of rows takes both halves, else one of them
+          const int ja = 2 * t + (turns == 1 ? 0 : st & 1), jb = turns == 1 ? ja + 1 : ja;
+          const bool a = sh.mine(ja), b = turns == 1 && sh.mine(jb);
+          if (!a && !b) {                                     // others' alone: let go of it
+            ok = wait(C->k_full[s], par) && wait(C->v_ok[s], par);
+            if (ok && lane == 0) {
+              mbar_arrive(smem_u32(&C->k_empty[s]));
+              mbar_arrive(smem_u32(&C->v_empty[s]));
+            }
+            __syncwarp();
+            continue;
+          }
+#pragma unroll 1
+          for (int j = a ? ja : jb; j <= (b ? jb : ja); ++j) {
+            const bool done = j == (b ? jb : ja), first = j == sh.j0, last = sh.last(j);
+            const int nb = sh.blocks(j);
+            const uint32_t half = (uint32_t)(s * (kTileBytes / 16) + (j & 1) * (kTileBytes / 32));
             // The P that this S overwrites has been read: products of one CTA run in the order of their issue.
-            const int nb = sh.blocks(t);
             ok = wait(C->k_full[s], par);
             if (!ok) break;
             tc_after();
             if (elect_one()) {
 #pragma unroll
               for (int ks = 0; ks < 4; ++ks)
-                umma_ss(ts, desc128(q_lo + 2 * ks), desc128(k_lo + s * (kTileBytes / 16) + 2 * ks),
-                        kIdescQK | (uint32_t)(2 * nb) << 17, ks);
+                umma_ss(ts, desc128(q_lo + 2 * ks), desc128(k_lo + half + 2 * ks), kIdescQK | (uint32_t)(2 * nb) << 17, ks);
               umma_commit(smem_u32(&C->s_full[st]));
-              umma_commit(smem_u32(&C->k_empty[s]));
-              if (sh.last(t)) umma_commit(smem_u32(&C->q_empty[w]));
+              if (done) umma_commit(smem_u32(&C->k_empty[s]));
+              if (last) umma_commit(smem_u32(&C->q_empty[tile]));
             }
             __syncwarp();
-            const bool first = t == sh.t0;
-            ok = wait(C->v_ok[s], par) &&
-                 (!first || wait(C->o_empty[st], ((uint32_t)items & 1u) ^ 1u)) && wait(C->p_full[st], (uint32_t)n & 1u);
+            ok = wait(C->v_ok[s], par) && (!first || wait(C->o_empty[st], ((uint32_t)items & 1u) ^ 1u)) &&
+                 wait(C->p_full[st], (uint32_t)n & 1u);
             if (!ok) break;
             tc_after();
             if (elect_one()) {
 #pragma unroll
               for (int ks = 0; ks < kHalf; ++ks)   // a block of 16 keys each
-                if (ks < nb) umma_ts(to, ts + 8 * ks, desc128(v_lo + s * (kTileBytes / 16) + 128 * ks), kIdescPV, !(first && ks == 0));
-              if (sh.last(t)) umma_commit(smem_u32(&C->o_full[st]));
-              umma_commit(smem_u32(&C->v_empty[s]));
+                if (ks < nb) umma_ts(to, ts + 8 * ks, desc128(v_lo + half + 128 * ks), kIdescPV, !(first && ks == 0));
+              if (last) umma_commit(smem_u32(&C->o_full[st]));
+              if (done) umma_commit(smem_u32(&C->v_empty[s]));
             }
             __syncwarp();
             ++n;
-          } else if (!narrow || (t & 1) == w) {   // other streams' alone: let go of it
-            ok = wait(C->k_full[s], par) && wait(C->v_full[s], par) && wait(C->v_ok[s], par);
-            if (ok && lane == 0) {
-              mbar_arrive(smem_u32(&C->k_empty[s]));
-              mbar_arrive(smem_u32(&C->v_empty[s]));
-            }
-            __syncwarp();
           }
         }
         if (sh.on()) ++items;
       }
     } else if (warp == 20) {
       // ================================================================= work records, queries, packed keys and values
-      const int T = narrow ? kRowTokens : 2 * kRowTokens;
+      const int T = kRowTokens * (4 / turns);
       const int per_tile = P.Hkv * P.splits;
       int b0 = 0, before = 0;           // a window of 32 sequences and the tiles of those before it
       int cnt = 0, upto = 0, st = 0, len = 0, ntok = 0;
@@ -636,27 +637,29 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
       }
     } else if (warp == 22) {
       // ================================================================= queries
-      int q_n[2] = {0, 0};
+      int q_n[4] = {0, 0, 0, 0};
       Record r;
       bool ok = true;
       for (int it = 0; ok && get_record(it, r); ++it) {
         release(it);
-        for (int w = 0; w < 2; ++w) {
-          if (!Share(r, w, 0, narrow, window).on() && !Share(r, w, 1, narrow, window).on()) continue;
-          ok = ok && wait(C->q_empty[w], ((uint32_t)q_n[w] & 1u) ^ 1u);
-          if (!ok) break;
-          ++q_n[w];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (!ok || i * turns >= 4 || !Share(r, i * turns, turns, window).any()) continue;
+          ok = wait(C->q_empty[i], ((uint32_t)q_n[i] & 1u) ^ 1u);
+          if (!ok) continue;
+          ++q_n[i];
           if (elect_one()) {
-            const uint32_t bar = smem_u32(&C->q_full[w]);
+            const uint32_t bar = smem_u32(&C->q_full[i]);
             mbar_arrive_expect_tx(bar, kTileBytes);
-            tma_load_3d(q_at + w * kTileBytes, &P.tmQ, 0, r.kvh * kGroup, r.row0 + (narrow ? 0 : kRowTokens * w), bar);
+            tma_load_3d(q_at + i * kTileBytes, &P.tmQ, 0, r.kvh * kGroup, r.row0 + kRowTokens * i, bar);
           }
           __syncwarp();
         }
       }
       if (C->abort)   // the copies in flight end before the shared memory is given back
-        for (int w = 0; w < 2; ++w)
-          if (q_n[w] > 0) mbar_wait_bounded(smem_u32(&C->q_full[w]), (uint32_t)(q_n[w] - 1) & 1u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (q_n[i] > 0) mbar_wait_bounded(smem_u32(&C->q_full[i]), (uint32_t)(q_n[i] - 1) & 1u);
     } else if (K::kPaged && warp >= 24) {
      if constexpr (K::kPaged) {
       // ================================================================= blocks of the cache, four warps
@@ -840,14 +843,14 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
   } else {
     // =================================================================== softmax, four warpgroups, thread = row
     regs_up<K::kRegsSoftmax>();
-    const int st = warp >> 2, w = st >> 1, h = st & 1, wq = warp & 3, row = 32 * wq + lane;
+    const int st = warp >> 2, tile = st / turns, wq = warp & 3, row = 32 * wq + lane;
     const uint32_t quad = (uint32_t)(32 * wq) << 16;
     const uint32_t ts = tmem + kTmemS + 64 * st + quad, to = tmem + kTmemO + quad;
     int n = 0, items = 0;   // tiles and items of this stream
     Record r;
     bool ok = true;
     for (int it = 0; ok && get_record(it, r); ++it) {
-      const Share sh(r, w, h, narrow, window);
+      const Share sh(r, st, turns, window);
       float c = P.sm_scale_log2e;
       if (K::kCodes && P.k_scale) c *= P.k_scale[r.kvh];
       const bool odd = !(c > 0.f && c < INFINITY);   // then logits are scaled before their maximum is taken
@@ -856,8 +859,8 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
       const int p = sh.pos + (row >> 3);                       // this row's position; it sees [lo, hi)
       const int hi = p + 1, lo = window > 0 ? p - window + 1 : 0;
       float m = -INFINITY, ref = -1e30f, l = 0.f;   // weights are 2^(c s - ref), ref = c m - shift; none yet: any logit is far above
-      for (int t = sh.t0; t < sh.t1; t += sh.step, ++n) {
-        const int nb = sh.blocks(t), k0 = (r.kb0 + t * NBLK + kHalf * h) * kBlock;
+      for (int j0 = sh.j0; j0 < sh.j_hi; j0 += turns, ++n) {
+        const int nb = sh.blocks(j0), k0 = (r.kb0 + j0 * kHalf) * kBlock;
         ok = wait(C->s_full[st], (uint32_t)n & 1u);
         if (!ok) break;
         tc_after();
@@ -867,7 +870,7 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         // do all tokens of this warp see all keys?
         const bool edge = odd || k0 + TK / 2 > p0 + 1 || (window > 0 && k0 < p0 + 3 - window + 1);
         float part = 0.f;
-        for (bool look = t == sh.t0;; look = true) {
+        for (bool look = j0 == sh.j0;; look = true) {
           tmem_ld32(ts, u);
           if (nb > 2) tmem_ld32(ts + 32, u + 32);
           else
@@ -904,7 +907,7 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
                 ref = now;
               }
               l *= alpha;
-              if (t != sh.t0) {        // the product before has ended: this S was issued behind it
+              if (j0 != sh.j0) {       // the product before has ended: this S was issued behind it
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                   uint32_t o[16];
@@ -950,101 +953,106 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         ++items;
       }
       if (m == -INFINITY) ref = -INFINITY;   // no logit above -inf: the sum is 0, or a NaN
-      C->join[it & 1][st][row] = make_float2(ref, l);
-      tc_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&C->join_full[narrow ? 0 : w]));
-      ok = wait(C->join_full[narrow ? 0 : w], (uint32_t)it & 1u);
-      if (!ok) break;
+      const int g0 = st & ~(turns - 1), cols = 64 / turns, col0 = cols * (st - g0);
+      const float own = ref;
+      float own_l = l;
+      if (turns > 1) {
+        C->join[it & 1][st][row] = make_float2(ref, l);
+        tc_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&C->join_full[tile]));
+        ok = wait(C->join_full[tile], (uint32_t)it & 1u);
+        if (!ok) break;
+        for (int i = g0; i < g0 + turns; ++i) ref = fmaxf(ref, C->join[it & 1][i][row].x);
+      }
       tc_after();
-      const int g0 = narrow ? 0 : 2 * w, parts = narrow ? 4 : 2, cols = 64 / parts, col0 = cols * (st - g0);
-      ref = -INFINITY;
-      for (int i = 0; i < parts; ++i) ref = fmaxf(ref, C->join[it & 1][g0 + i][row].x);
       const float zero = ref == -INFINITY ? 0.f : ref;
       l = 0.f;
-      float o[32];
-#pragma unroll
-      for (int j = 0; j < 32; ++j) o[j] = 0.f;
-      for (int i = 0; i < parts; ++i) {
-        const float2 side = C->join[it & 1][g0 + i][row];
-        const float a = ex2(side.x - zero);
-        l += side.y * a;
-        if (Share(r, narrow ? i >> 1 : w, i & 1, narrow, window).on()) {
-          uint32_t v[16];
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-            if (16 * q < cols) {
-              tmem_ld16(to + 64 * (g0 + i) + col0 + 16 * q, v);
-              tmem_wait_ld();
-#pragma unroll
-              for (int j = 0; j < 16; ++j) o[16 * q + j] += __uint_as_float(v[j]) * a;
-            }
-          tc_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&C->o_empty[g0 + i]));
-        }
+      for (int i = g0; i < g0 + turns; ++i) {
+        const float2 side = turns > 1 ? C->join[it & 1][i][row] : make_float2(own, own_l);
+        l += side.y * ex2(side.x - zero);
       }
       const bool real = (row >> 3) < sh.ntok;
-      if (real && *reinterpret_cast<volatile int*>(&C->rec[it % kRing].bad_v)) {
-        const int from = max(max(lo, 0), r.kb0 * kBlock), to_key = min(hi, r.kb_end * kBlock);
-        const long long first_row = (long long)r.row0 - r.pos0;
-        for (int key = from; key < to_key; ++key) {
-          const int t = (key / kBlock - r.kb0) / NBLK;
-          if (all_see(r, t, window)) {          // the product has them
-            key = (r.kb0 + (t + 1) * NBLK) * kBlock - 1;
-            continue;
-          }
+      const int g = r.kvh * kGroup + (row & 7);
+      const long long at = (r.row0 + kRowTokens * tile + (long long)(row >> 3)) * (P.Hkv * kGroup) + g;
+      float z = l, big = ref;
+      if (real && P.splits == 1 && P.sinks) {
+        const float sk = P.sinks[g] * kLog2e;
+        big = sk > ref ? sk : ref;             // a NaN sink is not above; it comes in through z
+        const float base = big == -INFINITY ? 0.f : big;
+        z = l * ex2(ref - base) + ex2(sk - base);
+      }
+      const float base = big == -INFINITY ? 0.f : big;
+      float f = ex2(ref - base) * (K::kCodes && P.v_scale ? P.v_scale[r.kvh] : 1.f) / z;
+      float lse = (base + lg2(z)) * kLn2;
+      const size_t part_row = (size_t)r.part * ((size_t)P.total * (P.Hkv * kGroup)) + at;
+      if (P.splits > 1) {
+        if (l == 0.f) lse = -INFINITY;         // no key in this part, or none above -inf
+        if (real && col0 == 0) P.part_lse[part_row] = lse;
+      } else {
+        if (z == 0.f) {                        // nothing seen: zeros; nothing but logits of -inf: 0 / 0
+          f = hi > 0 ? NAN : 0.f;
+          lse = hi > 0 ? NAN : -INFINITY;
+        }
+        if (real && P.lse_out && col0 == 0) P.lse_out[at] = lse;
+      }
+      const bool bad = *reinterpret_cast<volatile int*>(&C->rec[it % kRing].bad_v) != 0;
 #pragma unroll 1
-          for (int d = 0; d < cols; ++d) {
-            const float v = value_at<SRC>(P, r.b, r.kvh, first_row, key, col0 + d);
-            if (!(fabsf(v) < INFINITY)) {
+      for (int c0 = col0; c0 < col0 + cols; c0 += 16) {
+        float o[16];
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (j == d) o[j] += v;
+        for (int j = 0; j < 16; ++j) o[j] = 0.f;
+        for (int i = g0; i < g0 + turns; ++i) {
+          if (!Share(r, i, turns, window).on()) continue;
+          const float a = ex2((turns > 1 ? C->join[it & 1][i][row].x : own) - zero);
+          uint32_t v[16];
+          tmem_ld16(to + 64 * i + c0, v);
+          tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[j] += __uint_as_float(v[j]) * a;
+        }
+        if (real && bad) {
+          const int from = max(max(lo, 0), r.kb0 * kBlock), to_key = min(hi, r.kb_end * kBlock);
+          const long long first_row = (long long)r.row0 - r.pos0;
+          for (int key = from; key < to_key; ++key) {
+            const int t = (key / kBlock - r.kb0) / NBLK;
+            if (all_see(r, t, window)) {       // the product has them
+              key = (r.kb0 + (t + 1) * NBLK) * kBlock - 1;
+              continue;
+            }
+#pragma unroll 1
+            for (int d = 0; d < 16; ++d) {
+              const float v = value_at<SRC>(P, r.b, r.kvh, first_row, key, c0 + d);
+              if (!(fabsf(v) < INFINITY)) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                  if (j == d) o[j] += v;
+              }
             }
           }
         }
-      }
-      release(it);
-      if (real) {
-        const int g = r.kvh * kGroup + (row & 7);
-        const long long token = r.row0 + (narrow ? 0 : kRowTokens * w) + (row >> 3);
-        const long long at = token * (P.Hkv * kGroup) + g;
-        const float vs = K::kCodes && P.v_scale ? P.v_scale[r.kvh] : 1.f;
-        float z = l, big = ref;
-        if (P.splits == 1 && P.sinks) {
-          const float sk = P.sinks[g] * kLog2e;
-          big = sk > ref ? sk : ref;             // a NaN sink is not above; it comes in through z
-          const float base = big == -INFINITY ? 0.f : big;
-          z = l * ex2(ref - base) + ex2(sk - base);
-        }
-        const float base = big == -INFINITY ? 0.f : big;
-        float f = ex2(ref - base) * vs / z;
-        float lse = (base + lg2(z)) * kLn2;
+        __syncwarp();
+        if (!real) continue;
         if (P.splits > 1) {
-          if (l == 0.f) lse = -INFINITY;         // no key in this part, or none above -inf
-          const size_t to_row = (size_t)r.part * ((size_t)P.total * (P.Hkv * kGroup)) + at;
-          if (st == g0) P.part_lse[to_row] = lse;
           if (lse != -INFINITY) {
-            float4* dst = reinterpret_cast<float4*>(P.part_o + to_row * kHeadDim + col0);
+            float4* dst = reinterpret_cast<float4*>(P.part_o + part_row * kHeadDim + c0);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (4 * j < cols) dst[j] = make_float4(o[4 * j] * f, o[4 * j + 1] * f, o[4 * j + 2] * f, o[4 * j + 3] * f);
+            for (int j = 0; j < 4; ++j) dst[j] = make_float4(o[4 * j] * f, o[4 * j + 1] * f, o[4 * j + 2] * f, o[4 * j + 3] * f);
           }
         } else {
-          if (z == 0.f) {                        // nothing seen: zeros; nothing but logits of -inf: 0 / 0
-            f = hi > 0 ? NAN : 0.f;
-            lse = hi > 0 ? NAN : -INFINITY;
-          }
-          uint4* dst = reinterpret_cast<uint4*>(P.out + at * kHeadDim + col0);
+          uint4* dst = reinterpret_cast<uint4*>(P.out + at * kHeadDim + c0);
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (8 * j < cols)
-              dst[j] = make_uint4(f32x2_to_bf16x2(o[8 * j] * f, o[8 * j + 1] * f), f32x2_to_bf16x2(o[8 * j + 2] * f, o[8 * j + 3] * f),
-                                  f32x2_to_bf16x2(o[8 * j + 4] * f, o[8 * j + 5] * f), f32x2_to_bf16x2(o[8 * j + 6] * f, o[8 * j + 7] * f));
-          if (P.lse_out && st == g0) P.lse_out[at] = lse;
+          for (int j = 0; j < 2; ++j)
+            dst[j] = make_uint4(f32x2_to_bf16x2(o[8 * j] * f, o[8 * j + 1] * f), f32x2_to_bf16x2(o[8 * j + 2] * f, o[8 * j + 3] * f),
+                                f32x2_to_bf16x2(o[8 * j + 4] * f, o[8 * j + 5] * f), f32x2_to_bf16x2(o[8 * j + 6] * f, o[8 * j + 7] * f));
         }
       }
+      __syncwarp();
+      tc_before();
+      if (lane == 0)
+        for (int i = g0; i < g0 + turns; ++i)
+          if (Share(r, i, turns, window).on()) mbar_arrive(smem_u32(&C->o_empty[i]));
+      release(it);
       __syncwarp();
     }
   }
@@ -1111,7 +1119,7 @@ cudaError_t launch(const PromptParams& P, int sm_count, cudaStream_t s, int* sme
     if (e != cudaSuccess) return e;
     *smem_limit = need;
   }
-  const int T = P.narrow ? kRowTokens : 2 * kRowTokens;
+  const int T = kRowTokens * (4 / P.turns);
   const long long tiles = P.total / T + std::min(P.batch, P.total);   // no more than these, whatever the lengths
   const long long items = tiles * P.Hkv * P.splits;
   if (items > 0x7fffffff) return cudaErrorInvalidValue;
@@ -1128,26 +1136,29 @@ cudaError_t launch(const PromptParams& P, int sm_count, cudaStream_t s, int* sme
 
 }  // namespace
 
-// Groups of 32 tokens unless sequences have 16 or fewer on average, or there are fewer such groups than SMs and no way to cut their
-// keys instead: the streams of a narrow group take the tiles of keys in turn, which fetches (and converts) twice as many for the
-// same rows (512 tokens over 64K E4M3 keys: narrow 1224 us, wide and cut 963).
-// Keys are cut into the number of parts that takes the SM with the most of them the fewest tiles, a part's own cost counted as five
-// tiles; none has fewer than four tiles, and there are at most 8 parts per SM, which bounds the partials.
-PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool may_split, int sm_count) {
-  const long long seqs = std::min(batch, total);
-  PromptPlan plan;
-  const long long wide = std::max<long long>((total + 2 * kRowTokens - 1) / (2 * kRowTokens), seqs) * Hkv;
-  const long long tiles = (key_bound + TK - 1) / TK;
-  plan.narrow = total <= kRowTokens * seqs || (wide < sm_count && (!may_split || tiles < 16));
-  const long long items = plan.narrow ? std::max<long long>((total + kRowTokens - 1) / kRowTokens, seqs) * Hkv : wide;
-  plan.splits = 1;
-  if (may_split) {
-    double best = 1e30;
-    for (long long n = 1; n == 1 || (n <= tiles / 4 && n * items <= 8ll * sm_count); ++n) {
-      const double cost = (double)((items * n + sm_count - 1) / sm_count) * ((double)tiles / n + 5);
+static long long groups_of(long long batch, long long total, int turns, int Hkv) {   // at least so many
+  const long long T = kRowTokens * (4 / turns);
+  return std::max<long long>((total + T - 1) / T, std::min(batch, total)) * Hkv;
+}
+
+// The size of a group (64, 32 or 16 tokens: 1, 2 or 4 streams to a tile of rows) and the parts that its keys are cut into: what takes
+// the SM with the most items the least time, in steps of 64 keys of a stream.  A tile of keys is 2, 1 or 1/2 steps of each stream, and
+// fetching it (converting it, for codes) some of a step whatever the group; an item costs about five steps beside its keys.  Parts
+// have four tiles at least, and there are at most 8 items per SM where keys are cut, which bounds the partials.  (512 tokens over 64K
+// E4M3 keys: groups of 16 uncut 1224 us, of 32 in 8 parts 849.)
+PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool may_split, double fetch, int sm_count) {
+  PromptPlan plan = {1, 4};
+  double best = 1e30;
+  for (int turns = 1; turns <= 4; turns *= 2) {
+    const long long items = groups_of(batch, total, turns, Hkv), T = kRowTokens * (4 / turns);
+    const double tiles = std::max(1.0, (double)(key_bound + T) / TK);
+    for (long long n = 1; n == 1 || (may_split && n <= tiles / 4 && n * items <= 8ll * sm_count); ++n) {
+      const double rounds = (double)((items * n + sm_count - 1) / sm_count);
+      const double cost = rounds * (tiles / n * (2.0 / turns + fetch) + 5) + (n > 1 ? 4 : 0);
       if (cost < best * 0.98) {   // a little gain is not worth the partials
         best = cost;
         plan.splits = (int)n;
+        plan.turns = turns;
       }
     }
   }
@@ -1159,10 +1170,7 @@ size_t prompt_partial_bytes(int total, int Hkv, int splits) {
 }
 // The most parts that prompt_plan cuts into, whatever the context's length.
 int prompt_most_splits(int batch, int total, int Hkv, int sm_count) {
-  const long long seqs = std::min(batch, total);
-  const long long wide = std::max<long long>((total + 2 * kRowTokens - 1) / (2 * kRowTokens), seqs) * Hkv;
-  const long long narrow = std::max<long long>((total + kRowTokens - 1) / kRowTokens, seqs) * Hkv;
-  return (int)std::max<long long>(1, 8ll * sm_count / std::max<long long>(1, total <= kRowTokens * seqs ? narrow : wide));
+  return (int)std::max<long long>(1, 8ll * sm_count / std::max<long long>(1, groups_of(batch, total, 1, Hkv)));
 }
 
 cudaError_t launch_prompt_attn(const PromptParams& P, PromptSource src, int sm_count, cudaStream_t s, int* smem_limit) {

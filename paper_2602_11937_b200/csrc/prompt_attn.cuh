@@ -22,16 +22,17 @@ struct PromptParams {
   float *lse_out, *part_o, *part_lse;
   int32_t* dev_status;
   long long num_blocks;
-  int batch, total, Hkv, max_blocks_per_seq, window, splits, narrow;
+  int batch, total, Hkv, max_blocks_per_seq, window, splits, turns;
   float sm_scale_log2e;
 };
 
 // splits: parts that the keys of a group of tokens are cut into (1: the kernel writes the output, else partials that a second
-// kernel merges).  narrow: groups of 16 tokens instead of 32.
+// kernel merges).  turns: streams to a tile of rows; a group is 64 / turns tokens.
 struct PromptPlan {
-  int splits, narrow;
+  int splits, turns;
 };
-PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool may_split, int sm_count);
+// fetch: what bringing a tile of 128 keys in costs, in steps of 64 keys.
+PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool may_split, double fetch, int sm_count);
 int prompt_most_splits(int batch, int total, int Hkv, int sm_count);
 size_t prompt_partial_bytes(int total, int Hkv, int splits);
 cudaError_t launch_prompt_attn(const PromptParams& P, PromptSource src, int sm_count, cudaStream_t s, int* smem_limit);
