@@ -22,11 +22,16 @@
 //  * One warp plans the work and loads queries (and packed keys and values) by TMA, one looks at the values of tiles that not
 //    every row sees (below).  Over a cache four more warps fetch the blocks of a tile through the block table and convert the
 //    codes: K to bf16, V to f16, both exact for E4M3 and for E2M1 times its scale.
-//  * The reference that weights are relative to is the largest logit of a row's first 64 keys.  It is looked at again, and O
-//    rescaled, only where the weights of 64 keys sum to more than the type of P can take: usual tiles need no maximum (740 -> 707
-//    us).  The weights of a bf16 V are bf16 (half a step, 2^-8 of each, the rounding of the output itself) with float32's range: the
-//    limit is 2^40.  Those of a converted V are f16 (2^-11) and lie at 2^9 of their value, so that the sum of 64 at the reference
-//    stays below the limit, f16's largest number, and weights down to 2^-23 of the reference keep all their bits.  Sums are float32.
+//  * The reference that weights are relative to is the largest logit of a row's first 32 keys that it sees any of.  It is looked at
+//    again, and O rescaled, only where the weights sum to more than the type of P can take: usual tiles need no maximum.  The weights
+//    of a bf16 V are bf16 (half a step, 2^-8 of each, the rounding of the output itself) with float32's range: the limit is 2^40.
+//    Those of a converted V are f16 (2^-11) and lie at 2^9 of their value, so that the sum of 64 at the reference stays below the
+//    limit, f16's largest number, and weights down to 2^-23 of the reference keep all their bits.  Sums are float32.
+//  * A quarter of the exponentials of usual tiles goes through a polynomial on the FMA units.  The special function unit's queue is
+//    shared with shared and tensor memory: a warp that fills it holds up the loads and arrivals of the others (8192 tokens: none of
+//    them 775 us, an eighth 670, a quarter 643, a third 641, half 736).
+//  * Tiles at an edge (diagonal, window, first of a row) go 32 keys at a time through code of half the length: with few tiles per row
+//    every warp fetches its instructions anew (prompts with a window of 128: 64 at a time 280 us, 32 at a time 252).
 //  * Work comes by request (cluster launch control): a CTA asks for the next block of the grid while it works on one.  Blocks are
 //    ordered long ones first within a sequence.
 //  * MMAs and copies are issued by one elected lane out of a converged warp, with operands that the compiler knows to be uniform
@@ -52,6 +57,9 @@ constexpr int kTileBytes = TK * kHeadDim * 2;
 constexpr int kRing = 4;                    // work records: of the item being worked on and the next ones
 constexpr int kShortTiles = 4;              // items of no more tiles are asked for that far ahead, longer ones one ahead
 constexpr unsigned kFull = 0xffffffffu;
+constexpr float kPoly5 = 0.0013274633f, kPoly4 = 0.0096719619f, kPoly3 = 0.0555067845f, kPoly2 = 0.2402223498f,
+                kPoly1 = 0.6931470633f;
+constexpr float kUnset = -1e30f;            // a reference that any logit is far above
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kHalf = NBLK / 2;             // blocks of a stream's half of a tile
 // tensor memory: S (and P over it) of the four streams, then O
@@ -180,6 +188,29 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
+// 2^x for two arguments on the FMA units: x = i + f with i the nearest integer, 2^f by the polynomial of degree five with
+// constant 1 whose largest relative error on [-1/2, 1/2] is smallest (8e-8, found by linear programming over a fine grid), i added
+// to the exponent.  Arguments below -125 give 2^-125; those above 126, and NaN, nothing of use.
+__device__ __forceinline__ void exp2_poly(uint64_t x2, float& e0, float& e1) {
+  float x0, x1;
+  unpack2(x2, x0, x1);
+  x2 = pack2(fmaxf(x0, -125.f), fmaxf(x1, -125.f));
+  const uint64_t magic = pack2(12582912.f, 12582912.f), unmagic = pack2(-12582912.f, -12582912.f), minus = pack2(-1.f, -1.f);
+  const uint64_t t = add2(x2, magic);                        // its low bits hold i
+  const uint64_t f = fma2(add2(t, unmagic), minus, x2);
+  uint64_t p = pack2(kPoly5, kPoly5);
+  p = fma2(p, f, pack2(kPoly4, kPoly4));
+  p = fma2(p, f, pack2(kPoly3, kPoly3));
+  p = fma2(p, f, pack2(kPoly2, kPoly2));
+  p = fma2(p, f, pack2(kPoly1, kPoly1));
+  p = fma2(p, f, pack2(1.f, 1.f));
+  float t0, t1, p0, p1;
+  unpack2(t, t0, t1);
+  unpack2(p, p0, p1);
+  e0 = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
+  e1 = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
+}
+
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
@@ -216,6 +247,22 @@ __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t h) { return f32x2_t
 
 // The lowest n of 32 bits.
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
+
+// The 16 columns of weights that a thread has written, times alpha (a power of two).
+template <bool F16>
+__device__ __forceinline__ void rescale_weights(uint32_t at, float alpha) {
+  uint32_t y[16];
+  tmem_wait_st();
+  tmem_ld16(at, y);
+  tmem_wait_ld();
+  const uint32_t a = f32x2_to_bf16x2(alpha, alpha);
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    if constexpr (F16) y[j] = f32x2_to_f16x2(f16_lo_to_f32(y[j]) * alpha, f16_hi_to_f32(y[j]) * alpha);   // alpha may be below f16
+    else asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(y[j]) : "r"(a));
+  }
+  tmem_st16(at, y);
+}
 
 // Work by request: a CTA asks for a block of the grid that has not been started, and works in its place.  The answer goes to 16
 // bytes of shared memory.
@@ -846,6 +893,7 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
     const int st = warp >> 2, tile = st / turns, wq = warp & 3, row = 32 * wq + lane;
     const uint32_t quad = (uint32_t)(32 * wq) << 16;
     const uint32_t ts = tmem + kTmemS + 64 * st + quad, to = tmem + kTmemO + quad;
+    const bool wide_out = (reinterpret_cast<uintptr_t>(P.out) & 31) == 0;   // 32 bytes of a row in one store
     int n = 0, items = 0;   // tiles and items of this stream
     Record r;
     bool ok = true;
@@ -856,103 +904,142 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
       const bool odd = !(c > 0.f && c < INFINITY);   // then logits are scaled before their maximum is taken
       const float pre = c;
       if (odd) c = 1.f;
-      const int p = sh.pos + (row >> 3);                       // this row's position; it sees [lo, hi)
-      const int hi = p + 1, lo = window > 0 ? p - window + 1 : 0;
-      float m = -INFINITY, ref = -1e30f, l = 0.f;   // weights are 2^(c s - ref), ref = c m - shift; none yet: any logit is far above
+      const int p = sh.pos + (row >> 3), p0 = sh.pos + 4 * wq; // this row's position, the warp's first
+      const int hi = p + 1, lo = window > 0 ? p - window + 1 : 0;   // the row sees [lo, hi)
+      float ref = kUnset, l = 0.f;                             // weights are 2^(c s - ref)
       for (int j0 = sh.j0; j0 < sh.j_hi; j0 += turns, ++n) {
         const int nb = sh.blocks(j0), k0 = (r.kb0 + j0 * kHalf) * kBlock;
         ok = wait(C->s_full[st], (uint32_t)n & 1u);
         if (!ok) break;
         tc_after();
-        uint32_t u[64];
-        float* s = reinterpret_cast<float*>(u);
-        const int p0 = sh.pos + 4 * wq;
-        // do all tokens of this warp see all keys?
-        const bool edge = odd || k0 + TK / 2 > p0 + 1 || (window > 0 && k0 < p0 + 3 - window + 1);
-        float part = 0.f;
-        for (bool look = j0 == sh.j0;; look = true) {
+        bool done = false;
+        if (j0 != sh.j0 && !odd && k0 + TK / 2 <= p0 + 1 && (window == 0 || k0 >= p0 + 3 - window + 1)) {
+          // The usual half tile: every token of this warp sees all 64 keys, and their weights are in bounds.
+          uint32_t u[64];
+          const float* s = reinterpret_cast<const float*>(u);
+          float big = 0.f;
           tmem_ld32(ts, u);
-          if (nb > 2) tmem_ld32(ts + 32, u + 32);
-          else
-#pragma unroll
-            for (int j = 32; j < 64; ++j) s[j] = -INFINITY;
+          tmem_ld32(ts + 32, u + 32);
           tmem_wait_ld();
-          if (edge) {
-            if (odd)
-#pragma unroll
-              for (int j = 0; j < 64; ++j) s[j] *= pre;
-            const int jlo = lo - k0;
-            const unsigned wide = (unsigned)max(hi - lo, 0);
-#pragma unroll
-            for (int j = 0; j < 64; ++j)
-              if ((unsigned)(j - jlo) >= wide) s[j] = -INFINITY;
-          }
-          if (look) {
-            float x[4] = {s[0], s[1], s[2], s[3]};   // NaN beats everything
-#pragma unroll
-            for (int j = 0; j < 64; j += 8) {
-              x[0] = max3(x[0], s[j], s[j + 1]);
-              x[1] = max3(x[1], s[j + 2], s[j + 3]);
-              x[2] = max3(x[2], s[j + 4], s[j + 5]);
-              x[3] = max3(x[3], s[j + 6], s[j + 7]);
-            }
-            const float top = max3(max3(x[0], x[1], x[2]), x[3], x[3]);
-            const bool raise = top > m;
-            if (__any_sync(kFull, raise)) {
-              float alpha = 1.f;
-              if (raise) {
-                const float now = top * c - K::kShift;
-                alpha = m == -INFINITY ? 0.f : ex2(ref - now);
-                m = top;
-                ref = now;
-              }
-              l *= alpha;
-              if (j0 != sh.j0) {       // the product before has ended: this S was issued behind it
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                  uint32_t o[16];
-                  tmem_ld16(to + 64 * st + 16 * q, o);
-                  tmem_wait_ld();
-#pragma unroll
-                  for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
-                  tmem_st16(to + 64 * st + 16 * q, o);
-                }
-              }
-            }
-            // infinity - infinity, or a NaN: the whole row is NaN
-            if (!(top < INFINITY)) ref = NAN;
-          }
           const uint64_t c2 = pack2(c, c), r2 = pack2(-ref, -ref);
           uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
+            float x0, x1, e0, e1;
             const uint64_t x2 = fma2(pack2(s[2 * j], s[2 * j + 1]), c2, r2);
-            float x0, x1;
             unpack2(x2, x0, x1);
-            const float e0 = ex2(x0), e1 = ex2(x1);
+            if (j % 4 == 2) {   // a quarter of them on the FMA units
+              big = max3(big, x0, x1);
+              exp2_poly(x2, e0, e1);
+            } else {
+              e0 = ex2(x0);
+              e1 = ex2(x1);
+            }
             sum[j & 1] = add2(sum[j & 1], pack2(e0, e1));
             u[j] = K::kCodes ? f32x2_to_f16x2(e0, e1) : f32x2_to_bf16x2(e0, e1);
           }
           float a0, a1;
           unpack2(add2(sum[0], sum[1]), a0, a1);
-          part = a0 + a1;
-          if (look || !__any_sync(kFull, !(part < K::kMuch))) break;
+          done = !__any_sync(kFull, !(a0 + a1 < K::kMuch) || !(big < 100.f));
+          if (done) {
+            l += a0 + a1;
+            tmem_st32(ts, u);
+          }
         }
-        tmem_st32(ts, u);
+        if (!done) {
+        // 32 keys at a time.  P of the first 32 lies over their own logits.
+#pragma unroll 1
+        for (int q = 0; q < (nb > 2 ? 2 : 1); ++q) {
+          const int kc = k0 + 32 * q;
+          uint32_t y[16];
+          if (kc > p0 + 3 || (window > 0 && kc + 32 <= p0 - window + 1)) {   // no token of this warp sees any of them
+#pragma unroll
+            for (int j = 0; j < 16; ++j) y[j] = 0u;
+          } else {
+            uint32_t u[32];
+            float* s = reinterpret_cast<float*>(u);
+            tmem_ld32(ts + 32 * q, u);
+            tmem_wait_ld();
+            if (odd || kc + 32 > p0 + 1 || (window > 0 && kc < p0 + 3 - window + 1)) {   // some token does not see some of them
+              if (odd)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) s[j] *= pre;
+              const uint32_t seen = bits_below(p + 1 - kc) & ~(window > 0 ? bits_below(p - window + 1 - kc) : 0u);
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (!(seen & (1u << j))) s[j] = -INFINITY;
+            }
+            float part;
+            for (bool look = j0 == sh.j0 && q == 0;; look = true) {
+              if (look) {
+                float x[2] = {s[0], s[1]};   // NaN beats everything
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                  x[0] = max3(x[0], s[j], s[j + 1]);
+                  x[1] = max3(x[1], s[j + 2], s[j + 3]);
+                }
+                const float top = max3(x[0], x[1], x[1]), now = top * c - K::kShift;
+                const bool raise = now > ref;
+                if (__any_sync(kFull, raise)) {
+                  float alpha = 1.f;
+                  if (raise) {   // by whole powers of two: what was rounded before keeps its bits
+                    const float up = ref == kUnset ? now : ref + ceilf(now - ref);
+                    alpha = ref == kUnset ? 0.f : ex2(ref - up);
+                    ref = up;
+                  }
+                  l *= alpha;
+                  if (q == 1) rescale_weights<K::kCodes>(ts, alpha);
+                  if (j0 != sh.j0) {       // the product before has ended: this S was issued behind it
+#pragma unroll 1
+                    for (int i = 0; i < 4; ++i) {
+                      uint32_t o[16];
+                      tmem_ld16(to + 64 * st + 16 * i, o);
+                      tmem_wait_ld();
+#pragma unroll
+                      for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                      tmem_st16(to + 64 * st + 16 * i, o);
+                    }
+                  }
+                }
+                // infinity - infinity, or a NaN: the whole row is NaN
+                if (!(top < INFINITY)) ref = NAN;
+              }
+              const uint64_t c2 = pack2(c, c), r2 = pack2(-ref, -ref);
+              uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                float x0, x1;
+                unpack2(fma2(pack2(s[2 * j], s[2 * j + 1]), c2, r2), x0, x1);
+                const float e0 = ex2(x0), e1 = ex2(x1);
+                sum[j & 1] = add2(sum[j & 1], pack2(e0, e1));
+                y[j] = K::kCodes ? f32x2_to_f16x2(e0, e1) : f32x2_to_bf16x2(e0, e1);
+              }
+              float a0, a1;
+              unpack2(add2(sum[0], sum[1]), a0, a1);
+              part = a0 + a1;
+              if (look || !__any_sync(kFull, !(part < K::kMuch))) break;
+            }
+            l += part;
+          }
+          tmem_st16(ts + 16 * q, y);
+        }
+        }
         tmem_wait_st();
         tc_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&C->p_full[st]));
-        l += part;
       }
       if (!ok) break;
       // ---- the item's end: the streams of a tile of rows join, each for its part of the channels
+      const int g = r.kvh * kGroup + (row & 7);
+      float sk = -INFINITY;                    // (asked for before the wait)
+      if (P.splits == 1 && P.sinks) sk = P.sinks[g] * kLog2e;
       if (sh.on()) {
         ok = wait(C->o_full[st], (uint32_t)items & 1u);
         if (!ok) break;
         ++items;
       }
-      if (m == -INFINITY) ref = -INFINITY;   // no logit above -inf: the sum is 0, or a NaN
+      if (ref == kUnset) ref = -INFINITY;    // no logit above -inf: the sum is 0
       const int g0 = st & ~(turns - 1), cols = 64 / turns, col0 = cols * (st - g0);
       const float own = ref;
       float own_l = l;
@@ -973,11 +1060,9 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         l += side.y * ex2(side.x - zero);
       }
       const bool real = (row >> 3) < sh.ntok;
-      const int g = r.kvh * kGroup + (row & 7);
       const long long at = (r.row0 + kRowTokens * tile + (long long)(row >> 3)) * (P.Hkv * kGroup) + g;
       float z = l, big = ref;
-      if (real && P.splits == 1 && P.sinks) {
-        const float sk = P.sinks[g] * kLog2e;
+      if (P.splits == 1 && P.sinks) {
         big = sk > ref ? sk : ref;             // a NaN sink is not above; it comes in through z
         const float base = big == -INFINITY ? 0.f : big;
         z = l * ex2(ref - base) + ex2(sk - base);
@@ -997,13 +1082,17 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         if (real && P.lse_out && col0 == 0) P.lse_out[at] = lse;
       }
       const bool bad = *reinterpret_cast<volatile int*>(&C->rec[it % kRing].bad_v) != 0;
+      uint32_t with = sh.on() ? 1u << st : 0u;   // the streams that have an O
+      if (turns > 1)
+        for (int i = g0; i < g0 + turns; ++i) with |= Share(r, i, turns, window).on() ? 1u << i : 0u;
 #pragma unroll 1
       for (int c0 = col0; c0 < col0 + cols; c0 += 16) {
         float o[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[j] = 0.f;
+#pragma unroll 1
         for (int i = g0; i < g0 + turns; ++i) {
-          if (!Share(r, i, turns, window).on()) continue;
+          if (!(with >> i & 1u)) continue;
           const float a = ex2((turns > 1 ? C->join[it & 1][i][row].x : own) - zero);
           uint32_t v[16];
           tmem_ld16(to + 64 * i + c0, v);
@@ -1040,18 +1129,25 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
             for (int j = 0; j < 4; ++j) dst[j] = make_float4(o[4 * j] * f, o[4 * j + 1] * f, o[4 * j + 2] * f, o[4 * j + 3] * f);
           }
         } else {
-          uint4* dst = reinterpret_cast<uint4*>(P.out + at * kHeadDim + c0);
+          uint32_t y[8];
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            dst[j] = make_uint4(f32x2_to_bf16x2(o[8 * j] * f, o[8 * j + 1] * f), f32x2_to_bf16x2(o[8 * j + 2] * f, o[8 * j + 3] * f),
-                                f32x2_to_bf16x2(o[8 * j + 4] * f, o[8 * j + 5] * f), f32x2_to_bf16x2(o[8 * j + 6] * f, o[8 * j + 7] * f));
+          for (int j = 0; j < 8; ++j) y[j] = f32x2_to_bf16x2(o[2 * j] * f, o[2 * j + 1] * f);
+          __nv_bfloat16* dst = P.out + at * kHeadDim + c0;
+          if (wide_out) {
+            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]),
+                         "r"(y[4]), "r"(y[5]), "r"(y[6]), "r"(y[7])
+                         : "memory");
+          } else {
+            reinterpret_cast<uint4*>(dst)[0] = make_uint4(y[0], y[1], y[2], y[3]);
+            reinterpret_cast<uint4*>(dst)[1] = make_uint4(y[4], y[5], y[6], y[7]);
+          }
         }
       }
       __syncwarp();
       tc_before();
       if (lane == 0)
         for (int i = g0; i < g0 + turns; ++i)
-          if (Share(r, i, turns, window).on()) mbar_arrive(smem_u32(&C->o_empty[i]));
+          if (with >> i & 1u) mbar_arrive(smem_u32(&C->o_empty[i]));
       release(it);
       __syncwarp();
     }

@@ -249,4 +249,6 @@ def test_agrees_with_the_multi_token_kernel():
     P.puzzle_decode_attn_tokens_workspace_init(c.desc, 3, 4, ws)
     out = torch.empty(3, 4, c.hq, D, dtype=torch.bfloat16, device="cuda")
     P.puzzle_decode_attn_tokens(c.desc, c.view(), c.q.view(3, 4, c.hq, D), c.sinks, out, workspace=ws)
-    assert (out.view_as(c.out).double() - c.out.double()).abs().max() <= 2.0 ** -8 * 1.5
+    # both are rounded to bf16, each by at most 2^-8 of its value; their weights are off by 2^-11 and less
+    a, b = out.view_as(c.out).double(), c.out.double()
+    assert ((a - b).abs() <= 2.0 ** -7 * b.abs() + 2e-3).all()
