@@ -57,7 +57,7 @@ struct DeviceInfo {
   // dynamic shared-memory limits already set per kernel and cache type; 0 = not raised yet
   int smem_warp[3] = {}, smem_cta[2] = {}, smem_small[3] = {};
   int smem_tc = 0, smem_tokens = 0, smem_group[10] = {}, smem_tokens_group[10] = {};
-  int smem_prompt[4] = {};
+  int smem_prompt[8] = {};
 };
 DeviceInfo& device_info() {
   static DeviceInfo info[64];

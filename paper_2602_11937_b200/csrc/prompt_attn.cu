@@ -65,16 +65,17 @@ constexpr int kHalf = NBLK / 2;             // blocks of a stream's half of a ti
 // tensor memory: S (and P over it) of the four streams, then O
 constexpr int kTmemS = 0, kTmemO = 256;
 
-template <int SRC>
+// ROWS: tiles of rows that a group can have (4: any group; 1: of 16 tokens alone, which leaves room for more tiles of keys).
+template <int SRC, int ROWS>
 struct Cfg {
   static constexpr bool kPaged = SRC != kSrcPacked;
   static constexpr bool kCodes = SRC == kSrcFp8 || SRC == kSrcFp4;
   static constexpr int kThreads = kPaged ? 896 : 768;
-  static constexpr int kStages = kCodes ? 3 : 4;             // tiles of K and V in the form the MMAs read
+  static constexpr int kStages = kCodes ? (ROWS == 1 ? 4 : 3) : (ROWS == 1 ? 6 : 4);             // tiles of K and V in the form the MMAs read
   static constexpr int kBlockBytes = SRC == kSrcFp8 ? kBlock * kHeadDim : (SRC == kSrcFp4 ? kFp4BlockBytes : 0);
   static constexpr int kCodeTile = 2 * NBLK * kBlockBytes;   // codes of K and V of a tile as they lie in the cache
   // tiles whose copies are in flight; a bf16 tile is copied to where the MMAs read it, and has to leave two of these places
-  static constexpr int kCopySlots = SRC == kSrcFp8 ? 3 : (SRC == kSrcFp4 ? 5 : 3);
+  static constexpr int kCopySlots = SRC == kSrcFp8 ? (ROWS == 1 ? 4 : 3) : (SRC == kSrcFp4 ? (ROWS == 1 ? 6 : 5) : (ROWS == 1 ? 4 : 3));
   static constexpr int kCodeStages = kCodes ? kCopySlots : 0;
   static constexpr int kFullArrivals = kPaged ? 4 : 1;
   // Register shares of the softmax warpgroups and of the others.  They come out of what the launch has: 65536 / threads rounded
@@ -83,7 +84,7 @@ struct Cfg {
   static_assert(512 * kRegsSoftmax + (kThreads - 512) * kRegsOther <= kThreads * (65536 / kThreads / 8 * 8), "more than there are");
   static constexpr float kShift = kCodes ? 9.f : 0.f;                  // weights lie at 2^shift of their value
   static constexpr float kMuch = kCodes ? 65000.f : 1.0995116e12f;     // sum of 64 weights that calls for another reference
-  static constexpr int kSmem = 4 * kTileBytes + 2 * kStages * kTileBytes + kCodeStages * kCodeTile;
+  static constexpr int kSmem = ROWS * kTileBytes + 2 * kStages * kTileBytes + kCodeStages * kCodeTile;
 };
 
 struct Record {
@@ -92,12 +93,13 @@ struct Record {
 struct Ctl {
   uint64_t rec_full[kRing], rec_empty[kRing];
   uint64_t q_full[4], q_empty[4];                         // of the tiles of rows
-  uint64_t k_full[5], k_empty[5], v_full[5], v_empty[5], v_ok[5];
+  uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6], v_ok[6];
   uint64_t s_full[4], p_full[4], o_full[4], o_empty[4];   // of the streams
   uint64_t join_full[4];
   uint64_t next_full;
   alignas(16) uint4 next;   // answer to a request for work
-  uint64_t copied[4][8];
+  uint64_t copied[4][8];         // of a warp's blocks; of a tile's codes: the first row
+  uint64_t codes_empty[8];
   Record rec[kRing];
   float2 join[2][4][128];   // by turns: reference and sum of a stream's rows
   uint32_t tmem;
@@ -220,6 +222,12 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int 
 // 16 bytes from global to shared memory, zeros if !on.
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool on) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+// `bytes` bytes (a multiple of 16) from global to shared memory, counted on an mbarrier.
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
+               "r"(bar)
+               : "memory");
 }
 // One arrival of this thread once its copies so far have landed (the barrier's count includes it).
 __device__ __forceinline__ void cp_arrive(uint32_t bar) {
@@ -362,27 +370,37 @@ __device__ __forceinline__ bool all_see(const Record& r, int t, int window) {
   return k0 + TK <= r.pos0 + 1 && (window == 0 || k0 >= r.pos0 + r.ntok - window);
 }
 
+// Row (block, KV head) of the cache that holds block j of a record's sequence; -1: outside the record's keys, or none (flagged).
+__device__ __forceinline__ int cache_row(const PromptParams& P, const Record& r, int j) {
+  if (j >= r.kb_end) return -1;
+  const long long blk = P.block_table ? (long long)P.block_table[(size_t)r.b * P.max_blocks_per_seq + j]
+                                      : (long long)r.b * P.max_blocks_per_seq + j;
+  if (blk >= 0 && blk < P.num_blocks) return (int)(blk * P.Hkv + r.kvh);
+  if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
+  return -1;
+}
+
 }  // namespace
 
-template <int SRC>
-__global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(const __grid_constant__ PromptParams P) {
-  using K = Cfg<SRC>;
+template <int SRC, int ROWS>
+__global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kernel(const __grid_constant__ PromptParams P) {
+  using K = Cfg<SRC, ROWS>;
   constexpr int NS = K::kStages;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);
   Ctl* C = reinterpret_cast<Ctl*>(smem + K::kSmem);
-  const uint32_t q_at = smem_u32(smem), k_at = q_at + 4 * kTileBytes, v_at = k_at + NS * kTileBytes;
+  const uint32_t q_at = smem_u32(smem), k_at = q_at + ROWS * kTileBytes, v_at = k_at + NS * kTileBytes;
   [[maybe_unused]] const uint32_t code_at = v_at + NS * kTileBytes;
   const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // (uniform, as the compiler sees it)
-  const int turns = P.turns, window = P.window;
+  const int turns = ROWS == 1 ? 4 : P.turns, window = P.window;
   const Waiter wait{C, P.dev_status};
 
   if (threadIdx.x == 0) {
     const int users = turns == 4 ? 2 : 4;   // streams that read a tile of keys
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&C->rec_full[i]), 1);
-      mbar_init(smem_u32(&C->rec_empty[i]), 16 + 4 + 1 + 1 + (K::kPaged ? 4 : 0));
+      mbar_init(smem_u32(&C->rec_empty[i]), 16 + 4 + 1 + 1 + (K::kPaged ? 4 : 0) + (K::kCodes ? 1 : 0));
     }
     for (int i = 0; i < NS; ++i) {
       mbar_init(smem_u32(&C->k_full[i]), K::kFullArrivals);
@@ -401,7 +419,8 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
       mbar_init(smem_u32(&C->o_empty[i]), 4 * turns);   // the warps that join
     }
     mbar_init(smem_u32(&C->next_full), 1);
-    for (int i = 0; i < 4 * 8; ++i) mbar_init(smem_u32(&C->copied[0][0] + i), 32);
+    for (int i = 0; i < 4 * 8; ++i) mbar_init(smem_u32(&C->copied[0][0] + i), K::kCodes ? 1 : 32);
+    for (int i = 0; i < 8; ++i) mbar_init(smem_u32(&C->codes_empty[i]), 4);
     C->abort = 0;
     fence_mbar_init();
     tma_prefetch_desc(&P.tmQ);
@@ -707,22 +726,51 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (q_n[i] > 0) mbar_wait_bounded(smem_u32(&C->q_full[i]), (uint32_t)(q_n[i] - 1) & 1u);
+    } else if (K::kCodes && warp == 23) {
+      // ================================================================= codes of the cache, as they lie there
+      // One lane to a block of K or V of a tile; places in the cache are looked up for four tiles at a time, lane = 8 tile + block.
+      if constexpr (K::kCodes) {
+        int in = 0;
+        Record r;
+        bool ok = true;
+        for (int it = 0; ok && get_record(it, r); ++it) {
+          release(it);
+          const int nt = tiles_of(r);
+          int row = -1;
+          for (int t = 0; ok && t < nt; ++t, ++in) {
+            if ((t & 3) == 0) row = cache_row(P, r, r.kb0 + t * NBLK + lane);
+            const int mine = __shfl_sync(kFull, row, 8 * (t & 3) + ((lane & 15) >> 1)), slot = in % K::kCopySlots;
+            ok = wait(C->codes_empty[slot], ((uint32_t)(in / K::kCopySlots) & 1u) ^ 1u);
+            if (!ok) break;
+            const uint32_t to = code_at + slot * K::kCodeTile + (((lane & 1) * NBLK + ((lane & 15) >> 1))) * K::kBlockBytes;
+            const uint32_t bar = smem_u32(&C->copied[0][slot]);
+            const uint32_t there = __ballot_sync(kFull, lane < 16 && mine >= 0);
+            if (lane < 16 && mine < 0)   // no such block: zeros
+              for (int i = 0; i < K::kBlockBytes / 16; ++i) st_shared16(to + 16 * i, 0, 0, 0, 0);
+            __syncwarp();
+            if (lane == 0) {
+              if (there) mbar_arrive_expect_tx(bar, __popc(there) * K::kBlockBytes);
+              else mbar_arrive(bar);
+            }
+            __syncwarp();
+            if (there >> lane & 1u)
+              bulk_copy(to, static_cast<const char*>(lane & 1 ? P.v_cache : P.k_cache) + (size_t)mine * K::kBlockBytes, K::kBlockBytes,
+                        bar);
+            __syncwarp();
+          }
+        }
+        // no copy is in flight when the shared memory is given back
+        for (int i = max(in - K::kCopySlots, 0); i < in; ++i)
+          mbar_wait_bounded(smem_u32(&C->copied[0][i % K::kCopySlots]), (uint32_t)(i / K::kCopySlots) & 1u);
+      }
     } else if (K::kPaged && warp >= 24) {
-     if constexpr (K::kPaged) {
-      // ================================================================= blocks of the cache, four warps
-      // Warp lw has blocks lw and lw + 4 of every tile, K and V, from the copy to the converted form: nothing is shared with
-      // the other three.  Places in the cache are looked up for 16 tiles at a time, lane = 2 tile + block.
-      const int lw = warp - 24;
+     // ================================================================== tiles of the cache in the MMAs' form, four warps
+     // Warp lw has blocks lw and lw + 4 of every tile, K and V.
+     const int lw = warp - 24;
+     if constexpr (SRC == kSrcBf16) {
+      // Copied to where the MMAs read them.  Places in the cache are looked up for 16 tiles at a time, lane = 2 tile + block.
       constexpr int kSlots = K::kCopySlots;
-      auto lookup = [&](const Record& r, int t_first) -> int {   // row (block, KV head) of the cache, -1: none
-        const int j = r.kb0 + (t_first + (lane >> 1)) * NBLK + lw + 4 * (lane & 1);
-        if (j >= r.kb_end) return -1;
-        const long long blk = P.block_table ? (long long)P.block_table[(size_t)r.b * P.max_blocks_per_seq + j]
-                                            : (long long)r.b * P.max_blocks_per_seq + j;
-        if (blk >= 0 && blk < P.num_blocks) return (int)(blk * P.Hkv + r.kvh);
-        if (P.dev_status) atomicOr(P.dev_status, (int)PUZZLE_DEV_BAD_BLOCK);
-        return -1;
-      };
+      auto lookup = [&](const Record& r, int t_first) { return cache_row(P, r, r.kb0 + (t_first + (lane >> 1)) * NBLK + lw + 4 * (lane & 1)); };
       bool ok = true;
       // The next tile to copy.  Records of items that nothing is copied of yet are taken only as they come: their being
       // published can depend on tiles that this warp has still to hand on.
@@ -746,44 +794,44 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
       int in = 0, out = 0;                         // tiles whose copies are begun, tiles handed on
       auto begin_copy = [&]() {
         const int row0 = __shfl_sync(kFull, ent, 2 * (t & 15)), row1 = __shfl_sync(kFull, ent, 2 * (t & 15) + 1);
-        if constexpr (SRC == kSrcBf16) {
-          const int s = in % NS;
-          const uint32_t par = ((uint32_t)(in / NS) & 1u) ^ 1u;
-          ok = wait(C->k_empty[s], par) && wait(C->v_empty[s], par);
-          if (!ok) return;
+        const int s = in % NS;
+        const uint32_t par = ((uint32_t)(in / NS) & 1u) ^ 1u;
+        ok = wait(C->k_empty[s], par) && wait(C->v_empty[s], par);
+        if (!ok) return;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int row = h ? row1 : row0;
-            const size_t at = (size_t)max(row, 0) * (kBlock * kHeadDim * 2);
-            const char* ks = static_cast<const char*>(P.k_cache) + at;
-            const char* vs = static_cast<const char*>(P.v_cache) + at;
+        for (int h = 0; h < 2; ++h) {
+          const int row = h ? row1 : row0;
+          const size_t at = (size_t)max(row, 0) * (kBlock * kHeadDim * 2);
+          const char* ks = static_cast<const char*>(P.k_cache) + at;
+          const char* vs = static_cast<const char*>(P.v_cache) + at;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int cidx = lane + 32 * i, tok = (lw + 4 * h) * kBlock + (cidx >> 3);
-              const uint32_t dst = (uint32_t)(s * kTileBytes + tok * 128 + (((cidx & 7) ^ (tok & 7)) << 4));
-              cp_async16(k_at + dst, ks + 16 * cidx, row >= 0);
-              cp_async16(v_at + dst, vs + 16 * cidx, row >= 0);
-            }
-          }
-        } else {
-          const uint32_t dst = code_at + (in % kSlots) * K::kCodeTile;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int row = h ? row1 : row0;
-            const size_t at = (size_t)max(row, 0) * K::kBlockBytes;
-            const char* ks = static_cast<const char*>(P.k_cache) + at;
-            const char* vs = static_cast<const char*>(P.v_cache) + at;
-            const uint32_t kd = dst + (lw + 4 * h) * K::kBlockBytes, vd = kd + NBLK * K::kBlockBytes;
-            for (int i = lane; i < K::kBlockBytes / 16; i += 32) {
-              cp_async16(kd + 16 * i, ks + 16 * i, row >= 0);
-              cp_async16(vd + 16 * i, vs + 16 * i, row >= 0);
-            }
+          for (int i = 0; i < 4; ++i) {
+            const int cidx = lane + 32 * i, tok = (lw + 4 * h) * kBlock + (cidx >> 3);
+            const uint32_t dst = (uint32_t)(s * kTileBytes + tok * 128 + (((cidx & 7) ^ (tok & 7)) << 4));
+            cp_async16(k_at + dst, ks + 16 * cidx, row >= 0);
+            cp_async16(v_at + dst, vs + 16 * cidx, row >= 0);
           }
         }
         cp_arrive(smem_u32(&C->copied[lw][in % kSlots]));
         ++in;
         if (++t < nt && (t & 15) == 0) ent = lookup(r, t);
       };
+      while (ok) {
+        while (ok && in - out < kSlots && have_tile(in == out)) begin_copy();
+        if (!ok || in == out) break;
+        ok = wait(C->copied[lw][out % kSlots], (uint32_t)(out / kSlots) & 1u);
+        if (!ok) break;
+        const int s = out % NS;
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&C->k_full[s]));
+          mbar_arrive(smem_u32(&C->v_full[s]));
+        }
+        ++out;
+      }
+      cp_wait_all();   // none is in flight when the shared memory is given back
+     } else if constexpr (K::kCodes) {
       // Codes of a tile -> bf16 keys and f16 values in the swizzled rows that the MMAs read.
       auto convert = [&](uint32_t src, uint32_t dst, bool is_v) {
 #pragma unroll
@@ -861,19 +909,16 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bar));
       };
-      while (ok) {
-        while (ok && in - out < kSlots && have_tile(in == out)) begin_copy();
-        if (!ok || in == out) break;
-        ok = wait(C->copied[lw][out % kSlots], (uint32_t)(out / kSlots) & 1u);
-        if (!ok) break;
-        const int s = out % NS;
-        if constexpr (SRC == kSrcBf16) {
-          signal(C->k_full[s]);
-          signal(C->v_full[s]);
-        } else {
-          const uint32_t par = ((uint32_t)(out / NS) & 1u) ^ 1u;
-          const uint32_t src = code_at + (out % kSlots) * K::kCodeTile;
-          ok = wait(C->k_empty[s], par);
+      int n = 0;
+      Record r;
+      bool ok = true;
+      for (int it = 0; ok && get_record(it, r); ++it) {
+        release(it);
+        const int nt = tiles_of(r);
+        for (int t = 0; t < nt; ++t, ++n) {
+          const int s = n % NS, slot = n % K::kCopySlots;
+          const uint32_t par = ((uint32_t)(n / NS) & 1u) ^ 1u, src = code_at + slot * K::kCodeTile;
+          ok = wait(C->copied[0][slot], (uint32_t)(n / K::kCopySlots) & 1u) && wait(C->k_empty[s], par);
           if (!ok) break;
           convert(src, k_at + s * kTileBytes, false);
           signal(C->k_full[s]);
@@ -881,10 +926,9 @@ __global__ void __launch_bounds__(Cfg<SRC>::kThreads, 1) prompt_attn_kernel(cons
           if (!ok) break;
           convert(src + NBLK * K::kBlockBytes, v_at + s * kTileBytes, true);
           signal(C->v_full[s]);
+          if (lane == 0) mbar_arrive(smem_u32(&C->codes_empty[slot]));
         }
-        ++out;
       }
-      cp_wait_all();   // none is in flight when the shared memory is given back
      }
     }
   } else {
@@ -1207,11 +1251,11 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(const __grid_constant
   if (P.lse_out && o == 0) P.lse_out[at] = out_lse;
 }
 
-template <int SRC>
-cudaError_t launch(const PromptParams& P, int sm_count, cudaStream_t s, int* smem_limit) {
-  const int need = Cfg<SRC>::kSmem + (int)sizeof(Ctl) + 1024;
+template <int SRC, int ROWS>
+cudaError_t launch_as(const PromptParams& P, int sm_count, cudaStream_t s, int* smem_limit) {
+  const int need = Cfg<SRC, ROWS>::kSmem + (int)sizeof(Ctl) + 1024;
   if (*smem_limit == 0) {
-    const cudaError_t e = cudaFuncSetAttribute(prompt_attn_kernel<SRC>, cudaFuncAttributeMaxDynamicSharedMemorySize, need);
+    const cudaError_t e = cudaFuncSetAttribute(prompt_attn_kernel<SRC, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, need);
     if (e != cudaSuccess) return e;
     *smem_limit = need;
   }
@@ -1219,8 +1263,8 @@ cudaError_t launch(const PromptParams& P, int sm_count, cudaStream_t s, int* sme
   const long long tiles = P.total / T + std::min(P.batch, P.total);   // no more than these, whatever the lengths
   const long long items = tiles * P.Hkv * P.splits;
   if (items > 0x7fffffff) return cudaErrorInvalidValue;
-  cudaError_t e = launch_dependent(prompt_attn_kernel<SRC>, dim3((unsigned)items),
-                                   dim3(Cfg<SRC>::kThreads), need, s, P);
+  cudaError_t e = launch_dependent(prompt_attn_kernel<SRC, ROWS>, dim3((unsigned)items),
+                                   dim3(Cfg<SRC, ROWS>::kThreads), need, s, P);
   count_launch();
   if (e == cudaSuccess && P.splits > 1) {
     const size_t threads = (size_t)P.total * P.Hkv * kGroup * 16;
@@ -1228,6 +1272,11 @@ cudaError_t launch(const PromptParams& P, int sm_count, cudaStream_t s, int* sme
     count_launch();
   }
   return e;
+}
+
+template <int SRC>
+cudaError_t launch(const PromptParams& P, int sm_count, cudaStream_t s, int* smem_limit) {
+  return P.turns == 4 ? launch_as<SRC, 1>(P, sm_count, s, smem_limit + 4) : launch_as<SRC, 4>(P, sm_count, s, smem_limit);
 }
 
 }  // namespace
