@@ -265,7 +265,7 @@ PUZZLE_API puzzle_status puzzle_prompt_attn(const puzzle_layer_desc* desc, const
  *   a token whose position is negative sees no key: out = 0, lse = sink.  A sequence longer than its table row is clamped to it
  *   (PUZZLE_DEV_SEQ_TOO_LONG); keys behind a bad block-table entry count as zeros (PUZZLE_DEV_BAD_BLOCK).
  * Softmax weights are held in bf16 over a bf16 cache (off by 2^-8 of themselves at most) and in f16 over the others (2^-11, down to
- * 2^-23 of the largest, 2^-34 of that below).  Two calls on the same inputs give the same bits. */
+ * 2^-22 of the largest, by 2^-32 of that below).  Two calls on the same inputs give the same bits. */
 PUZZLE_API size_t puzzle_chunk_attn_workspace_bytes(const puzzle_layer_desc* desc, int32_t batch, int32_t total_tokens);
 PUZZLE_API puzzle_status puzzle_chunk_attn(const puzzle_layer_desc* desc, const puzzle_kv_view* kv, const void* q,
                                  int64_t q_token_stride, const int32_t* starts, const float* sinks, void* out,

@@ -14,19 +14,21 @@
 //    share nothing until their rows are done; then they join through tensor memory, each for a part of the channels.  The two
 //    halves of a tile are two streams, not one of twice the width, so that every scheduler has four softmax warps: the special
 //    function unit, which bounds the kernel (16 exponentials a clock and SM), is fed while others wait for loads and products.
-//    Measured on a prompt of 8192 tokens: 707 us, the unit busy for 72 % of the time; two streams of 128 keys, with S and P apart
-//    so that the next S is computed early, 966; the same with two threads to a row 802.
+//    Measured on a prompt of 8192 tokens when it was chosen: 740 us; two streams of 128 keys, with S and P apart so that the next S is
+//    computed early, 966; the same with two threads to a row 802.  Now 640 (860 TFLOP/s).
 //  * A group of 64, 32 or 16 tokens is 4, 2 or 1 tiles of rows with 1, 2 or 4 streams each; these take the halves of the tiles of keys
 //    in turn and join at the end.  Large groups fetch (and convert) a tile of keys once for many rows and have nothing to join, small
 //    ones make more items of few tokens.
-//  * One warp plans the work and loads queries (and packed keys and values) by TMA, one looks at the values of tiles that not
-//    every row sees (below).  Over a cache four more warps fetch the blocks of a tile through the block table and convert the
-//    codes: K to bf16, V to f16, both exact for E4M3 and for E2M1 times its scale.
+//  * One warp plans the work and loads packed keys and values by TMA, one loads queries, one looks at the values of tiles that not
+//    every row sees (below).  Over a code cache one copies blocks through the block table, and four convert them: K to bf16, V to f16,
+//    both exact for E4M3 and for E2M1 times its scale.  Over a bf16 cache these four copy to where the MMAs read.
 //  * The reference that weights are relative to is the largest logit of a row's first 32 keys that it sees any of.  It is looked at
 //    again, and O rescaled, only where the weights sum to more than the type of P can take: usual tiles need no maximum.  The weights
 //    of a bf16 V are bf16 (half a step, 2^-8 of each, the rounding of the output itself) with float32's range: the limit is 2^40.
 //    Those of a converted V are f16 (2^-11) and lie at 2^9 of their value, so that the sum of 64 at the reference stays below the
-//    limit, f16's largest number, and weights down to 2^-23 of the reference keep all their bits.  Sums are float32.
+//    limit, f16's largest number, and weights down to 2^-23 of the reference keep all their bits.  A reference is raised by whole
+//    powers of two, so that the weights of the keys before, in f16 already, are scaled exactly; it then lies less than a factor of two
+//    above the largest.  Sums are float32.
 //  * A quarter of the exponentials of usual tiles goes through a polynomial on the FMA units.  The special function unit's queue is
 //    shared with shared and tensor memory: a warp that fills it holds up the loads and arrivals of the others (8192 tokens: none of
 //    them 775 us, an eighth 670, a quarter 643, a third 641, half 736).
@@ -74,7 +76,7 @@ struct Cfg {
   static constexpr int kStages = kCodes ? (ROWS == 1 ? 4 : 3) : (ROWS == 1 ? 6 : 4);             // tiles of K and V in the form the MMAs read
   static constexpr int kBlockBytes = SRC == kSrcFp8 ? kBlock * kHeadDim : (SRC == kSrcFp4 ? kFp4BlockBytes : 0);
   static constexpr int kCodeTile = 2 * NBLK * kBlockBytes;   // codes of K and V of a tile as they lie in the cache
-  // tiles whose copies are in flight; a bf16 tile is copied to where the MMAs read it, and has to leave two of these places
+  // tiles whose copies are in flight; a bf16 tile is copied to where the MMAs read it, and has to leave one of these places
   static constexpr int kCopySlots = SRC == kSrcFp8 ? (ROWS == 1 ? 4 : 3) : (SRC == kSrcFp4 ? (ROWS == 1 ? 6 : 5) : (ROWS == 1 ? 4 : 3));
   static constexpr int kCodeStages = kCodes ? kCopySlots : 0;
   static constexpr int kFullArrivals = kPaged ? 4 : 1;
@@ -305,10 +307,10 @@ struct Waiter {
   }
   __device__ __forceinline__ bool slow(uint32_t a, uint32_t parity) const {
     bool ok = false;
-    for (uint32_t i = 0; i < (1u << 22); ++i) {
+    for (uint32_t i = 0; i < (1u << 24); ++i) {   // some waits last as long as an item does: more than a second, 10^7 keys and more
       if (mbar_try_wait(a, parity)) { ok = true; break; }
       if (C->abort) break;
-      if (i > 64) __nanosleep(32);
+      if (i > 64) __nanosleep(64);
     }
     ok = __all_sync(kFull, ok);
     if (!ok && !C->abort) {
@@ -396,38 +398,40 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
   const int turns = ROWS == 1 ? 4 : P.turns, window = P.window;
   const Waiter wait{C, P.dev_status};
 
-  if (threadIdx.x == 0) {
+  if (warp == 0) {   // lane i: the i-th of every kind
     const int users = turns == 4 ? 2 : 4;   // streams that read a tile of keys
-    for (int i = 0; i < kRing; ++i) {
-      mbar_init(smem_u32(&C->rec_full[i]), 1);
-      mbar_init(smem_u32(&C->rec_empty[i]), 16 + 4 + 1 + 1 + (K::kPaged ? 4 : 0) + (K::kCodes ? 1 : 0));
+    if (lane < kRing) {
+      mbar_init(smem_u32(&C->rec_full[lane]), 1);
+      mbar_init(smem_u32(&C->rec_empty[lane]), 16 + 4 + 1 + 1 + (K::kPaged ? 4 : 0) + (K::kCodes ? 1 : 0));
     }
-    for (int i = 0; i < NS; ++i) {
-      mbar_init(smem_u32(&C->k_full[i]), K::kFullArrivals);
-      mbar_init(smem_u32(&C->v_full[i]), K::kFullArrivals);
-      mbar_init(smem_u32(&C->k_empty[i]), users);
-      mbar_init(smem_u32(&C->v_empty[i]), users);
-      mbar_init(smem_u32(&C->v_ok[i]), 1);
+    if (lane < NS) {
+      mbar_init(smem_u32(&C->k_full[lane]), K::kFullArrivals);
+      mbar_init(smem_u32(&C->v_full[lane]), K::kFullArrivals);
+      mbar_init(smem_u32(&C->k_empty[lane]), users);
+      mbar_init(smem_u32(&C->v_empty[lane]), users);
+      mbar_init(smem_u32(&C->v_ok[lane]), 1);
     }
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(smem_u32(&C->q_full[i]), 1);
-      mbar_init(smem_u32(&C->q_empty[i]), turns);
-      mbar_init(smem_u32(&C->join_full[i]), 4 * turns);
-      mbar_init(smem_u32(&C->s_full[i]), 1);
-      mbar_init(smem_u32(&C->p_full[i]), 4);
-      mbar_init(smem_u32(&C->o_full[i]), 1);
-      mbar_init(smem_u32(&C->o_empty[i]), 4 * turns);   // the warps that join
+    if (lane < 4) {
+      mbar_init(smem_u32(&C->q_full[lane]), 1);
+      mbar_init(smem_u32(&C->q_empty[lane]), turns);
+      mbar_init(smem_u32(&C->join_full[lane]), 4 * turns);
+      mbar_init(smem_u32(&C->s_full[lane]), 1);
+      mbar_init(smem_u32(&C->p_full[lane]), 4);
+      mbar_init(smem_u32(&C->o_full[lane]), 1);
+      mbar_init(smem_u32(&C->o_empty[lane]), 4 * turns);   // the warps that join
     }
-    mbar_init(smem_u32(&C->next_full), 1);
-    for (int i = 0; i < 4 * 8; ++i) mbar_init(smem_u32(&C->copied[0][0] + i), K::kCodes ? 1 : 32);
-    for (int i = 0; i < 8; ++i) mbar_init(smem_u32(&C->codes_empty[i]), 4);
-    C->abort = 0;
+    mbar_init(smem_u32(&C->copied[0][0] + lane), K::kCodes ? 1 : 32);
+    if (lane < 8) mbar_init(smem_u32(&C->codes_empty[lane]), 4);
+    if (lane == 0) {
+      mbar_init(smem_u32(&C->next_full), 1);
+      C->abort = 0;
+      tma_prefetch_desc(&P.tmQ);
+      if constexpr (!K::kPaged) {
+        tma_prefetch_desc(&P.tmK);
+        tma_prefetch_desc(&P.tmV);
+      }
+    }
     fence_mbar_init();
-    tma_prefetch_desc(&P.tmQ);
-    if constexpr (!K::kPaged) {
-      tma_prefetch_desc(&P.tmK);
-      tma_prefetch_desc(&P.tmV);
-    }
   }
   if (warp == 16) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&C->tmem)) : "memory");
@@ -1297,7 +1301,9 @@ PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool 
   for (int turns = 1; turns <= 4; turns *= 2) {
     const long long items = groups_of(batch, total, turns, Hkv), T = kRowTokens * (4 / turns);
     const double tiles = std::max(1.0, (double)(key_bound + T) / TK);
-    for (long long n = 1; n == 1 || (may_split && n <= tiles / 4 && n * items <= 8ll * sm_count); ++n) {
+    for (int per_sm = 0; per_sm <= (may_split ? 8 : 0); ++per_sm) {   // uncut; as many parts as fill each SM once, twice ..
+      const long long n = per_sm == 0 ? 1 : per_sm * (long long)sm_count / items;
+      if (n < 1 || (n > 1 && n > tiles / 4)) continue;
       const double rounds = (double)((items * n + sm_count - 1) / sm_count);
       const double cost = rounds * (tiles / n * (2.0 / turns + fetch) + 5) + (n > 1 ? 4 : 0);
       if (cost < best * 0.98) {   // a little gain is not worth the partials

@@ -55,8 +55,8 @@ def multi_token_args(seq_lens: torch.Tensor, block_table, n_q: int, max_blocks_p
 
     The n_q rows of a sequence read the same cache blocks at about the same time (they are neighbours in the
     balanced schedule), so the repeats are served by L2 rather than HBM.  For FP8 and 4-bit caches
-    ``puzzle_decode_attn_tokens`` does the same job faster (pairs of query tokens share one pass over the tiles);
-    this form remains for bf16 caches and as a second way to the same result."""
+    ``puzzle_decode_attn_tokens`` does the same job faster (pairs of query tokens share one pass over the tiles), for more
+    than a few tokens ``puzzle_chunk_attn`` over every cache type; this form remains as a second way to the same result."""
     batch = seq_lens.shape[0]
     dev = seq_lens.device
     L = seq_lens.to(torch.int64)[:, None]

@@ -12,9 +12,10 @@ D, BLOCK = 64, 16
 KINDS = {"fp8": P.KV_FP8_E4M3, "bf16": P.KV_BF16, "fp4": P.KV_FP4_E2M1}
 # half a step of the type that softmax weights are rounded to
 WEIGHT = {"packed": 2.0 ** -8, "bf16": 2.0 ** -8, "fp8": 2.0 ** -11, "fp4": 2.0 ** -11}
-# An f16 weight lies at 2^9 of its value in units of the reference, which is at most the row's maximum: half a step of f16's
-# smallest numbers, 2^-25, is 2^-34 of the largest weight, and that much each of the keys that a row sees can add or lose.
-FLOOR = {"packed": 0.0, "bf16": 0.0, "fp8": 2.0 ** -34, "fp4": 2.0 ** -34}
+# An f16 weight lies at 2^9 of its value in units of the reference, which is less than twice the row's largest weight: half a step
+# of f16's smallest numbers, 2^-25, is 2^-33 of the largest weight, and a second rounding, where the reference moved between the
+# halves of 64 keys, half of that.  So much each of the keys that a row sees can add or lose: 1.5 x 2^-33 < 2^-32.
+FLOOR = {"packed": 0.0, "bf16": 0.0, "fp8": 2.0 ** -32, "fp4": 2.0 ** -32}
 SLOP = 2.0 ** -13      # float32 dot products of 64 terms, exponentials of arguments up to 2^5, sums: well inside
 
 
