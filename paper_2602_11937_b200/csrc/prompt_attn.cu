@@ -15,7 +15,7 @@
 //    halves of a tile are two streams, not one of twice the width, so that every scheduler has four softmax warps: the special
 //    function unit, which bounds the kernel (16 exponentials a clock and SM), is fed while others wait for loads and products.
 //    Measured on a prompt of 8192 tokens when it was chosen: 740 us; two streams of 128 keys, with S and P apart so that the next S is
-//    computed early, 966; the same with two threads to a row 802.  Now 640 (860 TFLOP/s).
+//    computed early, 966; the same with two threads to a row 802.  Now 610 (900 TFLOP/s).
 //  * A group of 64, 32 or 16 tokens is 4, 2 or 1 tiles of rows with 1, 2 or 4 streams each; these take the halves of the tiles of keys
 //    in turn and join at the end.  Large groups fetch (and convert) a tile of keys once for many rows and have nothing to join, small
 //    ones make more items of few tokens.
@@ -295,6 +295,19 @@ __device__ __forceinline__ int granted_block(uint32_t src) {
   return ok ? (int)x : -1;
 }
 
+// Has the phase with this parity completed?
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // Waits by whole warps: one decision for the 32 lanes.
 struct Waiter {
   Ctl* C;
@@ -475,7 +488,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
       constexpr uint32_t kIdescPV = (1u << 4) | (kFmt << 7) | (kFmt << 10) | (1u << 16) | (8u << 17) | (8u << 24);
       const uint32_t ts = tmem + kTmemS + 64 * st, to = tmem + kTmemO + 64 * st;
       const uint32_t q_lo = ((q_at + tile * kTileBytes) >> 4) + kDescLo, k_lo = (k_at >> 4) + kDescLo, v_lo = (v_at >> 4) + kDescLo;
-      int kt = 0, n = 0, items = 0, queries = 0;   // tiles of all items; half tiles, items and query tiles of this stream
+      int base = 0, n = 0, items = 0, queries = 0;   // tiles of the items before; half tiles, items and query tiles of this stream
       Record r;
       bool ok = true;
       for (int it = 0; ok && get_record(it, r); ++it) {
@@ -487,56 +500,73 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
           if (ok && !sh.on() && lane == 0) mbar_arrive(smem_u32(&C->q_empty[tile]));
         }
         const int nt = tiles_of(r);
-        for (int t = 0; ok && t < nt; ++t, ++kt) {
-          if (turns == 4 && (t & 1) != (st >> 1)) continue;   // two other streams' tile
-          const int s = kt % NS;
-          const uint32_t par = (uint32_t)(kt / NS) & 1u;
-          // one stream to a tile of rows takes both halves, else one of them
-          const int ja = 2 * t + (turns == 1 ? 0 : st & 1), jb = turns == 1 ? ja + 1 : ja;
-          const bool a = sh.mine(ja), b = turns == 1 && sh.mine(jb);
-          if (!a && !b) {                                     // others' alone: let go of it
-            ok = wait(C->k_full[s], par) && wait(C->v_ok[s], par);
+        auto parity = [&](int t) { return (uint32_t)((base + t) / NS) & 1u; };
+        auto skip = [&](int from, int to) {           // others' alone: let go of them
+          for (int t = from; ok && t < to; ++t) {
+            if (turns == 4 && (t & 1) != (st >> 1)) continue;   // two other streams' tile
+            const int s = (base + t) % NS;
+            ok = wait(C->k_full[s], parity(t)) && wait(C->v_ok[s], parity(t));
             if (ok && lane == 0) {
               mbar_arrive(smem_u32(&C->k_empty[s]));
               mbar_arrive(smem_u32(&C->v_empty[s]));
             }
             __syncwarp();
-            continue;
           }
-#pragma unroll 1
-          for (int j = a ? ja : jb; j <= (b ? jb : ja); ++j) {
-            const bool done = j == (b ? jb : ja), first = j == sh.j0, last = sh.last(j);
-            const int nb = sh.blocks(j);
-            const uint32_t half = (uint32_t)(s * (kTileBytes / 16) + (j & 1) * (kTileBytes / 32));
-            // The P that this S overwrites has been read: products of one CTA run in the order of their issue.
-            ok = wait(C->k_full[s], par);
-            if (!ok) break;
-            tc_after();
-            if (elect_one()) {
+        };
+        skip(0, sh.on() ? sh.j0 >> 1 : nt);
+        if (sh.on()) {
+          // S of half tile j and its signals; the half tile after which a tile is let go of: the stream's last one in it.
+          auto done = [&](int j) { return turns > 1 || (j & 1) || sh.last(j); };
+          auto logits = [&](int j) {
+            const int s = (base + (j >> 1)) % NS, nb = sh.blocks(j);
+            const uint32_t k = k_lo + (uint32_t)(s * (kTileBytes / 16) + (j & 1) * (kTileBytes / 32));
 #pragma unroll
-              for (int ks = 0; ks < 4; ++ks)
-                umma_ss(ts, desc128(q_lo + 2 * ks), desc128(k_lo + half + 2 * ks), kIdescQK | (uint32_t)(2 * nb) << 17, ks);
-              umma_commit(smem_u32(&C->s_full[st]));
-              if (done) umma_commit(smem_u32(&C->k_empty[s]));
-              if (last) umma_commit(smem_u32(&C->q_empty[tile]));
-            }
+            for (int ks = 0; ks < 4; ++ks)
+              umma_ss(ts, desc128(q_lo + 2 * ks), desc128(k + 2 * ks), kIdescQK | (uint32_t)(2 * nb) << 17, ks);
+            umma_commit(smem_u32(&C->s_full[st]));
+            if (done(j)) umma_commit(smem_u32(&C->k_empty[s]));
+            if (sh.last(j)) umma_commit(smem_u32(&C->q_empty[tile]));
+          };
+          int j = sh.j0;
+          ok = ok && wait(C->k_full[(base + (j >> 1)) % NS], parity(j >> 1));
+          if (ok) {
+            tc_after();
+            if (elect_one()) logits(j);
             __syncwarp();
-            ok = wait(C->v_ok[s], par) && (!first || wait(C->o_empty[st], ((uint32_t)items & 1u) ^ 1u)) &&
-                 wait(C->p_full[st], (uint32_t)n & 1u);
+          }
+          for (; ok && j < sh.j_hi; j += turns, ++n) {
+            const int s = (base + (j >> 1)) % NS, nb = sh.blocks(j), next = j + turns;
+            const bool first = j == sh.j0, more = next < sh.j_hi;
+            // all that can be looked at before the weights are
+            const uint64_t& k_next = C->k_full[(base + (next >> 1)) % NS];
+            ok = wait(C->v_ok[s], parity(j >> 1)) && (!first || wait(C->o_empty[st], ((uint32_t)items & 1u) ^ 1u));
+            const bool early = ok && more && __all_sync(kFull, mbar_test(smem_u32(&k_next), parity(next >> 1)));
+            ok = ok && wait(C->p_full[st], (uint32_t)n & 1u);
             if (!ok) break;
             tc_after();
             if (elect_one()) {
+              const uint32_t v = v_lo + (uint32_t)(s * (kTileBytes / 16) + (j & 1) * (kTileBytes / 32));
 #pragma unroll
               for (int ks = 0; ks < kHalf; ++ks)   // a block of 16 keys each
-                if (ks < nb) umma_ts(to, ts + 8 * ks, desc128(v_lo + half + 128 * ks), kIdescPV, !(first && ks == 0));
-              if (last) umma_commit(smem_u32(&C->o_full[st]));
-              if (done) umma_commit(smem_u32(&C->v_empty[s]));
+                if (ks < nb) umma_ts(to, ts + 8 * ks, desc128(v + 128 * ks), kIdescPV, !(first && ks == 0));
+              if (!more) umma_commit(smem_u32(&C->o_full[st]));
+              if (done(j)) umma_commit(smem_u32(&C->v_empty[s]));
+              // The P that the next S overwrites has been read by then: products of one CTA run in the order of their issue.
+              if (early) logits(next);
             }
             __syncwarp();
-            ++n;
+            if (more && !early) {
+              ok = wait(k_next, parity(next >> 1));
+              if (!ok) break;
+              tc_after();
+              if (elect_one()) logits(next);
+              __syncwarp();
+            }
           }
+          if (ok) skip(((sh.j_hi - 1 - ((sh.j_hi - 1 - sh.j0) & (turns - 1))) >> 1) + 1, nt);
+          ++items;
         }
-        if (sh.on()) ++items;
+        base += nt;
       }
     } else if (warp == 20) {
       // ================================================================= work records, queries, packed keys and values
@@ -768,10 +798,10 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
           mbar_wait_bounded(smem_u32(&C->copied[0][i % K::kCopySlots]), (uint32_t)(i / K::kCopySlots) & 1u);
       }
     } else if (K::kPaged && warp >= 24) {
-     // ================================================================== tiles of the cache in the MMAs' form, four warps
-     // Warp lw has blocks lw and lw + 4 of every tile, K and V.
-     const int lw = warp - 24;
-     if constexpr (SRC == kSrcBf16) {
+      // ================================================================= tiles of the cache in the MMAs' form, four warps
+      // Warp lw has blocks lw and lw + 4 of every tile, K and V.
+      const int lw = warp - 24;
+      if constexpr (SRC == kSrcBf16) {
       // Copied to where the MMAs read them.  Places in the cache are looked up for 16 tiles at a time, lane = 2 tile + block.
       constexpr int kSlots = K::kCopySlots;
       auto lookup = [&](const Record& r, int t_first) { return cache_row(P, r, r.kb0 + (t_first + (lane >> 1)) * NBLK + lw + 4 * (lane & 1)); };
@@ -942,7 +972,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
     const uint32_t quad = (uint32_t)(32 * wq) << 16;
     const uint32_t ts = tmem + kTmemS + 64 * st + quad, to = tmem + kTmemO + quad;
     const bool wide_out = (reinterpret_cast<uintptr_t>(P.out) & 31) == 0;   // 32 bytes of a row in one store
-    int n = 0, items = 0;   // tiles and items of this stream
+    int n = 0, items = 0;   // half tiles and items of this stream
     Record r;
     bool ok = true;
     for (int it = 0; ok && get_record(it, r); ++it) {
