@@ -259,7 +259,7 @@ PUZZLE_API puzzle_status puzzle_prompt_attn(const puzzle_layer_desc* desc, const
  * is the better call for up to four tokens per sequence over an E4M3 or 4-bit cache; this one shares a pass over the cache
  * among 16 or 32 tokens and has no bound on them.  (Same passages as puzzle_prompt_attn and puzzle_decode_attn_tokens.)
  *   q: packed rows of bf16, stride q_token_stride; out, lse_out, sinks as puzzle_prompt_attn;
- *   workspace: at least puzzle_chunk_attn_workspace_bytes(...) bytes for this batch and total_tokens, 16-byte aligned (below 90 MB
+ *   workspace: at least puzzle_chunk_attn_workspace_bytes(...) bytes for this batch and total_tokens, 16-byte aligned (at most 79 MB
  *     with 8 KV heads on 148 SMs, and next to nothing where there are many tokens); it needs no preparation, and nothing in it lasts
  *     from call to call.  Calls that share one must not overlap on the GPU;
  *   a token whose position is negative sees no key: out = 0, lse = sink.  A sequence longer than its table row is clamped to it

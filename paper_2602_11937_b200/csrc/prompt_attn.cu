@@ -1323,7 +1323,7 @@ static long long groups_of(long long batch, long long total, int turns, int Hkv)
 // The size of a group (64, 32 or 16 tokens: 1, 2 or 4 streams to a tile of rows) and the parts that its keys are cut into: what takes
 // the SM with the most items the least time, in steps of 64 keys of a stream.  A tile of keys is 2, 1 or 1/2 steps of each stream, and
 // fetching it (converting it, for codes) some of a step whatever the group; an item costs about five steps beside its keys.  Parts
-// have four tiles at least, and there are at most 8 items per SM where keys are cut, which bounds the partials.  (512 tokens over 64K
+// have four tiles at least, and there are at most 4 items per SM where keys are cut, which bounds the partials.  (512 tokens over 64K
 // E4M3 keys: groups of 16 uncut 1224 us, of 32 in 8 parts 849.)
 PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool may_split, double fetch, int sm_count) {
   PromptPlan plan = {1, 4};
@@ -1331,7 +1331,7 @@ PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool 
   for (int turns = 1; turns <= 4; turns *= 2) {
     const long long items = groups_of(batch, total, turns, Hkv), T = kRowTokens * (4 / turns);
     const double tiles = std::max(1.0, (double)(key_bound + T) / TK);
-    for (int per_sm = 0; per_sm <= (may_split ? 8 : 0); ++per_sm) {   // uncut; as many parts as fill each SM once, twice ..
+    for (int per_sm = 0; per_sm <= (may_split ? 4 : 0); ++per_sm) {   // uncut; as many parts as fill each SM once, twice ..
       const long long n = per_sm == 0 ? 1 : per_sm * (long long)sm_count / items;
       if (n < 1 || (n > 1 && n > tiles / 4)) continue;
       const double rounds = (double)((items * n + sm_count - 1) / sm_count);
@@ -1351,7 +1351,7 @@ size_t prompt_partial_bytes(int total, int Hkv, int splits) {
 }
 // The most parts that prompt_plan cuts into, whatever the context's length.
 int prompt_most_splits(int batch, int total, int Hkv, int sm_count) {
-  return (int)std::max<long long>(1, 8ll * sm_count / std::max<long long>(1, groups_of(batch, total, 1, Hkv)));
+  return (int)std::max<long long>(1, 4ll * sm_count / std::max<long long>(1, groups_of(batch, total, 1, Hkv)));
 }
 
 cudaError_t launch_prompt_attn(const PromptParams& P, PromptSource src, int sm_count, cudaStream_t s, int* smem_limit) {
