@@ -256,8 +256,8 @@ PUZZLE_API puzzle_status puzzle_prompt_attn(const puzzle_layer_desc* desc, const
 /* Attention of chunks of new tokens over the paged cache (E4M3, bf16 or 4-bit), after their append: pieces of long prompts,
  * drafted tokens, single tokens, in any mixture.  The n_b packed tokens of sequence b are its last ones: token i sits at
  * position p = seq_lens[b] - n_b + i and sees the keys [p + 1 - min(W, p + 1), p], as in puzzle_decode_attn_tokens, which
- * is the better call for up to four tokens per sequence over an E4M3 or 4-bit cache; this one shares a pass over the cache
- * among 16 or 32 tokens and has no bound on them.  (Same passages as puzzle_prompt_attn and puzzle_decode_attn_tokens.)
+ * is the better call for up to about six tokens per sequence over an E4M3 or 4-bit cache that fills the device; this one shares a
+ * pass over the cache among 16, 32 or 64 tokens and has no bound on them.  (Same passages as puzzle_prompt_attn and puzzle_decode_attn_tokens.)
  *   q: packed rows of bf16, stride q_token_stride; out, lse_out, sinks as puzzle_prompt_attn;
  *   workspace: at least puzzle_chunk_attn_workspace_bytes(...) bytes for this batch and total_tokens, 16-byte aligned (at most 79 MB
  *     with 8 KV heads on 148 SMs, and next to nothing where there are many tokens); it needs no preparation, and nothing in it lasts
