@@ -549,10 +549,15 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
 #pragma unroll
               for (int ks = 0; ks < kHalf; ++ks)   // a block of 16 keys each
                 if (ks < nb) umma_ts(to, ts + 8 * ks, desc128(v + 128 * ks), kIdescPV, !(first && ks == 0));
-              if (!more) umma_commit(smem_u32(&C->o_full[st]));
               if (done(j)) umma_commit(smem_u32(&C->v_empty[s]));
-              // The P that the next S overwrites has been read by then: products of one CTA run in the order of their issue.
-              if (early) logits(next);
+              if (!more) umma_commit(smem_u32(&C->o_full[st]));
+              // The next S overwrites this P.  Two products with different accumulators are not bound to run in the order of their
+              // issue; what is issued before a fence::before_thread_sync is ordered before all tcgen05 operations behind it.
+              tc_before();
+              if (early) {
+                tc_after();
+                logits(next);
+              }
             }
             __syncwarp();
             if (more && !early) {
