@@ -1070,6 +1070,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
                     alpha = ref == kUnset ? 0.f : ex2(ref - up);
                     ref = up;
                   }
+                  __syncwarp();            // what follows goes through tensor memory by whole warps
                   l *= alpha;
                   if (q == 1) rescale_weights<K::kCodes>(ts, alpha);
                   if (j0 != sh.j0) {       // the product before has ended: this S was issued behind it
@@ -1085,7 +1086,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
                   }
                 }
                 // infinity - infinity, or a NaN: the whole row is NaN
-                if (!(top < INFINITY)) ref = NAN;
+                ref = top < INFINITY ? ref : NAN;
               }
               const uint64_t c2 = pack2(c, c), r2 = pack2(-ref, -ref);
               uint64_t sum[2] = {0ull, 0ull};
@@ -1170,6 +1171,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         for (int i = g0; i < g0 + turns; ++i) with |= Share(r, i, turns, window).on() ? 1u << i : 0u;
 #pragma unroll 1
       for (int c0 = col0; c0 < col0 + cols; c0 += 16) {
+        __syncwarp();                            // tensor memory is read by whole warps; rows without a token store nothing
         float o[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[j] = 0.f;
@@ -1203,15 +1205,13 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
             }
           }
         }
-        __syncwarp();
-        if (!real) continue;
-        if (P.splits > 1) {
+        if (real && P.splits > 1) {
           if (lse != -INFINITY) {
             float4* dst = reinterpret_cast<float4*>(P.part_o + part_row * kHeadDim + c0);
 #pragma unroll
             for (int j = 0; j < 4; ++j) dst[j] = make_float4(o[4 * j] * f, o[4 * j + 1] * f, o[4 * j + 2] * f, o[4 * j + 3] * f);
           }
-        } else {
+        } else if (real) {
           uint32_t y[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) y[j] = f32x2_to_bf16x2(o[2 * j] * f, o[2 * j + 1] * f);
