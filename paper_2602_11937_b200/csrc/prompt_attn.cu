@@ -41,7 +41,9 @@
 //  * 0 x NaN: a tile of V that some row of the group does not see is searched for infinities and NaN before its product.  They
 //    are replaced by zero, and the rows that do see them get them added at the end, read again from where they come from.
 //
-// Every wait is bounded: one that runs out sets PUZZLE_DEV_WAIT_EXPIRED and a flag upon which every role leaves its loop.
+// Every wait is bounded: one that runs out sets PUZZLE_DEV_WAIT_EXPIRED and a flag upon which every role leaves its loop.  At its end,
+// whichever way it came there, a role waits (again with a limit) for what it has set going: products, copies, the request for work.
+// None is in flight when shared and tensor memory are given back.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -98,6 +100,7 @@ struct Ctl {
   uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6], v_ok[6];
   uint64_t s_full[4], p_full[4], o_full[4], o_empty[4];   // of the streams
   uint64_t join_full[4];
+  uint64_t ended[4];                                      // all products of a stream
   uint64_t next_full;
   alignas(16) uint4 next;   // answer to a request for work
   uint64_t copied[4][8];         // of a warp's blocks; of a tile's codes: the first row
@@ -430,6 +433,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
       mbar_init(smem_u32(&C->join_full[lane]), 4 * turns);
       mbar_init(smem_u32(&C->s_full[lane]), 1);
       mbar_init(smem_u32(&C->p_full[lane]), 4);
+      mbar_init(smem_u32(&C->ended[lane]), 1);
       mbar_init(smem_u32(&C->o_full[lane]), 1);
       mbar_init(smem_u32(&C->o_empty[lane]), 4 * turns);   // the warps that join
     }
@@ -573,6 +577,9 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         }
         base += nt;
       }
+      if (elect_one()) umma_commit(smem_u32(&C->ended[st]));
+      __syncwarp();
+      mbar_wait_bounded(smem_u32(&C->ended[st]), 0);
     } else if (warp == 20) {
       // ================================================================= work records, queries, packed keys and values
       const int T = kRowTokens * (4 / turns);
@@ -609,7 +616,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         }
       };
       load_window();
-      int kt = 0, before_tiles = 0;
+      int kt = 0, before_tiles = 0, asked = 0;
       bool ok = true;
       for (int it = 0;; ++it) {
         // blocks of the grid are items, long ones first; a long one is asked for when the one before the last has been done with
@@ -627,6 +634,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
             request_block(smem_u32(&C->next), bar);
           }
           __syncwarp();
+          ++asked;
           ok = wait(C->next_full, (uint32_t)(it - 1) & 1u);
           if (ok) item = granted_block(smem_u32(&C->next));
         }
@@ -697,11 +705,10 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         }
         if (!ok) break;
       }
-      if (C->abort) {   // the copies in flight end before the shared memory is given back
-        for (int i = max(kt - NS, 0); i < kt; ++i) {
-          mbar_wait_bounded(smem_u32(&C->k_full[i % NS]), (uint32_t)(i / NS) & 1u);
-          mbar_wait_bounded(smem_u32(&C->v_full[i % NS]), (uint32_t)(i / NS) & 1u);
-        }
+      if (asked > 0) mbar_wait_bounded(smem_u32(&C->next_full), (uint32_t)(asked - 1) & 1u);
+      for (int i = max(kt - NS, 0); i < kt; ++i) {
+        mbar_wait_bounded(smem_u32(&C->k_full[i % NS]), (uint32_t)(i / NS) & 1u);
+        mbar_wait_bounded(smem_u32(&C->v_full[i % NS]), (uint32_t)(i / NS) & 1u);
       }
     } else if (warp == 21) {
       // ================================================================= infinities and NaN among values not all rows see
@@ -761,10 +768,9 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
           __syncwarp();
         }
       }
-      if (C->abort)   // the copies in flight end before the shared memory is given back
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (q_n[i] > 0) mbar_wait_bounded(smem_u32(&C->q_full[i]), (uint32_t)(q_n[i] - 1) & 1u);
+      for (int i = 0; i < 4; ++i)
+        if (q_n[i] > 0) mbar_wait_bounded(smem_u32(&C->q_full[i]), (uint32_t)(q_n[i] - 1) & 1u);
     } else if (K::kCodes && warp == 23) {
       // ================================================================= codes of the cache, as they lie there
       // One lane to a block of K or V of a tile; places in the cache are looked up for four tiles at a time, lane = 8 tile + block.
@@ -798,7 +804,6 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
             __syncwarp();
           }
         }
-        // no copy is in flight when the shared memory is given back
         for (int i = max(in - K::kCopySlots, 0); i < in; ++i)
           mbar_wait_bounded(smem_u32(&C->copied[0][i % K::kCopySlots]), (uint32_t)(i / K::kCopySlots) & 1u);
       }
@@ -869,7 +874,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         }
         ++out;
       }
-      cp_wait_all();   // none is in flight when the shared memory is given back
+      cp_wait_all();
      } else if constexpr (K::kCodes) {
       // Codes of a tile -> bf16 keys and f16 values in the swizzled rows that the MMAs read.
       auto convert = [&](uint32_t src, uint32_t dst, bool is_v) {
@@ -1237,6 +1242,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
   }
   __syncthreads();
   if (warp == 16) {
+    __syncwarp();
     tc_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
