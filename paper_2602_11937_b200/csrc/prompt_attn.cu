@@ -1259,16 +1259,18 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(const __grid_constant
   grid_dependency_wait();
   if (at >= rows) return;
   const int token = (int)(at / Hq), g = (int)(at % Hq);
-  int lo = 0, hi = P.batch;             // the last sequence that starts at this row or before
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (P.starts[mid] <= token) lo = mid;
-    else hi = mid;
+  // The row's sequence: valid ones do not share rows, but with bad entries among them need not lie in order.
+  const unsigned sixteen = 0xffffu << (threadIdx.x & 16);
+  int seq = -1;
+  for (int b = o; b < P.batch; b += 16) {
+    const int st = P.starts[b], en = P.starts[b + 1];
+    if (st >= 0 && st <= token && token < en && en <= P.total) seq = b;
   }
-  const int st = P.starts[lo], en = P.starts[lo + 1];
-  if (st < 0 || en > P.total || token < st || token >= en) return;   // no sequence's row
-  const int len = min(max(P.seq_lens[lo], 0), P.max_blocks_per_seq * kBlock);
-  const bool sees = len - (en - token) >= 0;
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) seq = max(seq, __shfl_xor_sync(sixteen, seq, d));
+  if (seq < 0) return;                  // no sequence's row
+  const int len = min(max(P.seq_lens[seq], 0), P.max_blocks_per_seq * kBlock);
+  const bool sees = len - (P.starts[seq + 1] - token) >= 0;
   const float* lse = P.part_lse + at;
   float top = P.sinks ? P.sinks[g] : -INFINITY;
   const float sk = top;
