@@ -63,7 +63,8 @@ constexpr int kShortTiles = 4;              // items of no more tiles are asked 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kPoly5 = 0.0013274633f, kPoly4 = 0.0096719619f, kPoly3 = 0.0555067845f, kPoly2 = 0.2402223498f,
                 kPoly1 = 0.6931470633f;
-constexpr float kUnset = -1e30f;            // a reference that any logit is far above
+constexpr float kUnset = -3.402823466e38f;  // a reference that no logit is below
+constexpr float kLarge = 1048576.f;         // references beyond 2^20: see there
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kHalf = NBLK / 2;             // blocks of a stream's half of a tile
 // tensor memory: S (and P over it) of the four streams, then O
@@ -989,8 +990,9 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
       const Share sh(r, st, turns, window);
       float c = P.sm_scale_log2e;
       if (K::kCodes && P.k_scale) c *= P.k_scale[r.kvh];
-      const bool odd = !(c > 0.f && c < INFINITY);   // then logits are scaled before their maximum is taken
-      const float pre = c;
+      // Logits of some row (odd) are scaled before their maximum is taken: all rows', pre is 1 in those that do not need it.
+      bool odd = !(c > 0.f && c < INFINITY);
+      float pre = odd ? c : 1.f;
       if (odd) c = 1.f;
       const int p = sh.pos + (row >> 3), p0 = sh.pos + 4 * wq; // this row's position, the warp's first
       const int hi = p + 1, lo = window > 0 ? p - window + 1 : 0;   // the row sees [lo, hi)
@@ -1066,13 +1068,29 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
                   x[0] = max3(x[0], s[j], s[j + 1]);
                   x[1] = max3(x[1], s[j + 2], s[j + 3]);
                 }
-                const float top = max3(x[0], x[1], x[1]), now = top * c - K::kShift;
+                float top = max3(x[0], x[1], x[1]), now = top * c - K::kShift;
+                // A weight is 2^(c s - ref) rounded once, so what rounding took from the reference is a factor of all of the row's
+                // weights and falls out.  Beyond 2^20 that factor leaves the range of the weights: then the row's logits are scaled,
+                // and rounded, first, the reference is the largest of them itself, and the differences are exact.
+                const bool large = fabsf(top) < INFINITY && fabsf(now) > kLarge && pre == 1.f;
+                if (__any_sync(kFull, large)) {
+                  odd = true;
+                  const float by = large ? c : 1.f;
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) s[j] *= by;
+                  top *= by;
+                  if (large) {
+                    pre = c;
+                    c = 1.f;
+                  }
+                }
+                if (c == 1.f && fabsf(top) > kLarge) now = top;
                 const bool raise = now > ref;
                 if (__any_sync(kFull, raise)) {
                   float alpha = 1.f;
                   if (raise) {   // by whole powers of two: what was rounded before keeps its bits
-                    const float up = ref == kUnset ? now : ref + ceilf(now - ref);
-                    alpha = ref == kUnset ? 0.f : ex2(ref - up);
+                    const float up = now - ref > 128.f ? now : ref + ceilf(now - ref);   // (beyond 128 nothing is left of those)
+                    alpha = ex2(ref - up);
                     ref = up;
                   }
                   __syncwarp();            // what follows goes through tensor memory by whole warps
@@ -1128,7 +1146,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         if (!ok) break;
         ++items;
       }
-      if (ref == kUnset) ref = -INFINITY;    // no logit above -inf: the sum is 0
+      if (ref == kUnset && l == 0.f) ref = -INFINITY;    // no logit above -inf
       const int g0 = st & ~(turns - 1), cols = 64 / turns, col0 = cols * (st - g0);
       const float own = ref;
       float own_l = l;
