@@ -996,6 +996,9 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
       if (odd) c = 1.f;
       const int p = sh.pos + (row >> 3), p0 = sh.pos + 4 * wq; // this row's position, the warp's first
       const int hi = p + 1, lo = window > 0 ? p - window + 1 : 0;   // the row sees [lo, hi)
+      // Rows without a token hold what is behind the sequence: other sequences' queries, and logits from earlier items.  They do not
+      // take part in what a warp decides together, so that these change no bit of a result.
+      const bool real = (row >> 3) < sh.ntok;
       float ref = kUnset, l = 0.f;                             // weights are 2^(c s - ref)
       for (int j0 = sh.j0; j0 < sh.j_hi; j0 += turns, ++n) {
         const int nb = sh.blocks(j0), k0 = (r.kb0 + j0 * kHalf) * kBlock;
@@ -1030,7 +1033,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
           }
           float a0, a1;
           unpack2(add2(sum[0], sum[1]), a0, a1);
-          done = !__any_sync(kFull, !(a0 + a1 < K::kMuch) || !(big < 100.f));
+          done = !__any_sync(kFull, real && (!(a0 + a1 < K::kMuch) || !(big < 100.f)));
           if (done) {
             l += a0 + a1;
             tmem_st32(ts, u);
@@ -1072,7 +1075,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
                 // A weight is 2^(c s - ref) rounded once, so what rounding took from the reference is a factor of all of the row's
                 // weights and falls out.  Beyond 2^20 that factor leaves the range of the weights: then the row's logits are scaled,
                 // and rounded, first, the reference is the largest of them itself, and the differences are exact.
-                const bool large = fabsf(top) < INFINITY && fabsf(now) > kLarge && pre == 1.f;
+                const bool large = real && fabsf(top) < INFINITY && fabsf(now) > kLarge && pre == 1.f;
                 if (__any_sync(kFull, large)) {
                   odd = true;
                   const float by = large ? c : 1.f;
@@ -1085,7 +1088,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
                   }
                 }
                 if (c == 1.f && fabsf(top) > kLarge) now = top;
-                const bool raise = now > ref;
+                const bool raise = real && now > ref;
                 if (__any_sync(kFull, raise)) {
                   float alpha = 1.f;
                   if (raise) {   // by whole powers of two: what was rounded before keeps its bits
@@ -1124,7 +1127,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
               float a0, a1;
               unpack2(add2(sum[0], sum[1]), a0, a1);
               part = a0 + a1;
-              if (look || !__any_sync(kFull, !(part < K::kMuch))) break;
+              if (look || !__any_sync(kFull, real && !(part < K::kMuch))) break;
             }
             l += part;
           }
@@ -1166,7 +1169,6 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         const float2 side = turns > 1 ? C->join[it & 1][i][row] : make_float2(own, own_l);
         l += side.y * ex2(side.x - zero);
       }
-      const bool real = (row >> 3) < sh.ntok;
       const long long at = (r.row0 + kRowTokens * tile + (long long)(row >> 3)) * (P.Hkv * kGroup) + g;
       float z = l, big = ref;
       if (P.splits == 1 && P.sinks) {
