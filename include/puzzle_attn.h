@@ -262,6 +262,8 @@ PUZZLE_API puzzle_status puzzle_prompt_attn(const puzzle_layer_desc* desc, const
  *   workspace: at least puzzle_chunk_attn_workspace_bytes(...) bytes for this batch and total_tokens, 16-byte aligned (at most 79 MB
  *     with 8 KV heads on 148 SMs, and next to nothing where there are many tokens); it needs no preparation, and nothing in it lasts
  *     from call to call.  Calls that share one must not overlap on the GPU;
+ *   over a ring of R blocks (a window layer's table that repeats them) the append before it leaves the keys that these tokens
+ *     see only where a sequence has at most 16 R + 1 - W of them;
  *   a token whose position is negative sees no key: out = 0, lse = sink.  A sequence longer than its table row is clamped to it
  *   (PUZZLE_DEV_SEQ_TOO_LONG); keys behind a bad block-table entry count as zeros (PUZZLE_DEV_BAD_BLOCK).
  * Softmax weights are held in bf16 over a bf16 cache (off by 2^-8 of themselves at most) and in f16 over the others (2^-11, down to

@@ -44,6 +44,38 @@ def cache_blocks(windows, batch: int, max_blocks_per_seq: int) -> list:
     return [batch * (max_blocks_per_seq if w == 0 else min(max_blocks_per_seq, window_ring_blocks(w))) for w in windows]
 
 
+def blocks_twice(block_tables) -> torch.Tensor:
+    """Whether a row of a table [batch][max_blocks_per_seq] has a block more than once, as a ring's has: bool [tables][batch]."""
+    table = torch.stack(list(block_tables)).to(torch.int64)
+    alone = -1 - torch.arange(table.shape[2], device=table.device)       # equal to nothing
+    entry = torch.where(table >= 0, table, alone).sort(-1).values
+    return (entry[..., 1:] == entry[..., :-1]).any(-1)
+
+
+def window_keys_lost(block_tables, windows, num_blocks, seq_lens: torch.Tensor, new_lens: torch.Tensor, most_new: int,
+                     block: int = BLOCK) -> torch.Tensor:
+    """Whether the append of a sequence's last ``new_lens[b]`` tokens in one call overwrites keys that one of them sees, which
+    attention over the cache after it would then get wrong.  Over a ring of R blocks that is so for more than
+    ``16 R + 1 - W`` tokens.  For several window layers: one table [batch][max_blocks_per_seq], window and number of physical
+    blocks each; no sequence has more than ``most_new`` new tokens.  Returns bool [layers][batch] on the tables' device; nothing is
+    waited for.  Table entries that are no block count for nothing, nor do sequences longer than their table row."""
+    table = torch.stack(list(block_tables)).to(torch.int64)
+    layers, batch, width = table.shape
+    on_layers = lambda v: torch.tensor(list(v), dtype=torch.int64, device=table.device)[:, None]
+    n, new = seq_lens.to(torch.int64)[None], new_lens.to(torch.int64)[None]
+    appended = (n > 0) & (n <= width * block) & (new > 0)
+    first = (n - new + 1 - on_layers(windows)).clamp(min=0)              # the first key that one of the tokens sees
+    lo, last = first // block, (n - 1).clamp(min=0) // block
+    at = lo[..., None] + torch.arange(min(width, (max(windows) + most_new) // block + 2), device=table.device)
+    entry = table.gather(2, at.clamp(max=width - 1))
+    real = appended[..., None] & (at <= last[..., None]) & (entry >= 0) & (entry < on_layers(num_blocks)[..., None])
+    # the last block may lie over the first one if it is written only where nothing is seen of that one
+    behind = (at == last[..., None]) & (entry == entry[..., :1]) & (last > lo)[..., None] & ((n - 1) % block < first % block)[..., None]
+    alone = -1 - torch.arange(entry.shape[2], device=table.device)       # equal to nothing
+    entry = torch.where(real & ~behind, entry, alone).sort(-1).values
+    return (entry[..., 1:] == entry[..., :-1]).any(-1)
+
+
 def multi_token_args(seq_lens: torch.Tensor, block_table, n_q: int, max_blocks_per_seq: int = None, q_lens=None):
     """Arguments that make the decode kernels serve ``n_q`` query tokens per sequence with a causal mask (several
     tokens of a multi-token step, or a prompt chunk after its bulk append): query row i of sequence b sits at position

@@ -13,6 +13,7 @@ from typing import List, Optional, Sequence
 import torch
 
 from . import binding as B
+from .paging import blocks_twice, window_keys_lost
 
 
 class DecodeStack:
@@ -45,6 +46,7 @@ class DecodeStack:
         self.q_rotated = None if rope is None else torch.empty(
             self.batch, self.descs[0].num_q_heads, self.descs[0].head_dim, dtype=torch.bfloat16, device=dev)
         self.graph = None
+        self._no_rings = {}      # window layers whose tables have no block twice: those tables' versions
 
     def step(self, q: List[torch.Tensor], k_new: List[torch.Tensor], v_new: List[torch.Tensor],
              out: List[torch.Tensor], stream=None) -> None:
@@ -72,9 +74,14 @@ class DecodeStack:
         continued False: every sequence begins with these tokens; they attend to one another's keys and values as they are, and of
         a window layer only the tokens that a later step can see go into the cache (a ring of ``window_ring_blocks`` takes
         them).  continued True: pieces behind earlier tokens attend to the cache.  A window layer's cache then has to
-        hold the window before the piece's first token together with the piece, which a ring of that size does for very
-        short pieces only.  Not for capture: buffers are allocated as needed."""
+        hold the window before the piece's first token together with the piece, which a ring of R blocks does for
+        ``16 R + 1 - W`` tokens of a sequence; longer pieces over a ring are refused with a ValueError before anything is stored
+        (give the pieces in shorter ones, or the layer a longer ring).  To know, the call looks at the tables of
+        window layers and waits for the answer; not again at those that have no block twice, until torch changes them (36 layers, 8
+        x 5 tokens: 790 us a call, 1290 with a look).  Not for capture: buffers are allocated as needed."""
         tokens = q[0].shape[0]
+        if continued and tokens > 0:
+            self._check_rings(starts, tokens, stream)
         d0 = self.descs[0]
         rotate = self.rope is not None
         room = lambda heads: torch.empty(tokens, heads, d0.head_dim, dtype=torch.bfloat16, device=q[0].device)
@@ -99,6 +106,26 @@ class DecodeStack:
             else:
                 B.puzzle_prompt_attn(self.descs[i], q_i, k_i, v_new[i], starts, self.sinks[i], out[i], dev_status=self.status,
                                      stream=stream)
+
+    def _check_rings(self, starts: torch.Tensor, tokens: int, stream) -> None:
+        _, _, seq_lens, tables, _, _ = self._keep
+        version = lambda i: None if tables[i].is_inference() else tables[i]._version
+        layers = [i for i, w in enumerate(self.windows) if w > 0 and tables[i] is not None and
+                  (version(i) is None or self._no_rings.get(i) != version(i))]
+        if not layers:
+            return
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            first, end = starts[:-1].to(torch.int64), starts[1:].to(torch.int64)
+            new = torch.where((first >= 0) & (end >= first) & (end <= tokens), end - first, 0)
+            lost = window_keys_lost([tables[i] for i in layers], [self.windows[i] for i in layers],
+                                    [self.views[i].num_blocks for i in layers], seq_lens, new, tokens).any(1)
+            lost, twice = torch.stack([lost, blocks_twice([tables[i] for i in layers]).any(1)]).tolist()
+        if any(lost):
+            raise ValueError("a piece is too long for the ring of layer %d (window %d): its tokens would overwrite keys that its "
+                             "first ones see" % (layers[lost.index(True)], self.windows[layers[lost.index(True)]]))
+        self._no_rings.update((i, version(i)) for i, t in zip(layers, twice) if not t)
 
     def capture(self, q, k_new, v_new, out) -> "torch.cuda.CUDAGraph":
         """Records one step (with these argument tensors) into a CUDA graph; replay with ``graph.replay()``."""
