@@ -1358,24 +1358,30 @@ static long long groups_of(long long batch, long long total, int turns, int Hkv)
 // fetching it (converting it, for codes) some of a step whatever the group; an item costs about five steps beside its keys.  Parts
 // have four tiles at least, and there are at most 4 items per SM where keys are cut, which bounds the partials.  (512 tokens over 64K
 // E4M3 keys: groups of 16 uncut 1224 us, of 32 in 8 parts 849.)
+// Where none of these numbers of parts leaves four tiles to a part, as many as do are taken, though they fill fewer SMs: one sequence, one KV
+// head, 5 tokens over 65536 E4M3 keys uncut 534 us, in 128 parts 43; 8 KV heads, 9000 keys 81 and 23, 1500 keys 21 and 19.  (Keys
+// are counted by the table's row: 300 of them in a row for 9000 take 13 us uncut, 16 in parts.)
 PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool may_split, double fetch, int sm_count) {
   PromptPlan plan = {1, 4};
   double best = 1e30;
-  for (int turns = 1; turns <= 4; turns *= 2) {
-    const long long items = groups_of(batch, total, turns, Hkv), T = kRowTokens * (4 / turns);
-    const double tiles = std::max(1.0, (double)(key_bound + T) / TK);
-    for (int per_sm = 0; per_sm <= (may_split ? 4 : 0); ++per_sm) {   // uncut; as many parts as fill each SM once, twice ..
-      const long long n = per_sm == 0 ? 1 : per_sm * (long long)sm_count / items;
-      if (n < 1 || (n > 1 && n > tiles / 4)) continue;
-      const double rounds = (double)((items * n + sm_count - 1) / sm_count);
-      const double cost = rounds * (tiles / n * (2.0 / turns + fetch) + 5) + (n > 1 ? 4 : 0);
-      if (cost < best * 0.98) {   // a little gain is not worth the partials
-        best = cost;
-        plan.splits = (int)n;
-        plan.turns = turns;
+  for (int fewer = 0; fewer < 2 && plan.splits == 1; ++fewer)
+    for (int turns = 1; turns <= 4; turns *= 2) {
+      const long long items = groups_of(batch, total, turns, Hkv), T = kRowTokens * (4 / turns);
+      const double tiles = std::max(1.0, (double)(key_bound + T) / TK);
+      const long long most = (long long)(tiles / 4);
+      for (int per_sm = 0; per_sm <= (may_split ? 4 : 0); ++per_sm) {   // uncut; as many parts as fill each SM once, twice ..
+        long long n = per_sm == 0 ? 1 : per_sm * (long long)sm_count / items;
+        if (fewer) n = std::min(n, most);
+        if (n < 1 || (n > 1 && n > most)) continue;
+        const double rounds = (double)((items * n + sm_count - 1) / sm_count);
+        const double cost = rounds * (tiles / n * (2.0 / turns + fetch) + 5) + (n > 1 ? 4 : 0);
+        if (cost < best * 0.98) {   // a little gain is not worth the partials
+          best = cost;
+          plan.splits = (int)n;
+          plan.turns = turns;
+        }
       }
     }
-  }
   return plan;
 }
 
