@@ -607,7 +607,7 @@ puzzle_status puzzle_prompt_attn(const puzzle_layer_desc* desc, const puzzle_qkv
   long long keys = total_tokens / std::min(batch, total_tokens) / 2;   // on average, where lengths are alike
   if (desc->window > 0) keys = std::min<long long>(keys, desc->window);
   P.turns = prompt_plan(batch, total_tokens, Hkv, keys, false, 0.05, grid_ctas()).turns;
-  const cudaError_t e = launch_prompt_attn(P, kSrcPacked, grid_ctas(), static_cast<cudaStream_t>(stream), device_info().smem_prompt);
+  const cudaError_t e = launch_prompt_attn(P, kSrcPacked, static_cast<cudaStream_t>(stream), device_info().smem_prompt);
   return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
 }
 
@@ -649,7 +649,7 @@ puzzle_status puzzle_chunk_attn(const puzzle_layer_desc* desc, const puzzle_kv_v
   P.part_o = static_cast<float*>(workspace);
   P.part_lse = P.part_o + (size_t)plan.splits * total_tokens * desc->num_q_heads * kHeadDim;
   const PromptSource src = desc->kv_dtype == PUZZLE_KV_FP8_E4M3 ? kSrcFp8 : (desc->kv_dtype == PUZZLE_KV_BF16 ? kSrcBf16 : kSrcFp4);
-  const cudaError_t e = launch_prompt_attn(P, src, grid_ctas(), static_cast<cudaStream_t>(stream), device_info().smem_prompt);
+  const cudaError_t e = launch_prompt_attn(P, src, static_cast<cudaStream_t>(stream), device_info().smem_prompt);
   return e == cudaSuccess ? PUZZLE_OK : PUZZLE_ERR_CUDA;
 }
 

@@ -13,9 +13,10 @@
 //    P over them as the A operand of O += P V, and O stays in 64 columns of its own: 4 x (64 + 64) = all 512 columns.  Streams
 //    share nothing until their rows are done; then they join through tensor memory, each for a part of the channels.  The two
 //    halves of a tile are two streams, not one of twice the width, so that every scheduler has four softmax warps: the special
-//    function unit, which bounds the kernel (16 exponentials a clock and SM), is fed while others wait for loads and products.
+//    function unit (16 exponentials a clock and SM), the busiest unit at 64 %, is fed while others wait for loads and products.
+//    What bounds a long prompt is that each stream is a chain (S, exponentials, P V, next S) and four do not cover each other's waits.
 //    Measured on a prompt of 8192 tokens when it was chosen: 740 us; two streams of 128 keys, with S and P apart so that the next S is
-//    computed early, 966; the same with two threads to a row 802.  Now 610 (900 TFLOP/s).
+//    computed early, 966; the same with two threads to a row 802.  Now 600 to 610 (900 TFLOP/s).
 //  * A group of 64, 32 or 16 tokens is 4, 2 or 1 tiles of rows with 1, 2 or 4 streams each; these take the halves of the tiles of keys
 //    in turn and join at the end.  Large groups fetch (and convert) a tile of keys once for many rows and have nothing to join, small
 //    ones make more items of few tokens.
@@ -196,9 +197,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// 2^x for two arguments on the FMA units: x = i + f with i the nearest integer, 2^f by the polynomial of degree five with
-// constant 1 whose largest relative error on [-1/2, 1/2] is smallest (8e-8, found by linear programming over a fine grid), i added
-// to the exponent.  Arguments below -125 give 2^-125; those above 126, and NaN, nothing of use.
+// 2^x for two arguments on the FMA units: x = i + f with i the nearest integer, 2^f by a polynomial of degree five with constant 1,
+// fitted to the relative error on [-1/2, 1/2] (1.11e-7 at most, 1.55e-7 with float32's roundings), i added to the exponent.  Arguments
+// below -125 give 2^-125; those above 126, and NaN, nothing of use.
 __device__ __forceinline__ void exp2_poly(uint64_t x2, float& e0, float& e1) {
   float x0, x1;
   unpack2(x2, x0, x1);
@@ -355,7 +356,6 @@ struct Share {
   }
   __device__ __forceinline__ bool any() const { return j_hi > j_lo; }      // one of the streams of these tokens
   __device__ __forceinline__ bool on() const { return j_hi > j0; }
-  __device__ __forceinline__ bool mine(int j) const { return j >= j0 && j < j_hi; }   // j of this stream's turn
   __device__ __forceinline__ bool last(int j) const { return j + turns >= j_hi; }
   __device__ __forceinline__ int blocks(int j) const { return min(end - j * kHalf, kHalf); }
 };
@@ -1319,7 +1319,7 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(const __grid_constant
 }
 
 template <int SRC, int ROWS>
-cudaError_t launch_as(const PromptParams& P, int sm_count, cudaStream_t s, int* smem_limit) {
+cudaError_t launch_as(const PromptParams& P, cudaStream_t s, int* smem_limit) {
   const int need = Cfg<SRC, ROWS>::kSmem + (int)sizeof(Ctl) + 1024;
   if (*smem_limit == 0) {
     const cudaError_t e = cudaFuncSetAttribute(prompt_attn_kernel<SRC, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, need);
@@ -1342,8 +1342,8 @@ cudaError_t launch_as(const PromptParams& P, int sm_count, cudaStream_t s, int* 
 }
 
 template <int SRC>
-cudaError_t launch(const PromptParams& P, int sm_count, cudaStream_t s, int* smem_limit) {
-  return P.turns == 4 ? launch_as<SRC, 1>(P, sm_count, s, smem_limit + 4) : launch_as<SRC, 4>(P, sm_count, s, smem_limit);
+cudaError_t launch(const PromptParams& P, cudaStream_t s, int* smem_limit) {
+  return P.turns == 4 ? launch_as<SRC, 1>(P, s, smem_limit + 4) : launch_as<SRC, 4>(P, s, smem_limit);
 }
 
 }  // namespace
@@ -1393,12 +1393,12 @@ int prompt_most_splits(int batch, int total, int Hkv, int sm_count) {
   return (int)std::max<long long>(1, 4ll * sm_count / std::max<long long>(1, groups_of(batch, total, 1, Hkv)));
 }
 
-cudaError_t launch_prompt_attn(const PromptParams& P, PromptSource src, int sm_count, cudaStream_t s, int* smem_limit) {
+cudaError_t launch_prompt_attn(const PromptParams& P, PromptSource src, cudaStream_t s, int* smem_limit) {
   switch (src) {
-    case kSrcPacked: return launch<kSrcPacked>(P, sm_count, s, smem_limit + 0);
-    case kSrcBf16: return launch<kSrcBf16>(P, sm_count, s, smem_limit + 1);
-    case kSrcFp8: return launch<kSrcFp8>(P, sm_count, s, smem_limit + 2);
-    default: return launch<kSrcFp4>(P, sm_count, s, smem_limit + 3);
+    case kSrcPacked: return launch<kSrcPacked>(P, s, smem_limit + 0);
+    case kSrcBf16: return launch<kSrcBf16>(P, s, smem_limit + 1);
+    case kSrcFp8: return launch<kSrcFp8>(P, s, smem_limit + 2);
+    default: return launch<kSrcFp4>(P, s, smem_limit + 3);
   }
 }
 

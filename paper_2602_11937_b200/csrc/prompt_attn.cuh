@@ -35,6 +35,6 @@ struct PromptPlan {
 PromptPlan prompt_plan(int batch, int total, int Hkv, long long key_bound, bool may_split, double fetch, int sm_count);
 int prompt_most_splits(int batch, int total, int Hkv, int sm_count);
 size_t prompt_partial_bytes(int total, int Hkv, int splits);
-cudaError_t launch_prompt_attn(const PromptParams& P, PromptSource src, int sm_count, cudaStream_t s, int* smem_limit);
+cudaError_t launch_prompt_attn(const PromptParams& P, PromptSource src, cudaStream_t s, int* smem_limit);
 
 }  // namespace puzzle
