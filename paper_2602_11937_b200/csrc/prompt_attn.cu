@@ -42,9 +42,9 @@
 //  * 0 x NaN: a tile of V that some row of the group does not see is searched for infinities and NaN before its product.  They
 //    are replaced by zero, and the rows that do see them get them added at the end, read again from where they come from.
 //
-// Every wait is bounded: one that runs out sets PUZZLE_DEV_WAIT_EXPIRED and a flag upon which every role leaves its loop.  At its end,
-// whichever way it came there, a role waits (again with a limit) for what it has set going: products, copies, the request for work.
-// None is in flight when shared and tensor memory are given back.
+// Every wait is bounded: one that runs out sets PUZZLE_DEV_WAIT_EXPIRED and a flag upon which every role leaves its loop.  When all have,
+// those that set something going (products, copies, the request for work) wait for it, again with a limit, so that none is in
+// flight when shared and tensor memory are given back.  Copies that no barrier of the others follows are waited for in any case.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -241,6 +241,8 @@ __device__ __forceinline__ void cp_arrive(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void cp_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// All threads of the CTA, from either side of the split of registers (code behind the join has to do with the smaller share).
+__device__ __forceinline__ void sync_cta() { asm volatile("barrier.sync 0;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void regs_up() {
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
@@ -485,6 +487,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
 
   if (warp >= 16) {
     regs_down<K::kRegsOther>();
+    int it = 0, kt = 0, q_n[4] = {0, 0, 0, 0};   // items asked for, tiles and query tiles loaded by this warp
     if (warp < 20) {
       // ================================================================= MMA issue, one warp per stream
       const int st = warp - 16, tile = st / turns;
@@ -578,9 +581,6 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         }
         base += nt;
       }
-      if (elect_one()) umma_commit(smem_u32(&C->ended[st]));
-      __syncwarp();
-      mbar_wait_bounded(smem_u32(&C->ended[st]), 0);
     } else if (warp == 20) {
       // ================================================================= work records, queries, packed keys and values
       const int T = kRowTokens * (4 / turns);
@@ -617,9 +617,9 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         }
       };
       load_window();
-      int kt = 0, before_tiles = 0, asked = 0;
+      int before_tiles = 0;
       bool ok = true;
-      for (int it = 0;; ++it) {
+      for (;; ++it) {
         // blocks of the grid are items, long ones first; a long one is asked for when the one before the last has been done with
         int item = blockIdx.x;
         const int slot = it % kRing;
@@ -635,7 +635,6 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
             request_block(smem_u32(&C->next), bar);
           }
           __syncwarp();
-          ++asked;
           ok = wait(C->next_full, (uint32_t)(it - 1) & 1u);
           if (ok) item = granted_block(smem_u32(&C->next));
         }
@@ -706,11 +705,6 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         }
         if (!ok) break;
       }
-      if (asked > 0) mbar_wait_bounded(smem_u32(&C->next_full), (uint32_t)(asked - 1) & 1u);
-      for (int i = max(kt - NS, 0); i < kt; ++i) {
-        mbar_wait_bounded(smem_u32(&C->k_full[i % NS]), (uint32_t)(i / NS) & 1u);
-        mbar_wait_bounded(smem_u32(&C->v_full[i % NS]), (uint32_t)(i / NS) & 1u);
-      }
     } else if (warp == 21) {
       // ================================================================= infinities and NaN among values not all rows see
       constexpr uint32_t kInf = K::kCodes ? 0x7c007c00u : 0x7f807f80u;
@@ -750,7 +744,6 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
       }
     } else if (warp == 22) {
       // ================================================================= queries
-      int q_n[4] = {0, 0, 0, 0};
       Record r;
       bool ok = true;
       for (int it = 0; ok && get_record(it, r); ++it) {
@@ -769,9 +762,6 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
           __syncwarp();
         }
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (q_n[i] > 0) mbar_wait_bounded(smem_u32(&C->q_full[i]), (uint32_t)(q_n[i] - 1) & 1u);
     } else if (K::kCodes && warp == 23) {
       // ================================================================= codes of the cache, as they lie there
       // One lane to a block of K or V of a tile; places in the cache are looked up for four tiles at a time, lane = 8 tile + block.
@@ -976,6 +966,26 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
       }
      }
     }
+    sync_cta();
+    if (C->abort) {   // what is still under way ends before shared and tensor memory are given back
+      if (warp < 20) {
+        if (elect_one()) umma_commit(smem_u32(&C->ended[warp - 16]));
+        __syncwarp();
+        mbar_wait_bounded(smem_u32(&C->ended[warp - 16]), 0);
+      } else if (warp == 20) {
+        if (it > 0) mbar_wait_bounded(smem_u32(&C->next_full), (uint32_t)(it - 1) & 1u);
+#pragma unroll 1
+        for (int i = max(kt - NS, 0); i < kt; ++i) {
+          mbar_wait_bounded(smem_u32(&C->k_full[i % NS]), (uint32_t)(i / NS) & 1u);
+          mbar_wait_bounded(smem_u32(&C->v_full[i % NS]), (uint32_t)(i / NS) & 1u);
+        }
+      } else if (warp == 22) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (q_n[i] > 0) mbar_wait_bounded(smem_u32(&C->q_full[i]), (uint32_t)(q_n[i] - 1) & 1u);
+      }
+      __syncwarp();
+    }
   } else {
     // =================================================================== softmax, four warpgroups, thread = row
     regs_up<K::kRegsSoftmax>();
@@ -988,12 +998,10 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
     bool ok = true;
     for (int it = 0; ok && get_record(it, r); ++it) {
       const Share sh(r, st, turns, window);
-      float c = P.sm_scale_log2e;
-      if (K::kCodes && P.k_scale) c *= P.k_scale[r.kvh];
-      // Logits of some row (odd) are scaled before their maximum is taken: all rows', pre is 1 in those that do not need it.
-      bool odd = !(c > 0.f && c < INFINITY);
-      float pre = odd ? c : 1.f;
-      if (odd) c = 1.f;
+      float scale = P.sm_scale_log2e;
+      if (K::kCodes && P.k_scale) scale *= P.k_scale[r.kvh];
+      // scaled: this row's logits are scaled before their maximum is taken; odd: some row's of this warp
+      bool odd = !(scale > 0.f && scale < INFINITY), scaled = odd;
       const int p = sh.pos + (row >> 3), p0 = sh.pos + 4 * wq; // this row's position, the warp's first
       const int hi = p + 1, lo = window > 0 ? p - window + 1 : 0;   // the row sees [lo, hi)
       // Rows without a token hold what is behind the sequence: other sequences' queries, and logits from earlier items.  They do not
@@ -1014,7 +1022,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
           tmem_ld32(ts, u);
           tmem_ld32(ts + 32, u + 32);
           tmem_wait_ld();
-          const uint64_t c2 = pack2(c, c), r2 = pack2(-ref, -ref);
+          const uint64_t c2 = pack2(scale, scale), r2 = pack2(-ref, -ref);
           uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
@@ -1056,7 +1064,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
             if (odd || kc + 32 > p0 + 1 || (window > 0 && kc < p0 + 3 - window + 1)) {   // some token does not see some of them
               if (odd)
 #pragma unroll
-                for (int j = 0; j < 32; ++j) s[j] *= pre;
+                for (int j = 0; j < 32; ++j) s[j] *= scaled ? scale : 1.f;
               const uint32_t seen = bits_below(p + 1 - kc) & ~(window > 0 ? bits_below(p - window + 1 - kc) : 0u);
 #pragma unroll
               for (int j = 0; j < 32; ++j)
@@ -1071,23 +1079,20 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
                   x[0] = max3(x[0], s[j], s[j + 1]);
                   x[1] = max3(x[1], s[j + 2], s[j + 3]);
                 }
-                float top = max3(x[0], x[1], x[1]), now = top * c - K::kShift;
+                float top = max3(x[0], x[1], x[1]), now = top * (scaled ? 1.f : scale) - K::kShift;
                 // A weight is 2^(c s - ref) rounded once, so what rounding took from the reference is a factor of all of the row's
                 // weights and falls out.  Beyond 2^20 that factor leaves the range of the weights: then the row's logits are scaled,
                 // and rounded, first, the reference is the largest of them itself, and the differences are exact.
-                const bool large = real && fabsf(top) < INFINITY && fabsf(now) > kLarge && pre == 1.f;
+                const bool large = real && fabsf(top) < INFINITY && fabsf(now) > kLarge && !scaled;
                 if (__any_sync(kFull, large)) {
                   odd = true;
-                  const float by = large ? c : 1.f;
+                  const float by = large ? scale : 1.f;
 #pragma unroll
                   for (int j = 0; j < 32; ++j) s[j] *= by;
                   top *= by;
-                  if (large) {
-                    pre = c;
-                    c = 1.f;
-                  }
+                  scaled |= large;
                 }
-                if (c == 1.f && fabsf(top) > kLarge) now = top;
+                if (scaled && fabsf(top) > kLarge) now = top;
                 const bool raise = real && now > ref;
                 if (__any_sync(kFull, raise)) {
                   float alpha = 1.f;
@@ -1114,6 +1119,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
                 // infinity - infinity, or a NaN: the whole row is NaN
                 ref = top < INFINITY ? ref : NAN;
               }
+              const float c = scaled ? 1.f : scale;
               const uint64_t c2 = pack2(c, c), r2 = pack2(-ref, -ref);
               uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
@@ -1259,8 +1265,9 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
       release(it);
       __syncwarp();
     }
+    sync_cta();
   }
-  __syncthreads();
+  if (C->abort) sync_cta();   // (no role is left that could set it)
   if (warp == 16) {
     __syncwarp();
     tc_after();
@@ -1279,18 +1286,6 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(const __grid_constant
   grid_dependency_wait();
   if (at >= rows) return;
   const int token = (int)(at / Hq), g = (int)(at % Hq);
-  // The row's sequence: valid ones do not share rows, but with bad entries among them need not lie in order.
-  const unsigned sixteen = 0xffffu << (threadIdx.x & 16);
-  int seq = -1;
-  for (int b = o; b < P.batch; b += 16) {
-    const int st = P.starts[b], en = P.starts[b + 1];
-    if (st >= 0 && st <= token && token < en && en <= P.total) seq = b;
-  }
-#pragma unroll
-  for (int d = 8; d > 0; d >>= 1) seq = max(seq, __shfl_xor_sync(sixteen, seq, d));
-  if (seq < 0) return;                  // no sequence's row
-  const int len = min(max(P.seq_lens[seq], 0), P.max_blocks_per_seq * kBlock);
-  const bool sees = len - (P.starts[seq + 1] - token) >= 0;
   const float* lse = P.part_lse + at;
   float top = P.sinks ? P.sinks[g] : -INFINITY;
   const float sk = top;
@@ -1309,6 +1304,18 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(const __grid_constant
     acc.z += wgt * v.z;
     acc.w += wgt * v.w;
   }
+  // The row's sequence: valid ones do not share rows, but with bad entries among them need not lie in order.
+  const unsigned sixteen = 0xffffu << (threadIdx.x & 16);
+  int seq = -1;
+  for (int b = o; b < P.batch; b += 16) {
+    const int st = P.starts[b], en = P.starts[b + 1];
+    if (st >= 0 && st <= token && token < en && en <= P.total) seq = b;
+  }
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) seq = max(seq, __shfl_xor_sync(sixteen, seq, d));
+  if (seq < 0) return;                  // no sequence's row: what was read of it means nothing
+  const int len = min(max(P.seq_lens[seq], 0), P.max_blocks_per_seq * kBlock);
+  const bool sees = len - (P.starts[seq + 1] - token) >= 0;
   float f = 1.f / z, out_lse = base + lg2(z) * kLn2;
   if (z == 0.f) {
     f = sees ? NAN : 0.f;
