@@ -108,6 +108,7 @@ struct Ctl {
   uint64_t copied[4][8];         // of a warp's blocks; of a tile's codes: the first row
   uint64_t codes_empty[8];
   Record rec[kRing];
+  int asked, loaded, q_loaded[4];   // at the end of the warps that did it: requests for work, tiles, tiles of queries
   float2 join[2][4][128];   // by turns: reference and sum of a stream's rows
   uint32_t tmem;
   volatile int abort;
@@ -487,7 +488,6 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
 
   if (warp >= 16) {
     regs_down<K::kRegsOther>();
-    int it = 0, kt = 0, q_n[4] = {0, 0, 0, 0};   // items asked for, tiles and query tiles loaded by this warp
     if (warp < 20) {
       // ================================================================= MMA issue, one warp per stream
       const int st = warp - 16, tile = st / turns;
@@ -617,7 +617,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         }
       };
       load_window();
-      int before_tiles = 0;
+      int it = 0, kt = 0, before_tiles = 0;
       bool ok = true;
       for (;; ++it) {
         // blocks of the grid are items, long ones first; a long one is asked for when the one before the last has been done with
@@ -705,6 +705,10 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         }
         if (!ok) break;
       }
+      if (lane == 0) {
+        C->asked = it;
+        C->loaded = kt;
+      }
     } else if (warp == 21) {
       // ================================================================= infinities and NaN among values not all rows see
       constexpr uint32_t kInf = K::kCodes ? 0x7c007c00u : 0x7f807f80u;
@@ -744,6 +748,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
       }
     } else if (warp == 22) {
       // ================================================================= queries
+      int q_n[4] = {0, 0, 0, 0};
       Record r;
       bool ok = true;
       for (int it = 0; ok && get_record(it, r); ++it) {
@@ -762,6 +767,9 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
           __syncwarp();
         }
       }
+      if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) C->q_loaded[i] = q_n[i];
     } else if (K::kCodes && warp == 23) {
       // ================================================================= codes of the cache, as they lie there
       // One lane to a block of K or V of a tile; places in the cache are looked up for four tiles at a time, lane = 8 tile + block.
@@ -973,6 +981,7 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
         __syncwarp();
         mbar_wait_bounded(smem_u32(&C->ended[warp - 16]), 0);
       } else if (warp == 20) {
+        const int it = C->asked, kt = C->loaded;
         if (it > 0) mbar_wait_bounded(smem_u32(&C->next_full), (uint32_t)(it - 1) & 1u);
 #pragma unroll 1
         for (int i = max(kt - NS, 0); i < kt; ++i) {
@@ -980,9 +989,9 @@ __global__ void __launch_bounds__(Cfg<SRC, ROWS>::kThreads, 1) prompt_attn_kerne
           mbar_wait_bounded(smem_u32(&C->v_full[i % NS]), (uint32_t)(i / NS) & 1u);
         }
       } else if (warp == 22) {
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < 4; ++i)
-          if (q_n[i] > 0) mbar_wait_bounded(smem_u32(&C->q_full[i]), (uint32_t)(q_n[i] - 1) & 1u);
+          if (C->q_loaded[i] > 0) mbar_wait_bounded(smem_u32(&C->q_full[i]), (uint32_t)(C->q_loaded[i] - 1) & 1u);
       }
       __syncwarp();
     }
