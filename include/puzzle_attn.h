@@ -245,7 +245,7 @@ PUZZLE_API puzzle_status puzzle_kv_append_packed(const puzzle_layer_desc* desc, 
  * when window == 0), which are read as they are, in bf16, not from a cache.  (Paper: the input half of the fixed-length
  * scenarios, Section "Optimized Scenarios"; window layers, Section "Window attention for long-context inference".)  Computed on
  * the 5th-generation tensor cores in one pass, softmax weights rounded to bf16 and everything else held in float32.  Long prompts
- * run at 53 to 60 % of the products' rate (exponentials, the busiest unit, at 64 %), short and windowed ones less.
+ * run at 53 to 57 % of the products' rate (exponentials, the busiest unit, at 64 %), short and windowed ones less.
  *   qkv: packed rows; sinks: float32 [num_q_heads] or NULL; out: bf16 [total_tokens][num_q_heads][head_dim]; lse_out: float32
  *   [total_tokens][num_q_heads] or NULL.  desc->kv_dtype has no meaning here.  Unlike the balanced schedules, two calls on the same
  *   inputs give the same bits. */
