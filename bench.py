@@ -492,8 +492,8 @@ NCU_CAPTURE = {
     "source": "profiles/decode_attn_cta_fp8_c3_64k_ncu_full.md (one launch, ncu --set full --clock-control none)",
     "workload": 3, "kernel": "mma", "splits": 0,
     "sources": ("decode_attn_cta.cu", "decode_tile.cuh", "decode_sched.cuh", "common.cuh", "decode_attn.cuh"),
-    "sha256": "88124c170b8fca62530c7d8ebada642bccee0742d3375bd3e5a6b6f20cda471b",
-    "dram_bytes_per_launch": 1075479000 + 4624128,
+    "sha256": "d823bcdf306b5b78abc6ec09ddf59a74600573b9d0b4bfdfd367373e6218c4e8",
+    "dram_bytes_per_launch": 1075521536 + 3347200,
 }
 
 
